@@ -434,6 +434,133 @@ zsaa_status zsaa_op_attention_ex(const void* qkv, int B, int N, int Hq, int Hkv,
 zsaa_status zsaa_op_colmass_ex(const void* qkv, const float* lse, int B, int N, int Hq, int Hkv,
                                int hd, int dtype, int causal, float* colmass, zsaa_stream stream);
 
+/* ---- Several continuations of one prompt over paged caches.
+ *
+ * A decode step of zsaa_decode_step keeps one cache per sequence.  These calls are
+ * the steps of a generation in which several sequences continue one prompt (beams,
+ * samples, drafted tokens): the prompt's entries are kept and read once, and each
+ * sequence has pages of its own for what it adds.  The prompt may be pruned: entry i
+ * of a layer's cache need not be position i (Sec. 3.3 removes rows), so positions are
+ * given apart from entries, and every layer has its own prefix lengths.
+ *
+ * zsaa_pages: one layer's cache as a pool of pages (device memory of the caller's),
+ * k and v each [n_pages, n_kv_heads, page_size, head_dim] of `dtype`, 16-byte aligned.
+ * page_size: 16, 32, 64, 128 or 256 entries.  head_dim 64 or 128 (bf16), 32, 64 or 128
+ * (float32).  n_pages * n_kv_heads * page_size < 2^31.
+ *
+ * A table row lists a sequence's pages in order (device int32, `cols` to a row): entry
+ * i lies in page row[i / page_size].  Entries of a row past the last page in use are
+ * not read.  lens[s] counts the entries of sequence s, the ones that the current step
+ * appends included.  A page number outside [0, n_pages) or a length beyond the row is
+ * reported by zsaa_device_status as ZSAA_ERR_INVALID_ARG: nothing out of range is read
+ * or written, and what the sequence got is unspecified.
+ *
+ * All pointers are device pointers on the current device unless stated; every call
+ * may be captured into a graph (call one once before, outside capture: the status word
+ * is allocated on first use).  Workspaces belong to the caller and need no
+ * initialisation: calls whose work may overlap on the GPU, two graphs' among them, need
+ * one each. */
+typedef struct {
+  void* k;
+  void* v;
+  int n_pages;
+  int page_size;
+  int n_kv_heads;
+  int head_dim;
+  int dtype; /* ZSAA_F32 or ZSAA_BF16 */
+} zsaa_pages;
+
+/* zsaa_op_paged_append: a projection's new rows into the cache, position rotation
+ * (as epilogue 4 of zsaa_op_linear: rotate-half pairing, base rope_theta) on the way.
+ *   qkv    : [T, ld] rows of Hq query heads, then the pool's key heads, then its value
+ *            heads, without rotation; qkv_dtype ZSAA_F32 or the pool's, each value
+ *            rounded once; 16-byte aligned, ld * element size a multiple of 16
+ *   pos    : int32 [T] positions of the rows (any int32)
+ *   cu_rows: int32 [S+1], sequence s has rows cu_rows[s] .. cu_rows[s+1]-1, its entries
+ *            lens[s] - (its rows) .. lens[s] - 1 in order; NULL: T = S, one row each.
+ *            Rows before cu_rows[0] and from cu_rows[S] on are padding
+ *   table  : int32 [S, cols];  lens: int32 [S]
+ *   q_out  : [T, Hq, head_dim] of the pool's dtype, the rotated queries, or NULL; must
+ *            not overlap qkv
+ * A padding row, and one whose entry number is negative (lens[s] below the sequence's
+ * rows: left padding), writes nothing, neither to the cache nor to q_out.  Two rows of
+ * a call on one entry of one page leave one of them or a mix of both there. */
+zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t ld, int qkv_dtype,
+                                 int T, int Hq, const int32_t* pos, float rope_theta,
+                                 const int32_t* cu_rows, int S, const int32_t* table, int cols,
+                                 const int32_t* lens, void* q_out, zsaa_stream stream);
+
+/* zsaa_op_paged_attention: grouped-query attention (Eq. 1) of n_q new entries per
+ * sequence over a shared prefix and the sequence's own entries.  n_q = 1 generates;
+ * up to 16 checks drafted tokens together.
+ *   q      : [S, n_q, Hq, head_dim] of the pool's dtype (rotated); query j of sequence s
+ *            stands at entry lens[s] - n_q + j and sees its group's prefix and the
+ *            sequence's entries up to its own
+ *   table  : int32 [S, cols];  lens: int32 [S]
+ *   cu_seqs: int32 [G+1], non-decreasing, group g holds sequences cu_seqs[g] ..
+ *            cu_seqs[g+1]-1 (possibly none).  Sequences outside [cu_seqs[0], cu_seqs[G])
+ *            are padding: their rows of out and lse stay as they were
+ *   prefix_table: int32 [G, prefix_cols];  prefix_lens: int32 [G] (0: no prefix)
+ *   G = 0  : no prefixes and no padding; the four above are ignored
+ *   out    : as q (must not overlap it);  lse: float32 [S, n_q, Hq] or NULL, log2 of the
+ *            normaliser as zsaa_op_attention gives it
+ * A query that sees no entry gets zeros and lse -inf.  Entries that a query does not
+ * see never touch its result, whatever they hold.  The prefix of a group is read once
+ * for all of its queries.  Results do not depend on timing.  ws: 16-byte aligned,
+ * ws_bytes at least what zsaa_op_paged_attention_workspace returns for these sizes
+ * (host only; prefix_cols is ignored with G = 0). */
+zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
+                                              int cols, int prefix_cols, size_t* bytes);
+zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, int n_q, int Hq,
+                                    const int32_t* table, int cols, const int32_t* lens,
+                                    const int32_t* cu_seqs, int G, const int32_t* prefix_table,
+                                    int prefix_cols, const int32_t* prefix_lens, void* out,
+                                    float* lse, void* ws, size_t ws_bytes, zsaa_stream stream);
+
+/* zsaa_op_beam_select: the K best continuations of each of B batch elements with W
+ * beams over a vocabulary of V tokens.  Continuation (w, v) has the total
+ * scores[w] + logits[w, v] - log sum_u exp(logits[w, u]), in 64 bits from the stored
+ * float32 logits (the sum of exponentials in parts of 32 bits, joined in 64).
+ *   logits : float32 [B*W, ld], ld >= V (not read past V);  V <= 2^26
+ *   scores : float32 [B, W] or NULL (all 0);  1 <= W <= 64, 1 <= K <= 64, K <= W*V
+ *   done   : uint8 [B, W] or NULL; a beam with a flag other than 0 has ended: its logits
+ *            are not read, its only continuation is `eos` at its score (every other
+ *            token counts as -inf).  eos: a token, or -1 without done
+ *   scores_out, parent, token, done_out: float32, int32, int32, uint8 [B, K], best
+ *            first: the total rounded to float32, the beam it continues, the token, and
+ *            whether the continuation has ended (its parent has, or token == eos).
+ *            done_out may be NULL; scores_out must not overlap scores, nor done_out done
+ * Order: the higher total; equal totals: the lower beam; within a beam the higher
+ * logit, then the lower token.  A logit of -inf (a banned token) has the total -inf and
+ * ranks by its token; a beam with a NaN or +inf logit, or a NaN score, has NaN totals,
+ * which rank below every number.  ws: 16-byte aligned, of at least the bytes that
+ * zsaa_op_beam_select_workspace returns (host only). */
+zsaa_status zsaa_op_beam_select_workspace(int B, int W, int V, int K, size_t* bytes);
+zsaa_status zsaa_op_beam_select(const float* logits, int64_t ld, int B, int W, int V,
+                                const float* scores, const uint8_t* done, int eos, int K,
+                                float* scores_out, int32_t* parent, int32_t* token,
+                                uint8_t* done_out, void* ws, size_t ws_bytes, zsaa_stream stream);
+
+/* zsaa_op_beam_reorder: page tables of B*K sequences that continue chosen beams of B*W.
+ * Slot j of batch element b follows beam parent[b, j]: it shares the parent's whole
+ * pages; of the parent's last, partly filled page the first slot that follows the
+ * parent keeps the original, and each later one gets the entries copied into a page of
+ * its own, in every layer.
+ *   layers : HOST array of n_layers pools (1..64) of the same sizes and dtype; one table
+ *            serves them all
+ *   parent : int32 [B, K] in [0, W) (1 <= W, K <= 64; what zsaa_op_beam_select gives)
+ *   table, lens: int32 [B*W, cols] and [B*W];  table_out, lens_out: [B*K, cols], [B*K]
+ *            (neither may overlap its input)
+ *   fresh  : int32 [B*K], a free page for each slot, all different and in no sequence's
+ *            use.  Slot i uses it as its next page (table_out[i, lens / page_size]) when
+ *            the last page is full or kept by an earlier slot; else it stays free
+ * lens_out[i] is the parent's length; entries of table_out past the next page stay as
+ * they were.  A parent out of range is reported as above, with lens_out 0. */
+zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, int W, int K,
+                                 const int32_t* parent, const int32_t* table, int32_t* table_out,
+                                 int cols, const int32_t* lens, int32_t* lens_out,
+                                 const int32_t* fresh, zsaa_stream stream);
+
 /* Per-kernel timing of the forward pass.  After zsaa_trace_begin every
  * kernel the model launches is bracketed by CUDA events recorded on the launch
  * stream (this adds a small gap between launches, so traced forwards are not

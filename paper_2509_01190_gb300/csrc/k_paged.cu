@@ -1,0 +1,476 @@
+// Appending to a paged cache and attention over it.
+//
+// A cache is a pool of pages [n_pages, Hkv, page, hd] for keys and one for values; a
+// sequence's table row lists its pages in order, entry i lies in page row[i / page].
+// Appending rotates keys (and the call's queries) to their positions on the way, so
+// keys are written once and the projection needs no position.
+//
+// Attention: sequence s of group g has n_q new entries, its last; query j sees the
+// group's prefix and the sequence's entries i <= len - n_q + j.  The prefix is read
+// once for all queries of the group (paged.cuh has the decomposition); the joining
+// kernel adds the partial results and the at most n_q - 1 entries that only some of
+// the queries see, one by one and so without a mask: a value hidden from a query,
+// finite or not, never enters its sums.
+#include <cmath>
+
+#include "paged.cuh"
+
+namespace zsaa {
+namespace {
+
+// ---------------------------------------------------------------- append
+
+// RPC rows per CTA, kAppendThreads threads.  A thread handles 8 dims of a head's first
+// half and the 8 that they pair with, so a rotation is thread-local; the row's sines
+// and cosines (one set for all heads) go through shared memory.
+// Angle: the position times the frequency in 2^-64 turns, modulo a turn, is one 64-bit
+// product: exact for every 32-bit position.  The nearest quarter turn is taken off
+// before the conversion to float, so sine and cosine are good to about 1e-7.
+// Bound by bytes on prompts, by the chain table -> address -> store on single tokens.
+constexpr int kAppendThreads = 256;
+
+template <typename TI>
+__device__ __forceinline__ void load8(const TI* p, float (&x)[8]) {
+  if constexpr (sizeof(TI) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    x[0] = bf16lo(u.x), x[1] = bf16hi(u.x), x[2] = bf16lo(u.y), x[3] = bf16hi(u.y);
+    x[4] = bf16lo(u.z), x[5] = bf16hi(u.z), x[6] = bf16lo(u.w), x[7] = bf16hi(u.w);
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+}
+template <typename TO>
+__device__ __forceinline__ void store8(TO* p, const float (&x)[8]) {
+  if constexpr (sizeof(TO) == 2) {  // the one rounding
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                              pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  }
+}
+
+__device__ __forceinline__ float2 turn_cos_sin(unsigned long long turn) {
+  const unsigned quarter = static_cast<unsigned>((turn + (1ull << 61)) >> 62);
+  const long long rest = static_cast<long long>(turn - (static_cast<unsigned long long>(quarter) << 62));
+  float s, c;
+  sincospif(static_cast<float>(rest) * 0x1p-63f, &s, &c);  // half turns, at most 1/4
+  switch (quarter & 3) {
+    case 0: return make_float2(c, s);
+    case 1: return make_float2(-s, c);
+    case 2: return make_float2(-c, -s);
+    default: return make_float2(s, -c);
+  }
+}
+
+template <typename TI, typename TO, int HD, int RPC>
+__global__ void __launch_bounds__(kAppendThreads)
+    append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns) {
+  constexpr int HALF = HD / 2, UNITS = HALF / 8;  // 8-dim pairs of a head
+  __shared__ float2 cs[RPC][HALF];
+  __shared__ long long s_at[RPC];  // element offset of the row's entry for head 0, or -1
+  pdl_trigger();
+  pdl_wait();
+  const int tid = threadIdx.x;
+  const int row0 = blockIdx.x * RPC, n = min(RPC, a.T - row0);
+  const int32_t* pos = after_wait(a.pos);
+  for (int i = tid; i < n * HALF; i += kAppendThreads) {
+    const int r = i / HALF, c = i % HALF;
+    cs[r][c] = turn_cos_sin(static_cast<unsigned long long>(static_cast<long long>(pos[row0 + r])) * turns.f[c]);
+  }
+  if (tid < n) {
+    const int t = row0 + tid;
+    int s = t, back = 1;  // back: 1 for the sequence's last row, 2 for the one before, ...
+    if (a.cu_rows != nullptr) {
+      const int32_t* cu = after_wait(a.cu_rows);
+      int lo = -1, hi = a.S;  // the last sequence that starts at or before row t
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu[mid] <= t) lo = mid; else hi = mid;
+      }
+      s = lo;
+      back = s >= 0 ? cu[s + 1] - t : 0;
+    }
+    long long at = -1;
+    if (s >= 0 && back > 0) {  // not a row before the first sequence or behind the last
+      const int e = after_wait(a.lens)[s] - back;
+      if (e >= 0) {
+        if (e >> a.page_shift < a.cols) {
+          const int page = after_wait(a.table)[static_cast<size_t>(s) * a.cols + (e >> a.page_shift)];
+          if (page >= 0 && page < a.n_pages)
+            at = (((static_cast<long long>(page) * a.Hkv) << a.page_shift) + (e & ((1 << a.page_shift) - 1))) * HD;
+        }
+        if (at < 0) atomicOr(a.status, kStatusBadIndex);
+      }
+    }
+    s_at[tid] = at;
+  }
+  __syncthreads();
+  const int h0 = a.q_out != nullptr ? 0 : a.Hq, heads = a.Hq + 2 * a.Hkv - h0;
+  const int per_row = heads * UNITS;
+  const TI* src = after_wait(static_cast<const TI*>(a.qkv));
+  for (int i = tid; i < n * per_row; i += kAppendThreads) {
+    const int r = i / per_row, k = i % per_row;
+    const int h = h0 + k / UNITS, c = (k % UNITS) * 8;
+    const long long at = s_at[r];
+    if (at < 0) continue;
+    const TI* p = src + static_cast<long long>(row0 + r) * a.ld + h * HD + c;
+    float x[8], y[8];
+    load8(p, x);
+    load8(p + HALF, y);
+    if (h < a.Hq + a.Hkv) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float2 w = cs[r][c + j];
+        const float u = x[j] * w.x - y[j] * w.y, v = y[j] * w.x + x[j] * w.y;
+        x[j] = u;
+        y[j] = v;
+      }
+    }
+    TO* d;
+    if (h < a.Hq) {
+      d = static_cast<TO*>(a.q_out) + (static_cast<long long>(row0 + r) * a.Hq + h) * HD;
+    } else {
+      const bool key = h < a.Hq + a.Hkv;
+      const int g = h - a.Hq - (key ? 0 : a.Hkv);
+      d = static_cast<TO*>(key ? a.k : a.v) + at + ((static_cast<long long>(g) << a.page_shift) * HD);
+    }
+    store8(d + c, x);
+    store8(d + c + HALF, y);
+  }
+}
+
+template <typename TI, typename TO, int HD>
+cudaError_t run_append(const AppendArgs& a, const RopeTurns& t, int sms, cudaStream_t s) {
+  // four rows per CTA share its prologue; fewer rows than would fill the SMs so go one by one
+  if (a.T >= 8 * sms)
+    ZSAA_LAUNCH(append_kernel<TI, TO, HD, 4>, dim3((a.T + 3) / 4), dim3(kAppendThreads), 0, s, a, t);
+  else
+    ZSAA_LAUNCH(append_kernel<TI, TO, HD, 1>, dim3(a.T), dim3(kAppendThreads), 0, s, a, t);
+  return cudaSuccess;
+}
+
+// ---------------------------------------------------------------- attention, CUDA cores
+
+constexpr int kSimtThreads = 128, kSimtRows = 16, kSimtKeys = 32;
+
+// One part at a time: 16 query rows against blocks of 32 keys in shared memory, online
+// softmax (log2 domain) in 32 bits.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kSimtThreads)
+    paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
+  constexpr int MT = kSimtRows, BN = kSimtKeys, LD = HD + 4;
+  constexpr int QUADS = HD / 4, GROUPS = kSimtThreads / QUADS, RPG = MT / GROUPS;  // P V: 4 dims of RPG rows a thread
+  __shared__ __align__(16) float sq[MT][LD], sk[BN][LD], sv[BN][HD];
+  __shared__ float ss[MT][BN + 1], s_corr[MT], s_l[MT], s_m[MT];
+  __shared__ PagedPlanShared plan;
+  const int tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  PagedSpan span;
+  if (!paged_plan<kSimtThreads, MT, BN>(a, w, plan, span)) return;
+  const T* q = after_wait(static_cast<const T*>(a.q));
+  const T* K = after_wait(static_cast<const T*>(a.k));
+  const T* V = after_wait(static_cast<const T*>(a.v));
+  const int ty = tid >> 4, tx = tid & 15;           // scores: rows 2 ty, 2 ty + 1, keys tx, tx + 16
+  const int sr = tid >> 3, sc = (tid & 7) * 4;      // softmax: row, first of 4 keys
+  const int quad = (tid % QUADS) * 4, rg = tid / QUADS;
+  PagedPart p;
+  while (paged_next<MT, BN>(a, w, span, p)) {
+    const int rows = min(MT, p.x.rows - p.r * MT);
+    __syncthreads();  // the part before is done with shared memory
+    for (int i = tid; i < MT * (HD / 8); i += kSimtThreads) {
+      const int r = i / (HD / 8), c = (i % (HD / 8)) * 8;
+      float x[8] = {};
+      if (r < rows) load8(q + paged_q_at<HD>(a, p, p.r * MT + r) + c, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sq[r][c + j] = x[j];
+    }
+    const int32_t* table = paged_row(a, p);
+    float m = -INFINITY, l = 0.f;  // of row sr, the same in its 8 threads
+    float acc[RPG][4] = {};
+    for (int b = p.b0; b < p.b1; ++b) {
+      const int k0 = b * BN, keys = min(BN, p.x.keys - k0);
+      for (int i = tid; i < BN * (HD / 8); i += kSimtThreads) {
+        const int r = i / (HD / 8), c = (i % (HD / 8)) * 8;
+        float x[8] = {}, y[8] = {};
+        if (r < keys) {
+          const size_t at = paged_at<HD>(a, paged_page(a, table, k0 + r), p.h, k0 + r) + c;
+          load8(K + at, x);
+          load8(V + at, y);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sk[r][c + j] = x[j];
+          sv[r][c + j] = y[j];
+        }
+      }
+      __syncthreads();
+      float s[2][2] = {};
+#pragma unroll 4
+      for (int c = 0; c < HD; c += 4) {
+        const float4 q0 = *reinterpret_cast<const float4*>(&sq[2 * ty][c]);
+        const float4 q1 = *reinterpret_cast<const float4*>(&sq[2 * ty + 1][c]);
+        const float4 k0v = *reinterpret_cast<const float4*>(&sk[tx][c]);
+        const float4 k1v = *reinterpret_cast<const float4*>(&sk[tx + 16][c]);
+        auto dot = [](const float4& x, const float4& y, float z) {
+          return fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, z))));
+        };
+        s[0][0] = dot(q0, k0v, s[0][0]);
+        s[0][1] = dot(q0, k1v, s[0][1]);
+        s[1][0] = dot(q1, k0v, s[1][0]);
+        s[1][1] = dot(q1, k1v, s[1][1]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) ss[2 * ty + i][tx + 16 * j] = tx + 16 * j < keys ? s[i][j] * a.scale_log2 : -INFINITY;
+      __syncthreads();
+      float v[4], mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = ss[sr][sc + j];
+        mx = fmaxf(mx, v[j]);
+      }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float mn = fmaxf(m, mx), base = mn == -INFINITY ? 0.f : mn;
+      const float corr = exp2f(m - base);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = exp2f(v[j] - base);
+        sum += v[j];
+        ss[sr][sc + j] = v[j];
+      }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      l = l * corr + sum;
+      m = mn;
+      if ((tid & 7) == 0) s_corr[sr] = corr;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < RPG; ++i) {
+        const float f = s_corr[rg * RPG + i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] *= f;
+      }
+      for (int k = 0; k < keys; ++k) {
+        const float4 x = *reinterpret_cast<const float4*>(&sv[k][quad]);
+#pragma unroll
+        for (int i = 0; i < RPG; ++i) {
+          const float pk = ss[rg * RPG + i][k];
+          acc[i][0] = fmaf(pk, x.x, acc[i][0]);
+          acc[i][1] = fmaf(pk, x.y, acc[i][1]);
+          acc[i][2] = fmaf(pk, x.z, acc[i][2]);
+          acc[i][3] = fmaf(pk, x.w, acc[i][3]);
+        }
+      }
+      __syncthreads();
+    }
+    if ((tid & 7) == 0) {
+      s_l[sr] = l;
+      s_m[sr] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < RPG; ++i) {
+      const int r = rg * RPG + i;
+      if (r >= rows) continue;
+      const float inv = s_l[r] > 0.f ? 1.f / s_l[r] : s_l[r];  // (NaN stays NaN)
+      float* o = w.o + (static_cast<size_t>(p.slot) * MT + r) * HD + quad;
+      *reinterpret_cast<float4*>(o) = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
+      if (quad == 0) w.lse2[static_cast<size_t>(p.slot) * MT + r] = s_m[r] + log2f(s_l[r]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- joining the partial results
+
+constexpr int kJoinThreads = 128;
+
+// One warp per query row: the row's partials in the order of their keys, then the
+// entries that the row sees and its sequence's earlier queries do not.
+template <typename T, int HD>
+__global__ void __launch_bounds__(kJoinThreads)
+    paged_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork wp,
+                      const __grid_constant__ PagedWork ws) {
+  constexpr int DPL = HD / 32;  // dims per lane
+  const int lane = threadIdx.x & 31;
+  const long long row = (blockIdx.x * static_cast<long long>(kJoinThreads) + threadIdx.x) >> 5;
+  const int Hq = a.Hkv * a.per;
+  pdl_trigger();
+  pdl_wait();
+  if (row >= static_cast<long long>(a.S) * a.n_q * Hq) return;
+  const int h = static_cast<int>(row % Hq), j = static_cast<int>(row / Hq % a.n_q);
+  const int s = static_cast<int>(row / Hq / a.n_q);
+  const int g = h / a.per;
+  float m = -INFINITY, l = 0.f, acc[DPL] = {};
+  auto add = [&](float lse, const float (&x)[DPL]) {  // a part with log2 sum lse and result x
+    const float mn = fmaxf(m, lse), base = mn == -INFINITY ? 0.f : mn;
+    const float f = exp2f(m - base), e = exp2f(lse - base);
+    l = l * f + e;
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, x[d], acc[d] * f);
+    m = mn;
+  };
+  // rr: the row's number among its entry's rows for head g
+  auto parts = [&](const PagedWork& w, int e, const PagedEntry& x, int rr) {
+    const int per = after_wait(w.head)[0];
+    if (per == 0 || x.keys == 0) return;
+    const int nb = (x.keys + w.bn - 1) / w.bn, rt = (x.rows + w.mt - 1) / w.mt;
+    const int item = g * rt + rr / w.mt;
+    const int t0 = w.head[1 + e - w.e0] + item * nb;
+    const int row_tiles = (a.n_q * a.per + w.mt - 1) / w.mt;
+    const int first = e < a.G ? (x.seq0 * a.n_q * a.per / w.mt + e) * a.Hkv
+                              : (w.e0 < a.G ? (a.S * a.n_q * a.per / w.mt + a.G) * a.Hkv : 0) + x.seq0 * row_tiles * a.Hkv;
+    for (int c = t0 / per; c <= (t0 + nb - 1) / per; ++c) {
+      const size_t at = static_cast<size_t>(c + first + item) * w.mt + rr % w.mt;
+      const float* o = w.o + at * HD + lane * DPL;
+      float y[DPL];
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) y[d] = o[d];
+      add(w.lse2[at], y);
+    }
+  };
+  if (a.G > 0) {
+    int lo = -1, hi = a.G;  // the last group that starts at or before s
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (paged_group_at(a, mid) <= s) lo = mid; else hi = mid;
+    }
+    if (lo < 0 || s >= paged_group_at(a, a.G)) return;  // a row behind the last sequence stays as it was
+    const PagedEntry x = paged_entry(a, lo);
+    if (lane == 0 && a.plens[lo] > a.pcols << a.page_shift) atomicOr(a.status, kStatusBadIndex);
+    const int rr = ((s - x.seq0) * a.n_q + j) * a.per + h % a.per;
+    if (rr < x.rows)
+      parts(wp, lo, x, rr);
+    else if (lane == 0)
+      atomicOr(a.status, kStatusBadIndex);  // group bounds that run backwards
+  }
+  parts(ws, a.G + s, paged_entry(a, a.G + s), j * a.per + h % a.per);
+  const int cap = a.cols << a.page_shift, len = min(a.lens[s], cap);
+  if (lane == 0 && a.lens[s] > cap) atomicOr(a.status, kStatusBadIndex);
+  const size_t q_at = static_cast<size_t>(row) * HD + lane * DPL;
+  if (a.n_q > 1) {
+    float q[DPL];
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) q[d] = to_f(static_cast<const T*>(a.q)[q_at + d]);
+    for (int i = max(0, len - a.n_q + 1); i <= len - a.n_q + j; ++i) {
+      const int page = paged_page(a, a.table + static_cast<size_t>(s) * a.cols, i);
+      const size_t at = paged_at<HD>(a, page, g, i) + lane * DPL;
+      float dot = 0.f, y[DPL];
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) {
+        dot = fmaf(q[d], to_f(static_cast<const T*>(a.k)[at + d]), dot);
+        y[d] = to_f(static_cast<const T*>(a.v)[at + d]);
+      }
+      add(warp_sum(dot) * a.scale_log2, y);
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : l;  // no key: zeros (NaN stays NaN)
+#pragma unroll
+  for (int d = 0; d < DPL; ++d) static_cast<T*>(a.out)[q_at + d] = from_f<T>(acc[d] * inv);
+  if (a.lse != nullptr && lane == 0) a.lse[row] = m + log2f(l);
+}
+
+// ---------------------------------------------------------------- launches
+
+struct Tiles {
+  int mt, bn, ctas, min_blocks;
+};
+Tiles simt_tiles(int sms) { return Tiles{kSimtRows, kSimtKeys, 4 * sms, 4}; }
+
+long long items_of(const PagedArgs& a, int mt, bool prefixes, bool sequences) {
+  const long long row = static_cast<long long>(a.n_q) * a.per;
+  long long n = 0;
+  if (prefixes) n += (a.S * row / mt + a.G) * a.Hkv;
+  if (sequences) n += static_cast<long long>(a.S) * ((row + mt - 1) / mt) * a.Hkv;
+  return n;
+}
+long long blocks_of(const PagedArgs& a, int mt, int bn) {
+  const long long row = static_cast<long long>(a.n_q) * a.per;
+  const long long pk = (static_cast<long long>(a.pcols) << a.page_shift) / bn + 1;
+  const long long sk = (static_cast<long long>(a.cols) << a.page_shift) / bn + 1;
+  return (a.S * row / mt + a.G) * a.Hkv * pk + a.S * ((row + mt - 1) / mt) * a.Hkv * sk;
+}
+
+// Fills in a launch's share of the workspace from *at on and moves it.
+PagedWork work_share(const PagedArgs& a, const Tiles& t, bool prefixes, bool sequences, int hd, uintptr_t* at) {
+  auto take = [&](size_t bytes) {
+    const uintptr_t p = *at;
+    *at += (bytes + 255) & ~static_cast<size_t>(255);
+    return p;
+  };
+  PagedWork w{};
+  w.e0 = prefixes ? 0 : a.G;
+  w.e1 = sequences ? a.G + a.S : a.G;
+  w.min_blocks = t.min_blocks;
+  w.mt = t.mt;
+  w.bn = t.bn;
+  const size_t slots = static_cast<size_t>(t.ctas) + static_cast<size_t>(items_of(a, t.mt, prefixes, sequences));
+  w.head = reinterpret_cast<int*>(take(sizeof(int) * (1 + static_cast<size_t>(w.e1 - w.e0))));
+  w.lse2 = reinterpret_cast<float*>(take(sizeof(float) * slots * t.mt));
+  w.o = reinterpret_cast<float*>(take(sizeof(float) * slots * t.mt * hd));
+  return w;
+}
+
+constexpr int kMostSms = 256;  // the workspace holds a device of up to this many SMs
+
+template <typename T, int HD>
+cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
+  const Tiles t = simt_tiles(sms < kMostSms ? sms : kMostSms);
+  uintptr_t at = reinterpret_cast<uintptr_t>(ws);
+  const PagedWork w = work_share(a, t, true, true, HD, &at);
+  ZSAA_LAUNCH(paged_simt_kernel<T, HD>, dim3(t.ctas), dim3(kSimtThreads), 0, s, a, w);
+  const long long rows = static_cast<long long>(a.S) * a.n_q * a.Hkv * a.per;
+  const unsigned grid = static_cast<unsigned>((rows * 32 + kJoinThreads - 1) / kJoinThreads);
+  ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(grid), dim3(kJoinThreads), 0, s, a, w, w);
+  return cudaSuccess;
+}
+
+}  // namespace
+
+cudaError_t launch_paged_append(const AppendArgs& a, int in_dtype, int dtype, int hd, float theta, int sms,
+                                cudaStream_t s) {
+  RopeTurns t{};
+  for (int c = 0; c < hd / 2; ++c) {
+    const double f = std::pow(static_cast<double>(theta), -2.0 * c / hd) / 6.283185307179586476925;
+    t.f[c] = static_cast<unsigned long long>(std::ldexp(f, 64));
+  }
+  if (dtype == ZSAA_F32) {
+    if (hd == 32) return run_append<float, float, 32>(a, t, sms, s);
+    if (hd == 64) return run_append<float, float, 64>(a, t, sms, s);
+    if (hd == 128) return run_append<float, float, 128>(a, t, sms, s);
+  } else if (in_dtype == ZSAA_F32) {
+    if (hd == 64) return run_append<float, bf16, 64>(a, t, sms, s);
+    if (hd == 128) return run_append<float, bf16, 128>(a, t, sms, s);
+  } else {
+    if (hd == 64) return run_append<bf16, bf16, 64>(a, t, sms, s);
+    if (hd == 128) return run_append<bf16, bf16, 128>(a, t, sms, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+size_t paged_attention_workspace(const PagedArgs& a, int dtype, int hd) {
+  const Tiles t = simt_tiles(kMostSms);
+  if (items_of(a, t.mt, true, true) + t.ctas > 0x7fffffff || blocks_of(a, t.mt, t.bn) > 0x7fffffff - 0x200000) return 0;
+  uintptr_t at = 0;
+  work_share(a, t, true, true, hd, &at);
+  return at;
+}
+
+cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* ws, int sms, cudaStream_t s) {
+  if (dtype == ZSAA_F32) {
+    if (hd == 32) return run_paged_attention<float, 32>(a, ws, sms, s);
+    if (hd == 64) return run_paged_attention<float, 64>(a, ws, sms, s);
+    if (hd == 128) return run_paged_attention<float, 128>(a, ws, sms, s);
+  } else {
+    if (hd == 64) return run_paged_attention<bf16, 64>(a, ws, sms, s);
+    if (hd == 128) return run_paged_attention<bf16, 128>(a, ws, sms, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace zsaa

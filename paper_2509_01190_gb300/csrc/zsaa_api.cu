@@ -22,6 +22,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "paged.h"
 
 using namespace zsaa;
 
@@ -283,6 +284,7 @@ bool op_rope_table(float theta, int hd, RopeTable* out) {
 
 namespace zsaa {
 void set_last_error(const char* msg) { g_last_error = msg; }
+int* shared_status_word() { return shared_status(); }
 
 EncodeTiledFn get_encode_tiled() {
   std::call_once(g_encode_once, [] {
@@ -1408,7 +1410,7 @@ zsaa_status read_status(int* word, cudaStream_t s, bool whole_device) {
     ZCK(cudaMemset(word, 0, sizeof(int)));
     if (v & kStatusTimeout)
       return fail(ZSAA_ERR_TIMEOUT, "a kernel gave up a bounded wait (status 0x%x)", v);
-    return fail(ZSAA_ERR_INVALID_ARG, "a token id or forced index was out of range (status 0x%x)", v);
+    return fail(ZSAA_ERR_INVALID_ARG, "a token id, index, page or length was out of range (status 0x%x)", v);
   }
   return ZSAA_OK;
 }

@@ -31,7 +31,8 @@ EXPORTED = [
     "zsaa_prefill", "zsaa_decode_step", "zsaa_cache_layer", "zsaa_cache_bytes",
     "zsaa_op_attention_ex", "zsaa_op_colmass_ex", "zsaa_plan_varlen_config", "zsaa_plan_varlen",
     "zsaa_forward_varlen", "zsaa_forward_masked", "zsaa_forward_marked", "zsaa_selftest_wait_timeout",
-    "zsaa_gemm_schedule",
+    "zsaa_gemm_schedule", "zsaa_op_paged_append", "zsaa_op_paged_attention_workspace",
+    "zsaa_op_paged_attention", "zsaa_op_beam_select_workspace", "zsaa_op_beam_select", "zsaa_op_beam_reorder",
 ]
 
 
@@ -65,6 +66,12 @@ class zsaa_forward_opts(C.Structure):
 class zsaa_trace_row(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("launches", C.c_int), ("ms", C.c_double),
                 ("flops", C.c_double), ("bytes", C.c_double)]
+
+
+class zsaa_pages(C.Structure):
+    """One layer's paged cache (the pools' tensors are kept alive by ``tensors``)."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int), ("page_size", C.c_int),
+                ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int)]
 
 
 _LIB = None
@@ -118,6 +125,12 @@ def lib():
             "zsaa_cache_layer": ([_P, _I, C.POINTER(_P), C.POINTER(_P), C.POINTER(_P), C.POINTER(_I),
                                   C.POINTER(_I), C.POINTER(_I)], _I),
             "zsaa_cache_bytes": ([_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)], _I),
+            "zsaa_op_paged_append": ([_P, _P, C.c_int64, _I, _I, _I, _P, C.c_float, _P, _I, _P, _I, _P, _P, _P], _I),
+            "zsaa_op_paged_attention_workspace": ([_P, _I, _I, _I, _I, _I, _I, C.POINTER(C.c_size_t)], _I),
+            "zsaa_op_paged_attention": ([_P, _P, _I, _I, _I, _P, _I, _P, _P, _I, _P, _I, _P, _P, _P, _P, C.c_size_t, _P], _I),
+            "zsaa_op_beam_select_workspace": ([_I, _I, _I, _I, C.POINTER(C.c_size_t)], _I),
+            "zsaa_op_beam_select": ([_P, C.c_int64, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, C.c_size_t, _P], _I),
+            "zsaa_op_beam_reorder": ([_P, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P], _I),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -481,6 +494,133 @@ def zsaa_op_colmass_ex(qkv, lse, B: int, N: int, Hq: int, Hkv: int, hd: int, dty
                        causal: bool, colmass, stream=None):
     _check(lib().zsaa_op_colmass_ex(_ptr(qkv), _ptr(lse), B, N, Hq, Hkv, hd, dtype,
                                     1 if causal else 0, _ptr(colmass), _stream(stream)))
+
+
+# ------------------------------------------------------------------ paged caches and beams
+
+def _at(t, dtypes, n, name, current):
+    """Pointer of a contiguous tensor of at least n elements on the current device
+    (an int or None passes as it is)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype not in dtypes or not t.is_cuda or t.get_device() != current or not t.is_contiguous() or t.numel() < n:
+        raise ZsaaError(ZSAA_ERR_INVALID_ARG,
+                        f"{name}: needs a contiguous tensor of {dtypes} with {n} or more elements on the current device")
+    return t.data_ptr()
+
+
+_HAS_GPU = None
+
+
+def _torch():
+    global _HAS_GPU
+    import torch
+    if _HAS_GPU is None:
+        _HAS_GPU = torch.cuda.is_available()
+    return torch, torch.cuda.current_device() if _HAS_GPU else -1
+
+
+def _stored(torch, dtype):
+    return (torch.bfloat16,) if dtype == ZSAA_BF16 else (torch.float32,)
+
+
+def make_pages(k, v) -> zsaa_pages:
+    """zsaa_pages of two pools [n_pages, n_kv_heads, page_size, head_dim]."""
+    import torch
+    if (k.shape != v.shape or k.dim() != 4 or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32)
+            or k.device != v.device or not (k.is_cuda and k.is_contiguous() and v.is_contiguous())):
+        raise ZsaaError(ZSAA_ERR_INVALID_ARG, "k and v: contiguous CUDA pools [n_pages, n_kv_heads, page_size, head_dim]"
+                                              " of one shape, device and dtype (bfloat16 or float32)")
+    n_pages, heads, page, hd = k.shape
+    p = zsaa_pages(k.data_ptr(), v.data_ptr(), n_pages, page, heads, hd,
+                   ZSAA_BF16 if k.dtype == torch.bfloat16 else ZSAA_F32)
+    p.tensors = (k, v)
+    return p
+
+
+def make_pages_list(ks, vs):
+    """Array of zsaa_pages, one per layer, for zsaa_op_beam_reorder."""
+    pages = [make_pages(k, v) for k, v in zip(ks, vs)]
+    if not pages or len(ks) != len(vs):
+        raise ZsaaError(ZSAA_ERR_INVALID_ARG, "one key and one value pool for each layer")
+    arr = (zsaa_pages * len(pages))(*pages)
+    arr.tensors = [p.tensors for p in pages]
+    return arr
+
+
+def _pools_here(kv, current):
+    """The pools' tensors, where the struct has them, lie on the current device."""
+    held = getattr(kv, "tensors", None)
+    if held:
+        first = held[0][0] if isinstance(held, list) else held[0]
+        if first.get_device() != current:
+            raise ZsaaError(ZSAA_ERR_INVALID_ARG, "the pools are not on the current device")
+
+
+def zsaa_op_paged_append(kv: zsaa_pages, qkv, ld: int, qkv_dtype: int, T: int, Hq: int, pos, rope_theta: float, cu_rows,
+                         S: int, table, cols: int, lens, q_out=None, stream=None):
+    torch, dev = _torch()
+    i32 = (torch.int32,)
+    _pools_here(kv, dev)
+    width = (Hq + 2 * kv.n_kv_heads) * kv.head_dim
+    _check(lib().zsaa_op_paged_append(
+        C.addressof(kv), _at(qkv, _stored(torch, qkv_dtype), (T - 1) * ld + width, "qkv", dev), ld, qkv_dtype, T, Hq,
+        _at(pos, i32, T, "pos", dev), rope_theta, _at(cu_rows, i32, S + 1, "cu_rows", dev), S,
+        _at(table, i32, S * cols, "table", dev), cols, _at(lens, i32, S, "lens", dev),
+        _at(q_out, _stored(torch, kv.dtype), T * Hq * kv.head_dim, "q_out", dev), _stream(stream)))
+
+
+def zsaa_op_paged_attention_workspace(kv: zsaa_pages, S: int, n_q: int, Hq: int, G: int, cols: int,
+                                      prefix_cols: int) -> int:
+    n = C.c_size_t()
+    _check(lib().zsaa_op_paged_attention_workspace(C.addressof(kv), S, n_q, Hq, G, cols, prefix_cols, C.byref(n)))
+    return n.value
+
+
+def zsaa_op_paged_attention(kv: zsaa_pages, q, S: int, n_q: int, Hq: int, table, cols: int, lens, cu_seqs, G: int,
+                            prefix_table, prefix_cols: int, prefix_lens, out, lse, ws, ws_bytes: int, stream=None):
+    torch, dev = _torch()
+    i32, own = (torch.int32,), _stored(torch, kv.dtype)
+    _pools_here(kv, dev)
+    rows = S * n_q * Hq
+    _check(lib().zsaa_op_paged_attention(
+        C.addressof(kv), _at(q, own, rows * kv.head_dim, "q", dev), S, n_q, Hq, _at(table, i32, S * cols, "table", dev),
+        cols, _at(lens, i32, S, "lens", dev), _at(cu_seqs, i32, G + 1, "cu_seqs", dev), G,
+        _at(prefix_table, i32, G * prefix_cols, "prefix_table", dev), prefix_cols,
+        _at(prefix_lens, i32, G, "prefix_lens", dev), _at(out, own, rows * kv.head_dim, "out", dev),
+        _at(lse, (torch.float32,), rows, "lse", dev), _at(ws, (torch.uint8,), ws_bytes, "ws", dev), ws_bytes,
+        _stream(stream)))
+
+
+def zsaa_op_beam_select_workspace(B: int, W: int, V: int, K: int) -> int:
+    n = C.c_size_t()
+    _check(lib().zsaa_op_beam_select_workspace(B, W, V, K, C.byref(n)))
+    return n.value
+
+
+def zsaa_op_beam_select(logits, ld: int, B: int, W: int, V: int, scores, done, eos: int, K: int, scores_out, parent,
+                        token, done_out, ws, ws_bytes: int, stream=None):
+    torch, dev = _torch()
+    f32, i32, flag = (torch.float32,), (torch.int32,), (torch.uint8, torch.bool)
+    _check(lib().zsaa_op_beam_select(
+        _at(logits, f32, (B * W - 1) * ld + V, "logits", dev), ld, B, W, V, _at(scores, f32, B * W, "scores", dev),
+        _at(done, flag, B * W, "done", dev), eos, K, _at(scores_out, f32, B * K, "scores_out", dev),
+        _at(parent, i32, B * K, "parent", dev), _at(token, i32, B * K, "token", dev),
+        _at(done_out, flag, B * K, "done_out", dev), _at(ws, (torch.uint8,), ws_bytes, "ws", dev), ws_bytes,
+        _stream(stream)))
+
+
+def zsaa_op_beam_reorder(layers, B: int, W: int, K: int, parent, table, table_out, cols: int, lens, lens_out, fresh,
+                         stream=None):
+    """layers: what make_pages_list returns (or a ctypes array of zsaa_pages)."""
+    torch, dev = _torch()
+    i32 = (torch.int32,)
+    _pools_here(layers, dev)
+    _check(lib().zsaa_op_beam_reorder(
+        C.addressof(layers), len(layers), B, W, K, _at(parent, i32, B * K, "parent", dev),
+        _at(table, i32, B * W * cols, "table", dev), _at(table_out, i32, B * K * cols, "table_out", dev), cols,
+        _at(lens, i32, B * W, "lens", dev), _at(lens_out, i32, B * K, "lens_out", dev),
+        _at(fresh, i32, B * K, "fresh", dev), _stream(stream)))
 
 
 def zsaa_device_status():
