@@ -151,13 +151,13 @@ cudaError_t run_append(const AppendArgs& a, const RopeTurns& t, int sms, cudaStr
   return cudaSuccess;
 }
 
-// ---------------------------------------------------------------- attention, CUDA cores
+// ---------------------------------------------------------------- attention, float32
 
 constexpr int kSimtThreads = 128, kSimtRows = 16, kSimtKeys = 32;
 
 // One part at a time: 16 query rows against blocks of 32 keys in shared memory, online
 // softmax (log2 domain) in 32 bits.
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(kSimtThreads)
     paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
   constexpr int MT = kSimtRows, BN = kSimtKeys, LD = HD + 4;
@@ -170,9 +170,9 @@ __global__ void __launch_bounds__(kSimtThreads)
   pdl_wait();
   PagedSpan span;
   if (!paged_plan<kSimtThreads, MT, BN>(a, w, plan, span)) return;
-  const T* q = after_wait(static_cast<const T*>(a.q));
-  const T* K = after_wait(static_cast<const T*>(a.k));
-  const T* V = after_wait(static_cast<const T*>(a.v));
+  const float* q = after_wait(static_cast<const float*>(a.q));
+  const float* K = after_wait(static_cast<const float*>(a.k));
+  const float* V = after_wait(static_cast<const float*>(a.v));
   const int ty = tid >> 4, tx = tid & 15;           // scores: rows 2 ty, 2 ty + 1, keys tx, tx + 16
   const int sr = tid >> 3, sc = (tid & 7) * 4;      // softmax: row, first of 4 keys
   const int quad = (tid % QUADS) * 4, rg = tid / QUADS;
@@ -377,10 +377,9 @@ __global__ void __launch_bounds__(kJoinThreads)
 
 // ---------------------------------------------------------------- launches
 
-struct Tiles {
-  int mt, bn, ctas, min_blocks;
-};
-Tiles simt_tiles(int sms) { return Tiles{kSimtRows, kSimtKeys, 4 * sms, 4}; }
+PagedTiles tiles_of(int dtype, int hd, int sms) {
+  return dtype == ZSAA_F32 ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 4} : paged_mma_tiles(hd, sms);
+}
 
 long long items_of(const PagedArgs& a, int mt, bool prefixes, bool sequences) {
   const long long row = static_cast<long long>(a.n_q) * a.per;
@@ -397,7 +396,7 @@ long long blocks_of(const PagedArgs& a, int mt, int bn) {
 }
 
 // Fills in a launch's share of the workspace from *at on and moves it.
-PagedWork work_share(const PagedArgs& a, const Tiles& t, bool prefixes, bool sequences, int hd, uintptr_t* at) {
+PagedWork work_share(const PagedArgs& a, const PagedTiles& t, bool prefixes, bool sequences, int hd, uintptr_t* at) {
   auto take = [&](size_t bytes) {
     const uintptr_t p = *at;
     *at += (bytes + 255) & ~static_cast<size_t>(255);
@@ -420,10 +419,16 @@ constexpr int kMostSms = 256;  // the workspace holds a device of up to this man
 
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
-  const Tiles t = simt_tiles(sms < kMostSms ? sms : kMostSms);
+  constexpr bool f32 = sizeof(T) == 4;
+  const PagedTiles t = tiles_of(f32 ? ZSAA_F32 : ZSAA_BF16, HD, sms < kMostSms ? sms : kMostSms);
   uintptr_t at = reinterpret_cast<uintptr_t>(ws);
   const PagedWork w = work_share(a, t, true, true, HD, &at);
-  ZSAA_LAUNCH(paged_simt_kernel<T, HD>, dim3(t.ctas), dim3(kSimtThreads), 0, s, a, w);
+  if constexpr (f32) {
+    ZSAA_LAUNCH(paged_simt_kernel<HD>, dim3(t.ctas), dim3(kSimtThreads), 0, s, a, w);
+  } else {
+    const cudaError_t e = launch_paged_mma(a, w, HD, t.ctas, s);
+    if (e != cudaSuccess) return e;
+  }
   const long long rows = static_cast<long long>(a.S) * a.n_q * a.Hkv * a.per;
   const unsigned grid = static_cast<unsigned>((rows * 32 + kJoinThreads - 1) / kJoinThreads);
   ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(grid), dim3(kJoinThreads), 0, s, a, w, w);
@@ -454,7 +459,7 @@ cudaError_t launch_paged_append(const AppendArgs& a, int in_dtype, int dtype, in
 }
 
 size_t paged_attention_workspace(const PagedArgs& a, int dtype, int hd) {
-  const Tiles t = simt_tiles(kMostSms);
+  const PagedTiles t = tiles_of(dtype, hd, kMostSms);
   if (items_of(a, t.mt, true, true) + t.ctas > 0x7fffffff || blocks_of(a, t.mt, t.bn) > 0x7fffffff - 0x200000) return 0;
   uintptr_t at = 0;
   work_share(a, t, true, true, hd, &at);
