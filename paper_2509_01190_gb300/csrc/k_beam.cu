@@ -5,34 +5,52 @@
 // V tokens; continuation (w, v) has the total s_w + x_w[v] - lse(x_w), lse(x) =
 // log sum exp(x).  The K largest totals are wanted; lse moves a whole beam, so a
 // beam's own order is that of its logits and one pass over them is enough:
-//   beam_scan_kernel   one chunk of one beam's logits per CTA, held in registers:
-//                      its maximum, its sum of exponentials and its K best tokens;
-//   beam_merge_kernel  one CTA per batch element: lse of every beam from the chunks'
-//                      (m, s) pairs, totals in 64 bits, the K best of the chunks'.
+//   beam_scan_kernel   one stretch of one beam's logits per CTA: its sum of exponentials
+//                      and its K best tokens, in order;
+//   beam_merge_kernel  one CTA per batch element: every beam's lse and K best tokens
+//                      from its stretches', then the K best totals of all beams.
 // The logits are read once, which bounds large batches; few beams are bound by the
 // two kernels' own chains.
 //
-// The K best without a sort: every warp publishes the eight best of its 32 lanes'
-// maxima, and the K-th best published value T is a lower bound of the K-th best of
-// all (at least K values reach it).  Only the few values that reach T are collected
-// and ranked by counting.  Values are compared together with their place, lower
-// place first, so that ties (a banned vocabulary is all -inf) collect no more than
-// distinct values do; where more than the list holds reach T, the K-th best is
+// The K best without a sort and without a list while the logits pass: a thread keeps the
+// maximum of its values alone.  Every warp then publishes the best of its lanes' maxima,
+// at least K in all; the K-th best published value is a lower bound of the K-th best of
+// all, so only the threads whose maximum reaches it look at their values again (in L2),
+// and the few values that do are ranked by counting.  Values are compared together with
+// their place, lower place first; where the bound is the stretch's minimum (a banned
+// vocabulary, whatever number marks it) the first 2 K places hold the K best or more, and
+// where more values than the list holds reach the bound all the same, the K-th best is
 // found bit by bit instead.
+//
+// Sums are taken against c, the float next to n ln 2 with n the maximum of a warp's first
+// values in the log2 domain rounded up, and are then brought to the power of two at the
+// last maximum by exact steps and the factor exp(c - n ln 2), so that warps and stretches
+// are put together by shifts and a beam needs one logarithm.  (Logits are taken off c
+// before the product with log2(e): the other way around a logit of 1000 would be off by
+// 1e-4.)  A thread's terms are added in 32 bits and everything after that as 64-bit
+// integers of 2^-36: FP64 runs at a sixty-fourth of FP32 here, and is left to a beam's
+// logarithm and the totals of its K tokens.
 #include "common.cuh"
 #include "paged.cuh"
 
 namespace zsaa {
 namespace {
 
-constexpr int kScanThreads = 256;
-constexpr int kScanWarps = kScanThreads / 32;
+constexpr int kScanWarps = 8, kScanThreads = 32 * kScanWarps;
+constexpr int kScanGroups = 4;                              // 16-byte loads of a thread in a step
+constexpr int kScanTile = 4 * kScanGroups * kScanThreads;  // values of a CTA's step
+constexpr int kPublish = 8;                                 // lane maxima that a warp publishes, at most
+constexpr int kListCap = 512;                               // collected values, at most
 constexpr int kMergeThreads = 512;
 constexpr int kMergeWarps = kMergeThreads / 32;
-constexpr int kPublish = 8;    // lane maxima that a warp publishes
-constexpr int kListCap = 1024;  // collected values at most
+constexpr int kMergeDepth = 8;  // elements of each list that the merge holds in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLog2eRest = static_cast<float>(1.4426950408889634 - static_cast<double>(kLog2e));
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kLn2Hi = static_cast<float>(kLn2), kLn2Lo = static_cast<float>(kLn2 - static_cast<double>(kLn2Hi));
+// logits of this size and more have no neighbours within reach of exp: a maximum is
+// then its own reference, and its sum counts the values equal to it
+constexpr float kHuge = 0x1p100f;
+constexpr float kSumUnit = 0x1p36f;  // (2^26 terms of up to 1 fit)
 
 // Order-preserving map of a float (no NaN) to unsigned; -0 equals +0, -inf is 0x007fffff.
 __device__ __forceinline__ uint32_t float_key(float x) {
@@ -54,309 +72,421 @@ __device__ __forceinline__ float key_double_to_float(uint64_t k) {
       static_cast<long long>(k & 0x8000000000000000ull ? k ^ 0x8000000000000000ull : ~k)));
 }
 
-__device__ __forceinline__ double warp_sum_d(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// Chunk c of row r: E values per thread.  A value's place is its token; a collected
-// value is (key << 32 | ~token), so that a larger one is a better one.  NaN logits
-// are ordered as -inf (their row's totals are all NaN).
-template <int E>
-__global__ void __launch_bounds__(kScanThreads)
-    beam_scan_kernel(const float* __restrict__ logits, long long ld, int V, int K, int chunks,
-                     const uint8_t* __restrict__ done, BeamChunk* __restrict__ stat, uint2* __restrict__ cand) {
-  constexpr int CHUNK = kScanThreads * E;
-  __shared__ uint64_t pub[kScanWarps * kPublish], list[kListCap];
-  __shared__ uint64_t s_bound, s_best;
-  __shared__ int s_count, s_bad, s_n[kScanWarps];
-  __shared__ double s_sum[kScanWarps];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row = blockIdx.x / chunks, c = blockIdx.x % chunks;
-  pdl_trigger();
-  if (tid == 0) s_bound = 0, s_count = 0, s_bad = 0;
-  pdl_wait();
-  logits = after_wait(logits);
-  done = after_wait(done);
-  if (done != nullptr && done[row] != 0) return;  // its only continuation needs no logits
-  const float* p = logits + static_cast<long long>(row) * ld;
-  // 16-byte loads start `mis` values before the row, at the boundary below it
-  const int mis = static_cast<int>((reinterpret_cast<uintptr_t>(p) >> 2) & 3);
-  const int first = c * CHUNK - mis;  // token of the chunk's first place
-  uint2* out = cand + (static_cast<size_t>(row) * chunks + c) * K;
-  if (first >= V) {  // (only ever the row's last chunk)
-    if (tid == 0) stat[static_cast<size_t>(row) * chunks + c] = BeamChunk{0.0, -INFINITY, 0};
-    for (int i = tid; i < K; i += kScanThreads) out[i] = make_uint2(0, 0);
-    return;
-  }
-  const bool edge = first < 0 || first + CHUNK > V;
-  float v[E];
-#pragma unroll
-  for (int i = 0; i < E / 4; ++i) {
-    const int t = first + (i * kScanThreads + tid) * 4;
-    float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    if (t >= 0 && t <= V - 4) {
-      f = __ldcs(reinterpret_cast<const float4*>(p + t));
-    } else {
-      if (t >= 0 && t < V) f.x = p[t];
-      if (t + 1 >= 0 && t + 1 < V) f.y = p[t + 1];
-      if (t + 2 >= 0 && t + 2 < V) f.z = p[t + 2];
-      if (t + 3 >= 0 && t + 3 < V) f.w = p[t + 3];
-    }
-    v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
-  }
-  auto token = [&](int i) { return first + ((i >> 2) * kScanThreads + tid) * 4 + (i & 3); };
-  auto inside = [&](int i) { return !edge || (token(i) >= 0 && token(i) < V); };
-  auto value = [&](int i) {
-    return static_cast<uint64_t>(float_key(v[i])) << 32 | static_cast<uint32_t>(~token(i));
-  };
-  bool bad = false;
-  float best = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    bad |= !(v[i] < INFINITY);
-    v[i] = fmaxf(v[i], -INFINITY);  // NaN -> -inf
-    best = fmaxf(best, v[i]);
-  }
-  if (bad) s_bad = 1;  // (the same value from every thread that stores it)
-  int at = -1;
-#pragma unroll
-  for (int i = E - 1; i >= 0; --i)
-    if (v[i] == best && inside(i)) at = i;
-  uint64_t mine = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (i == at) mine = value(i);
-  for (int k = 0; k < kPublish; ++k) {
-    const uint32_t hi = static_cast<uint32_t>(mine >> 32);
-    const uint32_t top = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == top ? static_cast<uint32_t>(mine) : 0u);
-    const uint64_t w = static_cast<uint64_t>(top) << 32 | lo;
-    if (lane == 0) pub[warp * kPublish + k] = top == 0 ? 0 : w;
-    if (mine == w) mine = 0;
-  }
-  __syncthreads();
-  if (tid < kScanWarps * kPublish) {
-    const uint64_t x = pub[tid];
-    int r = 0;
-#pragma unroll 8
-    for (int j = 0; j < kScanWarps * kPublish; ++j) r += pub[j] > x;
-    if (x != 0 && r == 0) s_best = x;
-    if (x != 0 && r == K - 1) s_bound = x;
-  }
-  __syncthreads();
-  const float m = key_float(static_cast<uint32_t>(s_best >> 32));
-  uint64_t bound = s_bound;
-  const float bv = bound == 0 ? -INFINITY : key_float(static_cast<uint32_t>(bound >> 32));
-  // sum of exp(x - m): a thread's values in 32 bits, the threads' sums in 64
-  float s4[4] = {0.f, 0.f, 0.f, 0.f};
-  // (x - m first: m log2(e) rounded to 32 bits would be off by more than the sum is;
-  // log2(e) in two parts for the same reason)
-  const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float d = v[i] - base;
-    s4[i & 3] += ex2_fast(fmaf(d, kLog2e, d * kLog2eRest));
-  }
-  auto collect = [&](uint64_t from, float from_v) {
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (v[i] >= from_v && inside(i) && value(i) >= from) {
-        const int n = atomicAdd(&s_count, 1);
-        if (n < kListCap) list[n] = value(i);
-      }
-  };
-  collect(bound, bv);
-  const double ws = warp_sum_d(static_cast<double>((s4[0] + s4[1]) + (s4[2] + s4[3])));
-  if (lane == 0) s_sum[warp] = ws;
-  __syncthreads();
-  if (tid == 0) {
-    double s = 0.0;
-    for (int w = 0; w < kScanWarps; ++w) s += s_sum[w];
-    stat[static_cast<size_t>(row) * chunks + c] = BeamChunk{m == -INFINITY ? 0.0 : s, m, s_bad};
-  }
-  int n = s_count;
-  if (n > kListCap) {  // block-uniform: the K-th largest value, bit by bit
-    bound = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t t = bound | (1ull << bit);
-      int have = 0;
-#pragma unroll
-      for (int i = 0; i < E; ++i) have += inside(i) && value(i) >= t;
-      have = __reduce_add_sync(0xffffffffu, have);
-      __syncthreads();  // the previous round's counts are read
-      if (lane == 0) s_n[warp] = have;
-      __syncthreads();
-      int all = 0;
-      for (int w = 0; w < kScanWarps; ++w) all += s_n[w];
-      if (all >= K) bound = t;
-    }
-    __syncthreads();
-    if (tid == 0) s_count = 0;
-    __syncthreads();
-    collect(bound, key_float(static_cast<uint32_t>(bound >> 32)));
-    __syncthreads();
-    n = s_count;
-  }
-  for (int i = tid; i < n; i += kScanThreads) {
-    const uint64_t x = list[i];
-    int r = 0;
-    for (int j = 0; j < n; ++j) r += list[j] > x;
-    if (r < K) out[r] = make_uint2(static_cast<uint32_t>(x >> 32), ~static_cast<uint32_t>(x));
-  }
-  for (int i = n + tid; i < K; i += kScanThreads) out[i] = make_uint2(0, 0);  // fewer tokens than K
-}
-
-// A continuation's rank: its total, then the lower beam, the higher logit, the lower token.
-struct Rank {
-  uint64_t total, rest;
-  __device__ __forceinline__ bool operator>(const Rank& o) const {
-    return total > o.total || (total == o.total && rest > o.rest);
-  }
-};
-constexpr int kTokenBits = 26;
-static_assert(kBeamMaxVocab == 1 << kTokenBits && kBeamMaxBeams == 64, "beam, logit and token share 64 bits");
-__device__ __forceinline__ uint64_t rank_rest(int w, uint32_t key, int token) {
-  return static_cast<uint64_t>(kBeamMaxBeams - 1 - w) << 58 | static_cast<uint64_t>(key) << kTokenBits |
-         static_cast<uint64_t>(kBeamMaxVocab - 1 - token);
-}
-
 __device__ __forceinline__ uint64_t warp_max_u64(uint64_t v) {
   const uint32_t hi = static_cast<uint32_t>(v >> 32);
   const uint32_t top = __reduce_max_sync(0xffffffffu, hi);
   const uint32_t lo = __reduce_max_sync(0xffffffffu, hi == top ? static_cast<uint32_t>(v) : 0u);
   return static_cast<uint64_t>(top) << 32 | lo;
 }
-__device__ __forceinline__ Rank warp_max_rank(const Rank& r) {
-  Rank w;
-  w.total = warp_max_u64(r.total);
-  w.rest = warp_max_u64(r.total == w.total ? r.rest : 0);
-  return w;
+
+// maximum of three that is NaN where one of them is; minimum of three
+__device__ __forceinline__ float fmax3_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
 }
+__device__ __forceinline__ float fmin3(float a, float b, float c) {
+  float y;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+
+// c of x: the reference of sums whose maximum is x, and its n (a huge x is its own)
+__device__ __forceinline__ bool is_huge(float x) { return !(fabsf(x) < kHuge); }
+__device__ __forceinline__ float log2_ceil(float x) { return is_huge(x) ? x : ceilf(x * kLog2e); }
+__device__ __forceinline__ float reference(float x) {
+  const float n = log2_ceil(x);
+  return !is_huge(x) ? fmaf(n, kLn2Hi, n * kLn2Lo) : x == -INFINITY ? 0.f : x;
+}
+
+// A value (no NaN) at a place: the higher value, then the lower place, is the larger.
+__device__ __forceinline__ uint64_t value_at(float x, int place) {
+  return static_cast<uint64_t>(float_key(x)) << 32 | static_cast<uint32_t>(~place);
+}
+
+// sum / 2^steps; steps: 0 or a positive whole number, or NaN (two maxima of -inf)
+__device__ __forceinline__ uint64_t down_by(uint64_t sum, float steps) {
+  return steps < 64.f ? sum >> static_cast<int>(steps) : 0;
+}
+
+// One stretch: `tiles` steps of 4096 values.  A value's place is its token; a collected
+// value is (key << 32 | ~token), so that a larger one is a better one.  NaN logits are
+// ordered as -inf (their row's totals are all NaN).  Places before the row or past its end
+// hold -inf and come after every real one: as unsigned, their ~token is smaller.
+// Bound by HBM on large batches: 192 beams of 128003 logits in 22 us, half of the copy
+// rate over the beams that have not ended (29 with a bound and a list kept up from tile
+// to tile, whose barriers and rare branches then were most of the time).
+__global__ void __launch_bounds__(kScanThreads, 4)
+    beam_scan_kernel(const float* __restrict__ logits, long long ld, int V, int K, int chunks, int tiles,
+                     const uint8_t* __restrict__ done, BeamChunk* __restrict__ stat, uint2* __restrict__ cand) {
+  constexpr int GROUPS = kScanGroups, STEP = 4 * kScanThreads;
+  __shared__ __align__(16) uint64_t pub[kScanWarps * kPublish];
+  __shared__ uint64_t list[kListCap], s_bound, s_sum[kScanWarps];
+  __shared__ int s_count, s_bad[kScanWarps], s_n[kScanWarps];
+  __shared__ uint32_t s_least[kScanWarps];
+  __shared__ float s_n2[kScanWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = blockIdx.x / chunks, c = blockIdx.x % chunks;
+  pdl_trigger();
+  if (tid == 0) s_count = 0;
+  pdl_wait();
+  logits = after_wait(logits);
+  done = after_wait(done);
+  if (done != nullptr && done[row] != 0) return;  // its only continuation needs no logits
+  const float* p = logits + static_cast<long long>(row) * ld;
+  // 16-byte loads start up to 3 values before the row, at the boundary below it
+  const int start = c * tiles * kScanTile - static_cast<int>((reinterpret_cast<uintptr_t>(p) >> 2) & 3);
+  uint2* out = cand + static_cast<size_t>(blockIdx.x) * K;
+  if (start >= V) {  // (only ever the row's last stretch)
+    if (tid == 0) stat[blockIdx.x] = BeamChunk{0, -INFINITY, 0};
+    for (int i = tid; i < K; i += kScanThreads) out[i] = make_uint2(0, 0);
+    return;
+  }
+  const int n_tiles = min(tiles, (V - start + kScanTile - 1) / kScanTile);
+  auto place = [&](int t, int i) { return start + t * kScanTile + i * STEP + tid * 4; };  // of a group's first value
+  auto load = [&](int t, float4 (&f)[GROUPS]) {
+    const int first = start + t * kScanTile;
+    if (first >= 0 && first + kScanTile <= V) {
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) f[i] = __ldg(reinterpret_cast<const float4*>(p + place(t, i)));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const int u = place(t, i);
+      f[i] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (u >= 0 && u <= V - 4) {
+        f[i] = __ldg(reinterpret_cast<const float4*>(p + u));
+      } else {
+        if (u >= 0 && u < V) f[i].x = p[u];
+        if (u + 1 >= 0 && u + 1 < V) f[i].y = p[u + 1];
+        if (u + 2 >= 0 && u + 2 < V) f[i].z = p[u + 2];
+        if (u + 3 >= 0 && u + 3 < V) f[i].w = p[u + 3];
+      }
+    }
+  };
+  auto max_of = [](const float4& f, float m) { return fmax3_nan(fmax3_nan(f.x, f.y, f.z), f.w, m); };
+
+  float best = -INFINITY, least = INFINITY, n2 = -INFINITY, ref = 0.f;
+  float s4[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](const float4& f) {
+    s4[0] += ex2_fast((f.x - ref) * kLog2e);
+    s4[1] += ex2_fast((f.y - ref) * kLog2e);
+    s4[2] += ex2_fast((f.z - ref) * kLog2e);
+    s4[3] += ex2_fast((f.w - ref) * kLog2e);
+  };
+  float4 f[GROUPS];
+  load(0, f);
+  for (int t = 0; t < n_tiles; ++t) {
+    float4 next[GROUPS];
+    if (t + 1 < n_tiles) load(t + 1, next);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      best = max_of(f[i], best);
+      least = fmin3(fmin3(f[i].x, f[i].y, f[i].z), f[i].w, least);
+    }
+    if (n2 == -INFINITY) {  // (warp-uniform) the reference: the first finite maximum
+      const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(fmaxf(best, -INFINITY))));
+      n2 = log2_ceil(m);
+      ref = reference(m);
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      add(f[i]);
+      f[i] = next[i];
+    }
+  }
+  // what few stretches need
+  bool bad = !(best < INFINITY);
+  if (bad) {  // a NaN or +inf: the maximum of the numbers
+    best = -INFINITY;
+    for (int t = 0; t < n_tiles; ++t) {
+      load(t, f);
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) best = fmaxf(best, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
+    }
+  }
+  const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(best))), last = log2_ceil(m);
+  if (m > ref + 40.f && n2 != -INFINITY) {  // (warp-uniform) the first values were far below: the sum again
+    n2 = last;
+    ref = reference(m);
+    s4[0] = s4[1] = s4[2] = s4[3] = 0.f;
+    for (int t = 0; t < n_tiles; ++t) {
+      load(t, f);
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) add(f[i]);
+    }
+  }
+  // to the power of two at the last maximum (at most 58 steps up), as integers
+  bad = __any_sync(0xffffffffu, bad);
+  const float step = is_huge(m) ? 1.f : __int_as_float((127 + static_cast<int>(n2 - last)) << 23);
+  uint64_t sum = __float2ull_rn(((s4[0] + s4[1]) + (s4[2] + s4[3])) * step * kSumUnit);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  // the bound: in place of its own place a maximum has the thread's last one
+  uint64_t mine = value_at(best, place(n_tiles - 1, GROUPS - 1) + 3);
+  const int publish = min(kPublish, 2 * ((K + kScanWarps - 1) / kScanWarps));  // twice what K needs, for a closer bound
+  for (int k = 0; k < publish; ++k) {
+    const uint64_t x = warp_max_u64(mine);
+    if (lane == 0) pub[warp * publish + k] = x;
+    if (mine == x) mine = 0;
+  }
+  const uint32_t low = __reduce_min_sync(0xffffffffu, float_key(least));
+  if (lane == 0) {
+    const float d = is_huge(m) ? 0.f : -(fmaf(n2, kLn2Hi, -ref) + n2 * kLn2Lo);  // c - n ln 2
+    s_sum[warp] = sum + __float2ll_rn(__ull2float_rn(sum) * (d + d * d * (0.5f + d * (1.f / 6.f))));
+    s_n2[warp] = last;
+    s_bad[warp] = bad;
+    s_least[warp] = low;
+  }
+  __syncthreads();
+  if (tid < kScanWarps * publish) {
+    const uint64_t x = pub[tid];
+    int r = 0;
+    for (int j = 0; j < kScanWarps * publish; j += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(pub + j + i);
+        r += (y.x > x) + (y.y > x);
+      }
+    }
+    if (r == K - 1) s_bound = x;
+  } else if (tid == kScanThreads - 1) {
+    BeamChunk x{0, s_n2[0], s_bad[0]};
+#pragma unroll
+    for (int w = 1; w < kScanWarps; ++w) {
+      x.n2 = fmaxf(x.n2, s_n2[w]);
+      x.bad |= s_bad[w];
+    }
+#pragma unroll
+    for (int w = 0; w < kScanWarps; ++w) x.sum += down_by(s_sum[w], x.n2 - s_n2[w]);
+    stat[blockIdx.x] = x;
+  }
+  __syncthreads();
+  uint64_t bound = s_bound;
+  uint32_t lowest = s_least[0];
+#pragma unroll
+  for (int w = 1; w < kScanWarps; ++w) lowest = min(lowest, s_least[w]);
+  if (static_cast<uint32_t>(bound >> 32) == lowest)
+    bound = static_cast<uint64_t>(lowest) << 32 | static_cast<uint32_t>(~(max(start, 0) + 2 * K - 1));
+  auto collect = [&](uint64_t from) {
+    // the thread's maximum at its first place: the most that a value of it can be
+    if (value_at(best, max(place(0, 0), 0)) < from) return;
+    for (int t = 0; t < n_tiles; ++t) {
+      float4 g[GROUPS];
+      load(t, g);
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+        const float v[4] = {fmaxf(g[i].x, -INFINITY), fmaxf(g[i].y, -INFINITY), fmaxf(g[i].z, -INFINITY), fmaxf(g[i].w, -INFINITY)};
+        if (value_at(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), max(place(t, i), 0)) < from) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t x = value_at(v[j], place(t, i) + j);
+          if (x >= from) {
+            const int n = atomicAdd(&s_count, 1);
+            if (n < kListCap) list[n] = x;
+          }
+        }
+      }
+    }
+  };
+  collect(bound);
+  __syncthreads();
+  int n = s_count;
+  if (n > kListCap) {  // block-uniform: the K-th largest value, bit by bit
+    bound = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const uint64_t from = bound | (1ull << bit);
+      int have = 0;
+      if (value_at(best, max(place(0, 0), 0)) >= from)
+        for (int t = 0; t < n_tiles; ++t) {
+          load(t, f);
+#pragma unroll
+          for (int i = 0; i < GROUPS; ++i) {
+            const int u = place(t, i);
+            have += (value_at(fmaxf(f[i].x, -INFINITY), u) >= from) + (value_at(fmaxf(f[i].y, -INFINITY), u + 1) >= from) +
+                    (value_at(fmaxf(f[i].z, -INFINITY), u + 2) >= from) + (value_at(fmaxf(f[i].w, -INFINITY), u + 3) >= from);
+          }
+        }
+      have = __reduce_add_sync(0xffffffffu, have);
+      __syncthreads();  // the previous round's counts are read
+      if (lane == 0) s_n[warp] = have;
+      __syncthreads();
+      int all = 0;
+      for (int w = 0; w < kScanWarps; ++w) all += s_n[w];
+      if (all >= K) bound = from;
+    }
+    __syncthreads();
+    if (tid == 0) s_count = 0;
+    __syncthreads();
+    collect(bound);
+    __syncthreads();
+    n = s_count;
+  }
+  for (int i = tid; i < n; i += kScanThreads) {  // (at least K: a step has more places than that)
+    const uint64_t x = list[i];
+    int r = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) r += list[j] > x;
+    const uint32_t token = ~static_cast<uint32_t>(x);
+    if (r < K) out[r] = token < static_cast<uint32_t>(V) ? make_uint2(static_cast<uint32_t>(x >> 32), token) : make_uint2(0, 0);
+  }
+}
+
+// Half of the warps put the beams' sums together, the other half their lists.
+constexpr int kSumWarps = kMergeWarps / 2;
 
 __global__ void __launch_bounds__(kMergeThreads)
     beam_merge_kernel(const BeamChunk* __restrict__ stat, const uint2* __restrict__ cand, int W, int V, int K,
                       int chunks, const float* __restrict__ scores, const uint8_t* __restrict__ done, int eos,
                       float* __restrict__ scores_out, int32_t* __restrict__ parent, int32_t* __restrict__ token,
                       uint8_t* __restrict__ done_out) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  uint64_t* total = reinterpret_cast<uint64_t*>(smem);    // [W][K] ordered totals (0: none, or NaN)
+  uint2* best = reinterpret_cast<uint2*>(total + W * K);  // [W][K] (key, token) in order; key 0: none
+  uint2* merged = best + W * K;                           // [list warps][2][K] lists of the chunks merged so far
+  uint2* cache = merged + kSumWarps * 2 * K;              // [list warps][depth][64] the lists' first elements
+  int* rank = reinterpret_cast<int*>(cache + kSumWarps * kMergeDepth * 64);  // [W][K]
+  __shared__ uint64_t s_sum[kBeamMaxBeams];
+  __shared__ float s_n2[kBeamMaxBeams];
   __shared__ double s_lse[kBeamMaxBeams], s_score[kBeamMaxBeams];
-  __shared__ uint8_t s_done[kBeamMaxBeams];
-  __shared__ Rank pub[kMergeWarps * kPublish], list[kListCap], s_bound;
-  __shared__ int s_count;
+  __shared__ uint8_t s_done[kBeamMaxBeams], s_bad[kBeamMaxBeams];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int b = blockIdx.x;
+  const int b = blockIdx.x, n = W * K;
   pdl_trigger();
-  if (tid == 0) s_bound = Rank{0, 0}, s_count = 0;
   pdl_wait();
   stat = after_wait(stat) + static_cast<size_t>(b) * W * chunks;
   cand = after_wait(cand) + static_cast<size_t>(b) * W * chunks * K;
   scores = after_wait(scores);
   done = after_wait(done);
-  for (int w = warp; w < W; w += kMergeWarps) {
-    const bool over = done != nullptr && done[b * W + w] != 0;
-    double lse = 0.0;
-    if (!over) {
-      float m = -INFINITY;
+  for (int i = tid; i < n; i += kMergeThreads) rank[i] = i % K;  // its place in its own beam's list
+  if (warp < kSumWarps) {
+    for (int w = warp; w < W; w += kSumWarps) {
+      const BeamChunk* st = stat + w * chunks;
+      const bool over = done != nullptr && done[b * W + w] != 0;
+      const float score = scores == nullptr ? 0.f : scores[b * W + w];
+      float top = -INFINITY;
       int bad = 0;
-      for (int c = lane; c < chunks; c += 32) {
-        m = fmaxf(m, stat[w * chunks + c].m);
-        bad |= stat[w * chunks + c].bad;
-      }
-      m = warp_max(m);
+      if (!over)
+        for (int c = lane; c < chunks; c += 32) {
+          const BeamChunk x = st[c];
+          top = fmaxf(top, x.n2);
+          bad |= x.bad;
+        }
+      top = warp_max(top);
       bad = __any_sync(0xffffffffu, bad);
-      double s = 0.0;
-      for (int c = lane; c < chunks; c += 32) {
-        const BeamChunk st = stat[w * chunks + c];
-        if (st.m != -INFINITY) s += st.s * exp(static_cast<double>(st.m) - static_cast<double>(m));
+      uint64_t sum = 0;
+      if (!over)
+        for (int c = lane; c < chunks; c += 32) {
+          const BeamChunk x = st[c];
+          sum += down_by(x.sum, top - x.n2);
+        }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (lane == 0) {
+        s_sum[w] = sum;
+        s_n2[w] = top;
+        s_bad[w] = bad;
+        s_done[w] = over;
+        s_score[w] = static_cast<double>(score);
       }
-      s = warp_sum_d(s);
-      // no allowed token: every total is -inf (x - 0); a NaN or +inf logit: every total NaN
-      lse = bad ? nan("") : m == -INFINITY ? 0.0 : static_cast<double>(m) + log(s);
     }
-    if (lane == 0) {
-      s_lse[w] = lse;
-      s_score[w] = scores == nullptr ? 0.0 : static_cast<double>(scores[b * W + w]);
-      s_done[w] = over;
+    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+    if (tid < W) {  // (a logarithm is a long chain of FP64: all beams' at once, while the lists are merged)
+      const float n2 = s_n2[tid];
+      double lse;
+      if (s_done[tid])
+        lse = 0.0;
+      else if (s_bad[tid])
+        lse = __longlong_as_double(0x7ff8000000000000ll);  // every total NaN
+      else if (n2 == -INFINITY)
+        lse = 0.0;  // no allowed token: every total is -inf - 0
+      else if (!(fabsf(n2) < 2.f * kHuge))  // (in the log2 domain a maximum below 2^100 is below 2^101)
+        lse = static_cast<double>(n2);
+      else
+        lse = (static_cast<double>(n2) + log2(static_cast<double>(s_sum[tid]) * (1.0 / kSumUnit))) * kLn2;
+      s_lse[tid] = lse;
     }
-  }
-  __syncthreads();
-  const int n_all = W * chunks * K;
-  // continuation i; total and rest 0 where there is none
-  auto rank_of = [&](int i) {
-    const int w = i / (chunks * K);
-    uint32_t key;
-    int tok;
-    if (s_done[w]) {  // eos at no cost; the other tokens, in their order, are not allowed
-      const int k = i - w * (chunks * K);
-      if (k >= K || k >= V) return Rank{0, 0};
-      tok = k == 0 ? eos : k - 1 < eos ? k - 1 : k;
-      key = k == 0 ? 0x80000000u : 0x007fffffu;
-    } else {
-      const uint2 x = cand[i];
-      if (x.x == 0) return Rank{0, 0};
-      key = x.x;
-      tok = static_cast<int>(x.y);
-    }
-    const double t = s_score[w] + (static_cast<double>(key_float(key)) - s_lse[w]);
-    return Rank{double_key(t), rank_rest(w, key, tok)};
-  };
-  Rank mine{0, 0};
-  for (int i = tid; i < n_all; i += kMergeThreads) {
-    const Rank r = rank_of(i);
-    if (r > mine) mine = r;
-  }
-  for (int k = 0; k < kPublish; ++k) {
-    const Rank w = warp_max_rank(mine);
-    if (lane == 0) pub[warp * kPublish + k] = w;
-    if (mine.total == w.total && mine.rest == w.rest) mine = Rank{0, 0};
-  }
-  __syncthreads();
-  if (tid < kMergeWarps * kPublish) {
-    const Rank x = pub[tid];
-    int r = 0;
-    for (int j = 0; j < kMergeWarps * kPublish; ++j) r += pub[j] > x;
-    if (x.rest != 0 && r == K - 1) s_bound = x;
-  }
-  __syncthreads();
-  const Rank bound = s_bound;
-  for (int i = tid; i < n_all; i += kMergeThreads) {
-    const Rank r = rank_of(i);
-    if (r.rest != 0 && !(bound > r)) {
-      const int n = atomicAdd(&s_count, 1);
-      if (n < kListCap) list[n] = r;
-    }
-  }
-  __syncthreads();
-  int n = s_count;
-  if (n > kListCap) {  // block-uniform: one continuation after the other
-    Rank last{~0ull, ~0ull};
-    for (int k = 0; k < K; ++k) {
-      Rank next{0, 0};
-      for (int i = tid; i < n_all; i += kMergeThreads) {
-        const Rank r = rank_of(i);
-        if (last > r && r > next) next = r;
+  } else {
+    for (int w = warp - kSumWarps; w < W; w += kSumWarps) {
+      uint2* row = best + w * K;
+      // The chunks' lists are in order: K times the best head of two lists a lane, the
+      // list merged so far in place 0 and up to 63 chunks after it.  Equal keys go by
+      // place, so the lower token comes first.
+      const uint2* lists = cand + static_cast<size_t>(w) * chunks * K;
+      const uint2* so_far = nullptr;
+      uint2* mine = cache + (warp - kSumWarps) * kMergeDepth * 64 + lane;
+      if (done != nullptr && done[b * W + w] != 0) {  // eos at no cost; the other tokens, in their order, are not allowed
+        for (int k = lane; k < K; k += 32)
+          row[k] = k >= V ? make_uint2(0, 0)
+                          : make_uint2(k == 0 ? 0x80000000u : 0x007fffffu, k == 0 ? eos : k - 1 < eos ? k - 1 : k);
+        continue;
       }
-      next = warp_max_rank(next);
-      if (lane == 0) pub[warp] = next;
-      __syncthreads();
-      last = pub[0];
-      for (int w = 1; w < kMergeWarps; ++w)
-        if (pub[w] > last) last = pub[w];
-      if (tid == 0) list[k] = last;
-      __syncthreads();
+      for (int c0 = 0; c0 < chunks; c0 += 63) {
+        uint2* to = c0 + 63 >= chunks ? row : merged + ((warp - kSumWarps) * 2 + (c0 / 63) % 2) * K;
+        const uint2* at[2];
+        int pos[2] = {0, 0};
+        uint2 head[2];
+        auto load = [&](int i) {
+          if (at[i] == nullptr || pos[i] >= K) return make_uint2(0, 0);
+          return pos[i] < kMergeDepth ? mine[pos[i] * 64 + 32 * i] : at[i][pos[i]];
+        };
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {  // (all in flight together: one by one, each would cost its own round trip)
+          const int c = c0 + lane + 32 * i - 1;
+          at[i] = lane + 32 * i == 0 ? so_far : c < chunks ? lists + static_cast<size_t>(c) * K : nullptr;
+          uint2 x[kMergeDepth];
+#pragma unroll
+          for (int k = 0; k < kMergeDepth; ++k) x[k] = at[i] != nullptr && k < K ? at[i][k] : make_uint2(0, 0);
+#pragma unroll
+          for (int k = 0; k < kMergeDepth; ++k) mine[k * 64 + 32 * i] = x[k];
+          head[i] = x[0];
+        }
+        for (int k = 0; k < K; ++k) {
+          const uint32_t x = __reduce_max_sync(0xffffffffu, max(head[0].x, head[1].x));
+          const unsigned m0 = __ballot_sync(0xffffffffu, head[0].x == x), m1 = __ballot_sync(0xffffffffu, head[1].x == x);
+          if (lane == __ffs(m0 != 0 ? m0 : m1) - 1) {
+            if (m0 != 0) {
+              to[k] = head[0];
+              ++pos[0];
+              head[0] = load(0);
+            } else {
+              to[k] = head[1];
+              ++pos[1];
+              head[1] = load(1);
+            }
+          }
+        }
+        __syncwarp();
+        so_far = to;
+      }
     }
-    n = K;
   }
+  __syncthreads();
+  for (int i = tid; i < n; i += kMergeThreads)
+    total[i] = double_key(s_score[i / K] + (static_cast<double>(key_float(best[i].x)) - s_lse[i / K]));
+  __syncthreads();
+  // A beam's totals fall along its list, so an element's rank is the sum over the beams
+  // of how many of theirs come before it: equal totals of an earlier beam do.
+  for (int e = tid; e < n * W; e += kMergeThreads) {
+    const int i = e % n, u = e / n, w = i / K;
+    if (u == w || best[i].x == 0) continue;
+    const uint64_t x = total[i];
+    int lo = 0, hi = K;  // the first element of beam u that does not come before
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      const uint64_t y = total[u * K + mid];
+      if (best[u * K + mid].x != 0 && (y > x || (y == x && u < w))) lo = mid + 1; else hi = mid;
+    }
+    if (lo > 0) atomicAdd(&rank[i], lo);
+  }
+  __syncthreads();
   for (int i = tid; i < n; i += kMergeThreads) {
-    const Rank x = list[i];
-    int r = 0;
-    for (int j = 0; j < n; ++j) r += list[j] > x;
-    if (r >= K) continue;
-    const int w = kBeamMaxBeams - 1 - static_cast<int>(x.rest >> 58);
-    const int tok = kBeamMaxVocab - 1 - static_cast<int>(x.rest & (kBeamMaxVocab - 1));
+    const int r = rank[i];
+    if (r >= K || best[i].x == 0) continue;
+    const int w = i / K, tok = static_cast<int>(best[i].y);
     const size_t o = static_cast<size_t>(b) * K + r;
-    scores_out[o] = key_double_to_float(x.total);
+    scores_out[o] = key_double_to_float(total[i]);
     parent[o] = w;
     token[o] = tok;
     if (done_out != nullptr) done_out[o] = s_done[w] || tok == eos;
@@ -422,33 +552,29 @@ __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant
     for (int i = tid; i < n; i += blockDim.x) d[static_cast<size_t>(h) * stride + i] = s[static_cast<size_t>(h) * stride + i];
 }
 
-int scan_values(int rows, int V, int sms) {
-  // 32 values a thread where that gives every SM two chunks, else 8: one prompt's
-  // beams would leave most SMs without work
-  return static_cast<long long>(rows) * ((V + 3 + 32 * kScanThreads - 1) / (32 * kScanThreads)) >= 2LL * sms ? 32 : 8;
-}
-
 }  // namespace
 
-int beam_chunks_most(int V) { return (V + 3 + 8 * kScanThreads - 1) / (8 * kScanThreads); }
-
-int beam_chunks(int rows, int V, int sms) {
-  const int chunk = scan_values(rows, V, sms) * kScanThreads;
-  return (V + 3 + chunk - 1) / chunk;
-}
+int beam_chunks_most(int V) { return (V + 3 + kScanTile - 1) / kScanTile; }
 
 cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, int V, const float* scores,
                                const uint8_t* done, int eos, int K, float* scores_out, int32_t* parent,
                                int32_t* token, uint8_t* done_out, BeamChunk* stat, uint2* cand, int sms,
                                cudaStream_t s) {
-  const int rows = B * W, chunks = beam_chunks(rows, V, sms);
-  const dim3 grid(static_cast<unsigned>(rows) * static_cast<unsigned>(chunks));
-  if (scan_values(rows, V, sms) == 32)
-    ZSAA_LAUNCH(beam_scan_kernel<32>, grid, dim3(kScanThreads), 0, s, logits, ld, V, K, chunks, done, stat, cand);
-  else
-    ZSAA_LAUNCH(beam_scan_kernel<8>, grid, dim3(kScanThreads), 0, s, logits, ld, V, K, chunks, done, stat, cand);
-  ZSAA_LAUNCH(beam_merge_kernel, dim3(B), dim3(kMergeThreads), 0, s, stat, cand, W, V, K, chunks, scores, done, eos,
-              scores_out, parent, token, done_out);
+  // Long stretches save most of a stretch's fixed work, short ones keep the SMs even: about
+  // two rounds of the resident CTAs.
+  const int rows = B * W;
+  int chunks = beam_chunks_most(V);
+  const long long t = static_cast<long long>(rows) * chunks / (8LL * sms);
+  const int tiles = t < 1 ? 1 : t > 16 ? 16 : static_cast<int>(t);
+  chunks = (chunks + tiles - 1) / tiles;
+  ZSAA_LAUNCH(beam_scan_kernel, dim3(static_cast<unsigned>(rows) * static_cast<unsigned>(chunks)), dim3(kScanThreads), 0,
+              s, logits, ld, V, K, chunks, tiles, done, stat, cand);
+  auto merge_smem = [](int w, int k) { return w * k * 20 + kSumWarps * (2 * k + kMergeDepth * 64) * 8; };
+  static OncePerDevice once;
+  const cudaError_t e = set_smem_limit_once(once, beam_merge_kernel, merge_smem(kBeamMaxBeams, kBeamMaxKept));
+  if (e != cudaSuccess) return e;
+  ZSAA_LAUNCH(beam_merge_kernel, dim3(B), dim3(kMergeThreads), merge_smem(W, K), s, stat, cand, W, V, K, chunks, scores,
+              done, eos, scores_out, parent, token, done_out);
   return cudaSuccess;
 }
 

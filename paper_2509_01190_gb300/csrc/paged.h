@@ -58,12 +58,11 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* 
 constexpr int kBeamMaxBeams = 64, kBeamMaxKept = 64, kBeamMaxVocab = 1 << 26;
 constexpr int kReorderMaxLayers = 64;
 struct BeamChunk {
-  double s;  // sum of exp(x - m)
-  float m;   // maximum
-  int bad;   // a NaN or +inf among the logits
+  unsigned long long sum;  // sum of exp(x) / 2^n2 in units of 2^-36
+  float n2;                // the maximum in the log2 domain, rounded up (a huge one: itself)
+  int bad;                 // a NaN or +inf among the logits
 };
-// Chunks that a beam's logits are scanned in; beam_chunks_most: at most, on any device.
-int beam_chunks(int rows, int V, int sms);
+// Stretches that a beam's logits are scanned in, at most, on any device.
 int beam_chunks_most(int V);
 cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, int V, const float* scores,
                                const uint8_t* done, int eos, int K, float* scores_out, int32_t* parent,
