@@ -11,6 +11,7 @@
 // kernel adds the partial results and the at most n_q - 1 entries that only some of
 // the queries see, one by one and so without a mask: a value hidden from a query,
 // finite or not, never enters its sums.
+#include <algorithm>
 #include <cmath>
 
 #include "paged.cuh"
@@ -377,10 +378,6 @@ __global__ void __launch_bounds__(kJoinThreads)
 
 // ---------------------------------------------------------------- launches
 
-PagedTiles tiles_of(int dtype, int hd, int sms) {
-  return dtype == ZSAA_F32 ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 4} : paged_mma_tiles(hd, sms);
-}
-
 long long items_of(const PagedArgs& a, int mt, bool prefixes, bool sequences) {
   const long long row = static_cast<long long>(a.n_q) * a.per;
   long long n = 0;
@@ -417,21 +414,57 @@ PagedWork work_share(const PagedArgs& a, const PagedTiles& t, bool prefixes, boo
 
 constexpr int kMostSms = 256;  // the workspace holds a device of up to this many SMs
 
+// The attention launches of a call: which kernel takes the prefixes, which the sequences
+// (one launch where it is the same), and their shares of the workspace.
+struct Launches {
+  int n;
+  bool tc[2];
+  PagedTiles tiles[2];
+  PagedWork work[2];
+  size_t bytes;
+  long long most;  // items and blocks that number the slots and the line
+};
+
+// Rows of an entry for a KV head from which the 128-row tiles are taken.
+constexpr int kTcRows = 17;
+
+Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
+  Launches r{};
+  const long long row = static_cast<long long>(a.n_q) * a.per;
+  const bool bf = dtype == ZSAA_BF16;
+  const bool tc_seq = bf && row >= kTcRows;
+  const bool tc_pre = a.G > 0 ? bf && a.S * row >= static_cast<long long>(kTcRows) * a.G : tc_seq;  // on average
+  r.n = tc_seq == tc_pre ? 1 : 2;
+  uintptr_t at = reinterpret_cast<uintptr_t>(ws);
+  for (int i = 0; i < r.n; ++i) {
+    const bool pre = i == 0, seq = i == r.n - 1;
+    r.tc[i] = pre ? tc_pre : tc_seq;
+    r.tiles[i] = !bf ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 4} : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
+    r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
+    const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
+    const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
+    r.most = std::max(r.most, std::max(slots, blocks));
+  }
+  r.bytes = at - reinterpret_cast<uintptr_t>(ws);
+  return r;
+}
+
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
   constexpr bool f32 = sizeof(T) == 4;
-  const PagedTiles t = tiles_of(f32 ? ZSAA_F32 : ZSAA_BF16, HD, sms < kMostSms ? sms : kMostSms);
-  uintptr_t at = reinterpret_cast<uintptr_t>(ws);
-  const PagedWork w = work_share(a, t, true, true, HD, &at);
-  if constexpr (f32) {
-    ZSAA_LAUNCH(paged_simt_kernel<HD>, dim3(t.ctas), dim3(kSimtThreads), 0, s, a, w);
-  } else {
-    const cudaError_t e = launch_paged_mma(a, w, HD, t.ctas, s);
-    if (e != cudaSuccess) return e;
+  const Launches r = launches_of(a, f32 ? ZSAA_F32 : ZSAA_BF16, HD, std::min(sms, kMostSms), ws);
+  for (int i = 0; i < r.n; ++i) {
+    if constexpr (f32) {
+      ZSAA_LAUNCH(paged_simt_kernel<HD>, dim3(r.tiles[i].ctas), dim3(kSimtThreads), 0, s, a, r.work[i]);
+    } else {
+      const cudaError_t e = r.tc[i] ? launch_paged_tc(a, r.work[i], HD, r.tiles[i].ctas, s)
+                                    : launch_paged_mma(a, r.work[i], HD, r.tiles[i].ctas, s);
+      if (e != cudaSuccess) return e;
+    }
   }
   const long long rows = static_cast<long long>(a.S) * a.n_q * a.Hkv * a.per;
   const unsigned grid = static_cast<unsigned>((rows * 32 + kJoinThreads - 1) / kJoinThreads);
-  ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(grid), dim3(kJoinThreads), 0, s, a, w, w);
+  ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(grid), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
   return cudaSuccess;
 }
 
@@ -459,11 +492,8 @@ cudaError_t launch_paged_append(const AppendArgs& a, int in_dtype, int dtype, in
 }
 
 size_t paged_attention_workspace(const PagedArgs& a, int dtype, int hd) {
-  const PagedTiles t = tiles_of(dtype, hd, kMostSms);
-  if (items_of(a, t.mt, true, true) + t.ctas > 0x7fffffff || blocks_of(a, t.mt, t.bn) > 0x7fffffff - 0x200000) return 0;
-  uintptr_t at = 0;
-  work_share(a, t, true, true, hd, &at);
-  return at;
+  const Launches r = launches_of(a, dtype, hd, kMostSms, nullptr);
+  return r.most > 0x7fffffff - 0x200000 ? 0 : r.bytes;
 }
 
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* ws, int sms, cudaStream_t s) {

@@ -50,6 +50,9 @@ struct PagedTiles {
 // bf16, tiles of 16 rows (k_paged_mma.cu)
 PagedTiles paged_mma_tiles(int hd, int sms);
 cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);
+// bf16, tiles of 128 rows (k_paged_tc.cu)
+PagedTiles paged_tc_tiles(int sms);
+cudaError_t launch_paged_tc(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);
 // Bytes of workspace that a call of these sizes needs (0: sizes beyond its index range).
 size_t paged_attention_workspace(const PagedArgs& a, int dtype, int hd);
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* ws, int sms, cudaStream_t s);
