@@ -165,12 +165,12 @@ __global__ void __launch_bounds__(kSimtThreads)
   constexpr int QUADS = HD / 4, GROUPS = kSimtThreads / QUADS, RPG = MT / GROUPS;  // P V: 4 dims of RPG rows a thread
   __shared__ __align__(16) float sq[MT][LD], sk[BN][LD], sv[BN][HD];
   __shared__ float ss[MT][BN + 1], s_corr[MT], s_l[MT], s_m[MT];
-  __shared__ PagedPlanShared plan;
   const int tid = threadIdx.x;
   pdl_trigger();
   pdl_wait();
+  __shared__ PagedSpan told;
   PagedSpan span;
-  if (!paged_plan<kSimtThreads, MT, BN>(a, w, plan, span)) return;
+  if (!paged_plan<MT, BN>(a, w, told, span)) return;
   const float* q = after_wait(static_cast<const float*>(a.q));
   const float* K = after_wait(static_cast<const float*>(a.k));
   const float* V = after_wait(static_cast<const float*>(a.v));
@@ -291,68 +291,120 @@ __global__ void __launch_bounds__(kSimtThreads)
 
 constexpr int kJoinThreads = 128;
 
+// The partial results of a query row from one launch: n of them, one slot after the other.
+struct JoinParts {
+  const float *o, *lse2;
+  size_t step;  // rows from one slot to the next
+  int n;
+};
+// rr: the row's number among its entry's rows for KV head g; per, t_entry: the stretch
+// length and the entry's first block
+__device__ __forceinline__ JoinParts join_parts(const PagedArgs& a, const PagedWork& w, int e, const PagedEntry& x,
+                                                int per, int t_entry, int g, int rr, int hd) {
+  if (per == 0 || x.keys == 0) return JoinParts{nullptr, nullptr, 0, 0};
+  const int ms = w.mt_shift, up = (1 << ms) - 1;
+  const int nb = (x.keys + (1 << w.bn_shift) - 1) >> w.bn_shift, rt = (x.rows + up) >> ms;
+  const int item = g * rt + (rr >> ms), row = a.n_q * a.per;
+  const unsigned t0 = static_cast<unsigned>(t_entry + item * nb);
+  const int first = e < a.G ? (((x.seq0 * row) >> ms) + e) * a.Hkv
+                            : (w.e0 < a.G ? (((a.S * row) >> ms) + a.G) * a.Hkv : 0) + x.seq0 * ((row + up) >> ms) * a.Hkv;
+  const unsigned c0 = t0 / static_cast<unsigned>(per), c1 = (t0 + nb - 1) / static_cast<unsigned>(per);
+  const size_t at = (static_cast<size_t>(static_cast<int>(c0) + first + item) << ms) + (rr & up);
+  return JoinParts{w.o + at * hd, w.lse2 + at, static_cast<size_t>(1) << ms, static_cast<int>(c1 - c0) + 1};
+}
+
+template <int N>
+__device__ __forceinline__ void load_dims(const float* p, float (&x)[N]) {
+  if constexpr (N == 4) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else if constexpr (N == 2) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    x[0] = v.x, x[1] = v.y;
+  } else {
+    x[0] = *p;
+  }
+}
+
 // One warp per query row: the row's partials in the order of their keys, then the
-// entries that the row sees and its sequence's earlier queries do not.
+// entries that the row sees and its sequence's earlier queries do not.  Bound by its chain
+// of round trips to L2, some 900 clocks each, so there are three: everything about the
+// row's sequence and, a lane per group, about its group; the log2 sums; the results, 8 at
+// a time.
 template <typename T, int HD>
-__global__ void __launch_bounds__(kJoinThreads)
+__global__ void __launch_bounds__(kJoinThreads, 4)
     paged_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork wp,
                       const __grid_constant__ PagedWork ws) {
   constexpr int DPL = HD / 32;  // dims per lane
-  const int lane = threadIdx.x & 31;
-  const long long row = (blockIdx.x * static_cast<long long>(kJoinThreads) + threadIdx.x) >> 5;
-  const int Hq = a.Hkv * a.per;
+  auto ex2 = [](float x) { return sizeof(T) == 4 ? exp2f(x) : ex2_fast(x); };
+  const int lane = threadIdx.x & 31, Hq = a.Hkv * a.per;
+  const int token = static_cast<int>(blockIdx.x), h = static_cast<int>(blockIdx.y) * (kJoinThreads / 32) + (threadIdx.x >> 5);
   pdl_trigger();
+  if (h >= Hq) return;
+  const int s = token / a.n_q, j = token - s * a.n_q, g = h / a.per;
+  const long long row = static_cast<long long>(token) * Hq + h;
   pdl_wait();
-  if (row >= static_cast<long long>(a.S) * a.n_q * Hq) return;
-  const int h = static_cast<int>(row % Hq), j = static_cast<int>(row / Hq % a.n_q);
-  const int s = static_cast<int>(row / Hq / a.n_q);
-  const int g = h / a.per;
-  float m = -INFINITY, l = 0.f, acc[DPL] = {};
-  auto add = [&](float lse, const float (&x)[DPL]) {  // a part with log2 sum lse and result x
-    const float mn = fmaxf(m, lse), base = mn == -INFINITY ? 0.f : mn;
-    const float f = exp2f(m - base), e = exp2f(lse - base);
-    l = l * f + e;
-#pragma unroll
-    for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, x[d], acc[d] * f);
-    m = mn;
-  };
-  // rr: the row's number among its entry's rows for head g
-  auto parts = [&](const PagedWork& w, int e, const PagedEntry& x, int rr) {
-    const int per = after_wait(w.head)[0];
-    if (per == 0 || x.keys == 0) return;
-    const int nb = (x.keys + w.bn - 1) / w.bn, rt = (x.rows + w.mt - 1) / w.mt;
-    const int item = g * rt + rr / w.mt;
-    const int t0 = w.head[1 + e - w.e0] + item * nb;
-    const int row_tiles = (a.n_q * a.per + w.mt - 1) / w.mt;
-    const int first = e < a.G ? (x.seq0 * a.n_q * a.per / w.mt + e) * a.Hkv
-                              : (w.e0 < a.G ? (a.S * a.n_q * a.per / w.mt + a.G) * a.Hkv : 0) + x.seq0 * row_tiles * a.Hkv;
-    for (int c = t0 / per; c <= (t0 + nb - 1) / per; ++c) {
-      const size_t at = static_cast<size_t>(c + first + item) * w.mt + rr % w.mt;
-      const float* o = w.o + at * HD + lane * DPL;
-      float y[DPL];
-#pragma unroll
-      for (int d = 0; d < DPL; ++d) y[d] = o[d];
-      add(w.lse2[at], y);
-    }
-  };
+  const int cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
+  const int own_per = ws.head[0], own_t = ws.head[1 + a.G + s - ws.e0];
+  JoinParts shared{nullptr, nullptr, 0, 0};
   if (a.G > 0) {
-    int lo = -1, hi = a.G;  // the last group that starts at or before s
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (paged_group_at(a, mid) <= s) lo = mid; else hi = mid;
+    const int pre_per = wp.head[0], end = paged_group_at(a, a.G);
+    int found = -1, g0 = 0, g1 = 0, plen = 0, pre_t = 0;  // the last group that starts at or before s
+    for (int i = 0; i < a.G; i += 32) {
+      const int e = min(i + lane, a.G - 1);
+      const int c0 = paged_group_at(a, e), c1 = paged_group_at(a, e + 1), pl = a.plens[e], pt = wp.head[1 + e - wp.e0];
+      const unsigned m = __ballot_sync(0xffffffffu, i + lane < a.G && c0 <= s);
+      if (m == 0) break;
+      const int src = 31 - __clz(m);
+      found = i + src;
+      g0 = __shfl_sync(0xffffffffu, c0, src);
+      g1 = __shfl_sync(0xffffffffu, c1, src);
+      plen = __shfl_sync(0xffffffffu, pl, src);
+      pre_t = __shfl_sync(0xffffffffu, pt, src);
     }
-    if (lo < 0 || s >= paged_group_at(a, a.G)) return;  // a row behind the last sequence stays as it was
-    const PagedEntry x = paged_entry(a, lo);
-    if (lane == 0 && a.plens[lo] > a.pcols << a.page_shift) atomicOr(a.status, kStatusBadIndex);
-    const int rr = ((s - x.seq0) * a.n_q + j) * a.per + h % a.per;
-    if (rr < x.rows)
-      parts(wp, lo, x, rr);
-    else if (lane == 0)
-      atomicOr(a.status, kStatusBadIndex);  // group bounds that run backwards
+    if (found < 0 || s >= end) return;  // a row behind the last sequence stays as it was
+    const int most = a.pcols << a.page_shift;
+    const PagedEntry x{min(max(plen, 0), most), max(0, g1 - g0) * a.n_q * a.per, g0};
+    const int rr = ((s - g0) * a.n_q + j) * a.per + h % a.per;
+    if (lane == 0 && (plen > most || rr >= x.rows)) atomicOr(a.status, kStatusBadIndex);  // (bounds that run backwards)
+    if (rr < x.rows) shared = join_parts(a, wp, found, x, pre_per, pre_t, g, rr, HD);
   }
-  parts(ws, a.G + s, paged_entry(a, a.G + s), j * a.per + h % a.per);
-  const int cap = a.cols << a.page_shift, len = min(a.lens[s], cap);
-  if (lane == 0 && a.lens[s] > cap) atomicOr(a.status, kStatusBadIndex);
+  if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
+  const PagedEntry mine{max(0, len - (a.n_q - 1)), a.n_q * a.per, s};
+  const JoinParts own = join_parts(a, ws, a.G + s, mine, own_per, own_t, g, j * a.per + h % a.per, HD);
+
+  const int n = shared.n + own.n;
+  auto log2_sum = [&](int i) {
+    return i < shared.n ? shared.lse2[i * shared.step] : i < n ? own.lse2[(i - shared.n) * own.step] : -INFINITY;
+  };
+  float m = -INFINITY, l = 0.f, acc[DPL] = {};
+  for (int i0 = 0; i0 < n; i0 += 32) m = fmaxf(m, log2_sum(i0 + lane));
+  m = warp_max(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const float weight = ex2(log2_sum(i0 + lane) - base);  // (0 past the last part; NaN stays NaN)
+    l += warp_sum(weight);
+    const int most = min(32, n - i0);
+    for (int k0 = 0; k0 < most; k0 += 8) {
+      float x[8][DPL];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k0 + k;
+        if (k0 + k < most)
+          load_dims(i < shared.n ? shared.o + i * shared.step * HD + lane * DPL
+                                 : own.o + (i - shared.n) * own.step * HD + lane * DPL, x[k]);
+        else
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) x[k][d] = 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = __shfl_sync(0xffffffffu, weight, k0 + k);
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, x[k][d], acc[d]);
+      }
+    }
+  }
   const size_t q_at = static_cast<size_t>(row) * HD + lane * DPL;
   if (a.n_q > 1) {
     float q[DPL];
@@ -367,12 +419,24 @@ __global__ void __launch_bounds__(kJoinThreads)
         dot = fmaf(q[d], to_f(static_cast<const T*>(a.k)[at + d]), dot);
         y[d] = to_f(static_cast<const T*>(a.v)[at + d]);
       }
-      add(warp_sum(dot) * a.scale_log2, y);
+      const float lse = warp_sum(dot) * a.scale_log2;
+      const float mn = fmaxf(m, lse), b = mn == -INFINITY ? 0.f : mn;
+      const float f = ex2(m - b), e = ex2(lse - b);
+      l = l * f + e;
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, y[d], acc[d] * f);
+      m = mn;
     }
   }
   const float inv = l > 0.f ? 1.f / l : l;  // no key: zeros (NaN stays NaN)
+  T* out = static_cast<T*>(a.out) + q_at;
+  if constexpr (DPL == 4 && sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+  else if constexpr (DPL == 2 && sizeof(T) == 2)
+    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  else
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) static_cast<T*>(a.out)[q_at + d] = from_f<T>(acc[d] * inv);
+    for (int d = 0; d < DPL; ++d) out[d] = from_f<T>(acc[d] * inv);
   if (a.lse != nullptr && lane == 0) a.lse[row] = m + log2f(l);
 }
 
@@ -403,8 +467,8 @@ PagedWork work_share(const PagedArgs& a, const PagedTiles& t, bool prefixes, boo
   w.e0 = prefixes ? 0 : a.G;
   w.e1 = sequences ? a.G + a.S : a.G;
   w.min_blocks = t.min_blocks;
-  w.mt = t.mt;
-  w.bn = t.bn;
+  while ((1 << w.mt_shift) < t.mt) ++w.mt_shift;
+  while ((1 << w.bn_shift) < t.bn) ++w.bn_shift;
   const size_t slots = static_cast<size_t>(t.ctas) + static_cast<size_t>(items_of(a, t.mt, prefixes, sequences));
   w.head = reinterpret_cast<int*>(take(sizeof(int) * (1 + static_cast<size_t>(w.e1 - w.e0))));
   w.lse2 = reinterpret_cast<float*>(take(sizeof(float) * slots * t.mt));
@@ -462,9 +526,8 @@ cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStrea
       if (e != cudaSuccess) return e;
     }
   }
-  const long long rows = static_cast<long long>(a.S) * a.n_q * a.Hkv * a.per;
-  const unsigned grid = static_cast<unsigned>((rows * 32 + kJoinThreads - 1) / kJoinThreads);
-  ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(grid), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
+  const int heads = a.Hkv * a.per, per_cta = kJoinThreads / 32;
+  ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(a.S * a.n_q, (heads + per_cta - 1) / per_cta), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
   return cudaSuccess;
 }
 
@@ -493,7 +556,7 @@ cudaError_t launch_paged_append(const AppendArgs& a, int in_dtype, int dtype, in
 
 size_t paged_attention_workspace(const PagedArgs& a, int dtype, int hd) {
   const Launches r = launches_of(a, dtype, hd, kMostSms, nullptr);
-  return r.most > 0x7fffffff - 0x200000 ? 0 : r.bytes;
+  return r.most >= 0x3fffffff ? 0 : r.bytes;
 }
 
 cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* ws, int sms, cudaStream_t s) {

@@ -44,7 +44,6 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
     paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
   using C = MmCfg<HD>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ PagedPlanShared plan;
   __shared__ float s_m[MM_WARPS][MM_ROWS], s_l[MM_WARPS][MM_ROWS];
   float* join = reinterpret_cast<float*>(smem + MM_WARPS * C::RING);  // [warps][rows][MM_JOIN_LD]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -52,28 +51,31 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   const uint32_t ring = smem_u32(smem) + warp * C::RING;
   pdl_trigger();
   pdl_wait();
+  __shared__ PagedSpan told;
   PagedSpan span;
-  if (!paged_plan<MM_THREADS, MM_ROWS, MM_KEYS>(a, w, plan, span)) return;
+  if (!paged_plan<MM_ROWS, MM_KEYS>(a, w, told, span)) return;
   const bf16* q = static_cast<const bf16*>(a.q);
 
-  // the tile to load next
+  // the tile to load next; its page number is looked at when it is loaded, a tile later
   PagedSpan ls = span;
   PagedPart lp;
+  const int32_t* row = nullptr;
   int lb = 0, lpage = 0;
   bool more = true;
   auto find = [&](bool next_part) {
     if (next_part) {
       more = paged_next<MM_ROWS, MM_KEYS>(a, w, ls, lp);
       lb = lp.b0;
+      row = paged_row(a, lp);
     }
     const int k0 = lb * MM_KEYS + 16 * warp;
-    if (more && k0 < lp.x.keys) lpage = paged_page(a, paged_row(a, lp), k0);
+    if (more && k0 < lp.x.keys) lpage = row[k0 >> a.page_shift];
   };
   auto load = [&](int stage) {
     if (more) {
       const int k0 = lb * MM_KEYS + 16 * warp, keys = lp.x.keys - k0;
       if (keys > 0) {
-        const size_t at = paged_at<HD>(a, lpage, lp.h, k0);
+        const size_t at = paged_at<HD>(a, paged_sound(a, lpage), lp.h, k0);
         const uint32_t sk = ring + stage * (2 * C::TILE), sv = sk + C::TILE;
         constexpr int CH = HD / 8, STEP = 32 / CH;  // chunks per row, rows per round
         const int c = lane % CH;

@@ -84,7 +84,6 @@ __global__ void __launch_bounds__(TC_THREADS, 2)
   uint64_t *k_full = bars + 5, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_empty + ST);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  __shared__ PagedPlanShared plan;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -112,8 +111,9 @@ __global__ void __launch_bounds__(TC_THREADS, 2)
   pdl_wait();
   pdl_trigger();  // after the wait: a kernel that starts now may read what came before this one
 
+  __shared__ PagedSpan told;
   PagedSpan span;
-  const bool work = paged_plan<TC_THREADS, TC_ROWS, TC_KEYS>(a, w, plan, span);
+  const bool work = paged_plan<TC_ROWS, TC_KEYS>(a, w, told, span);
   PagedPart p;
   if (work && warp == 0) {
     // ---------------------------------------------------------------- TMA producer

@@ -32,22 +32,33 @@ __device__ __forceinline__ float ex2_fast(float x) {
 // first sequence of group g (numbers outside [0, S] are brought inside)
 __device__ __forceinline__ int paged_group_at(const PagedArgs& a, int g) { return min(max(a.cu_seqs[g], 0), a.S); }
 
+// the sequences that are not padding: [lo, hi)
+struct PagedLive {
+  int lo, hi;
+};
+__device__ __forceinline__ PagedLive paged_live(const PagedArgs& a) {
+  if (a.G == 0) return PagedLive{0, a.S};
+  return PagedLive{paged_group_at(a, 0), paged_group_at(a, a.G)};
+}
+
 struct PagedEntry {
   int keys, rows;  // keys of the entry, query rows per KV head
   int seq0;        // first sequence
 };
-__device__ __forceinline__ PagedEntry paged_entry(const PagedArgs& a, int e) {
-  PagedEntry x;
-  if (e < a.G) {
-    x.seq0 = paged_group_at(a, e);
-    x.rows = max(0, paged_group_at(a, e + 1) - x.seq0) * a.n_q * a.per;
-    x.keys = min(max(a.plens[e], 0), a.pcols << a.page_shift);
-  } else {
-    x.seq0 = e - a.G;
-    const bool live = a.G == 0 || (x.seq0 >= paged_group_at(a, 0) && x.seq0 < paged_group_at(a, a.G));
-    x.rows = live ? a.n_q * a.per : 0;
-    x.keys = max(0, min(a.lens[x.seq0], a.cols << a.page_shift) - (a.n_q - 1));
+// (loads first, and the same ones for either kind of entry: one round trip)
+__device__ __forceinline__ PagedEntry paged_entry(const PagedArgs& a, const PagedLive& live, int e) {
+  const bool shared = e < a.G;
+  const int s = e - a.G;
+  const int len = shared ? a.plens[e] : a.lens[s];
+  int c0 = 0, c1 = 0;
+  if (a.G > 0) {
+    c0 = paged_group_at(a, min(e, a.G));
+    c1 = paged_group_at(a, min(e + 1, a.G));
   }
+  PagedEntry x;
+  x.seq0 = shared ? c0 : s;
+  x.rows = (shared ? max(0, c1 - c0) : s >= live.lo && s < live.hi ? 1 : 0) * a.n_q * a.per;
+  x.keys = max(0, min(len, (shared ? a.pcols : a.cols) << a.page_shift) - (shared ? 0 : a.n_q - 1));
   return x;
 }
 // blocks of an entry for one tile of rows
@@ -68,72 +79,68 @@ __device__ __forceinline__ int paged_first_item(const PagedArgs& a, const PagedW
 }
 
 // This CTA's stretch [t, end) of the line; t lies in entry e, whose first block is
-// number t0.  CTA 0 also leaves what the joining kernel needs: the stretch length
-// (0: nothing was done) and every entry's first block.  All NT threads; false: no work.
+// number t0.  The first warp works it out (its lanes over the entries; sums stop growing
+// at kMostBlocks, since group bounds that run backwards could pass any number) and tells
+// the others; more warps would only queue for the same lines of L2.  CTA 0 also leaves
+// what the joining kernel needs: the stretch length (0: nothing is done) and every entry's
+// first block.  All threads; false: no work.
 struct PagedSpan {
   int t, end, e, t0;
+  PagedLive live;
 };
-struct PagedPlanShared {
-  long long warp[32];
-  int e, t0;
-};
-template <int NT, int MT, int BN>
-__device__ __forceinline__ bool paged_plan(const PagedArgs& a, const PagedWork& w, PagedPlanShared& sh, PagedSpan& s) {
-  const int tid = threadIdx.x, lane = tid & 31;
-  const int n = w.e1 - w.e0, q = (n + NT - 1) / NT;
-  const int lo = min(n, tid * q), hi = min(n, lo + q);
-  auto blocks = [&](int i) {
-    const PagedEntry x = paged_entry(a, w.e0 + i);
-    return static_cast<long long>(paged_blocks<BN>(x)) * paged_tiles<MT>(x) * a.Hkv;
-  };
-  long long sum = 0;
-  for (int i = lo; i < hi; ++i) sum += blocks(i);
-  long long upto = sum;
+constexpr int kMostBlocks = 0x3fffffff;
+template <int MT, int BN>
+__device__ __forceinline__ bool paged_plan(const PagedArgs& a, const PagedWork& w, PagedSpan& told, PagedSpan& s) {
+  if (threadIdx.x < 32) {
+    const int lane = threadIdx.x, n = w.e1 - w.e0, q = (n + 31) / 32;
+    const int lo = min(n, lane * q), hi = min(n, lo + q), grid = static_cast<int>(gridDim.x);
+    const PagedLive live = paged_live(a);
+    auto blocks = [&](int i) {
+      const PagedEntry x = paged_entry(a, live, w.e0 + i);
+      return paged_blocks<BN>(x) * paged_tiles<MT>(x) * a.Hkv;
+    };
+    int sum = 0;
+#pragma unroll 2
+    for (int i = lo; i < hi; ++i) sum = min(sum + blocks(i), kMostBlocks);
+    int upto = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 31) sh.warp[tid >> 5] = upto;
-  __syncthreads();
-  long long total = 0, before = 0;
-#pragma unroll
-  for (int k = 0; k < NT / 32; ++k) {
-    if (k < (tid >> 5)) before += sh.warp[k];
-    total += sh.warp[k];
-  }
-  // (group bounds that run backwards could pass any number of blocks)
-  const bool sound = total <= 0x7fffffff - 0x100000;
-  const long long per = max(static_cast<long long>(w.min_blocks), (total + gridDim.x - 1) / gridDim.x);
-  const long long start = static_cast<long long>(blockIdx.x) * per;
-  long long at = before + upto - sum;
-  if (blockIdx.x == 0) {
-    if (tid == 0) {
-      w.head[0] = sound ? static_cast<int>(per) : 0;
-      if (!sound) atomicOr(a.status, kStatusBadIndex);
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto = min(upto + v, kMostBlocks);
     }
-    long long f = at;
-    for (int i = lo; i < hi; ++i) {
-      w.head[1 + i] = static_cast<int>(f);
-      f += blocks(i);
+    const int total = __shfl_sync(0xffffffffu, upto, 31);
+    const int per = max(w.min_blocks, static_cast<int>(static_cast<unsigned>(total + grid - 1) / static_cast<unsigned>(grid)));
+    const int start = static_cast<int>(blockIdx.x) * per;
+    const bool work = total < kMostBlocks && start < total;
+    int at = upto - sum;
+    if (lane == 0) told.end = work ? min(start + per, total) : -1;
+    if (work && start >= at && start < at + sum) {
+      int i = lo;
+      for (; i + 1 < hi; ++i) {
+        const int b = blocks(i);
+        if (start < at + b) break;
+        at += b;
+      }
+      told.t = start;
+      told.e = w.e0 + i;
+      told.t0 = at;
+      told.live = live;
     }
-  }
-  if (!sound || start >= total) return false;
-  if (start >= at && start < at + sum) {
-    int i = lo;
-    for (long long b = blocks(i); start >= at + b; b = blocks(i)) {
-      at += b;
-      ++i;
+    if (blockIdx.x == 0) {
+      at = upto - sum;
+      for (int i = lo; i < hi; ++i) {
+        w.head[1 + i] = at;
+        at = min(at + blocks(i), kMostBlocks);
+      }
+      if (lane == 0) {
+        w.head[0] = total < kMostBlocks ? per : 0;
+        if (total >= kMostBlocks) atomicOr(a.status, kStatusBadIndex);
+      }
     }
-    sh.e = w.e0 + i;
-    sh.t0 = static_cast<int>(at);
   }
   __syncthreads();
-  s.t = static_cast<int>(start);
-  s.end = static_cast<int>(min(start + per, total));
-  s.e = sh.e;
-  s.t0 = sh.t0;
-  return true;
+  s = told;
+  return s.end >= 0;
 }
 
 // The next part of the stretch: one tile of rows of one head over blocks [b0, b1).
@@ -148,7 +155,7 @@ __device__ __forceinline__ bool paged_next(const PagedArgs& a, const PagedWork& 
   if (s.t >= s.end) return false;
   int nb, rt;
   while (true) {
-    p.x = paged_entry(a, s.e);
+    p.x = paged_entry(a, s.live, s.e);
     nb = paged_blocks<BN>(p.x);
     rt = paged_tiles<MT>(p.x);
     const int all = nb * rt * a.Hkv;
@@ -156,26 +163,29 @@ __device__ __forceinline__ bool paged_next(const PagedArgs& a, const PagedWork& 
     s.t0 += all;
     ++s.e;
   }
-  const int u = s.t - s.t0, item = u / nb;
+  const unsigned u = static_cast<unsigned>(s.t - s.t0), item = u / static_cast<unsigned>(nb);
   p.e = s.e;
   p.shared = s.e < a.G;
-  p.h = item / rt;
-  p.r = item % rt;
-  p.b0 = u % nb;
+  p.h = rt == 1 ? item : item / static_cast<unsigned>(rt);
+  p.r = static_cast<int>(item) - p.h * rt;
+  p.b0 = static_cast<int>(u - item * static_cast<unsigned>(nb));
   p.b1 = min(nb, p.b0 + s.end - s.t);
-  p.slot = blockIdx.x + paged_first_item<MT>(a, w, p.x, s.e) + item;
+  p.slot = blockIdx.x + paged_first_item<MT>(a, w, p.x, s.e) + static_cast<int>(item);
   s.t += p.b1 - p.b0;
   return true;
 }
 
-// Page of entry i; a page number out of range is reported and page 0 read instead.
-__device__ __forceinline__ int paged_page(const PagedArgs& a, const int32_t* row, int i) {
-  int page = row[i >> a.page_shift];
+// A page number out of range is reported, and page 0 read instead.
+__device__ __forceinline__ int paged_sound(const PagedArgs& a, int page) {
   if (page < 0 || page >= a.n_pages) {
     atomicOr(a.status, kStatusBadIndex);
     page = 0;
   }
   return page;
+}
+// Page of entry i
+__device__ __forceinline__ int paged_page(const PagedArgs& a, const int32_t* row, int i) {
+  return paged_sound(a, row[i >> a.page_shift]);
 }
 __device__ __forceinline__ const int32_t* paged_row(const PagedArgs& a, const PagedPart& p) {
   return p.shared ? a.ptable + static_cast<size_t>(p.e) * a.pcols : a.table + static_cast<size_t>(p.x.seq0) * a.cols;

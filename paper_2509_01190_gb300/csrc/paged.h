@@ -38,10 +38,10 @@ struct PagedArgs {
 struct PagedWork {
   int e0, e1;      // entries [e0, e1) of the groups' prefixes, then the sequences
   int min_blocks;  // a CTA's stretch is at least this long
-  int mt, bn;      // rows of a tile, keys of a block
+  int mt_shift, bn_shift;  // rows of a tile, keys of a block: powers of two
   int* head;       // [1 + entries]
-  float* o;        // [slots][mt][hd]
-  float* lse2;     // [slots][mt]
+  float* o;        // [slots][rows of a tile][hd]
+  float* lse2;     // [slots][rows of a tile]
 };
 // A kernel's tiles, the CTAs it is launched with, and the least blocks a CTA takes.
 struct PagedTiles {
