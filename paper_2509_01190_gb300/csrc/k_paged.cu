@@ -535,10 +535,17 @@ cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStrea
 
 cudaError_t launch_paged_append(const AppendArgs& a, int in_dtype, int dtype, int hd, float theta, int sms,
                                 cudaStream_t s) {
-  RopeTurns t{};
-  for (int c = 0; c < hd / 2; ++c) {
-    const double f = std::pow(static_cast<double>(theta), -2.0 * c / hd) / 6.283185307179586476925;
-    t.f[c] = static_cast<unsigned long long>(std::ldexp(f, 64));
+  // the last call's frequencies: a model's calls all have the same
+  thread_local RopeTurns t{};
+  thread_local float t_theta = 0.f;
+  thread_local int t_hd = 0;
+  if (theta != t_theta || hd != t_hd) {
+    for (int c = 0; c < hd / 2; ++c) {
+      const double f = std::pow(static_cast<double>(theta), -2.0 * c / hd) / 6.283185307179586476925;
+      t.f[c] = static_cast<unsigned long long>(std::ldexp(f, 64));
+    }
+    t_theta = theta;
+    t_hd = hd;
   }
   if (dtype == ZSAA_F32) {
     if (hd == 32) return run_append<float, float, 32>(a, t, sms, s);

@@ -20,15 +20,14 @@ namespace {
 
 constexpr int MM_WARPS = 4, MM_THREADS = 32 * MM_WARPS, MM_ROWS = 16, MM_KEYS = 16 * MM_WARPS;
 constexpr int MM_STAGES = 3;
-constexpr int MM_JOIN = 32;           // dims that the warps' results are joined by at a time
-constexpr int MM_JOIN_LD = MM_JOIN + 8;  // (8 floats on: the rows of a store fall into different banks)
+constexpr int MM_JOIN = 1024;  // floats of a warp in the buffer that joins results: 8 rows of 128 dims, 16 of 64
 constexpr float MM_RESCALE_LOG2 = 8.f;
 
 template <int HD>
 struct MmCfg {
   static constexpr int TILE = 16 * HD * 2;  // 16 keys, or their values
   static constexpr int RING = MM_STAGES * 2 * TILE;  // a warp's
-  static constexpr int JOIN = MM_WARPS * MM_ROWS * MM_JOIN_LD * 4;
+  static constexpr int JOIN = MM_WARPS * MM_JOIN * 4;
   static constexpr int SMEM = MM_WARPS * RING + JOIN;
   static constexpr int CTAS = HD == 128 ? 2 : 3;  // resident per SM
 };
@@ -45,7 +44,7 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   using C = MmCfg<HD>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_m[MM_WARPS][MM_ROWS], s_l[MM_WARPS][MM_ROWS];
-  float* join = reinterpret_cast<float*>(smem + MM_WARPS * C::RING);  // [warps][rows][MM_JOIN_LD]
+  float* join = reinterpret_cast<float*>(smem + MM_WARPS * C::RING);  // [warps][MM_JOIN]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gid = lane >> 2, tig = lane & 3, mi = lane >> 3;
   const uint32_t ring = smem_u32(smem) + warp * C::RING;
@@ -92,37 +91,40 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
     }
     cp_async_commit();
   };
+  PagedPart p;
+  bool have = paged_next<MM_ROWS, MM_KEYS>(a, w, span, p);
+  // Q as the A operand: rows gid and gid + 8, dims 2 tig, 2 tig + 1 and those + 8
+  uint32_t qf[HD / 16][4];
+  auto load_q = [&]() {
+    const int r0 = p.r * MM_ROWS + gid;
+    const bool in0 = r0 < p.x.rows, in1 = r0 + 8 < p.x.rows;
+    const bf16* q0 = q + (in0 ? paged_q_at<HD>(a, p, r0) : 0) + 2 * tig;
+    const bf16* q1 = q + (in1 ? paged_q_at<HD>(a, p, r0 + 8) : 0) + 2 * tig;
+#pragma unroll
+    for (int kk = 0; kk < HD / 16; ++kk) {
+      qf[kk][0] = in0 ? *reinterpret_cast<const uint32_t*>(q0 + 16 * kk) : 0u;
+      qf[kk][1] = in1 ? *reinterpret_cast<const uint32_t*>(q1 + 16 * kk) : 0u;
+      qf[kk][2] = in0 ? *reinterpret_cast<const uint32_t*>(q0 + 16 * kk + 8) : 0u;
+      qf[kk][3] = in1 ? *reinterpret_cast<const uint32_t*>(q1 + 16 * kk + 8) : 0u;
+    }
+  };
   find(true);
+  load_q();
 #pragma unroll
   for (int i = 0; i < MM_STAGES - 1; ++i) load(i);
 
   int use = 0, fill = MM_STAGES - 1;  // stages
-  PagedPart p;
-  while (paged_next<MM_ROWS, MM_KEYS>(a, w, span, p)) {
-    const int rows = min(MM_ROWS, p.x.rows - p.r * MM_ROWS);
-    // Q as the A operand: rows gid and gid + 8, dims 2 tig, 2 tig + 1 and those + 8
-    uint32_t qf[HD / 16][4];
-    {
-      const int r0 = p.r * MM_ROWS + gid;
-      const bf16* q0 = q + (gid < rows ? paged_q_at<HD>(a, p, r0) : 0) + 2 * tig;
-      const bf16* q1 = q + (gid + 8 < rows ? paged_q_at<HD>(a, p, r0 + 8) : 0) + 2 * tig;
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) {
-        qf[kk][0] = gid < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * kk) : 0u;
-        qf[kk][1] = gid + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * kk) : 0u;
-        qf[kk][2] = gid < rows ? *reinterpret_cast<const uint32_t*>(q0 + 16 * kk + 8) : 0u;
-        qf[kk][3] = gid + 8 < rows ? *reinterpret_cast<const uint32_t*>(q1 + 16 * kk + 8) : 0u;
-      }
-    }
+  while (have) {
+    const int rows = min(MM_ROWS, p.x.rows - p.r * MM_ROWS), all = p.x.keys, b1 = p.b1, slot = p.slot;
     float o[HD / 8][4];
 #pragma unroll
     for (int i = 0; i < HD / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of rows gid, gid + 8; l of this thread's keys
-    for (int b = p.b0; b < p.b1; ++b) {
+    for (int b = p.b0; b < b1; ++b) {
       load(fill);
       cp_async_wait<MM_STAGES - 1>();
       __syncwarp();
-      const int keys = p.x.keys - (b * MM_KEYS + 16 * warp);
+      const int keys = all - (b * MM_KEYS + 16 * warp);
       if (keys > 0) {
         const uint32_t sk = ring + use * (2 * C::TILE), sv = sk + C::TILE;
         float s[2][4] = {};
@@ -191,7 +193,9 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
       use = use + 1 == MM_STAGES ? 0 : use + 1;
       fill = fill + 1 == MM_STAGES ? 0 : fill + 1;
     }
-    // the part's result from the four warps'
+    // the next part's queries are on their way while this one's results are joined
+    have = paged_next<MM_ROWS, MM_KEYS>(a, w, span, p);
+    if (have) load_q();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
@@ -201,19 +205,22 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
         s_l[warp][gid + 8 * i] = l[i];
       }
     }
+    // The part's result from the four warps', all dims at once for up to 8 rows (more rows
+    // of 128 dims: half of the dims at a time).  A row's groups of 8 floats are XORed by its
+    // number, which keeps stores and loads clear of bank conflicts.
+    const int dims = rows > 8 ? min(64, HD) : HD;
+    for (int d0 = 0; d0 < HD; d0 += dims) {
 #pragma unroll
-    for (int d0 = 0; d0 < HD; d0 += MM_JOIN) {
-      __syncthreads();  // the round before is read
-#pragma unroll
-      for (int i = 0; i < MM_JOIN / 8; ++i) {
-        const float* x = o[d0 / 8 + i];
-        float* j0 = join + (warp * MM_ROWS + gid) * MM_JOIN_LD + 8 * i + 2 * tig;
-        if (gid < rows) *reinterpret_cast<float2*>(j0) = make_float2(x[0], x[1]);
-        if (gid + 8 < rows) *reinterpret_cast<float2*>(j0 + 8 * MM_JOIN_LD) = make_float2(x[2], x[3]);
-      }
+      for (int i = 0; i < HD / 8; ++i)
+        if (8 * i >= d0 && 8 * i < d0 + dims) {
+          float* j0 = join + warp * MM_JOIN + gid * dims + ((8 * i - d0) ^ ((gid & 3) * 8)) + 2 * tig;
+          if (gid < rows) *reinterpret_cast<float2*>(j0) = make_float2(o[i][0], o[i][1]);
+          if (gid + 8 < rows) *reinterpret_cast<float2*>(j0 + 8 * dims) = make_float2(o[i][2], o[i][3]);
+        }
       __syncthreads();
-      for (int i = tid; i < rows * (MM_JOIN / 4); i += MM_THREADS) {
-        const int r = i / (MM_JOIN / 4), c = (i % (MM_JOIN / 4)) * 4;
+      const int quads = dims / 4;
+      for (int i = tid; i < rows * quads; i += MM_THREADS) {
+        const int r = i / quads, c = (i - r * quads) * 4;
         float top = s_m[0][r];
 #pragma unroll
         for (int k = 1; k < MM_WARPS; ++k) top = fmaxf(top, s_m[k][r]);
@@ -223,17 +230,17 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
 #pragma unroll
         for (int k = 0; k < MM_WARPS; ++k) {
           const float f = ex2_fast(s_m[k][r] - base);
-          const float4 y = *reinterpret_cast<const float4*>(join + (k * MM_ROWS + r) * MM_JOIN_LD + c);
+          const float4 y = *reinterpret_cast<const float4*>(join + k * MM_JOIN + r * dims + (c ^ ((r & 3) * 8)));
           sum = fmaf(f, s_l[k][r], sum);
           x.x = fmaf(f, y.x, x.x), x.y = fmaf(f, y.y, x.y), x.z = fmaf(f, y.z, x.z), x.w = fmaf(f, y.w, x.w);
         }
         const float inv = sum > 0.f ? 1.f / sum : sum;  // (NaN stays NaN)
-        const size_t at = static_cast<size_t>(p.slot) * MM_ROWS + r;
+        const size_t at = static_cast<size_t>(slot) * MM_ROWS + r;
         *reinterpret_cast<float4*>(w.o + at * HD + d0 + c) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-        if (d0 == 0 && c == 0) w.lse2[at] = top + log2f(sum);
+        if (d0 + c == 0) w.lse2[at] = top + log2f(sum);
       }
+      __syncthreads();  // the buffer and the warps' maxima and sums are read
     }
-    __syncthreads();  // s_m, s_l and the last round are read
   }
   cp_async_wait<0>();
 }

@@ -498,30 +498,48 @@ def zsaa_op_colmass_ex(qkv, lse, B: int, N: int, Hq: int, Hkv: int, hd: int, dty
 
 # ------------------------------------------------------------------ paged caches and beams
 
-def _at(t, dtypes, n, name, current):
-    """Pointer of a contiguous tensor of at least n elements on the current device
-    (an int or None passes as it is)."""
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype not in dtypes or not t.is_cuda or t.get_device() != current or not t.is_contiguous() or t.numel() < n:
-        raise ZsaaError(ZSAA_ERR_INVALID_ARG,
-                        f"{name}: needs a contiguous tensor of {dtypes} with {n} or more elements on the current device")
-    return t.data_ptr()
+def _at(t, dtype, n, name, dev):
+    """Pointer of a contiguous tensor of at least n elements on device `dev`, the
+    current one (an int or None passes as it is)."""
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= n:
+            return t.data_ptr()
+    except AttributeError:
+        if t is None or isinstance(t, int):
+            return t
+    raise ZsaaError(ZSAA_ERR_INVALID_ARG,
+                    f"{name}: needs a contiguous {dtype} tensor with {n} or more elements on the current device")
 
 
-_HAS_GPU = None
+def _flags(t, n, name, dev):
+    """_at for flags: uint8 or bool."""
+    if t is not None and not isinstance(t, int) and t.element_size() == 1 and not t.dtype.is_signed:
+        return _at(t, t.dtype, n, name, dev)
+    return _at(t, _types()[2], n, name, dev)
 
 
-def _torch():
-    global _HAS_GPU
-    import torch
-    if _HAS_GPU is None:
-        _HAS_GPU = torch.cuda.is_available()
-    return torch, torch.cuda.current_device() if _HAS_GPU else -1
+_TORCH = None
 
 
-def _stored(torch, dtype):
-    return (torch.bfloat16,) if dtype == ZSAA_BF16 else (torch.float32,)
+def _types():
+    """(float32, int32, uint8, bfloat16, the current device's number, the current
+    stream's handle by device number); torch is imported with the first call."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        if torch.cuda.is_available():
+            device, stream = torch.cuda.current_device, lambda dev: torch.cuda.current_stream(dev).cuda_stream
+        else:
+            device, stream = (lambda: -2), (lambda dev: None)  # (no tensor is on device -2)
+        # the same two in one call each, where torch has them
+        device = getattr(torch._C, "_cuda_getDevice", device) if torch.cuda.is_available() else device
+        stream = getattr(torch._C, "_cuda_getCurrentRawStream", stream) if torch.cuda.is_available() else stream
+        _TORCH = (torch.float32, torch.int32, torch.uint8, torch.bfloat16, device, stream)
+    return _TORCH
+
+
+def _here(stream, dev, current):
+    return current(dev) if stream is None else _stream(stream)
 
 
 def make_pages(k, v) -> zsaa_pages:
@@ -534,7 +552,7 @@ def make_pages(k, v) -> zsaa_pages:
     n_pages, heads, page, hd = k.shape
     p = zsaa_pages(k.data_ptr(), v.data_ptr(), n_pages, page, heads, hd,
                    ZSAA_BF16 if k.dtype == torch.bfloat16 else ZSAA_F32)
-    p.tensors = (k, v)
+    p.tensors, p.device = (k, v), k.get_device()
     return p
 
 
@@ -543,31 +561,31 @@ def make_pages_list(ks, vs):
     pages = [make_pages(k, v) for k, v in zip(ks, vs)]
     if not pages or len(ks) != len(vs):
         raise ZsaaError(ZSAA_ERR_INVALID_ARG, "one key and one value pool for each layer")
+    if any(p.device != pages[0].device for p in pages):
+        raise ZsaaError(ZSAA_ERR_INVALID_ARG, "the layers' pools are on different devices")
     arr = (zsaa_pages * len(pages))(*pages)
-    arr.tensors = [p.tensors for p in pages]
+    arr.tensors, arr.device = [p.tensors for p in pages], pages[0].device
     return arr
 
 
-def _pools_here(kv, current):
+def _pools_here(kv, dev):
     """The pools' tensors, where the struct has them, lie on the current device."""
-    held = getattr(kv, "tensors", None)
-    if held:
-        first = held[0][0] if isinstance(held, list) else held[0]
-        if first.get_device() != current:
-            raise ZsaaError(ZSAA_ERR_INVALID_ARG, "the pools are not on the current device")
+    if getattr(kv, "device", dev) != dev:
+        raise ZsaaError(ZSAA_ERR_INVALID_ARG, "the pools are not on the current device")
 
 
 def zsaa_op_paged_append(kv: zsaa_pages, qkv, ld: int, qkv_dtype: int, T: int, Hq: int, pos, rope_theta: float, cu_rows,
                          S: int, table, cols: int, lens, q_out=None, stream=None):
-    torch, dev = _torch()
-    i32 = (torch.int32,)
+    f32, i32, _, bf16, device, current = _types()
+    dev = device()
     _pools_here(kv, dev)
-    width = (Hq + 2 * kv.n_kv_heads) * kv.head_dim
+    hd = kv.head_dim
     _check(lib().zsaa_op_paged_append(
-        C.addressof(kv), _at(qkv, _stored(torch, qkv_dtype), (T - 1) * ld + width, "qkv", dev), ld, qkv_dtype, T, Hq,
-        _at(pos, i32, T, "pos", dev), rope_theta, _at(cu_rows, i32, S + 1, "cu_rows", dev), S,
+        C.addressof(kv),
+        _at(qkv, bf16 if qkv_dtype == ZSAA_BF16 else f32, (T - 1) * ld + (Hq + 2 * kv.n_kv_heads) * hd, "qkv", dev), ld,
+        qkv_dtype, T, Hq, _at(pos, i32, T, "pos", dev), rope_theta, _at(cu_rows, i32, S + 1, "cu_rows", dev), S,
         _at(table, i32, S * cols, "table", dev), cols, _at(lens, i32, S, "lens", dev),
-        _at(q_out, _stored(torch, kv.dtype), T * Hq * kv.head_dim, "q_out", dev), _stream(stream)))
+        _at(q_out, bf16 if kv.dtype == ZSAA_BF16 else f32, T * Hq * hd, "q_out", dev), _here(stream, dev, current)))
 
 
 def zsaa_op_paged_attention_workspace(kv: zsaa_pages, S: int, n_q: int, Hq: int, G: int, cols: int,
@@ -579,17 +597,21 @@ def zsaa_op_paged_attention_workspace(kv: zsaa_pages, S: int, n_q: int, Hq: int,
 
 def zsaa_op_paged_attention(kv: zsaa_pages, q, S: int, n_q: int, Hq: int, table, cols: int, lens, cu_seqs, G: int,
                             prefix_table, prefix_cols: int, prefix_lens, out, lse, ws, ws_bytes: int, stream=None):
-    torch, dev = _torch()
-    i32, own = (torch.int32,), _stored(torch, kv.dtype)
+    f32, i32, u8, bf16, device, current = _types()
+    dev = device()
     _pools_here(kv, dev)
-    rows = S * n_q * Hq
+    own, rows = bf16 if kv.dtype == ZSAA_BF16 else f32, S * n_q * Hq
+    n = rows * kv.head_dim
+    if G > 0:
+        cu_seqs = _at(cu_seqs, i32, G + 1, "cu_seqs", dev)
+        prefix_table = _at(prefix_table, i32, G * prefix_cols, "prefix_table", dev)
+        prefix_lens = _at(prefix_lens, i32, G, "prefix_lens", dev)
+    else:
+        cu_seqs = prefix_table = prefix_lens = None
     _check(lib().zsaa_op_paged_attention(
-        C.addressof(kv), _at(q, own, rows * kv.head_dim, "q", dev), S, n_q, Hq, _at(table, i32, S * cols, "table", dev),
-        cols, _at(lens, i32, S, "lens", dev), _at(cu_seqs, i32, G + 1, "cu_seqs", dev), G,
-        _at(prefix_table, i32, G * prefix_cols, "prefix_table", dev), prefix_cols,
-        _at(prefix_lens, i32, G, "prefix_lens", dev), _at(out, own, rows * kv.head_dim, "out", dev),
-        _at(lse, (torch.float32,), rows, "lse", dev), _at(ws, (torch.uint8,), ws_bytes, "ws", dev), ws_bytes,
-        _stream(stream)))
+        C.addressof(kv), _at(q, own, n, "q", dev), S, n_q, Hq, _at(table, i32, S * cols, "table", dev), cols,
+        _at(lens, i32, S, "lens", dev), cu_seqs, G, prefix_table, prefix_cols, prefix_lens, _at(out, own, n, "out", dev),
+        _at(lse, f32, rows, "lse", dev), _at(ws, u8, ws_bytes, "ws", dev), ws_bytes, _here(stream, dev, current)))
 
 
 def zsaa_op_beam_select_workspace(B: int, W: int, V: int, K: int) -> int:
@@ -600,27 +622,28 @@ def zsaa_op_beam_select_workspace(B: int, W: int, V: int, K: int) -> int:
 
 def zsaa_op_beam_select(logits, ld: int, B: int, W: int, V: int, scores, done, eos: int, K: int, scores_out, parent,
                         token, done_out, ws, ws_bytes: int, stream=None):
-    torch, dev = _torch()
-    f32, i32, flag = (torch.float32,), (torch.int32,), (torch.uint8, torch.bool)
+    """done, done_out: uint8 or bool."""
+    f32, i32, u8, _, device, current = _types()
+    dev = device()
+    n = B * K
     _check(lib().zsaa_op_beam_select(
         _at(logits, f32, (B * W - 1) * ld + V, "logits", dev), ld, B, W, V, _at(scores, f32, B * W, "scores", dev),
-        _at(done, flag, B * W, "done", dev), eos, K, _at(scores_out, f32, B * K, "scores_out", dev),
-        _at(parent, i32, B * K, "parent", dev), _at(token, i32, B * K, "token", dev),
-        _at(done_out, flag, B * K, "done_out", dev), _at(ws, (torch.uint8,), ws_bytes, "ws", dev), ws_bytes,
-        _stream(stream)))
+        _flags(done, B * W, "done", dev), eos, K, _at(scores_out, f32, n, "scores_out", dev),
+        _at(parent, i32, n, "parent", dev), _at(token, i32, n, "token", dev), _flags(done_out, n, "done_out", dev),
+        _at(ws, u8, ws_bytes, "ws", dev), ws_bytes, _here(stream, dev, current)))
 
 
 def zsaa_op_beam_reorder(layers, B: int, W: int, K: int, parent, table, table_out, cols: int, lens, lens_out, fresh,
                          stream=None):
     """layers: what make_pages_list returns (or a ctypes array of zsaa_pages)."""
-    torch, dev = _torch()
-    i32 = (torch.int32,)
+    _, i32, _, _, device, current = _types()
+    dev = device()
     _pools_here(layers, dev)
     _check(lib().zsaa_op_beam_reorder(
         C.addressof(layers), len(layers), B, W, K, _at(parent, i32, B * K, "parent", dev),
         _at(table, i32, B * W * cols, "table", dev), _at(table_out, i32, B * K * cols, "table_out", dev), cols,
         _at(lens, i32, B * W, "lens", dev), _at(lens_out, i32, B * K, "lens_out", dev),
-        _at(fresh, i32, B * K, "fresh", dev), _stream(stream)))
+        _at(fresh, i32, B * K, "fresh", dev), _here(stream, dev, current)))
 
 
 def zsaa_device_status():
