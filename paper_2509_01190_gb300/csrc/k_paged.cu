@@ -23,11 +23,14 @@ namespace {
 
 // RPC rows per CTA, kAppendThreads threads.  A thread handles 8 dims of a head's first
 // half and the 8 that they pair with, so a rotation is thread-local; the row's sines
-// and cosines (one set for all heads) go through shared memory.
+// and cosines (one set for all heads) go through shared memory.  A thread's first loads are
+// out before the sines and the lookup of the entries.
 // Angle: the position times the frequency in 2^-64 turns, modulo a turn, is one 64-bit
 // product: exact for every 32-bit position.  The nearest quarter turn is taken off
 // before the conversion to float, so sine and cosine are good to about 1e-7.
-// Bound by bytes on prompts, by the chain table -> address -> store on single tokens.
+// Bound by bytes on prompts (9000 rows of 6144 bf16: 35 us, 5.8 TB/s; more units a thread in
+// flight cost occupancy and up to twice that), by the chain table -> address -> store on
+// single tokens (8 rows: 2.5 us).
 constexpr int kAppendThreads = 256;
 
 template <typename TI>
@@ -66,19 +69,42 @@ __device__ __forceinline__ float2 turn_cos_sin(unsigned long long turn) {
 }
 
 template <typename TI, typename TO, int HD, int RPC>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, RPC == 1 ? 1 : 8)
     append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ RopeTurns turns) {
   constexpr int HALF = HD / 2, UNITS = HALF / 8;  // 8-dim pairs of a head
-  __shared__ float2 cs[RPC][HALF];
+  constexpr int BATCH = RPC == 1 ? 2 : 1;  // units of a thread in flight
+  __shared__ float2 cs[RPC][HALF];  // dim 8 u + j at j * UNITS + u: a warp's reads fall into different banks
   __shared__ long long s_at[RPC];  // element offset of the row's entry for head 0, or -1
   pdl_trigger();
   pdl_wait();
   const int tid = threadIdx.x;
   const int row0 = blockIdx.x * RPC, n = min(RPC, a.T - row0);
+  const int h0 = a.q_out != nullptr ? 0 : a.Hq, per_row = (a.Hq + 2 * a.Hkv - h0) * UNITS, all = n * per_row;
+  const TI* src = after_wait(static_cast<const TI*>(a.qkv));
+  struct Unit {
+    int r, h, c;  // row of the CTA, head, first dim
+  };
+  auto unit = [&](int i) {
+    const int r = RPC == 1 ? 0 : static_cast<int>(static_cast<unsigned>(i) / static_cast<unsigned>(per_row)), k = i - r * per_row;
+    return Unit{r, h0 + k / UNITS, (k % UNITS) * 8};
+  };
+  float x[BATCH][8], y[BATCH][8];
+  auto load = [&](int base) {
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = base + b * kAppendThreads + tid;
+      if (i >= all) continue;
+      const Unit u = unit(i);
+      const TI* p = src + static_cast<long long>(row0 + u.r) * a.ld + u.h * HD + u.c;
+      load8(p, x[b]);
+      load8(p + HALF, y[b]);
+    }
+  };
+  load(0);
   const int32_t* pos = after_wait(a.pos);
   for (int i = tid; i < n * HALF; i += kAppendThreads) {
     const int r = i / HALF, c = i % HALF;
-    cs[r][c] = turn_cos_sin(static_cast<unsigned long long>(static_cast<long long>(pos[row0 + r])) * turns.f[c]);
+    cs[r][(c & 7) * UNITS + (c >> 3)] = turn_cos_sin(static_cast<unsigned long long>(static_cast<long long>(pos[row0 + r])) * turns.f[c]);
   }
   if (tid < n) {
     const int t = row0 + tid;
@@ -108,45 +134,43 @@ __global__ void __launch_bounds__(kAppendThreads)
     s_at[tid] = at;
   }
   __syncthreads();
-  const int h0 = a.q_out != nullptr ? 0 : a.Hq, heads = a.Hq + 2 * a.Hkv - h0;
-  const int per_row = heads * UNITS;
-  const TI* src = after_wait(static_cast<const TI*>(a.qkv));
-  for (int i = tid; i < n * per_row; i += kAppendThreads) {
-    const int r = i / per_row, k = i % per_row;
-    const int h = h0 + k / UNITS, c = (k % UNITS) * 8;
-    const long long at = s_at[r];
-    if (at < 0) continue;
-    const TI* p = src + static_cast<long long>(row0 + r) * a.ld + h * HD + c;
-    float x[8], y[8];
-    load8(p, x);
-    load8(p + HALF, y);
-    if (h < a.Hq + a.Hkv) {
+  for (int base = 0; base < all; base += BATCH * kAppendThreads) {
+    if (base > 0) load(base);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 w = cs[r][c + j];
-        const float u = x[j] * w.x - y[j] * w.y, v = y[j] * w.x + x[j] * w.y;
-        x[j] = u;
-        y[j] = v;
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = base + b * kAppendThreads + tid;
+      if (i >= all) continue;
+      const Unit u = unit(i);
+      const long long at = s_at[u.r];
+      if (at < 0) continue;
+      if (u.h < a.Hq + a.Hkv) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 w = cs[u.r][j * UNITS + (u.c >> 3)];
+          const float p = x[b][j] * w.x - y[b][j] * w.y, q = y[b][j] * w.x + x[b][j] * w.y;
+          x[b][j] = p;
+          y[b][j] = q;
+        }
       }
+      TO* d;
+      if (u.h < a.Hq) {
+        d = static_cast<TO*>(a.q_out) + (static_cast<long long>(row0 + u.r) * a.Hq + u.h) * HD;
+      } else {
+        const bool key = u.h < a.Hq + a.Hkv;
+        const int g = u.h - a.Hq - (key ? 0 : a.Hkv);
+        d = static_cast<TO*>(key ? a.k : a.v) + at + ((static_cast<long long>(g) << a.page_shift) * HD);
+      }
+      store8(d + u.c, x[b]);
+      store8(d + u.c + HALF, y[b]);
     }
-    TO* d;
-    if (h < a.Hq) {
-      d = static_cast<TO*>(a.q_out) + (static_cast<long long>(row0 + r) * a.Hq + h) * HD;
-    } else {
-      const bool key = h < a.Hq + a.Hkv;
-      const int g = h - a.Hq - (key ? 0 : a.Hkv);
-      d = static_cast<TO*>(key ? a.k : a.v) + at + ((static_cast<long long>(g) << a.page_shift) * HD);
-    }
-    store8(d + c, x);
-    store8(d + c + HALF, y);
   }
 }
 
 template <typename TI, typename TO, int HD>
 cudaError_t run_append(const AppendArgs& a, const RopeTurns& t, int sms, cudaStream_t s) {
-  // four rows per CTA share its prologue; fewer rows than would fill the SMs so go one by one
+  // two rows per CTA share its prologue; fewer rows than would fill the SMs so go one by one
   if (a.T >= 8 * sms)
-    ZSAA_LAUNCH(append_kernel<TI, TO, HD, 4>, dim3((a.T + 3) / 4), dim3(kAppendThreads), 0, s, a, t);
+    ZSAA_LAUNCH(append_kernel<TI, TO, HD, 2>, dim3((a.T + 1) / 2), dim3(kAppendThreads), 0, s, a, t);
   else
     ZSAA_LAUNCH(append_kernel<TI, TO, HD, 1>, dim3(a.T), dim3(kAppendThreads), 0, s, a, t);
   return cudaSuccess;
