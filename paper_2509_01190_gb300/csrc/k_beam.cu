@@ -269,23 +269,30 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   for (int w = 1; w < kScanWarps; ++w) lowest = min(lowest, s_least[w]);
   if (static_cast<uint32_t>(bound >> 32) == lowest)
     bound = static_cast<uint64_t>(lowest) << 32 | static_cast<uint32_t>(~(max(start, 0) + 2 * K - 1));
+  // The values of the threads whose maximum, at its first place, reaches the bound: the
+  // whole warp looks at them, a group a lane, in a round trip or two.
   auto collect = [&](uint64_t from) {
-    // the thread's maximum at its first place: the most that a value of it can be
-    if (value_at(best, max(place(0, 0), 0)) < from) return;
-    for (int t = 0; t < n_tiles; ++t) {
-      float4 g[GROUPS];
-      load(t, g);
+    const unsigned todo = __ballot_sync(0xffffffffu, value_at(best, max(place(0, 0), 0)) >= from);
+    const unsigned per = n_tiles * GROUPS, all = __popc(todo) * per;
+    for (unsigned e = lane; e < all; e += 32) {
+      const unsigned k = e / per, g = e - k * per;  // the k-th of those threads, its group
+      unsigned t = todo;
+      for (unsigned i = 0; i < k; ++i) t &= t - 1;
+      const int u = start + (warp * 32 + __ffs(t) - 1) * 4 + static_cast<int>(g / GROUPS * kScanTile + g % GROUPS * STEP);
+      float v[4];
+      if (u >= 0 && u <= V - 4) {
+        const float4 x = __ldg(reinterpret_cast<const float4*>(p + u));
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+      } else {
 #pragma unroll
-      for (int i = 0; i < GROUPS; ++i) {
-        const float v[4] = {fmaxf(g[i].x, -INFINITY), fmaxf(g[i].y, -INFINITY), fmaxf(g[i].z, -INFINITY), fmaxf(g[i].w, -INFINITY)};
-        if (value_at(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), max(place(t, i), 0)) < from) continue;
+        for (int j = 0; j < 4; ++j) v[j] = u + j >= 0 && u + j < V ? p[u + j] : -INFINITY;
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint64_t x = value_at(v[j], place(t, i) + j);
-          if (x >= from) {
-            const int n = atomicAdd(&s_count, 1);
-            if (n < kListCap) list[n] = x;
-          }
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t x = value_at(fmaxf(v[j], -INFINITY), u + j);
+        if (x >= from) {
+          const int n = atomicAdd(&s_count, 1);
+          if (n < kListCap) list[n] = x;
         }
       }
     }
@@ -362,25 +369,22 @@ __global__ void __launch_bounds__(kMergeThreads)
   for (int i = tid; i < n; i += kMergeThreads) rank[i] = i % K;  // its place in its own beam's list
   if (warp < kSumWarps) {
     for (int w = warp; w < W; w += kSumWarps) {
+      // (every load of a beam in one round trip: what an ended one's are is of no account)
       const BeamChunk* st = stat + w * chunks;
+      BeamChunk first = lane < chunks ? st[lane] : BeamChunk{0, -INFINITY, 0};
       const bool over = done != nullptr && done[b * W + w] != 0;
       const float score = scores == nullptr ? 0.f : scores[b * W + w];
-      float top = -INFINITY;
-      int bad = 0;
-      if (!over)
-        for (int c = lane; c < chunks; c += 32) {
-          const BeamChunk x = st[c];
-          top = fmaxf(top, x.n2);
-          bad |= x.bad;
-        }
+      float top = first.n2;
+      int bad = first.bad;
+      for (int c = lane + 32; c < chunks; c += 32) {
+        const BeamChunk x = st[c];
+        top = fmaxf(top, x.n2);
+        bad |= x.bad;
+      }
       top = warp_max(top);
       bad = __any_sync(0xffffffffu, bad);
-      uint64_t sum = 0;
-      if (!over)
-        for (int c = lane; c < chunks; c += 32) {
-          const BeamChunk x = st[c];
-          sum += down_by(x.sum, top - x.n2);
-        }
+      uint64_t sum = down_by(first.sum, top - first.n2);
+      for (int c = lane + 32; c < chunks; c += 32) sum += down_by(st[c].sum, top - st[c].n2);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       if (lane == 0) {
@@ -416,15 +420,10 @@ __global__ void __launch_bounds__(kMergeThreads)
       const uint2* lists = cand + static_cast<size_t>(w) * chunks * K;
       const uint2* so_far = nullptr;
       uint2* mine = cache + (warp - kSumWarps) * kMergeDepth * 64 + lane;
-      if (done != nullptr && done[b * W + w] != 0) {  // eos at no cost; the other tokens, in their order, are not allowed
-        for (int k = lane; k < K; k += 32)
-          row[k] = k >= V ? make_uint2(0, 0)
-                          : make_uint2(k == 0 ? 0x80000000u : 0x007fffffu, k == 0 ? eos : k - 1 < eos ? k - 1 : k);
-        continue;
-      }
+      const bool over = done != nullptr && done[b * W + w] != 0;
       for (int c0 = 0; c0 < chunks; c0 += 63) {
         uint2* to = c0 + 63 >= chunks ? row : merged + ((warp - kSumWarps) * 2 + (c0 / 63) % 2) * K;
-        const uint2* at[2];
+        const uint2* at[2] = {nullptr, nullptr};
         int pos[2] = {0, 0};
         uint2 head[2];
         auto load = [&](int i) {
@@ -442,6 +441,7 @@ __global__ void __launch_bounds__(kMergeThreads)
           for (int k = 0; k < kMergeDepth; ++k) mine[k * 64 + 32 * i] = x[k];
           head[i] = x[0];
         }
+        if (over) break;
         for (int k = 0; k < K; ++k) {
           const uint32_t x = __reduce_max_sync(0xffffffffu, max(head[0].x, head[1].x));
           const unsigned m0 = __ballot_sync(0xffffffffu, head[0].x == x), m1 = __ballot_sync(0xffffffffu, head[1].x == x);
@@ -460,6 +460,10 @@ __global__ void __launch_bounds__(kMergeThreads)
         __syncwarp();
         so_far = to;
       }
+      if (over)  // eos at no cost; the other tokens, in their order, are not allowed
+        for (int k = lane; k < K; k += 32)
+          row[k] = k >= V ? make_uint2(0, 0)
+                          : make_uint2(k == 0 ? 0x80000000u : 0x007fffffu, k == 0 ? eos : k - 1 < eos ? k - 1 : k);
     }
   }
   __syncthreads();

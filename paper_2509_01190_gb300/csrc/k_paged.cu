@@ -28,7 +28,7 @@ namespace {
 // Angle: the position times the frequency in 2^-64 turns, modulo a turn, is one 64-bit
 // product: exact for every 32-bit position.  The nearest quarter turn is taken off
 // before the conversion to float, so sine and cosine are good to about 1e-7.
-// Bound by bytes on prompts (9000 rows of 6144 bf16: 35 us, 5.8 TB/s; more units a thread in
+// Bound by bytes on prompts (8411 rows of 6144 bf16: 35 us, 5.8 TB/s; more units a thread in
 // flight cost occupancy and up to twice that), by the chain table -> address -> store on
 // single tokens (8 rows: 2.5 us).
 constexpr int kAppendThreads = 256;
