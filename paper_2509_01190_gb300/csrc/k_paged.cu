@@ -527,7 +527,7 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   for (int i = 0; i < r.n; ++i) {
     const bool pre = i == 0, seq = i == r.n - 1;
     r.tc[i] = pre ? tc_pre : tc_seq;
-    r.tiles[i] = !bf ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 4} : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
+    r.tiles[i] = !bf ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 1} : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
     r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
     const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
     const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
 }  // namespace
 
 PagedTiles paged_mma_tiles(int hd, int sms) {
-  return PagedTiles{MM_ROWS, MM_KEYS, (hd == 128 ? MmCfg<128>::CTAS : MmCfg<64>::CTAS) * sms, 2};
+  return PagedTiles{MM_ROWS, MM_KEYS, (hd == 128 ? MmCfg<128>::CTAS : MmCfg<64>::CTAS) * sms, 1};
 }
 
 template <int HD>
