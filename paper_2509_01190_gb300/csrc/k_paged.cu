@@ -513,15 +513,24 @@ struct Launches {
   long long most;  // items and blocks that number the slots and the line
 };
 
-// Rows of an entry for a KV head from which the 128-row tiles are taken.
-constexpr int kTcRows = 17;
+// The 128-row tiles take entries whose 16-row tiles would have more than six blocks of 64
+// keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64, by the tables' sizes): where
+// a head has 32 to 256 rows to a prefix of 32 to 16384 keys, in 1 to 16 groups of up to 8
+// KV heads, the whole call took the same time there.  With 8 heads of 128 dims, 128 rows,
+// 16-row and 128-row tiles: 512 keys 16 and 22 us, 1024 20 and 23, 2048 27 and 24, 8192 79
+// and 34.  Up to 16 rows there is one 16-row tile and nothing to gain.
+bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int heads) {
+  return rows > 16 && row_tiles * heads * (keys / 64) > (hd == 128 ? 6 * 304 : 6 * 456);
+}
 
 Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   Launches r{};
   const long long row = static_cast<long long>(a.n_q) * a.per;
   const bool bf = dtype == ZSAA_BF16;
-  const bool tc_seq = bf && row >= kTcRows;
-  const bool tc_pre = a.G > 0 ? bf && a.S * row >= static_cast<long long>(kTcRows) * a.G : tc_seq;  // on average
+  const bool tc_seq = bf && many_rows(hd, a.S * ((row + 15) / 16), row, static_cast<long long>(a.cols) << a.page_shift, a.Hkv);
+  const bool tc_pre = a.G == 0 ? tc_seq
+                               : bf && many_rows(hd, std::max(a.S * row / 16, static_cast<long long>(a.G)), a.S * row / a.G,
+                                                 static_cast<long long>(a.pcols) << a.page_shift, a.Hkv);
   r.n = tc_seq == tc_pre ? 1 : 2;
   uintptr_t at = reinterpret_cast<uintptr_t>(ws);
   for (int i = 0; i < r.n; ++i) {

@@ -117,6 +117,9 @@ CASES = [
     ("bf16", 32, 8, 128, 128, 1, [6000], None, None),                   # one sequence over all SMs
     ("bf16", 8, 2, 64, 16, 5, [33] * 9, [0, 9], [4100]),
     ("bf16", 16, 16, 64, 16, 1, [100, 1, 63, 64, 65, 31], [0, 0, 6], [40, 16]),
+    ("bf16", 16, 2, 64, 16, 16, [16, 100, 3, 0], None, None),            # 128 rows of one sequence
+    ("bf16", 8, 1, 128, 32, 9, [9, 257, 30], [0, 2, 3], [128, 129]),
+    ("bf16", 5, 1, 64, 64, 3, [70, 3, 2], None, None),
     ("f32", 4, 4, 32, 16, 1, [1, 0, 50], None, None),
     ("f32", 4, 4, 32, 16, 3, [77, 3, 12, 40], [0, 1, 4], [413, 100]),
     ("f32", 8, 2, 64, 32, 1, [33, 64, 31], [0, 2, 3], [200, 0]),
@@ -126,16 +129,30 @@ CASES = [
 ]
 
 
+def widened(rows, cols):
+    """Table rows with room for more: what the call is planned for is the tables' width."""
+    return None if rows is None else [r + [-1] * (cols - len(r)) for r in rows]
+
+
+# Entries with more than 16 rows to a KV head take 128-row tiles where their tables are
+# wide: by the prefixes' tables alone, or (rows of one sequence) by both.
+ROOM = [(0, 0), (0, 4000), (4000, 4000)]
+
+
+@pytest.mark.parametrize("room", ROOM, ids=["", "wide_prefixes", "wide"])
 @pytest.mark.parametrize("dtype,Hq,Hkv,hd,page,n_q,lens,groups,plens", CASES)
-def test_attention(zlib, dtype, Hq, Hkv, hd, page, n_q, lens, groups, plens):
+def test_attention(zlib, dtype, Hq, Hkv, hd, page, n_q, lens, groups, plens, room):
+    if room != (0, 0) and (dtype == "f32" or (groups is None and room[0] == 0)):
+        pytest.skip("no other kernel")
     p, q, table, ptable = build(zlib, dtype, Hq, Hkv, hd, page, lens, n_q, groups, plens or ())
+    table, ptable = widened(table, room[0]), widened(ptable, room[1])
     out, lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
     check(p, q, table, lens, out, lse, groups, ptable, plens)
     again, lse2 = attend(zlib, p, q, table, lens, groups, ptable, plens)
     assert torch.equal(out, again) and torch.equal(lse, lse2), "two runs differ"
 
 
-@pytest.mark.parametrize("seed", range(8))
+@pytest.mark.parametrize("seed", range(16))
 def test_attention_of_drawn_sizes(zlib, seed):
     r = random.Random(seed)
     dtype = r.choice(["bf16", "bf16", "f32"])
@@ -146,14 +163,17 @@ def test_attention_of_drawn_sizes(zlib, seed):
     groups = sorted(r.randint(0, S) for _ in range(G + 1))
     plens = [r.choice([0, r.randint(1, 900)]) for _ in range(G)]
     p, q, table, ptable = build(zlib, dtype, Hkv * per, Hkv, hd, r.choice([16, 64]), lens, n_q, groups, plens, seed)
+    if seed % 2:
+        ptable = widened(ptable, 5000)
     out, lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
     check(p, q, table, lens, out, lse, groups, ptable, plens)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype):
+@pytest.mark.parametrize("dtype,cols", [("bf16", 10), ("bf16", 5000), ("f32", 10)])
+def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype, cols):
     lens, n_q = [20, 4, 35], 4
-    p, q, table, ptable = build(zlib, dtype, 4, 2, 64, 16, lens, n_q, [0, 3], [50])
+    p, q, table, ptable = build(zlib, dtype, 20, 2, 64, 16, lens, n_q, [0, 3], [50])
+    table, ptable = widened(table, cols), widened(ptable, cols)
     for s, n in enumerate(lens):  # the newest entry of every sequence
         page, off = table[s][(n - 1) // 16], (n - 1) % 16
         p.k[page, :, off] = float("nan")
@@ -167,9 +187,10 @@ def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype)
 @pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64)])
 def test_large_scores(zlib, dtype, hd):
     """Scores far apart, rising and falling along the keys: the running maximum moves
-    from block to block.  (Scaling keys by a power of two keeps products exact.)"""
-    for sign in (1.0, -1.0):
-        p, q, table, _ = build(zlib, dtype, 4, 1, hd, 16, [700], 1, seed=3)
+    from block to block."""
+    for sign, n_q, cols in ((1.0, 1, 50), (-1.0, 1, 50), (1.0, 5, 20000), (-1.0, 5, 20000)):
+        p, q, table, _ = build(zlib, dtype, 4, 1, hd, 16, [700], n_q, seed=3)
+        table = widened(table, cols)
         ramp = torch.linspace(0.0, 40.0, 700, device="cuda")
         for i in range(700):
             p.k[table[0][i // 16], :, i % 16] = sign * ramp[i] * (hd ** -0.5) * torch.sign(q[0, 0, 0]).to(p.k.dtype)
@@ -250,8 +271,10 @@ def test_pages_beyond_32_bit_offsets(zlib):
     check(small, q, [[2, 1, 0]], [T], out, lse)
 
 
-def test_bad_pages_and_lengths_are_reported(zlib):
-    p, q, table, ptable = build(zlib, "bf16", 4, 2, 64, 16, [40, 40], 1, [0, 2], [40])
+@pytest.mark.parametrize("cols", [3, 3000])
+def test_bad_pages_and_lengths_are_reported(zlib, cols):
+    p, q, table, ptable = build(zlib, "bf16", 40, 2, 64, 16, [40, 40], 1, [0, 2], [40])
+    table, ptable = widened(table, cols), widened(ptable, cols)
     p.k.nan_to_num_(0.0)
     p.v.nan_to_num_(0.0)
     keep = (p.k.clone(), p.v.clone())
@@ -283,8 +306,10 @@ def test_bad_pages_and_lengths_are_reported(zlib):
         assert torch.equal(changed, want)
 
 
-def test_group_bounds_that_run_backwards_stay_in_bounds(zlib):
-    p, q, table, ptable = build(zlib, "bf16", 4, 2, 64, 16, [20] * 4, 1, [0, 4], [40, 40, 40])
+@pytest.mark.parametrize("dtype,cols", [("bf16", 3), ("bf16", 3000), ("f32", 3)])
+def test_group_bounds_that_run_backwards_stay_in_bounds(zlib, dtype, cols):
+    p, q, table, ptable = build(zlib, dtype, 40, 2, 64, 16, [20] * 4, 1, [0, 4], [40, 40, 40])
+    ptable = widened(ptable, cols)
     for groups in ([4, 0, 4, 2], [-5, 9, 1, 4], [2 ** 31 - 1, -2 ** 31, 3, 4], [3, 1, 0, 0]):
         attend(zlib, p, q, table, [20] * 4, groups, ptable, [40, 40, 40])
         try:
