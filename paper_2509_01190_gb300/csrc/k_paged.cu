@@ -176,141 +176,6 @@ cudaError_t run_append(const AppendArgs& a, const RopeTurns& t, int sms, cudaStr
   return cudaSuccess;
 }
 
-// ---------------------------------------------------------------- attention, float32
-
-constexpr int kSimtThreads = 128, kSimtRows = 16, kSimtKeys = 32;
-
-// One part at a time: 16 query rows against blocks of 32 keys in shared memory, online
-// softmax (log2 domain) in 32 bits.
-template <int HD>
-__global__ void __launch_bounds__(kSimtThreads)
-    paged_simt_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
-  constexpr int MT = kSimtRows, BN = kSimtKeys, LD = HD + 4;
-  constexpr int QUADS = HD / 4, GROUPS = kSimtThreads / QUADS, RPG = MT / GROUPS;  // P V: 4 dims of RPG rows a thread
-  __shared__ __align__(16) float sq[MT][LD], sk[BN][LD], sv[BN][HD];
-  __shared__ float ss[MT][BN + 1], s_corr[MT], s_l[MT], s_m[MT];
-  const int tid = threadIdx.x;
-  pdl_trigger();
-  pdl_wait();
-  __shared__ PagedSpan told;
-  PagedSpan span;
-  if (!paged_plan<MT, BN>(a, w, told, span)) return;
-  const float* q = after_wait(static_cast<const float*>(a.q));
-  const float* K = after_wait(static_cast<const float*>(a.k));
-  const float* V = after_wait(static_cast<const float*>(a.v));
-  const int ty = tid >> 4, tx = tid & 15;           // scores: rows 2 ty, 2 ty + 1, keys tx, tx + 16
-  const int sr = tid >> 3, sc = (tid & 7) * 4;      // softmax: row, first of 4 keys
-  const int quad = (tid % QUADS) * 4, rg = tid / QUADS;
-  PagedPart p;
-  while (paged_next<MT, BN>(a, w, span, p)) {
-    const int rows = min(MT, p.x.rows - p.r * MT);
-    __syncthreads();  // the part before is done with shared memory
-    for (int i = tid; i < MT * (HD / 8); i += kSimtThreads) {
-      const int r = i / (HD / 8), c = (i % (HD / 8)) * 8;
-      float x[8] = {};
-      if (r < rows) load8(q + paged_q_at<HD>(a, p, p.r * MT + r) + c, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sq[r][c + j] = x[j];
-    }
-    const int32_t* table = paged_row(a, p);
-    float m = -INFINITY, l = 0.f;  // of row sr, the same in its 8 threads
-    float acc[RPG][4] = {};
-    for (int b = p.b0; b < p.b1; ++b) {
-      const int k0 = b * BN, keys = min(BN, p.x.keys - k0);
-      for (int i = tid; i < BN * (HD / 8); i += kSimtThreads) {
-        const int r = i / (HD / 8), c = (i % (HD / 8)) * 8;
-        float x[8] = {}, y[8] = {};
-        if (r < keys) {
-          const size_t at = paged_at<HD>(a, paged_page(a, table, k0 + r), p.h, k0 + r) + c;
-          load8(K + at, x);
-          load8(V + at, y);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sk[r][c + j] = x[j];
-          sv[r][c + j] = y[j];
-        }
-      }
-      __syncthreads();
-      float s[2][2] = {};
-#pragma unroll 4
-      for (int c = 0; c < HD; c += 4) {
-        const float4 q0 = *reinterpret_cast<const float4*>(&sq[2 * ty][c]);
-        const float4 q1 = *reinterpret_cast<const float4*>(&sq[2 * ty + 1][c]);
-        const float4 k0v = *reinterpret_cast<const float4*>(&sk[tx][c]);
-        const float4 k1v = *reinterpret_cast<const float4*>(&sk[tx + 16][c]);
-        auto dot = [](const float4& x, const float4& y, float z) {
-          return fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, z))));
-        };
-        s[0][0] = dot(q0, k0v, s[0][0]);
-        s[0][1] = dot(q0, k1v, s[0][1]);
-        s[1][0] = dot(q1, k0v, s[1][0]);
-        s[1][1] = dot(q1, k1v, s[1][1]);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) ss[2 * ty + i][tx + 16 * j] = tx + 16 * j < keys ? s[i][j] * a.scale_log2 : -INFINITY;
-      __syncthreads();
-      float v[4], mx = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = ss[sr][sc + j];
-        mx = fmaxf(mx, v[j]);
-      }
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      const float mn = fmaxf(m, mx), base = mn == -INFINITY ? 0.f : mn;
-      const float corr = exp2f(m - base);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = exp2f(v[j] - base);
-        sum += v[j];
-        ss[sr][sc + j] = v[j];
-      }
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      l = l * corr + sum;
-      m = mn;
-      if ((tid & 7) == 0) s_corr[sr] = corr;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < RPG; ++i) {
-        const float f = s_corr[rg * RPG + i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] *= f;
-      }
-      for (int k = 0; k < keys; ++k) {
-        const float4 x = *reinterpret_cast<const float4*>(&sv[k][quad]);
-#pragma unroll
-        for (int i = 0; i < RPG; ++i) {
-          const float pk = ss[rg * RPG + i][k];
-          acc[i][0] = fmaf(pk, x.x, acc[i][0]);
-          acc[i][1] = fmaf(pk, x.y, acc[i][1]);
-          acc[i][2] = fmaf(pk, x.z, acc[i][2]);
-          acc[i][3] = fmaf(pk, x.w, acc[i][3]);
-        }
-      }
-      __syncthreads();
-    }
-    if ((tid & 7) == 0) {
-      s_l[sr] = l;
-      s_m[sr] = m;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < RPG; ++i) {
-      const int r = rg * RPG + i;
-      if (r >= rows) continue;
-      const float inv = s_l[r] > 0.f ? 1.f / s_l[r] : s_l[r];  // (NaN stays NaN)
-      float* o = w.o + (static_cast<size_t>(p.slot) * MT + r) * HD + quad;
-      *reinterpret_cast<float4*>(o) = make_float4(acc[i][0] * inv, acc[i][1] * inv, acc[i][2] * inv, acc[i][3] * inv);
-      if (quad == 0) w.lse2[static_cast<size_t>(p.slot) * MT + r] = s_m[r] + log2f(s_l[r]);
-    }
-  }
-}
-
 // ---------------------------------------------------------------- joining the partial results
 
 constexpr int kJoinThreads = 128;
@@ -366,34 +231,19 @@ __global__ void __launch_bounds__(kJoinThreads, 4)
   pdl_trigger();
   if (h >= Hq) return;
   const int s = token / a.n_q, j = token - s * a.n_q, g = h / a.per;
-  const long long row = static_cast<long long>(token) * Hq + h;
   pdl_wait();
-  const int cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
+  const int len = min(a.lens[s], a.cols << a.page_shift);
   const int own_per = ws.head[0], own_t = ws.head[1 + a.G + s - ws.e0];
   JoinParts shared{nullptr, nullptr, 0, 0};
   if (a.G > 0) {
-    const int pre_per = wp.head[0], end = paged_group_at(a, a.G);
-    int found = -1, g0 = 0, g1 = 0, plen = 0, pre_t = 0;  // the last group that starts at or before s
-    for (int i = 0; i < a.G; i += 32) {
-      const int e = min(i + lane, a.G - 1);
-      const int c0 = paged_group_at(a, e), c1 = paged_group_at(a, e + 1), pl = a.plens[e], pt = wp.head[1 + e - wp.e0];
-      const unsigned m = __ballot_sync(0xffffffffu, i + lane < a.G && c0 <= s);
-      if (m == 0) break;
-      const int src = 31 - __clz(m);
-      found = i + src;
-      g0 = __shfl_sync(0xffffffffu, c0, src);
-      g1 = __shfl_sync(0xffffffffu, c1, src);
-      plen = __shfl_sync(0xffffffffu, pl, src);
-      pre_t = __shfl_sync(0xffffffffu, pt, src);
-    }
-    if (found < 0 || s >= end) return;  // a row behind the last sequence stays as it was
-    const int most = a.pcols << a.page_shift;
-    const PagedEntry x{min(max(plen, 0), most), max(0, g1 - g0) * a.n_q * a.per, g0};
-    const int rr = ((s - g0) * a.n_q + j) * a.per + h % a.per;
-    if (lane == 0 && (plen > most || rr >= x.rows)) atomicOr(a.status, kStatusBadIndex);  // (bounds that run backwards)
-    if (rr < x.rows) shared = join_parts(a, wp, found, x, pre_per, pre_t, g, rr, HD);
+    const int pre_per = wp.head[0];
+    const PagedGroup x = paged_group_of(a, s, wp.head + 1 - wp.e0);
+    if (x.g < 0) return;  // a row behind the last sequence stays as it was
+    const PagedEntry e{x.keys, max(0, x.end - x.seq0) * a.n_q * a.per, x.seq0};
+    const int rr = ((s - x.seq0) * a.n_q + j) * a.per + h % a.per;
+    if (lane == 0 && (x.beyond || rr >= e.rows)) atomicOr(a.status, kStatusBadIndex);  // (bounds that run backwards)
+    if (rr < e.rows) shared = join_parts(a, wp, x.g, e, pre_per, x.t0, g, rr, HD);
   }
-  if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
   const PagedEntry mine{max(0, len - (a.n_q - 1)), a.n_q * a.per, s};
   const JoinParts own = join_parts(a, ws, a.G + s, mine, own_per, own_t, g, j * a.per + h % a.per, HD);
 
@@ -429,39 +279,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4)
       }
     }
   }
-  const size_t q_at = static_cast<size_t>(row) * HD + lane * DPL;
-  if (a.n_q > 1) {
-    float q[DPL];
-#pragma unroll
-    for (int d = 0; d < DPL; ++d) q[d] = to_f(static_cast<const T*>(a.q)[q_at + d]);
-    for (int i = max(0, len - a.n_q + 1); i <= len - a.n_q + j; ++i) {
-      const int page = paged_page(a, a.table + static_cast<size_t>(s) * a.cols, i);
-      const size_t at = paged_at<HD>(a, page, g, i) + lane * DPL;
-      float dot = 0.f, y[DPL];
-#pragma unroll
-      for (int d = 0; d < DPL; ++d) {
-        dot = fmaf(q[d], to_f(static_cast<const T*>(a.k)[at + d]), dot);
-        y[d] = to_f(static_cast<const T*>(a.v)[at + d]);
-      }
-      const float lse = warp_sum(dot) * a.scale_log2;
-      const float mn = fmaxf(m, lse), b = mn == -INFINITY ? 0.f : mn;
-      const float f = ex2(m - b), e = ex2(lse - b);
-      l = l * f + e;
-#pragma unroll
-      for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, y[d], acc[d] * f);
-      m = mn;
-    }
-  }
-  const float inv = l > 0.f ? 1.f / l : l;  // no key: zeros (NaN stays NaN)
-  T* out = static_cast<T*>(a.out) + q_at;
-  if constexpr (DPL == 4 && sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-  else if constexpr (DPL == 2 && sizeof(T) == 2)
-    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  else
-#pragma unroll
-    for (int d = 0; d < DPL; ++d) out[d] = from_f<T>(acc[d] * inv);
-  if (a.lse != nullptr && lane == 0) a.lse[row] = m + log2f(l);
+  paged_finish<T, HD>(a, s, j, h, m, l, acc);
 }
 
 // ---------------------------------------------------------------- launches
@@ -536,7 +354,7 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   for (int i = 0; i < r.n; ++i) {
     const bool pre = i == 0, seq = i == r.n - 1;
     r.tc[i] = pre ? tc_pre : tc_seq;
-    r.tiles[i] = !bf ? PagedTiles{kSimtRows, kSimtKeys, 4 * sms, 1} : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
+    r.tiles[i] = !bf ? paged_f32_tiles(sms) : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
     r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
     const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
     const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
@@ -546,13 +364,43 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   return r;
 }
 
+// Calls that one CTA for each sequence, KV head and tile of 16 rows does at once, without
+// a plan and partial results.  Measured by the tables' sizes against the split over all SMs
+// (us, 8 KV heads of 128 dims, up to 16 rows to a head): 1 sequence of 512 keys 6.0 and 7.8,
+// of 1024 9.2 and 8.7, of 2048 15 and 11; 16 of 1024 14 and 21; 64 of 1024 47 and 52, of
+// 2048 86 and 92; 256 of 2048 311 and 338.  32 rows: 16 sequences of 1024 23 and 28, of
+// 2048 36 and 40; 128 of 1024 147 and 147, of 2048 263 and 227.  64 rows, 16 sequences of
+// 256: 41 and 35, with 64 dims 28 and 33; of 1024 46 and 38.  A shared prefix is read again
+// for every sequence: 64 sequences in 8 groups, 512 keys 20 and 23, 1024 33 and 27; with
+// 32 rows 62 and 78, 91 and 87.
+// In float32 a block of keys takes five times as long.  Heads of 32, 64 and 128 dims: 4
+// sequences of 32 keys 3.3 and 6.6, 3.5 and 7.4, 4.4 and 7.8, of 128 6.9 and 7.2, 8.2 and
+// 8.4, 12 and 7.8; 64 of 128 20 and 25, 23 and 27, 34 and 50; 64 in 8 groups, 32 keys 12 and
+// 17, 13 and 19, 17 and 21, 128 25 and 17, 29 and 18, 38 and 30.
+bool direct_call(const PagedArgs& a, bool bf16, int hd, long long* ctas) {
+  const long long keys = static_cast<long long>(a.cols + a.pcols) << a.page_shift;
+  const long long rows = static_cast<long long>(a.n_q) * a.per, tiles = a.Hkv * ((rows + 15) / 16);
+  *ctas = a.S * tiles;
+  if (tiles > 65535) return false;  // the grid's second dimension
+  if (!bf16) return keys * hd <= (a.G == 0 ? 4096 : 2048);
+  if (a.G > 0) return keys <= (*ctas <= 152 ? 1024 : 512);
+  if (rows > 32) return hd == 64 && keys <= 512;
+  return keys <= 1024 || (rows <= 16 && *ctas >= 4 * 304);
+}
+
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
   constexpr bool f32 = sizeof(T) == 4;
+  long long ctas = 0;
+  if (direct_call(a, !f32, HD, &ctas)) {
+    if constexpr (f32) return launch_paged_f32_direct(a, HD, s);
+    return launch_paged_direct(a, HD, ctas <= 152, s);  // (eight warps a CTA where four would leave SMs empty)
+  }
   const Launches r = launches_of(a, f32 ? ZSAA_F32 : ZSAA_BF16, HD, std::min(sms, kMostSms), ws);
   for (int i = 0; i < r.n; ++i) {
     if constexpr (f32) {
-      ZSAA_LAUNCH(paged_simt_kernel<HD>, dim3(r.tiles[i].ctas), dim3(kSimtThreads), 0, s, a, r.work[i]);
+      const cudaError_t e = launch_paged_f32(a, r.work[i], HD, r.tiles[i].ctas, s);
+      if (e != cudaSuccess) return e;
     } else {
       const cudaError_t e = r.tc[i] ? launch_paged_tc(a, r.work[i], HD, r.tiles[i].ctas, s)
                                     : launch_paged_mma(a, r.work[i], HD, r.tiles[i].ctas, s);

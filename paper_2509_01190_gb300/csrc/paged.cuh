@@ -195,11 +195,127 @@ template <int HD>
 __device__ __forceinline__ size_t paged_at(const PagedArgs& a, int page, int h, int i) {
   return (((static_cast<size_t>(page) * a.Hkv + h) << a.page_shift) + (i & ((1 << a.page_shift) - 1))) * HD;
 }
+// The group of sequence s (the last one that starts at or before it): a lane per group, so
+// one round trip for up to 32 groups; t0: first blocks of the entries, or null.  Whole warps.
+struct PagedGroup {
+  int g, seq0, end, keys, t0;  // g < 0: the sequence is padding
+  bool beyond;                 // the prefix is longer than its table
+};
+__device__ __forceinline__ PagedGroup paged_group_of(const PagedArgs& a, int s, const int* t0) {
+  const int lane = threadIdx.x & 31, end = paged_group_at(a, a.G), most = a.pcols << a.page_shift;
+  PagedGroup r{-1, 0, 0, 0, 0, false};
+  int len = 0;
+  for (int i = 0; i < a.G; i += 32) {
+    const int e = min(i + lane, a.G - 1);
+    const int c0 = paged_group_at(a, e), c1 = paged_group_at(a, e + 1), pl = a.plens[e], pt = t0 != nullptr ? t0[e] : 0;
+    const unsigned m = __ballot_sync(0xffffffffu, i + lane < a.G && c0 <= s);
+    if (m == 0) break;
+    const int src = 31 - __clz(m);
+    r.g = i + src;
+    r.seq0 = __shfl_sync(0xffffffffu, c0, src);
+    r.end = __shfl_sync(0xffffffffu, c1, src);
+    len = __shfl_sync(0xffffffffu, pl, src);
+    r.t0 = __shfl_sync(0xffffffffu, pt, src);
+  }
+  if (s >= end) r.g = -1;
+  r.keys = min(max(len, 0), most);
+  r.beyond = len > most;
+  return r;
+}
+
 // element offset, in q and out, of query row rr (of the entry's rows for head h)
 template <int HD>
 __device__ __forceinline__ size_t paged_q_at(const PagedArgs& a, const PagedPart& p, int rr) {
   const size_t tok = static_cast<size_t>(p.x.seq0) * a.n_q + rr / a.per;
   return (tok * (static_cast<size_t>(a.Hkv) * a.per) + static_cast<size_t>(p.h) * a.per + rr % a.per) * HD;
+}
+
+// N dims of a row in one load
+template <typename T, int N>
+__device__ __forceinline__ void paged_dims(const T* p, float (&x)[N]) {
+  auto two = [&](int i, uint32_t y) {  // (bf16 is the upper half of a float)
+    x[i] = __uint_as_float(y << 16);
+    x[i + 1] = __uint_as_float(y & 0xffff0000u);
+  };
+  if constexpr (sizeof(T) == 4 && N == 4) {
+    const float4 y = *reinterpret_cast<const float4*>(p);
+    x[0] = y.x, x[1] = y.y, x[2] = y.z, x[3] = y.w;
+  } else if constexpr (sizeof(T) == 4 && N == 2) {
+    const float2 y = *reinterpret_cast<const float2*>(p);
+    x[0] = y.x, x[1] = y.y;
+  } else if constexpr (sizeof(T) == 4) {
+    x[0] = p[0];
+  } else if constexpr (N == 4) {
+    const uint2 y = *reinterpret_cast<const uint2*>(p);
+    two(0, y.x);
+    two(2, y.y);
+  } else {
+    two(0, *reinterpret_cast<const uint32_t*>(p));
+  }
+}
+
+// The end of a query row, one warp: query j and head h of sequence s with maximum m (log2),
+// sum l and result acc (not divided) over what all of the sequence's queries see; a lane has
+// dims DPL lane .. + DPL - 1.  Adds the entries that this query sees and earlier ones do not,
+// divides and writes.
+template <typename T, int HD>
+__device__ __forceinline__ void paged_finish(const PagedArgs& a, int s, int j, int h, float m, float l,
+                                             float (&acc)[HD / 32]) {
+  constexpr int DPL = HD / 32;
+  auto ex2 = [](float x) { return sizeof(T) == 4 ? exp2f(x) : ex2_fast(x); };
+  const int lane = threadIdx.x & 31, g = h / a.per;
+  const int cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
+  if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
+  const size_t row = (static_cast<size_t>(s) * a.n_q + j) * (static_cast<size_t>(a.Hkv) * a.per) + h;
+  const size_t at_q = row * HD + lane * DPL;
+  const int first = max(0, len - a.n_q + 1), n = len - a.n_q + j + 1 - first;  // (up to 16, 0 where n_q is 1 and before entry 0)
+  if (a.n_q > 1 && n > 0) {
+    float q[DPL];
+    paged_dims<T>(static_cast<const T*>(a.q) + at_q, q);
+    const int pages = lane < n ? paged_page(a, a.table + static_cast<size_t>(s) * a.cols, first + lane) : 0;
+    for (int i = 0; i < n; i += 4) {  // four entries a round trip
+      float score[4], y[4][DPL], mn = m;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = min(i + u, n - 1);
+        const size_t at = paged_at<HD>(a, __shfl_sync(0xffffffffu, pages, k), g, first + k) + lane * DPL;
+        float x[DPL];
+        paged_dims<T>(static_cast<const T*>(a.k) + at, x);
+        paged_dims<T>(static_cast<const T*>(a.v) + at, y[u]);
+        score[u] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) score[u] = fmaf(q[d], x[d], score[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        score[u] = warp_sum(score[u]) * a.scale_log2;
+        mn = i + u < n ? fmaxf(mn, score[u]) : mn;
+      }
+      const float b = mn == -INFINITY ? 0.f : mn, f = ex2(m - b);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) acc[d] *= f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i + u < n) {
+          const float e = ex2(score[u] - b);
+          l += e;
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, y[u][d], acc[d]);
+        }
+      m = mn;
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : l;  // no key: zeros (NaN stays NaN)
+  T* out = static_cast<T*>(a.out) + at_q;
+  if constexpr (DPL == 4 && sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+  else if constexpr (DPL == 2 && sizeof(T) == 2)
+    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+  else
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) out[d] = from_f<T>(acc[d] * inv);
+  if (a.lse != nullptr && lane == 0) a.lse[row] = m + log2f(l);
 }
 
 }  // namespace zsaa

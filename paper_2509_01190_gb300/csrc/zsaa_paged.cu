@@ -97,6 +97,7 @@ zsaa_status attention_sizes(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
   if (S < 1 || Hq < 1) return bad("S and Hq must be >= 1");
   if (n_q < 1 || n_q > 16) return refuse(ZSAA_ERR_UNSUPPORTED, "n_q=%d outside [1, 16]", n_q);
   if (Hq % kv->n_kv_heads != 0) return bad("Hq must be a multiple of n_kv_heads");
+  if (Hq > 65536) return bad("more than 65536 heads");  // (a grid's second dimension)
   if (G < 0) return bad("G must be >= 0");
   ZTRY(check_cols(cols, kv->page_size));
   if (G > 0) ZTRY(check_cols(prefix_cols, kv->page_size));

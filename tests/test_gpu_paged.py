@@ -134,16 +134,20 @@ def widened(rows, cols):
     return None if rows is None else [r + [-1] * (cols - len(r)) for r in rows]
 
 
-# Entries with more than 16 rows to a KV head take 128-row tiles where their tables are
-# wide: by the prefixes' tables alone, or (rows of one sequence) by both.
-ROOM = [(0, 0), (0, 4000), (4000, 4000)]
+def rooms(dtype, page, groups):
+    """Widths of the two tables, in pages.  A call over narrow tables takes one launch, one
+    over wide ones is split over the SMs; entries with more than 16 rows to a KV head then
+    take 128-row tiles, by the prefixes' tables alone or (rows of one sequence) by both."""
+    some, many = 2100 // page, 64000 // page
+    wide = [(some, some)] + ([(many, many)] if dtype == "bf16" else [])
+    return [(0, 0)] + wide + ([(0, w) for _, w in wide] if groups is not None else [])
 
 
-@pytest.mark.parametrize("room", ROOM, ids=["", "wide_prefixes", "wide"])
-@pytest.mark.parametrize("dtype,Hq,Hkv,hd,page,n_q,lens,groups,plens", CASES)
+ROOMY = [c + (r,) for c in CASES for r in rooms(c[0], c[4], c[7])]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,page,n_q,lens,groups,plens,room", ROOMY)
 def test_attention(zlib, dtype, Hq, Hkv, hd, page, n_q, lens, groups, plens, room):
-    if room != (0, 0) and (dtype == "f32" or (groups is None and room[0] == 0)):
-        pytest.skip("no other kernel")
     p, q, table, ptable = build(zlib, dtype, Hq, Hkv, hd, page, lens, n_q, groups, plens or ())
     table, ptable = widened(table, room[0]), widened(ptable, room[1])
     out, lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
@@ -163,13 +167,15 @@ def test_attention_of_drawn_sizes(zlib, seed):
     groups = sorted(r.randint(0, S) for _ in range(G + 1))
     plens = [r.choice([0, r.randint(1, 900)]) for _ in range(G)]
     p, q, table, ptable = build(zlib, dtype, Hkv * per, Hkv, hd, r.choice([16, 64]), lens, n_q, groups, plens, seed)
-    if seed % 2:
+    if seed % 3 == 1:
         ptable = widened(ptable, 5000)
+    elif seed % 3 == 2:
+        table, ptable = widened(table, 200), widened(ptable, 200)
     out, lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
     check(p, q, table, lens, out, lse, groups, ptable, plens)
 
 
-@pytest.mark.parametrize("dtype,cols", [("bf16", 10), ("bf16", 5000), ("f32", 10)])
+@pytest.mark.parametrize("dtype,cols", [("bf16", 10), ("bf16", 100), ("bf16", 5000), ("f32", 4), ("f32", 100)])
 def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype, cols):
     lens, n_q = [20, 4, 35], 4
     p, q, table, ptable = build(zlib, dtype, 20, 2, 64, 16, lens, n_q, [0, 3], [50])
@@ -188,7 +194,7 @@ def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype,
 def test_large_scores(zlib, dtype, hd):
     """Scores far apart, rising and falling along the keys: the running maximum moves
     from block to block."""
-    for sign, n_q, cols in ((1.0, 1, 50), (-1.0, 1, 50), (1.0, 5, 20000), (-1.0, 5, 20000)):
+    for sign, n_q, cols in ((1.0, 1, 50), (-1.0, 1, 50), (1.0, 1, 500), (-1.0, 1, 500), (1.0, 5, 20000), (-1.0, 5, 20000)):
         p, q, table, _ = build(zlib, dtype, 4, 1, hd, 16, [700], n_q, seed=3)
         table = widened(table, cols)
         ramp = torch.linspace(0.0, 40.0, 700, device="cuda")
@@ -198,15 +204,17 @@ def test_large_scores(zlib, dtype, hd):
         check(p, q, table, [700], out, lse)
 
 
-def test_attention_without_lse_on_another_stream_and_as_two_graphs(zlib):
+@pytest.mark.parametrize("dtype,cols", [("bf16", 0), ("bf16", 100), ("bf16", 5000), ("f32", 0), ("f32", 100)])
+def test_attention_without_lse_on_another_stream_and_as_two_graphs(zlib, dtype, cols):
     lens, groups, plens = [40, 3, 66], [0, 2, 3], [90, 300]
-    p, q, table, ptable = build(zlib, "bf16", 8, 2, 128, 16, lens, 1, groups, plens)
+    p, q, table, ptable = build(zlib, dtype, 40, 2, 128, 16, lens, 1, groups, plens)
+    ptable = widened(ptable, cols)
     want, want_lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
     t, l, g, pt, pl = ints(table), ints(lens), ints(groups), ints(ptable), ints(plens)
-    n = zlib.zsaa_op_paged_attention_workspace(p.pages, 3, 1, 8, 2, len(table[0]), len(ptable[0]))
+    n = zlib.zsaa_op_paged_attention_workspace(p.pages, 3, 1, 40, 2, len(table[0]), len(ptable[0]))
 
     def call(out, lse, ws):
-        zlib.zsaa_op_paged_attention(p.pages, q, 3, 1, 8, t, len(table[0]), l, g, 2, pt, len(ptable[0]), pl, out, lse, ws,
+        zlib.zsaa_op_paged_attention(p.pages, q, 3, 1, 40, t, len(table[0]), l, g, 2, pt, len(ptable[0]), pl, out, lse, ws,
                                      ws.numel())
 
     torch.cuda.synchronize()
@@ -271,7 +279,7 @@ def test_pages_beyond_32_bit_offsets(zlib):
     check(small, q, [[2, 1, 0]], [T], out, lse)
 
 
-@pytest.mark.parametrize("cols", [3, 3000])
+@pytest.mark.parametrize("cols", [3, 100, 3000])
 def test_bad_pages_and_lengths_are_reported(zlib, cols):
     p, q, table, ptable = build(zlib, "bf16", 40, 2, 64, 16, [40, 40], 1, [0, 2], [40])
     table, ptable = widened(table, cols), widened(ptable, cols)
@@ -306,7 +314,7 @@ def test_bad_pages_and_lengths_are_reported(zlib, cols):
         assert torch.equal(changed, want)
 
 
-@pytest.mark.parametrize("dtype,cols", [("bf16", 3), ("bf16", 3000), ("f32", 3)])
+@pytest.mark.parametrize("dtype,cols", [("bf16", 3), ("bf16", 100), ("bf16", 3000), ("f32", 3), ("f32", 100)])
 def test_group_bounds_that_run_backwards_stay_in_bounds(zlib, dtype, cols):
     p, q, table, ptable = build(zlib, dtype, 40, 2, 64, 16, [20] * 4, 1, [0, 4], [40, 40, 40])
     ptable = widened(ptable, cols)

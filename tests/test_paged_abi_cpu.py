@@ -83,7 +83,7 @@ def test_append_refuses_bf16_rows_for_a_float32_pool(zlib):
     dict(q=None), dict(table=None), dict(lens=None), dict(out=None), dict(ws=None), dict(S=0), dict(Hq=0), dict(Hq=5),
     dict(G=-1), dict(cols=0), dict(pcols=0), dict(cu=None), dict(ptable=None), dict(plens=None), dict(q=A + 8),
     dict(out=FAR + 2), dict(ws=FAR + 8), dict(ws_bytes=64), dict(out=A + 256), dict(S=1 << 30), dict(G=1 << 30),
-    dict(cols=1 << 26, S=1 << 20)])
+    dict(cols=1 << 26, S=1 << 20), dict(Hq=1 << 17)])
 def test_attention_refusals(zlib, kw):
     refused(zlib, lambda: attention(zlib, **kw))
 
