@@ -180,41 +180,6 @@ cudaError_t run_append(const AppendArgs& a, const RopeTurns& t, int sms, cudaStr
 
 constexpr int kJoinThreads = 128;
 
-// The partial results of a query row from one launch: n of them, one slot after the other.
-struct JoinParts {
-  const float *o, *lse2;
-  size_t step;  // rows from one slot to the next
-  int n;
-};
-// rr: the row's number among its entry's rows for KV head g; per, t_entry: the stretch
-// length and the entry's first block
-__device__ __forceinline__ JoinParts join_parts(const PagedArgs& a, const PagedWork& w, int e, const PagedEntry& x,
-                                                int per, int t_entry, int g, int rr, int hd) {
-  if (per == 0 || x.keys == 0) return JoinParts{nullptr, nullptr, 0, 0};
-  const int ms = w.mt_shift, up = (1 << ms) - 1;
-  const int nb = (x.keys + (1 << w.bn_shift) - 1) >> w.bn_shift, rt = (x.rows + up) >> ms;
-  const int item = g * rt + (rr >> ms), row = a.n_q * a.per;
-  const unsigned t0 = static_cast<unsigned>(t_entry + item * nb);
-  const int first = e < a.G ? (((x.seq0 * row) >> ms) + e) * a.Hkv
-                            : (w.e0 < a.G ? (((a.S * row) >> ms) + a.G) * a.Hkv : 0) + x.seq0 * ((row + up) >> ms) * a.Hkv;
-  const unsigned c0 = t0 / static_cast<unsigned>(per), c1 = (t0 + nb - 1) / static_cast<unsigned>(per);
-  const size_t at = (static_cast<size_t>(static_cast<int>(c0) + first + item) << ms) + (rr & up);
-  return JoinParts{w.o + at * hd, w.lse2 + at, static_cast<size_t>(1) << ms, static_cast<int>(c1 - c0) + 1};
-}
-
-template <int N>
-__device__ __forceinline__ void load_dims(const float* p, float (&x)[N]) {
-  if constexpr (N == 4) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-  } else if constexpr (N == 2) {
-    const float2 v = *reinterpret_cast<const float2*>(p);
-    x[0] = v.x, x[1] = v.y;
-  } else {
-    x[0] = *p;
-  }
-}
-
 // One warp per query row: the row's partials in the order of their keys, then the
 // entries that the row sees and its sequence's earlier queries do not.  Bound by its chain
 // of round trips to L2, some 900 clocks each, so there are three: everything about the
@@ -224,8 +189,6 @@ template <typename T, int HD>
 __global__ void __launch_bounds__(kJoinThreads, 4)
     paged_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork wp,
                       const __grid_constant__ PagedWork ws) {
-  constexpr int DPL = HD / 32;  // dims per lane
-  auto ex2 = [](float x) { return sizeof(T) == 4 ? exp2f(x) : ex2_fast(x); };
   const int lane = threadIdx.x & 31, Hq = a.Hkv * a.per;
   const int token = static_cast<int>(blockIdx.x), h = static_cast<int>(blockIdx.y) * (kJoinThreads / 32) + (threadIdx.x >> 5);
   pdl_trigger();
@@ -239,47 +202,16 @@ __global__ void __launch_bounds__(kJoinThreads, 4)
     const int pre_per = wp.head[0];
     const PagedGroup x = paged_group_of(a, s, wp.head + 1 - wp.e0);
     if (x.g < 0) return;  // a row behind the last sequence stays as it was
-    const PagedEntry e{x.keys, max(0, x.end - x.seq0) * a.n_q * a.per, x.seq0};
-    const int rr = ((s - x.seq0) * a.n_q + j) * a.per + h % a.per;
-    if (lane == 0 && (x.beyond || rr >= e.rows)) atomicOr(a.status, kStatusBadIndex);  // (bounds that run backwards)
-    if (rr < e.rows) shared = join_parts(a, wp, x.g, e, pre_per, x.t0, g, rr, HD);
+    shared = join_prefix(a, wp, x, pre_per, s, g, j * a.per + h % a.per, HD);
   }
   const PagedEntry mine{max(0, len - (a.n_q - 1)), a.n_q * a.per, s};
   const JoinParts own = join_parts(a, ws, a.G + s, mine, own_per, own_t, g, j * a.per + h % a.per, HD);
 
-  const int n = shared.n + own.n;
-  auto log2_sum = [&](int i) {
-    return i < shared.n ? shared.lse2[i * shared.step] : i < n ? own.lse2[(i - shared.n) * own.step] : -INFINITY;
-  };
-  float m = -INFINITY, l = 0.f, acc[DPL] = {};
-  for (int i0 = 0; i0 < n; i0 += 32) m = fmaxf(m, log2_sum(i0 + lane));
-  m = warp_max(m);
-  const float base = m == -INFINITY ? 0.f : m;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const float weight = ex2(log2_sum(i0 + lane) - base);  // (0 past the last part; NaN stays NaN)
-    l += warp_sum(weight);
-    const int most = min(32, n - i0);
-    for (int k0 = 0; k0 < most; k0 += 8) {
-      float x[8][DPL];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int i = i0 + k0 + k;
-        if (k0 + k < most)
-          load_dims(i < shared.n ? shared.o + i * shared.step * HD + lane * DPL
-                                 : own.o + (i - shared.n) * own.step * HD + lane * DPL, x[k]);
-        else
-#pragma unroll
-          for (int d = 0; d < DPL; ++d) x[k][d] = 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float e = __shfl_sync(0xffffffffu, weight, k0 + k);
-#pragma unroll
-        for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, x[k][d], acc[d]);
-      }
-    }
-  }
-  paged_finish<T, HD>(a, s, j, h, m, l, acc);
+  PagedRows<HD, 1> x{};
+  x.rr[0] = j * a.per + h % a.per;
+  x.m[0] = -INFINITY;
+  paged_add_parts<T, HD, 1, 8>(x, {shared}, {own});
+  paged_finish<T, HD, 1>(a, s, g, x);
 }
 
 // ---------------------------------------------------------------- launches
@@ -324,6 +256,7 @@ constexpr int kMostSms = 256;  // the workspace holds a device of up to this man
 // (one launch where it is the same), and their shares of the workspace.
 struct Launches {
   int n;
+  bool own;  // the sequences' own entries belong to the launch that joins
   bool tc[2];
   PagedTiles tiles[2];
   PagedWork work[2];
@@ -331,37 +264,18 @@ struct Launches {
   long long most;  // items and blocks that number the slots and the line
 };
 
-// The 128-row tiles take entries whose 16-row tiles would have more than six blocks of 64
-// keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64, by the tables' sizes): where
-// a head has 32 to 256 rows to a prefix of 32 to 16384 keys, in 1 to 16 groups of up to 8
-// KV heads, the whole call took the same time there.  With 8 heads of 128 dims, 128 rows,
-// 16-row and 128-row tiles: 512 keys 16 and 22 us, 1024 20 and 23, 2048 27 and 24, 8192 79
-// and 34.  Up to 16 rows there is one 16-row tile and nothing to gain.
-bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int heads) {
-  return rows > 16 && row_tiles * heads * (keys / 64) > (hd == 128 ? 6 * 304 : 6 * 456);
-}
-
-Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
-  Launches r{};
-  const long long row = static_cast<long long>(a.n_q) * a.per;
-  const bool bf = dtype == ZSAA_BF16;
-  const bool tc_seq = bf && many_rows(hd, a.S * ((row + 15) / 16), row, static_cast<long long>(a.cols) << a.page_shift, a.Hkv);
-  const bool tc_pre = a.G == 0 ? tc_seq
-                               : bf && many_rows(hd, std::max(a.S * row / 16, static_cast<long long>(a.G)), a.S * row / a.G,
-                                                 static_cast<long long>(a.pcols) << a.page_shift, a.Hkv);
-  r.n = tc_seq == tc_pre ? 1 : 2;
-  uintptr_t at = reinterpret_cast<uintptr_t>(ws);
-  for (int i = 0; i < r.n; ++i) {
-    const bool pre = i == 0, seq = i == r.n - 1;
-    r.tc[i] = pre ? tc_pre : tc_seq;
-    r.tiles[i] = !bf ? paged_f32_tiles(sms) : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
-    r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
-    const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
-    const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
-    r.most = std::max(r.most, std::max(slots, blocks));
-  }
-  r.bytes = at - reinterpret_cast<uintptr_t>(ws);
-  return r;
+// The 128-row tiles take entries whose 16-row tiles would have more than `blocks` blocks of
+// 64 keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64, by the tables' sizes).
+// Up to 16 rows there is one 16-row tile and nothing to gain.  Six blocks where that saves
+// or costs no launch: 128 rows to a prefix without own entries (us, 16-row and 128-row
+// tiles, 8 heads of 128 dims) 512 keys 16 and 22, 1024 20 and 23, 2048 27 and 24, 8192 79
+// and 34; 24 sequences of 4 queries in 3 groups with 300 own entries 512 keys 30 and 29,
+// 1024 38 and 31, 2048 53 and 35; with 64 dims 19 and 19, 23 and 22, 30 and 23.  Forty where
+// the sequences' own entries, too many for the joining launch, then need a launch of their
+// own: those sequences with 1500 entries 1024 keys 49 and 62, 2048 58 and 67, 4096 80 and
+// 75, 8192 117 and 85; with 64 dims 4096 51 and 48, 8192 72 and 56.
+bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int heads, int blocks) {
+  return rows > 16 && row_tiles * heads * (keys / 64) > blocks * (hd == 128 ? 304 : 456);
 }
 
 // Calls that one CTA for each sequence, KV head and tile of 16 rows does at once, without
@@ -377,24 +291,59 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
 // sequences of 32 keys 3.3 and 6.6, 3.5 and 7.4, 4.4 and 7.8, of 128 6.9 and 7.2, 8.2 and
 // 8.4, 12 and 7.8; 64 of 128 20 and 25, 23 and 27, 34 and 50; 64 in 8 groups, 32 keys 12 and
 // 17, 13 and 19, 17 and 21, 128 25 and 17, 29 and 18, 38 and 30.
-bool direct_call(const PagedArgs& a, bool bf16, int hd, long long* ctas) {
+long long direct_ctas(const PagedArgs& a) {
+  return static_cast<long long>(a.S) * a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16);
+}
+// The sequences' own entries in bf16, alone or in the launch that joins them with the
+// prefixes' partial results.  That launch against two, after 128-row tiles, 300 entries: 24
+// sequences of 4 queries 36 and 44 us with 2048 keys to a prefix, with 64 dims 23 and 30; 64
+// sequences of 600 and a prefix of 32000 95 and 103; 8 of 8 queries, 64 rows, 1024 27 and 35.
+// (128 sequences of one query with 64 dims: 48 and 44.)  After 16-row tiles, which take
+// both kinds of entries in one launch, it gains nothing: 32 sequences in 8 groups 22 and 20.
+bool own_in_one(const PagedArgs& a, int hd) {
+  const long long keys = static_cast<long long>(a.cols) << a.page_shift, rows = static_cast<long long>(a.n_q) * a.per;
+  if (a.Hkv * ((rows + 15) / 16) > 65535) return false;  // the grid's second dimension
+  if (rows > 32) return (hd == 64 || a.G > 0) && keys <= 512;
+  return keys <= 1024 || (rows <= 16 && direct_ctas(a) >= 4 * 304);
+}
+bool direct_call(const PagedArgs& a, bool bf16, int hd) {
   const long long keys = static_cast<long long>(a.cols + a.pcols) << a.page_shift;
-  const long long rows = static_cast<long long>(a.n_q) * a.per, tiles = a.Hkv * ((rows + 15) / 16);
-  *ctas = a.S * tiles;
-  if (tiles > 65535) return false;  // the grid's second dimension
+  if (a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16) > 65535) return false;
   if (!bf16) return keys * hd <= (a.G == 0 ? 4096 : 2048);
-  if (a.G > 0) return keys <= (*ctas <= 152 ? 1024 : 512);
-  if (rows > 32) return hd == 64 && keys <= 512;
-  return keys <= 1024 || (rows <= 16 && *ctas >= 4 * 304);
+  return a.G == 0 ? own_in_one(a, hd) : keys <= (direct_ctas(a) <= 152 ? 1024 : 512);
+}
+
+Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
+  Launches r{};
+  const long long row = static_cast<long long>(a.n_q) * a.per;
+  const bool bf = dtype == ZSAA_BF16;
+  const bool own = bf && a.G > 0 && own_in_one(a, hd);
+  const bool tc_seq = bf && many_rows(hd, a.S * ((row + 15) / 16), row, static_cast<long long>(a.cols) << a.page_shift, a.Hkv, 6);
+  const bool tc_pre = a.G == 0 ? tc_seq
+                               : bf && many_rows(hd, std::max(a.S * row / 16, static_cast<long long>(a.G)), a.S * row / a.G,
+                                                 static_cast<long long>(a.pcols) << a.page_shift, a.Hkv, own || tc_seq ? 6 : 40);
+  r.own = own && tc_pre;
+  r.n = tc_seq == tc_pre || r.own ? 1 : 2;
+  uintptr_t at = reinterpret_cast<uintptr_t>(ws);
+  for (int i = 0; i < r.n; ++i) {
+    const bool pre = i == 0, seq = i == r.n - 1 && !r.own;
+    r.tc[i] = pre ? tc_pre : tc_seq;
+    r.tiles[i] = !bf ? paged_f32_tiles(sms) : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
+    r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
+    const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
+    const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
+    r.most = std::max(r.most, std::max(slots, blocks));
+  }
+  r.bytes = at - reinterpret_cast<uintptr_t>(ws);
+  return r;
 }
 
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
   constexpr bool f32 = sizeof(T) == 4;
-  long long ctas = 0;
-  if (direct_call(a, !f32, HD, &ctas)) {
+  if (direct_call(a, !f32, HD)) {
     if constexpr (f32) return launch_paged_f32_direct(a, HD, s);
-    return launch_paged_direct(a, HD, ctas <= 152, s);  // (eight warps a CTA where four would leave SMs empty)
+    return launch_paged_direct(a, nullptr, HD, direct_ctas(a) <= 152, s);  // (eight warps a CTA where four would leave SMs empty)
   }
   const Launches r = launches_of(a, f32 ? ZSAA_F32 : ZSAA_BF16, HD, std::min(sms, kMostSms), ws);
   for (int i = 0; i < r.n; ++i) {
@@ -407,6 +356,8 @@ cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStrea
       if (e != cudaSuccess) return e;
     }
   }
+  if constexpr (!f32)
+    if (r.own) return launch_paged_direct(a, &r.work[0], HD, direct_ctas(a) <= 152, s);
   const int heads = a.Hkv * a.per, per_cta = kJoinThreads / 32;
   ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(a.S * a.n_q, (heads + per_cta - 1) / per_cta), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
   return cudaSuccess;

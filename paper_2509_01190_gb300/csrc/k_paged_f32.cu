@@ -228,12 +228,18 @@ __global__ void __launch_bounds__(F_THREADS) paged_f32_direct_kernel(const __gri
     *reinterpret_cast<float4*>(&sh.k[rg * C::RPG + i][quad]) = make_float4(x.acc[i][0], x.acc[i][1], x.acc[i][2], x.acc[i][3]);
   __syncthreads();
   constexpr int DPL = HD / 32;
-  for (int r = warp; r < rows; r += F_THREADS / 32) {
-    float acc[DPL];
+  constexpr int W = F_THREADS / 32, R = F_ROWS / W;
+  PagedRows<HD, R> y;
 #pragma unroll
-    for (int d = 0; d < DPL; ++d) acc[d] = sh.k[r][lane * DPL + d];
-    paged_finish<float, HD>(a, s, (r0 + r) / a.per, g * a.per + (r0 + r) % a.per, sh.m[r], sh.l[r], acc);
+  for (int i = 0; i < R; ++i) {
+    const int r = warp + i * W;
+    y.rr[i] = r < rows ? r0 + r : -1;
+    y.m[i] = sh.m[r];
+    y.l[i] = sh.l[r];
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) y.acc[i][d] = sh.k[r][lane * DPL + d];
   }
+  paged_finish<float, HD, R>(a, s, g, y);
 }
 
 template <int HD>

@@ -272,12 +272,14 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   cp_async_wait<0>();
 }
 
-// Short calls: a CTA of W warps has up to 16 rows of a sequence and KV head over all that
-// they see, prefix and own entries one after the other, and writes the results: no plan, no
-// partial results, one launch.  The prefix is read once for every sequence, in L2.
-template <int HD, int W>
+// A CTA of W warps has up to 16 rows of a sequence and KV head over all that they see,
+// prefix and own entries one after the other, and writes the results: no plan, no partial
+// results, one launch.  The prefix is read once for every sequence, in L2.
+// PARTS: the prefixes' partial results are in w already (the 128-row tiles'), and this
+// launch has the sequences' own entries and joins.
+template <int HD, int W, bool PARTS>
 __global__ void __launch_bounds__(32 * W, 8 / W)
-    paged_direct_kernel(const __grid_constant__ PagedArgs a) {
+    paged_direct_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
   using C = MmCfg<HD>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_m[W][MM_ROWS], s_l[W][MM_ROWS];
@@ -298,10 +300,15 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   mm_clear<HD>(x);
   const int own = max(0, min(a.lens[s], a.cols << a.page_shift) - (a.n_q - 1));
   const int32_t *shared_row = nullptr, *own_row = a.table + static_cast<size_t>(s) * a.cols;
-  int shared = 0;
-  if (a.G > 0) {
-    const PagedGroup e = paged_group_of(a, s, nullptr);
+  int shared = 0, per = 0;
+  PagedGroup e{};
+  if (PARTS) {
+    per = w.head[0];
+    e = paged_group_of(a, s, w.head + 1);
     if (e.g < 0) return;  // a row behind the last sequence stays as it was
+  } else if (a.G > 0) {
+    e = paged_group_of(a, s, nullptr);
+    if (e.g < 0) return;
     if (threadIdx.x == 0 && e.beyond) atomicOr(a.status, kStatusBadIndex);
     shared = e.keys;
     shared_row = a.ptable + static_cast<size_t>(e.g) * a.pcols;
@@ -353,22 +360,37 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   }
   __syncthreads();
   constexpr int DPL = HD / 32;
-  for (int r = warp; r < rows; r += W) {
-    float m = s_m[0][r];
+  constexpr int R = MM_ROWS / W;
+  PagedRows<HD, R> y;
 #pragma unroll
-    for (int k = 1; k < W; ++k) m = fmaxf(m, s_m[k][r]);
-    const float base = m == -INFINITY ? 0.f : m;
-    float l = 0.f, acc[DPL] = {};
+  for (int i = 0; i < R; ++i) {
+    const int r = warp + i * W;
+    y.rr[i] = r < rows ? r0 + r : -1;
+    y.m[i] = s_m[0][r];
+#pragma unroll
+    for (int k = 1; k < W; ++k) y.m[i] = fmaxf(y.m[i], s_m[k][r]);
+    const float base = y.m[i] == -INFINITY ? 0.f : y.m[i];
+    y.l[i] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) y.acc[i][d] = 0.f;
+    if (r >= rows) continue;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
       const float f = ex2_fast(s_m[k][r] - base);
-      const float* y = join + (k * MM_ROWS + r) * HD + ((lane * DPL) ^ ((r & 3) * 8));
-      l = fmaf(f, s_l[k][r], l);
+      const float* z = join + (k * MM_ROWS + r) * HD + ((lane * DPL) ^ ((r & 3) * 8));
+      y.l[i] = fmaf(f, s_l[k][r], y.l[i]);
 #pragma unroll
-      for (int d = 0; d < DPL; ++d) acc[d] = fmaf(f, y[d], acc[d]);
+      for (int d = 0; d < DPL; ++d) y.acc[i][d] = fmaf(f, z[d], y.acc[i][d]);
     }
-    paged_finish<bf16, HD>(a, s, (r0 + r) / a.per, g * a.per + (r0 + r) % a.per, m, l, acc);
   }
+  if (PARTS) {
+    JoinParts pre[R], none[R] = {};
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+      pre[i] = y.rr[i] < 0 ? JoinParts{nullptr, nullptr, 0, 0} : join_prefix(a, w, e, per, s, g, y.rr[i], HD);
+    paged_add_parts<bf16, HD, R, 16 / R>(y, pre, none);
+  }
+  paged_finish<bf16, HD, R>(a, s, g, y);
 }
 
 }  // namespace
@@ -386,19 +408,24 @@ static cudaError_t run_mma(const PagedArgs& a, const PagedWork& w, int ctas, cud
   return cudaSuccess;
 }
 
-template <int HD, int W>
-static cudaError_t run_direct(const PagedArgs& a, cudaStream_t s) {
+template <int HD, int W, bool PARTS>
+static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream_t s) {
   static OncePerDevice once;
-  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<HD, W>, W * MmCfg<HD>::RING);
+  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<HD, W, PARTS>, W * MmCfg<HD>::RING);
   if (e != cudaSuccess) return e;
   const int tiles = (a.n_q * a.per + MM_ROWS - 1) / MM_ROWS;
-  ZSAA_LAUNCH(paged_direct_kernel<HD, W>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), W * MmCfg<HD>::RING, s, a);
+  ZSAA_LAUNCH(paged_direct_kernel<HD, W, PARTS>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), W * MmCfg<HD>::RING, s, a, w);
   return cudaSuccess;
 }
 
-cudaError_t launch_paged_direct(const PagedArgs& a, int hd, bool wide, cudaStream_t s) {
-  if (hd == 64) return wide ? run_direct<64, 8>(a, s) : run_direct<64, 4>(a, s);
-  return wide ? run_direct<128, 8>(a, s) : run_direct<128, 4>(a, s);
+cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int hd, bool wide, cudaStream_t s) {
+  const PagedWork w = prefixes != nullptr ? *prefixes : PagedWork{};
+  if (prefixes != nullptr) {
+    if (hd == 64) return wide ? run_direct<64, 8, true>(a, w, s) : run_direct<64, 4, true>(a, w, s);
+    return wide ? run_direct<128, 8, true>(a, w, s) : run_direct<128, 4, true>(a, w, s);
+  }
+  if (hd == 64) return wide ? run_direct<64, 8, false>(a, w, s) : run_direct<64, 4, false>(a, w, s);
+  return wide ? run_direct<128, 8, false>(a, w, s) : run_direct<128, 4, false>(a, w, s);
 }
 
 cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s) {

@@ -254,68 +254,174 @@ __device__ __forceinline__ void paged_dims(const T* p, float (&x)[N]) {
   }
 }
 
-// The end of a query row, one warp: query j and head h of sequence s with maximum m (log2),
-// sum l and result acc (not divided) over what all of the sequence's queries see; a lane has
-// dims DPL lane .. + DPL - 1.  Adds the entries that this query sees and earlier ones do not,
-// divides and writes.
-template <typename T, int HD>
-__device__ __forceinline__ void paged_finish(const PagedArgs& a, int s, int j, int h, float m, float l,
-                                             float (&acc)[HD / 32]) {
+// The partial results of a query row from one launch: n of them, one slot after the other.
+struct JoinParts {
+  const float *o, *lse2;
+  size_t step;  // rows from one slot to the next
+  int n;
+};
+// rr: the row's number among its entry's rows for KV head g; per, t_entry: the stretch
+// length and the entry's first block
+__device__ __forceinline__ JoinParts join_parts(const PagedArgs& a, const PagedWork& w, int e, const PagedEntry& x,
+                                                int per, int t_entry, int g, int rr, int hd) {
+  if (per == 0 || x.keys == 0) return JoinParts{nullptr, nullptr, 0, 0};
+  const int ms = w.mt_shift, up = (1 << ms) - 1;
+  const int nb = (x.keys + (1 << w.bn_shift) - 1) >> w.bn_shift, rt = (x.rows + up) >> ms;
+  const int item = g * rt + (rr >> ms), row = a.n_q * a.per;
+  const unsigned t0 = static_cast<unsigned>(t_entry + item * nb);
+  const int first = e < a.G ? (((x.seq0 * row) >> ms) + e) * a.Hkv
+                            : (w.e0 < a.G ? (((a.S * row) >> ms) + a.G) * a.Hkv : 0) + x.seq0 * ((row + up) >> ms) * a.Hkv;
+  const unsigned c0 = t0 / static_cast<unsigned>(per), c1 = (t0 + nb - 1) / static_cast<unsigned>(per);
+  const size_t at = (static_cast<size_t>(static_cast<int>(c0) + first + item) << ms) + (rr & up);
+  return JoinParts{w.o + at * hd, w.lse2 + at, static_cast<size_t>(1) << ms, static_cast<int>(c1 - c0) + 1};
+}
+
+// Those of row rr of sequence s, KV head g, from its group's prefix.
+__device__ __forceinline__ JoinParts join_prefix(const PagedArgs& a, const PagedWork& w, const PagedGroup& x, int per, int s,
+                                                 int g, int rr, int hd) {
+  const PagedEntry e{x.keys, max(0, x.end - x.seq0) * a.n_q * a.per, x.seq0};
+  rr += (s - x.seq0) * a.n_q * a.per;
+  if ((threadIdx.x & 31) == 0 && (x.beyond || rr >= e.rows)) atomicOr(a.status, kStatusBadIndex);  // (bounds that run backwards)
+  return rr < e.rows ? join_parts(a, w, x.g, e, per, x.t0, g, rr, hd) : JoinParts{nullptr, nullptr, 0, 0};
+}
+
+// Rows of one warp that belong to one sequence and KV head: maximum (log2), sum and result
+// (not divided); a lane has DPL dims from DPL lane on.
+template <int HD, int R>
+struct PagedRows {
+  int rr[R];  // row number among the sequence's n_q * per; below 0: none
+  float m[R], l[R], acc[R][HD / 32];
+};
+
+// Adds each row's partial results of up to two launches, in the order of their keys: for 32
+// of them the log2 sums, then the results, K of a row at a time.
+template <typename T, int HD, int R, int K>
+__device__ __forceinline__ void paged_add_parts(PagedRows<HD, R>& x, const JoinParts (&p)[R], const JoinParts (&p2)[R]) {
   constexpr int DPL = HD / 32;
-  auto ex2 = [](float x) { return sizeof(T) == 4 ? exp2f(x) : ex2_fast(x); };
-  const int lane = threadIdx.x & 31, g = h / a.per;
-  const int cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
-  if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
-  const size_t row = (static_cast<size_t>(s) * a.n_q + j) * (static_cast<size_t>(a.Hkv) * a.per) + h;
-  const size_t at_q = row * HD + lane * DPL;
-  const int first = max(0, len - a.n_q + 1), n = len - a.n_q + j + 1 - first;  // (up to 16, 0 where n_q is 1 and before entry 0)
-  if (a.n_q > 1 && n > 0) {
-    float q[DPL];
-    paged_dims<T>(static_cast<const T*>(a.q) + at_q, q);
-    const int pages = lane < n ? paged_page(a, a.table + static_cast<size_t>(s) * a.cols, first + lane) : 0;
-    for (int i = 0; i < n; i += 4) {  // four entries a round trip
-      float score[4], y[4][DPL], mn = m;
+  auto ex2 = [](float v) { return sizeof(T) == 4 ? exp2f(v) : ex2_fast(v); };
+  const int lane = threadIdx.x & 31;
+  int n = 0;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int k = min(i + u, n - 1);
-        const size_t at = paged_at<HD>(a, __shfl_sync(0xffffffffu, pages, k), g, first + k) + lane * DPL;
-        float x[DPL];
-        paged_dims<T>(static_cast<const T*>(a.k) + at, x);
-        paged_dims<T>(static_cast<const T*>(a.v) + at, y[u]);
-        score[u] = 0.f;
+  for (int r = 0; r < R; ++r) n = max(n, p[r].n + p2[r].n);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    float weight[R];
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) score[u] = fmaf(q[d], x[d], score[u]);
-      }
+    for (int r = 0; r < R; ++r) {
+      const int i = i0 + lane, i2 = i - p[r].n;
+      weight[r] = i2 < 0 ? p[r].lse2[i * p[r].step] : i2 < p2[r].n ? p2[r].lse2[i2 * p2[r].step] : -INFINITY;
+    }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        score[u] = warp_sum(score[u]) * a.scale_log2;
-        mn = i + u < n ? fmaxf(mn, score[u]) : mn;
-      }
-      const float b = mn == -INFINITY ? 0.f : mn, f = ex2(m - b);
-      l *= f;
+    for (int r = 0; r < R; ++r) {
+      const float mn = fmaxf(x.m[r], warp_max(weight[r])), base = mn == -INFINITY ? 0.f : mn;
+      const float f = ex2(x.m[r] - base);
+      weight[r] = ex2(weight[r] - base);  // (0 past the last part; NaN stays NaN)
+      x.m[r] = mn;
+      x.l[r] = x.l[r] * f + warp_sum(weight[r]);
 #pragma unroll
-      for (int d = 0; d < DPL; ++d) acc[d] *= f;
+      for (int d = 0; d < DPL; ++d) x.acc[r][d] *= f;
+    }
+    const int most = min(32, n - i0);
+    for (int k0 = 0; k0 < most; k0 += K) {
+      float y[R][K][DPL];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i + u < n) {
-          const float e = ex2(score[u] - b);
-          l += e;
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int d = 0; d < DPL; ++d) acc[d] = fmaf(e, y[u][d], acc[d]);
+        for (int k = 0; k < K; ++k) {
+          const int i = i0 + k0 + k, i2 = i - p[r].n;
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) y[r][k][d] = 0.f;
+          if (i2 < p2[r].n)
+            paged_dims<float>((i2 < 0 ? p[r].o + i * p[r].step * HD : p2[r].o + i2 * p2[r].step * HD) + lane * DPL, y[r][k]);
         }
-      m = mn;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          const float e = __shfl_sync(0xffffffffu, weight[r], k0 + k);
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) x.acc[r][d] = fmaf(e, y[r][k][d], x.acc[r][d]);
+        }
     }
   }
-  const float inv = l > 0.f ? 1.f / l : l;  // no key: zeros (NaN stays NaN)
-  T* out = static_cast<T*>(a.out) + at_q;
-  if constexpr (DPL == 4 && sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
-  else if constexpr (DPL == 2 && sizeof(T) == 2)
-    *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
-  else
+}
+
+// The end of rows of KV head g of sequence s, given what all of the sequence's queries see:
+// adds the entries that a row's query sees and earlier ones do not, divides and writes.
+template <typename T, int HD, int R>
+__device__ __forceinline__ void paged_finish(const PagedArgs& a, int s, int g, PagedRows<HD, R>& x) {
+  constexpr int DPL = HD / 32;
+  auto ex2 = [](float v) { return sizeof(T) == 4 ? exp2f(v) : ex2_fast(v); };
+  const int lane = threadIdx.x & 31, cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
+  if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
+  size_t row[R];
 #pragma unroll
-    for (int d = 0; d < DPL; ++d) out[d] = from_f<T>(acc[d] * inv);
-  if (a.lse != nullptr && lane == 0) a.lse[row] = m + log2f(l);
+  for (int r = 0; r < R; ++r) {
+    const int rr = max(x.rr[r], 0), j = rr / a.per;
+    row[r] = (static_cast<size_t>(s) * a.n_q + j) * (static_cast<size_t>(a.Hkv) * a.per) + g * a.per + rr - j * a.per;
+  }
+  if (a.n_q > 1) {
+    const int first = max(0, len - a.n_q + 1);
+    int n[R], most = 0;  // entries of a row, up to 16
+    float q[R][DPL];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      n[r] = x.rr[r] < 0 ? 0 : len - a.n_q + x.rr[r] / a.per + 1 - first;
+      most = max(most, n[r]);
+      paged_dims<T>(static_cast<const T*>(a.q) + row[r] * HD + lane * DPL, q[r]);
+    }
+    const int pages = lane < most ? paged_page(a, a.table + static_cast<size_t>(s) * a.cols, first + lane) : 0;
+    for (int i = 0; i < most; i += 4) {  // four entries a round trip
+      float k4[4][DPL], v4[4][DPL];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int e = min(i + u, most - 1);
+        const size_t at = paged_at<HD>(a, __shfl_sync(0xffffffffu, pages, e), g, first + e) + lane * DPL;
+        paged_dims<T>(static_cast<const T*>(a.k) + at, k4[u]);
+        paged_dims<T>(static_cast<const T*>(a.v) + at, v4[u]);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (i >= n[r]) continue;
+        float score[4], mn = x.m[r];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          score[u] = 0.f;
+#pragma unroll
+          for (int d = 0; d < DPL; ++d) score[u] = fmaf(q[r][d], k4[u][d], score[u]);
+          score[u] = warp_sum(score[u]) * a.scale_log2;
+          mn = i + u < n[r] ? fmaxf(mn, score[u]) : mn;
+        }
+        const float base = mn == -INFINITY ? 0.f : mn, f = ex2(x.m[r] - base);
+        x.l[r] *= f;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) x.acc[r][d] *= f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (i + u < n[r]) {
+            const float e = ex2(score[u] - base);
+            x.l[r] += e;
+#pragma unroll
+            for (int d = 0; d < DPL; ++d) x.acc[r][d] = fmaf(e, v4[u][d], x.acc[r][d]);
+          }
+        x.m[r] = mn;
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (x.rr[r] < 0) continue;
+    const float inv = x.l[r] > 0.f ? 1.f / x.l[r] : x.l[r];  // no key: zeros (NaN stays NaN)
+    T* out = static_cast<T*>(a.out) + row[r] * HD + lane * DPL;
+    const float(&o)[DPL] = x.acc[r];
+    if constexpr (DPL == 4 && sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    else if constexpr (DPL == 2 && sizeof(T) == 2)
+      *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(o[0] * inv, o[1] * inv);
+    else
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) out[d] = from_f<T>(o[d] * inv);
+    if (a.lse != nullptr && lane == 0) a.lse[row[r]] = x.m[r] + log2f(x.l[r]);
+  }
 }
 
 }  // namespace zsaa
