@@ -505,10 +505,13 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  *   out    : as q (must not overlap it);  lse: float32 [S, n_q, Hq] or NULL, log2 of the
  *            normaliser as zsaa_op_attention gives it
  * A query that sees no entry gets zeros and lse -inf.  Entries that a query does not
- * see never touch its result, whatever they hold.  The prefix of a group is read once
- * for all of its queries.  Results do not depend on timing.  ws: 16-byte aligned,
- * ws_bytes at least what zsaa_op_paged_attention_workspace returns for these sizes
- * (host only; prefix_cols is ignored with G = 0). */
+ * see never touch its result, whatever they hold.  But for short tables the prefix of a
+ * group is read once for all of its queries.  Results do not depend on timing.  The
+ * lengths stay on the device, so a call is planned by the widths of its tables, cols and
+ * prefix_cols: rows much wider than the lengths cost time.  At most 65536 heads.  ws:
+ * 16-byte aligned, ws_bytes at least what zsaa_op_paged_attention_workspace returns for
+ * these sizes (host only; prefix_cols is ignored with G = 0); calls that may run at the
+ * same time need workspaces of their own. */
 zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
                                               int cols, int prefix_cols, size_t* bytes);
 zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, int n_q, int Hq,
