@@ -510,8 +510,7 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  * lengths stay on the device, so a call is planned by the widths of its tables, cols and
  * prefix_cols: rows much wider than the lengths cost time.  At most 65536 heads.  ws:
  * 16-byte aligned, ws_bytes at least what zsaa_op_paged_attention_workspace returns for
- * these sizes (host only; prefix_cols is ignored with G = 0); calls that may run at the
- * same time need workspaces of their own. */
+ * these sizes (host only; prefix_cols is ignored with G = 0). */
 zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
                                               int cols, int prefix_cols, size_t* bytes);
 zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, int n_q, int Hq,

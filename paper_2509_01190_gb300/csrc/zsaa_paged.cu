@@ -37,6 +37,11 @@ zsaa_status launched(const char* call, cudaError_t e) {
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// int32 and float32 arrays (or null)
+template <typename... P>
+bool words(const P*... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0;
+}
 bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + bn && y < x + an;
@@ -143,6 +148,7 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
   ZTRY(check_pages(kv));
   ZTRY(check_pool(kv));
   if (qkv == nullptr || pos == nullptr || table == nullptr || lens == nullptr) return bad("null argument");
+  if (!words(pos, cu_rows, table, lens)) return bad("int32 arrays must be 4-byte aligned");
   if (T < 1 || S < 1 || Hq < 1) return bad("T, S and Hq must be >= 1");
   if (cu_rows == nullptr && T != S) return bad("without cu_rows every sequence has one row: T must equal S");
   if (Hq % kv->n_kv_heads != 0) return bad("Hq must be a multiple of n_kv_heads");
@@ -190,6 +196,8 @@ zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, 
   if (q == nullptr || table == nullptr || lens == nullptr || out == nullptr || ws == nullptr) return bad("null argument");
   if (G > 0 && (cu_seqs == nullptr || prefix_table == nullptr || prefix_lens == nullptr))
     return bad("groups need cu_seqs, prefix_table and prefix_lens");
+  if (!words(table, lens, lse) || (G > 0 && !words(cu_seqs, prefix_table, prefix_lens)))
+    return bad("int32 and float32 arrays must be 4-byte aligned");
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(ws, 16)) return bad("q, out and ws must be 16-byte aligned");
   if (ws_bytes < need) return refuse(ZSAA_ERR_INVALID_ARG, "ws_bytes %zu, needs %zu", ws_bytes, need);
   const size_t q_bytes = static_cast<size_t>(S) * n_q * Hq * kv->head_dim * element(kv->dtype);
@@ -223,7 +231,7 @@ zsaa_status zsaa_op_beam_select(const float* logits, int64_t ld, int B, int W, i
   if (logits == nullptr || scores_out == nullptr || parent == nullptr || token == nullptr || ws == nullptr)
     return bad("null argument");
   if (ld < V || ld > (1LL << 40)) return bad("ld is shorter than V");
-  if (!aligned(logits, 4)) return bad("logits must be 4-byte aligned");
+  if (!words(logits, scores, scores_out, parent, token)) return bad("int32 and float32 arrays must be 4-byte aligned");
   if (eos < -1 || eos >= V) return bad("eos must be a token or -1");
   if (done != nullptr && eos < 0) return bad("done needs an eos token");
   if (!aligned(ws, 16)) return bad("ws must be 16-byte aligned");
@@ -246,6 +254,7 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
   if (layers == nullptr || parent == nullptr || table == nullptr || table_out == nullptr || lens == nullptr ||
       lens_out == nullptr || fresh == nullptr)
     return bad("null argument");
+  if (!words(parent, table, table_out, lens, lens_out, fresh)) return bad("int32 arrays must be 4-byte aligned");
   if (n_layers < 1 || n_layers > kReorderMaxLayers) return refuse(ZSAA_ERR_INVALID_ARG, "n_layers=%d outside [1, 64]", n_layers);
   const void *k[kReorderMaxLayers], *v[kReorderMaxLayers];
   for (int l = 0; l < n_layers; ++l) {

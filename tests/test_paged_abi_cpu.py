@@ -69,7 +69,8 @@ def test_pools_are_checked_by_every_call(zlib, kw):
 @pytest.mark.parametrize("kw", [
     dict(qkv=None), dict(pos=None), dict(table=None), dict(lens=None), dict(T=0), dict(S=0), dict(Hq=0), dict(Hq=3),
     dict(cu=None), dict(qkv_dtype=5), dict(theta=0.5), dict(theta=float("inf")), dict(theta=float("nan")), dict(cols=0),
-    dict(cols=1 << 28), dict(ld=511), dict(ld=516), dict(qkv=A + 2), dict(q_out=FAR + 8), dict(q_out=A + 64), dict(ld=-8)])
+    dict(cols=1 << 28), dict(ld=511), dict(ld=516), dict(qkv=A + 2), dict(q_out=FAR + 8), dict(q_out=A + 64), dict(ld=-8),
+    dict(pos=A + 2), dict(cu=A + 1), dict(table=A + 2), dict(lens=A + 3)])
 def test_append_refusals(zlib, kw):
     refused(zlib, lambda: append(zlib, **kw))
 
@@ -83,7 +84,8 @@ def test_append_refuses_bf16_rows_for_a_float32_pool(zlib):
     dict(q=None), dict(table=None), dict(lens=None), dict(out=None), dict(ws=None), dict(S=0), dict(Hq=0), dict(Hq=5),
     dict(G=-1), dict(cols=0), dict(pcols=0), dict(cu=None), dict(ptable=None), dict(plens=None), dict(q=A + 8),
     dict(out=FAR + 2), dict(ws=FAR + 8), dict(ws_bytes=64), dict(out=A + 256), dict(S=1 << 30), dict(G=1 << 30),
-    dict(cols=1 << 26, S=1 << 20), dict(Hq=1 << 17)])
+    dict(cols=1 << 26, S=1 << 20), dict(Hq=1 << 17),
+    dict(table=A + 2), dict(lens=A + 1), dict(lse=A + 2), dict(cu=A + 2), dict(ptable=A + 2), dict(plens=A + 2)])
 def test_attention_refusals(zlib, kw):
     refused(zlib, lambda: attention(zlib, **kw))
 
@@ -108,7 +110,8 @@ def test_attention_workspace_needs_no_device_and_covers_smaller_calls(zlib):
     dict(logits=None), dict(scores_out=None), dict(parent=None), dict(token=None), dict(ws=None), dict(B=0), dict(W=0),
     dict(W=65), dict(V=0), dict(V=(1 << 26) + 1, ld=1 << 27), dict(K=0), dict(K=65), dict(V=3, W=1, K=4, eos=1),
     dict(ld=999), dict(logits=A + 2), dict(eos=-2), dict(eos=1000), dict(eos=-1), dict(ws=A + 8), dict(ws_bytes=100),
-    dict(scores_out=A + 16), dict(done_out=A + 4), dict(B=1 << 26)])
+    dict(scores_out=A + 16), dict(done_out=A + 4), dict(B=1 << 26),
+    dict(scores=A + 2), dict(scores_out=FAR + 1), dict(parent=A + 2), dict(token=A + 2)])
 def test_select_refusals(zlib, kw):
     refused(zlib, lambda: select(zlib, **kw))
 
@@ -122,7 +125,8 @@ def test_select_workspace(zlib):
 
 @pytest.mark.parametrize("kw", [
     dict(parent=None), dict(table=None), dict(table_out=None), dict(lens=None), dict(lens_out=None), dict(fresh=None),
-    dict(B=0), dict(W=0), dict(W=65), dict(K=0), dict(K=65), dict(cols=0), dict(table_out=A + 4), dict(lens_out=A + 4)])
+    dict(B=0), dict(W=0), dict(W=65), dict(K=0), dict(K=65), dict(cols=0), dict(table_out=A + 4), dict(lens_out=A + 4),
+    dict(parent=A + 2), dict(table=A + 2), dict(table_out=FAR + 2), dict(lens=A + 2), dict(lens_out=FAR + 2), dict(fresh=A + 2)])
 def test_reorder_refusals(zlib, kw):
     refused(zlib, lambda: reorder(zlib, **kw))
 
