@@ -9,6 +9,8 @@ stream, and prints the mean time with the algorithmic rate.
     python -m paper_2509_01190_gb300.opbench attention --model 1b --batch 8 --seq 512
     python -m paper_2509_01190_gb300.opbench colmass --model 1b --batch 8 --seq 512
     python -m paper_2509_01190_gb300.opbench score_select --batch 32 --seq 4096 --dim 4096 --accel 4
+    python -m paper_2509_01190_gb300.opbench paged_attention --model 8b --batch 64 --groups 1 --seq 8192 --own 600
+    python -m paper_2509_01190_gb300.opbench beam_select --model 1b --batch 24 --beams 8
 
 GEMM names follow the layer: qkv (RoPE epilogue), o (residual), gate_up
 (SwiGLU), down (residual), lm_head (float32 logits).
@@ -56,7 +58,7 @@ def _time(fn, warmup: int, iters: int, graph: bool = False) -> float:
 
 def main(argv=None) -> None:
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["gemm", "attention", "colmass", "score_select"])
+    ap.add_argument("op", choices=["gemm", "attention", "colmass", "score_select", "paged_attention", "beam_select"])
     ap.add_argument("which", nargs="?", default="gate_up",
                     choices=["qkv", "o", "gate_up", "down", "lm_head"])
     ap.add_argument("--model", default="1b", choices=sorted(SHAPES))
@@ -65,6 +67,11 @@ def main(argv=None) -> None:
     ap.add_argument("--seq", type=int, default=512)
     ap.add_argument("--dim", type=int, default=4096)
     ap.add_argument("--accel", type=float, default=4.0)
+    ap.add_argument("--groups", type=int, default=0, help="paged_attention: groups that share prefixes of --seq entries")
+    ap.add_argument("--own", type=int, default=128, help="paged_attention: a sequence's own entries")
+    ap.add_argument("--queries", type=int, default=1, help="paged_attention: new entries per sequence")
+    ap.add_argument("--page", type=int, default=64, help="paged_attention: entries of a page")
+    ap.add_argument("--beams", type=int, default=8, help="beam_select: beams of a batch element, all kept")
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--iters", type=int, default=10)
     ap.add_argument("--graph", action="store_true", help="time a CUDA-graph replay of the iters calls")
@@ -121,6 +128,35 @@ def main(argv=None) -> None:
         mult = 4 if a.op == "attention" else 2
         flops = mult * B * Hq * hd * N * (N + 1) / 2
         print(f"{a.op} B={B} N={N} Hq={Hq} Hkv={Hkv} hd={hd}: {us:.1f} us, {flops / us / 1e6:.1f} TFLOP/s")
+    elif a.op == "paged_attention":
+        S, G, page, n_q = a.batch, a.groups, a.page, a.queries
+        pages = lambda n: -(-n // page)
+        n_pre, n_own = G * pages(a.seq), S * pages(a.own)
+        k, v = (torch.randn(n_pre + n_own, Hkv, page, hd, device=dev, generator=g).to(bf) for _ in range(2))
+        kv = z.make_pages(k, v)
+        order = torch.randperm(n_pre + n_own, device=dev, generator=g).to(torch.int32)
+        i32 = lambda x: torch.tensor(x, device=dev, dtype=torch.int32)
+        prefix = (i32([S * i // G for i in range(G + 1)]), G, order[:n_pre].clone(), pages(a.seq), i32([a.seq] * G)) \
+            if G else (None, 0, None, 0, None)
+        table, lens = order[n_pre:].clone(), i32([a.own] * S)
+        q = torch.randn(S, n_q, Hq, hd, device=dev, generator=g).to(bf)
+        out, lse = torch.empty_like(q), torch.empty(S, n_q, Hq, device=dev)
+        ws = torch.empty(z.zsaa_op_paged_attention_workspace(kv, S, n_q, Hq, G, pages(a.own), prefix[3]), device=dev,
+                         dtype=torch.uint8)
+        us = _time(lambda: z.zsaa_op_paged_attention(kv, q, S, n_q, Hq, table, pages(a.own), lens, *prefix, out, lse, ws,
+                                                     ws.numel()), a.warmup, a.iters, a.graph)
+        nbytes = 4.0 * Hkv * hd * (G * a.seq + S * a.own) + 4.0 * q.numel()
+        print(f"paged_attention S={S} n_q={n_q} G={G} prefix={a.seq if G else 0} own={a.own} Hq={Hq} Hkv={Hkv} hd={hd}: "
+              f"{us:.1f} us, {nbytes / us / 1e3:.0f} GB/s")
+    elif a.op == "beam_select":
+        B, W, V = a.batch, a.beams, sh.vocab
+        logits = torch.randn(B * W, V, device=dev, generator=g)
+        scores, best = torch.zeros(B, W, device=dev), torch.empty(B, W, device=dev)
+        parent, token = (torch.empty(B, W, device=dev, dtype=torch.int32) for _ in range(2))
+        ws = torch.empty(z.zsaa_op_beam_select_workspace(B, W, V, W), device=dev, dtype=torch.uint8)
+        us = _time(lambda: z.zsaa_op_beam_select(logits, V, B, W, V, scores, None, -1, W, best, parent, token, None, ws,
+                                                 ws.numel()), a.warmup, a.iters, a.graph)
+        print(f"beam_select B={B} W={W} V={V}: {us:.1f} us, {4.0 * B * W * V / us / 1e3:.0f} GB/s")
     else:
         B, L, dd = a.batch, a.seq, a.dim
         k = int(L // a.accel)

@@ -120,7 +120,10 @@ CASES = [
     ("bf16", 16, 2, 64, 16, 16, [16, 100, 3, 0], None, None),            # 128 rows of one sequence
     ("bf16", 8, 1, 128, 32, 9, [9, 257, 30], [0, 2, 3], [128, 129]),
     ("bf16", 5, 1, 64, 64, 3, [70, 3, 2], None, None),
+    ("bf16", 8, 1, 64, 16, 3, [5, 40], [0, 2], [12000]),                 # more than 32 partial results to a row
+    ("bf16", 20, 1, 128, 16, 1, [3] * 70, list(range(71)), [17] * 70),  # more than 32 groups
     ("f32", 4, 4, 32, 16, 1, [1, 0, 50], None, None),
+    ("f32", 2, 1, 64, 16, 1, [3] * 40, list(range(41)), [17] * 40),
     ("f32", 4, 4, 32, 16, 3, [77, 3, 12, 40], [0, 1, 4], [413, 100]),
     ("f32", 8, 2, 64, 32, 1, [33, 64, 31], [0, 2, 3], [200, 0]),
     ("f32", 9, 3, 128, 16, 2, [2, 1, 130], [0, 3], [65]),
