@@ -30,6 +30,8 @@
 // 1e-4.)  A thread's terms are added in 32 bits and everything after that as 64-bit
 // integers of 2^-36: FP64 runs at a sixty-fourth of FP32 here, and is left to a beam's
 // logarithm and the totals of its K tokens.
+#include <algorithm>
+
 #include "common.cuh"
 #include "paged.cuh"
 
@@ -113,9 +115,9 @@ __device__ __forceinline__ uint64_t down_by(uint64_t sum, float steps) {
 // value is (key << 32 | ~token), so that a larger one is a better one.  NaN logits are
 // ordered as -inf (their row's totals are all NaN).  Places before the row or past its end
 // hold -inf and come after every real one: as unsigned, their ~token is smaller.
-// Bound by HBM on large batches: 192 beams of 128003 logits in 22 us, half of the copy
-// rate over the beams that have not ended (29 with a bound and a list kept up from tile
-// to tile, whose barriers and rare branches then were most of the time).
+// Bound by its loads on large batches, and then by the end of the stretches: 192 beams of
+// 128256 logits in 24 us from HBM, 4.1 TB/s, 60% of the copy rate (29 with a bound and a list kept
+// up from step to step, whose barriers and rare branches then were most of the time).
 __global__ void __launch_bounds__(kScanThreads, 4)
     beam_scan_kernel(const float* __restrict__ logits, long long ld, int V, int K, int chunks, int tiles,
                      const uint8_t* __restrict__ done, BeamChunk* __restrict__ stat, uint2* __restrict__ cand) {
@@ -340,33 +342,112 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   }
 }
 
-// Half of the warps put the beams' sums together, the other half their lists.
+// Half of the warps put the beams' sums together, the other half their lists; what more than
+// kSumWarps beams have, all of them.
 constexpr int kSumWarps = kMergeWarps / 2;
 
+// An element and another beam: up to so many such pairs are ranked by counting, more take a
+// merge of the beams' lists by one warp (us of 24 selections from 32000 logits a beam, counting
+// and merge: 8 beams with 8 tokens, 512 pairs, 11.7 and 12.7; with 16, 1024, 15.7 and 17.4; 16
+// beams with 16, 4096, 30.9 and 27.2).
+constexpr int kRankPairs = 1024;
+
+// 8 bytes from device memory to this thread's place in shared memory
+__device__ __forceinline__ void cp_async8(void* to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+
+// Bound by its chain of steps: 8 tokens of 8 beams 6 us, 64 of 64 beams 80 (cold).
 __global__ void __launch_bounds__(kMergeThreads)
     beam_merge_kernel(const BeamChunk* __restrict__ stat, const uint2* __restrict__ cand, int W, int V, int K,
                       int chunks, const float* __restrict__ scores, const uint8_t* __restrict__ done, int eos,
                       float* __restrict__ scores_out, int32_t* __restrict__ parent, int32_t* __restrict__ token,
                       uint8_t* __restrict__ done_out) {
   extern __shared__ __align__(16) uint8_t smem[];
+  const int list_warps = W > kSumWarps ? kMergeWarps : kSumWarps;
   uint64_t* total = reinterpret_cast<uint64_t*>(smem);    // [W][K] ordered totals (0: none, or NaN)
   uint2* best = reinterpret_cast<uint2*>(total + W * K);  // [W][K] (key, token) in order; key 0: none
   uint2* merged = best + W * K;                           // [list warps][2][K] lists of the chunks merged so far
-  uint2* cache = merged + kSumWarps * 2 * K;              // [list warps][depth][64] the lists' first elements
-  int* rank = reinterpret_cast<int*>(cache + kSumWarps * kMergeDepth * 64);  // [W][K]
+  uint2* cache = merged + list_warps * 2 * K;             // [list warps][depth][64] the lists' next elements
   __shared__ uint64_t s_sum[kBeamMaxBeams];
   __shared__ float s_n2[kBeamMaxBeams];
   __shared__ double s_lse[kBeamMaxBeams], s_score[kBeamMaxBeams];
   __shared__ uint8_t s_done[kBeamMaxBeams], s_bad[kBeamMaxBeams];
+  __shared__ int rank[kRankPairs];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = blockIdx.x, n = W * K;
+  const bool few = n * W <= kRankPairs;
   pdl_trigger();
   pdl_wait();
   stat = after_wait(stat) + static_cast<size_t>(b) * W * chunks;
   cand = after_wait(cand) + static_cast<size_t>(b) * W * chunks * K;
   scores = after_wait(scores);
   done = after_wait(done);
-  for (int i = tid; i < n; i += kMergeThreads) rank[i] = i % K;  // its place in its own beam's list
+  if (few)
+    for (int i = tid; i < n; i += kMergeThreads) rank[i] = i % K;  // its place in its own beam's list
+  // Beam w's best tokens in order.  The chunks' lists are in order: K times the best head of
+  // two lists a lane, the list merged so far in place 0 and up to 63 chunks after it.  Equal
+  // keys go by place, so the lower token comes first.  A list's next kMergeDepth elements
+  // are in shared memory or on their way there, one asked for with each that is taken.
+  auto merge_lists = [&](int w, int slot) {
+    uint2* row = best + w * K;
+    const uint2* lists = cand + static_cast<size_t>(w) * chunks * K;
+    const uint2* so_far = nullptr;
+    uint2* mine = cache + slot * kMergeDepth * 64 + lane;
+    const bool over = done != nullptr && done[b * W + w] != 0;
+    for (int c0 = 0; c0 < chunks; c0 += 63) {
+      uint2* to = c0 + 63 >= chunks ? row : merged + (slot * 2 + (c0 / 63) % 2) * K;
+      const uint2* at[2] = {nullptr, nullptr};
+      int pos[2] = {0, 0};
+      uint2 head[2];
+      auto advance = [&](int i) {
+        const int taken = pos[i]++;
+        if (K <= kMergeDepth) {  // all there
+          head[i] = pos[i] < K ? mine[pos[i] * 64 + 32 * i] : make_uint2(0, 0);
+          return;
+        }
+        if (taken + kMergeDepth < K) cp_async8(&mine[taken % kMergeDepth * 64 + 32 * i], at[i] + taken + kMergeDepth);
+        cp_async_commit();
+        cp_async_wait<kMergeDepth - 1>();
+        head[i] = pos[i] < K ? mine[pos[i] % kMergeDepth * 64 + 32 * i] : make_uint2(0, 0);
+      };
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {  // (all in flight together: one by one, each would cost its own round trip)
+        const int c = c0 + lane + 32 * i - 1;
+        at[i] = lane + 32 * i == 0 ? so_far : c < chunks ? lists + static_cast<size_t>(c) * K : nullptr;
+        uint2 x[kMergeDepth];
+#pragma unroll
+        for (int k = 0; k < kMergeDepth; ++k) x[k] = at[i] != nullptr && k < K ? at[i][k] : make_uint2(0, 0);
+#pragma unroll
+        for (int k = 0; k < kMergeDepth; ++k) mine[k * 64 + 32 * i] = x[k];
+        head[i] = x[0];
+      }
+      if (over) break;
+      for (int k = 0; k < K; ++k) {
+        const uint32_t x = __reduce_max_sync(0xffffffffu, max(head[0].x, head[1].x));
+        const unsigned m0 = __ballot_sync(0xffffffffu, head[0].x == x), m1 = __ballot_sync(0xffffffffu, head[1].x == x);
+        if (lane == __ffs(m0 != 0 ? m0 : m1) - 1) {
+          if (m0 == 0) {
+            to[k] = head[1];
+            advance(1);
+          } else if (lane > 0 || so_far == nullptr) {
+            to[k] = head[0];
+            if (at[0] != nullptr) advance(0);
+          } else {  // (the list merged so far is in shared memory)
+            to[k] = head[0];
+            head[0] = ++pos[0] < K ? so_far[pos[0]] : make_uint2(0, 0);
+          }
+        }
+      }
+      cp_async_wait<0>();
+      __syncwarp();
+      so_far = to;
+    }
+    if (over)  // eos at no cost; the other tokens, in their order, are not allowed
+      for (int k = lane; k < K; k += 32)
+        row[k] = k >= V ? make_uint2(0, 0)
+                        : make_uint2(k == 0 ? 0x80000000u : 0x007fffffu, k == 0 ? eos : k - 1 < eos ? k - 1 : k);
+  };
   if (warp < kSumWarps) {
     for (int w = warp; w < W; w += kSumWarps) {
       // (every load of a beam in one round trip: what an ended one's are is of no account)
@@ -411,89 +492,69 @@ __global__ void __launch_bounds__(kMergeThreads)
         lse = (static_cast<double>(n2) + log2(static_cast<double>(s_sum[tid]) * (1.0 / kSumUnit))) * kLn2;
       s_lse[tid] = lse;
     }
+    __syncwarp();
+    for (int w = kSumWarps + warp; w < W; w += kMergeWarps) merge_lists(w, kSumWarps + warp);
   } else {
-    for (int w = warp - kSumWarps; w < W; w += kSumWarps) {
-      uint2* row = best + w * K;
-      // The chunks' lists are in order: K times the best head of two lists a lane, the
-      // list merged so far in place 0 and up to 63 chunks after it.  Equal keys go by
-      // place, so the lower token comes first.
-      const uint2* lists = cand + static_cast<size_t>(w) * chunks * K;
-      const uint2* so_far = nullptr;
-      uint2* mine = cache + (warp - kSumWarps) * kMergeDepth * 64 + lane;
-      const bool over = done != nullptr && done[b * W + w] != 0;
-      for (int c0 = 0; c0 < chunks; c0 += 63) {
-        uint2* to = c0 + 63 >= chunks ? row : merged + ((warp - kSumWarps) * 2 + (c0 / 63) % 2) * K;
-        const uint2* at[2] = {nullptr, nullptr};
-        int pos[2] = {0, 0};
-        uint2 head[2];
-        auto load = [&](int i) {
-          if (at[i] == nullptr || pos[i] >= K) return make_uint2(0, 0);
-          return pos[i] < kMergeDepth ? mine[pos[i] * 64 + 32 * i] : at[i][pos[i]];
-        };
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {  // (all in flight together: one by one, each would cost its own round trip)
-          const int c = c0 + lane + 32 * i - 1;
-          at[i] = lane + 32 * i == 0 ? so_far : c < chunks ? lists + static_cast<size_t>(c) * K : nullptr;
-          uint2 x[kMergeDepth];
-#pragma unroll
-          for (int k = 0; k < kMergeDepth; ++k) x[k] = at[i] != nullptr && k < K ? at[i][k] : make_uint2(0, 0);
-#pragma unroll
-          for (int k = 0; k < kMergeDepth; ++k) mine[k * 64 + 32 * i] = x[k];
-          head[i] = x[0];
-        }
-        if (over) break;
-        for (int k = 0; k < K; ++k) {
-          const uint32_t x = __reduce_max_sync(0xffffffffu, max(head[0].x, head[1].x));
-          const unsigned m0 = __ballot_sync(0xffffffffu, head[0].x == x), m1 = __ballot_sync(0xffffffffu, head[1].x == x);
-          if (lane == __ffs(m0 != 0 ? m0 : m1) - 1) {
-            if (m0 != 0) {
-              to[k] = head[0];
-              ++pos[0];
-              head[0] = load(0);
-            } else {
-              to[k] = head[1];
-              ++pos[1];
-              head[1] = load(1);
-            }
-          }
-        }
-        __syncwarp();
-        so_far = to;
-      }
-      if (over)  // eos at no cost; the other tokens, in their order, are not allowed
-        for (int k = lane; k < K; k += 32)
-          row[k] = k >= V ? make_uint2(0, 0)
-                          : make_uint2(k == 0 ? 0x80000000u : 0x007fffffu, k == 0 ? eos : k - 1 < eos ? k - 1 : k);
-    }
+    for (int w = warp - kSumWarps; w < W; w += list_warps) merge_lists(w, warp - kSumWarps);
   }
   __syncthreads();
   for (int i = tid; i < n; i += kMergeThreads)
     total[i] = double_key(s_score[i / K] + (static_cast<double>(key_float(best[i].x)) - s_lse[i / K]));
   __syncthreads();
-  // A beam's totals fall along its list, so an element's rank is the sum over the beams
-  // of how many of theirs come before it: equal totals of an earlier beam do.
-  for (int e = tid; e < n * W; e += kMergeThreads) {
-    const int i = e % n, u = e / n, w = i / K;
-    if (u == w || best[i].x == 0) continue;
-    const uint64_t x = total[i];
-    int lo = 0, hi = K;  // the first element of beam u that does not come before
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      const uint64_t y = total[u * K + mid];
-      if (best[u * K + mid].x != 0 && (y > x || (y == x && u < w))) lo = mid + 1; else hi = mid;
-    }
-    if (lo > 0) atomicAdd(&rank[i], lo);
-  }
-  __syncthreads();
-  for (int i = tid; i < n; i += kMergeThreads) {
-    const int r = rank[i];
-    if (r >= K || best[i].x == 0) continue;
-    const int w = i / K, tok = static_cast<int>(best[i].y);
+  auto put = [&](int r, int w, int i, uint64_t x) {  // total x of element i, beam w's, has rank r
     const size_t o = static_cast<size_t>(b) * K + r;
-    scores_out[o] = key_double_to_float(total[i]);
+    const int tok = static_cast<int>(best[i].y);
+    scores_out[o] = key_double_to_float(x);
     parent[o] = w;
     token[o] = tok;
     if (done_out != nullptr) done_out[o] = s_done[w] || tok == eos;
+  };
+  // A beam's totals fall along its list.  Few: an element's rank is the sum over the beams of
+  // how many of theirs come before it (equal totals of an earlier beam do).
+  if (few) {
+    for (int e = tid; e < n * W; e += kMergeThreads) {
+      const int i = e % n, u = e / n, w = i / K;
+      if (u == w || best[i].x == 0) continue;
+      const uint64_t x = total[i];
+      int lo = 0, hi = K;  // the first element of beam u that does not come before
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        const uint64_t y = total[u * K + mid];
+        if (best[u * K + mid].x != 0 && (y > x || (y == x && u < w))) lo = mid + 1; else hi = mid;
+      }
+      if (lo > 0) atomicAdd(&rank[i], lo);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kMergeThreads)
+      if (rank[i] < K && best[i].x != 0) put(rank[i], i / K, i, total[i]);
+    return;
+  }
+  // Many: K times the best head of two beams a lane, equal totals by beam.
+  if (warp > 0) return;
+  uint64_t head[2];
+  bool there[2];
+  int pos[2] = {0, 0};
+  auto look = [&](int i) {
+    const int w = lane + 32 * i, at = w * K + pos[i];
+    there[i] = w < W && pos[i] < K && best[at].x != 0;
+    head[i] = there[i] ? total[at] : 0;
+  };
+  look(0);
+  look(1);
+  for (int r = 0; r < K; ++r) {
+    const uint64_t x = warp_max_u64(max(head[0], head[1]));
+    const unsigned m0 = __ballot_sync(0xffffffffu, there[0] && head[0] == x);
+    const unsigned m1 = __ballot_sync(0xffffffffu, there[1] && head[1] == x);
+    if (lane != __ffs(m0 != 0 ? m0 : m1) - 1) continue;
+    const int i = m0 != 0 ? 0 : 1, w = lane + 32 * i;
+    put(r, w, w * K + pos[i], x);
+    if (i == 0) {
+      ++pos[0];
+      look(0);
+    } else {
+      ++pos[1];
+      look(1);
+    }
   }
 }
 
@@ -564,16 +625,23 @@ cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, 
                                const uint8_t* done, int eos, int K, float* scores_out, int32_t* parent,
                                int32_t* token, uint8_t* done_out, BeamChunk* stat, uint2* cand, int sms,
                                cudaStream_t s) {
-  // Long stretches save most of a stretch's fixed work, short ones keep the SMs even: about
-  // two rounds of the resident CTAs.
-  const int rows = B * W;
-  int chunks = beam_chunks_most(V);
-  const long long t = static_cast<long long>(rows) * chunks / (8LL * sms);
-  const int tiles = t < 1 ? 1 : t > 16 ? 16 : static_cast<int>(t);
-  chunks = (chunks + tiles - 1) / tiles;
+  // Long stretches save most of a stretch's fixed work, short ones keep the SMs even: one
+  // round of the resident CTAs (four to an SM) while that is up to four steps each, else two.
+  // 128256 logits, us by steps: 64 beams (4 are one round) 18.4 with one, 14.3 with two,
+  // 13.9 with four, 15.5 with eight; 192 (11 and 6 steps) 28.4 with five, 27.6 with six, 29.0
+  // with 11; 256 (16 and 8) 30.7 with five, 31.1 with eight, 32.2 with 16.
+  const int rows = B * W, total = beam_chunks_most(V);
+  auto steps = [&](int rounds) {
+    const int c = std::max(1, std::min(total, rounds * 4 * sms / rows));
+    return (total + c - 1) / c;
+  };
+  const int tiles = steps(1) <= 4 ? steps(1) : std::min(steps(2), 16);
+  const int chunks = (total + tiles - 1) / tiles;
   ZSAA_LAUNCH(beam_scan_kernel, dim3(static_cast<unsigned>(rows) * static_cast<unsigned>(chunks)), dim3(kScanThreads), 0,
               s, logits, ld, V, K, chunks, tiles, done, stat, cand);
-  auto merge_smem = [](int w, int k) { return w * k * 20 + kSumWarps * (2 * k + kMergeDepth * 64) * 8; };
+  auto merge_smem = [](int w, int k) {
+    return w * k * 16 + (w > kSumWarps ? kMergeWarps : kSumWarps) * (2 * k + kMergeDepth * 64) * 8;
+  };
   static OncePerDevice once;
   const cudaError_t e = set_smem_limit_once(once, beam_merge_kernel, merge_smem(kBeamMaxBeams, kBeamMaxKept));
   if (e != cudaSuccess) return e;
