@@ -287,10 +287,11 @@ bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int 
 // 256: 41 and 35, with 64 dims 28 and 33; of 1024 46 and 38.  A shared prefix is read again
 // for every sequence: 64 sequences in 8 groups, 512 keys 20 and 23, 1024 33 and 27; with
 // 32 rows 62 and 78, 91 and 87.
-// In float32 a block of keys takes five times as long.  Heads of 32, 64 and 128 dims: 4
-// sequences of 32 keys 3.3 and 6.6, 3.5 and 7.4, 4.4 and 7.8, of 128 6.9 and 7.2, 8.2 and
-// 8.4, 12 and 7.8; 64 of 128 20 and 25, 23 and 27, 34 and 50; 64 in 8 groups, 32 keys 12 and
-// 17, 13 and 19, 17 and 21, 128 25 and 17, 29 and 18, 38 and 30.
+// In float32, 4 sequences and 4 heads of 32, 64 and 128 dims: 128 keys 3.7 and 6.5, 4.5 and
+// 7.0, 6.6 and 9.0, 512 7.3 and 8.0, 10.2 and 8.9, 17 and 10.5; 16 sequences and 8 heads: 1024
+// 12 and 17, 19 and 32, 33 and 41; 64: 43 and 41, 62 and 64, 112 and 120.  64 in 8 groups: 128
+// 11 and 12, 14 and 17, 23 and 25, 256 16 and 15, 22 and 20, 36 and 34, 512 25 and 20, 35 and
+// 26, 62 and 49.
 long long direct_ctas(const PagedArgs& a) {
   return static_cast<long long>(a.S) * a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16);
 }
@@ -309,7 +310,8 @@ bool own_in_one(const PagedArgs& a, int hd) {
 bool direct_call(const PagedArgs& a, bool bf16, int hd) {
   const long long keys = static_cast<long long>(a.cols + a.pcols) << a.page_shift;
   if (a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16) > 65535) return false;
-  if (!bf16) return keys * hd <= (a.G == 0 ? 4096 : 2048);
+  if (!bf16 && a.G == 0) return keys * hd <= 16384 || (direct_ctas(a) >= 96 && keys <= 1024);
+  if (!bf16) return keys <= 256 || keys * hd <= 16384;
   return a.G == 0 ? own_in_one(a, hd) : keys <= (direct_ctas(a) <= 152 ? 1024 : 512);
 }
 
@@ -328,7 +330,7 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   for (int i = 0; i < r.n; ++i) {
     const bool pre = i == 0, seq = i == r.n - 1 && !r.own;
     r.tc[i] = pre ? tc_pre : tc_seq;
-    r.tiles[i] = !bf ? paged_f32_tiles(sms) : r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(hd, sms);
+    r.tiles[i] = r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(dtype, hd, sms);
     r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
     const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
     const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
@@ -340,24 +342,16 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
 
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
-  constexpr bool f32 = sizeof(T) == 4;
-  if (direct_call(a, !f32, HD)) {
-    if constexpr (f32) return launch_paged_f32_direct(a, HD, s);
-    return launch_paged_direct(a, nullptr, HD, direct_ctas(a) <= 152, s);  // (eight warps a CTA where four would leave SMs empty)
-  }
-  const Launches r = launches_of(a, f32 ? ZSAA_F32 : ZSAA_BF16, HD, std::min(sms, kMostSms), ws);
+  constexpr int dtype = sizeof(T) == 4 ? ZSAA_F32 : ZSAA_BF16;
+  const bool wide = direct_ctas(a) <= 152;  // eight warps a CTA where four would leave SMs empty
+  if (direct_call(a, dtype == ZSAA_BF16, HD)) return launch_paged_direct(a, nullptr, dtype, HD, wide, s);
+  const Launches r = launches_of(a, dtype, HD, std::min(sms, kMostSms), ws);
   for (int i = 0; i < r.n; ++i) {
-    if constexpr (f32) {
-      const cudaError_t e = launch_paged_f32(a, r.work[i], HD, r.tiles[i].ctas, s);
-      if (e != cudaSuccess) return e;
-    } else {
-      const cudaError_t e = r.tc[i] ? launch_paged_tc(a, r.work[i], HD, r.tiles[i].ctas, s)
-                                    : launch_paged_mma(a, r.work[i], HD, r.tiles[i].ctas, s);
-      if (e != cudaSuccess) return e;
-    }
+    const cudaError_t e = r.tc[i] ? launch_paged_tc(a, r.work[i], HD, r.tiles[i].ctas, s)
+                                  : launch_paged_mma(a, r.work[i], dtype, HD, r.tiles[i].ctas, s);
+    if (e != cudaSuccess) return e;
   }
-  if constexpr (!f32)
-    if (r.own) return launch_paged_direct(a, &r.work[0], HD, direct_ctas(a) <= 152, s);
+  if (r.own) return launch_paged_direct(a, &r.work[0], dtype, HD, wide, s);
   const int heads = a.Hkv * a.per, per_cta = kJoinThreads / 32;
   ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(a.S * a.n_q, (heads + per_cta - 1) / per_cta), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
   return cudaSuccess;

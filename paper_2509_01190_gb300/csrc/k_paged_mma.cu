@@ -1,35 +1,46 @@
-// Attention over a paged cache for few query rows (bf16): tiles of 16 rows against the
-// keys of an entry on mma.sync m16n8k16.
+// Attention over a paged cache on mma.sync: tiles of 16 query rows against the keys of an
+// entry; few rows in bf16 (m16n8k16), any number in float32 (m16n8k8).
 //
 // A decode step has n_q * (Hq / Hkv) rows to each KV head, 4 or 8 as a rule, so the
 // keys and values stream past once and the tensor work is small: the kernel is bound
 // by HBM on long caches and by its chain of loads on short ones.  Each of the 4 warps
-// walks its own 16 keys of every block of 64 with a ring of cp.async stages of its own,
-// so nothing but the end of a part synchronises the CTA; 16 keys never leave a page.
-// The ring runs ahead over the ends of parts: a CTA with several short items has the
+// walks its own 16 keys (float32: 8) of every block with a ring of cp.async stages of its
+// own, so nothing but the end of a part synchronises the CTA; a warp's keys never leave a
+// page.  The ring runs ahead over the ends of parts: a CTA with several short items has the
 // next item's keys in flight while it joins its warps' results of the last.
 //
-// Per 16 keys: S = Q K^T, the running maximum (moved only when the tile's exceeds it by
-// 2^8: P entries up to 256 are exact in float32 and in the pair), P = 2^(S scale - m)
-// carried as the bf16 pair P_hi + P_lo (one bf16 would cost 0.1% in every output), and
-// O += P_hi V + P_lo V in float32.
+// Per tile of keys: S = Q K^T, the running maximum (moved only when the tile's exceeds it by
+// 2^8: P entries up to 256 are exact in float32 and in the pair), P = 2^(S scale - m), and
+// O += P V in float32.  In bf16, P is carried as the pair P_hi + P_lo (one bf16 would cost
+// 0.1% in every output).
+//
+// float32 operands are split into pairs of tf32: x = hi + lo, hi the nearest number of 11
+// significant bits, lo the rest rounded to 11, which leaves 2^-24 |x| at most, the rounding of
+// a float32; the products hi hi, hi lo and lo hi are taken and lo lo, below 2^-24 of the
+// product, is not.  The tensor cores' own sums may be rounded towards zero, so none is longer
+// than four products of a kind: scores are put together from such sums, and a tile's P V is
+// added to the output, in float32 additions.
+#include <algorithm>
+
 #include "paged.cuh"
 
 namespace zsaa {
 namespace {
 
-constexpr int MM_WARPS = 4, MM_THREADS = 32 * MM_WARPS, MM_ROWS = 16, MM_KEYS = 16 * MM_WARPS;
+constexpr int MM_WARPS = 4, MM_THREADS = 32 * MM_WARPS, MM_ROWS = 16;
 constexpr int MM_STAGES = 3;
 constexpr int MM_JOIN = 1024;  // floats of a warp in the buffer that joins results: 8 rows of 128 dims, 16 of 64
 constexpr float MM_RESCALE_LOG2 = 8.f;
 
-template <int HD>
+template <typename T, int HD>
 struct MmCfg {
-  static constexpr int TILE = 16 * HD * 2;  // 16 keys, or their values
+  static constexpr int KEYS = 32 / sizeof(T);    // of a warp's tile
+  static constexpr int BLOCK = KEYS * MM_WARPS;  // of a block
+  static constexpr int TILE = KEYS * HD * static_cast<int>(sizeof(T));  // bytes of a tile's keys, or their values
   static constexpr int RING = MM_STAGES * 2 * TILE;  // a warp's
   static constexpr int JOIN = MM_WARPS * MM_JOIN * 4;
   static constexpr int SMEM = MM_WARPS * RING + JOIN;
-  static constexpr int CTAS = HD == 128 ? 2 : 3;  // resident per SM
+  static constexpr int CTAS = HD == 128 ? 2 : HD == 64 ? 3 : 4;  // resident per SM
 };
 
 // byte offset of 16-byte chunk c of row r, chunks XOR-swizzled by the row (conflict-free ldmatrix)
@@ -41,14 +52,25 @@ __device__ __forceinline__ uint32_t mm_swz(int r, int c) {
 // A warp's rows: queries as the A operand (rows gid and gid + 8, dims 2 tig, 2 tig + 1 and
 // those + 8 of every 16), accumulators, and maximum and sum of rows gid and gid + 8 (the sum
 // of this thread's keys alone).
+template <typename T, int HD>
+struct MmRows;
 template <int HD>
-struct MmRows {
+struct MmRows<bf16, HD> {
   uint32_t q[HD / 16][4];
   float o[HD / 8][4];
   float m[2], l[2];
 };
+// float32: a product's 8 terms are dims 16 j + 4 tig + 2 (t & 1), + 1 of the four tig, for
+// t = 2 j or 2 j + 1, so that a thread's dims of a key lie together; o[4 i + k] has dims
+// 32 i + 8 tig + k and those + 4
 template <int HD>
-__device__ __forceinline__ void mm_clear(MmRows<HD>& x) {
+struct MmRows<float, HD> {
+  uint32_t qh[HD / 8][4], ql[HD / 8][4];
+  float o[HD / 8][4];
+  float m[2], l[2];
+};
+template <typename T, int HD>
+__device__ __forceinline__ void mm_clear(MmRows<T, HD>& x) {
 #pragma unroll
   for (int i = 0; i < HD / 8; ++i) x.o[i][0] = x.o[i][1] = x.o[i][2] = x.o[i][3] = 0.f;
   x.m[0] = x.m[1] = -INFINITY;
@@ -56,7 +78,7 @@ __device__ __forceinline__ void mm_clear(MmRows<HD>& x) {
 }
 // q0, q1: rows gid and gid + 8; in0, in1: whether there are such
 template <int HD>
-__device__ __forceinline__ void mm_load_q(MmRows<HD>& x, const bf16* q0, const bf16* q1, bool in0, bool in1) {
+__device__ __forceinline__ void mm_load_q(MmRows<bf16, HD>& x, const bf16* q0, const bf16* q1, bool in0, bool in1) {
   const int tig = threadIdx.x & 3;
 #pragma unroll
   for (int kk = 0; kk < HD / 16; ++kk) {
@@ -66,26 +88,92 @@ __device__ __forceinline__ void mm_load_q(MmRows<HD>& x, const bf16* q0, const b
     x.q[kk][3] = in1 ? *reinterpret_cast<const uint32_t*>(q1 + 16 * kk + 8 + 2 * tig) : 0u;
   }
 }
-// Asks for up to 16 keys and their values, which lie one after the other from element `at`
-// on; rows past `keys` are zero.
+__device__ __forceinline__ void mm_split(float x, uint32_t& hi, uint32_t& lo) {
+  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+  lo = (__float_as_uint(x - __uint_as_float(hi)) + 0x1000u) & 0xffffe000u;
+}
 template <int HD>
-__device__ __forceinline__ void mm_load_tile(const PagedArgs& a, uint32_t sk, size_t at, int keys) {
-  constexpr int CH = HD / 8, STEP = 32 / CH;  // chunks per row, rows per round
-  const int lane = threadIdx.x & 31, c = lane % CH;
-  const uint32_t sv = sk + MmCfg<HD>::TILE;
+__device__ __forceinline__ void mm_load_q(MmRows<float, HD>& x, const float* q0, const float* q1, bool in0, bool in1) {
+  const int tig = threadIdx.x & 3;
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < 16 / STEP; ++i) {
+  for (int j = 0; j < HD / 16; ++j) {
+    const float4 u = in0 ? *reinterpret_cast<const float4*>(q0 + 16 * j + 4 * tig) : zero;
+    const float4 v = in1 ? *reinterpret_cast<const float4*>(q1 + 16 * j + 4 * tig) : zero;
+    mm_split(u.x, x.qh[2 * j][0], x.ql[2 * j][0]);
+    mm_split(v.x, x.qh[2 * j][1], x.ql[2 * j][1]);
+    mm_split(u.y, x.qh[2 * j][2], x.ql[2 * j][2]);
+    mm_split(v.y, x.qh[2 * j][3], x.ql[2 * j][3]);
+    mm_split(u.z, x.qh[2 * j + 1][0], x.ql[2 * j + 1][0]);
+    mm_split(v.z, x.qh[2 * j + 1][1], x.ql[2 * j + 1][1]);
+    mm_split(u.w, x.qh[2 * j + 1][2], x.ql[2 * j + 1][2]);
+    mm_split(v.w, x.qh[2 * j + 1][3], x.ql[2 * j + 1][3]);
+  }
+}
+// A thread's results into rows gid and gid + 8 (where there are such) of a buffer of `dims`
+// floats a row, dims d0 on; a row's groups of 8 floats are XORed by its number, which keeps
+// stores and loads clear of bank conflicts.
+template <int HD>
+__device__ __forceinline__ void mm_put(const MmRows<bf16, HD>& x, float* row0, float* row8, int d0, int dims, bool in0, bool in1) {
+  const int lane = threadIdx.x & 31, flip = (lane >> 2 & 3) * 8, tig = lane & 3;
+#pragma unroll
+  for (int i = 0; i < HD / 8; ++i)
+    if (8 * i >= d0 && 8 * i < d0 + dims) {
+      const int c = ((8 * i - d0) ^ flip) + 2 * tig;
+      if (in0) *reinterpret_cast<float2*>(row0 + c) = make_float2(x.o[i][0], x.o[i][1]);
+      if (in1) *reinterpret_cast<float2*>(row8 + c) = make_float2(x.o[i][2], x.o[i][3]);
+    }
+}
+template <int HD>
+__device__ __forceinline__ void mm_put(const MmRows<float, HD>& x, float* row0, float* row8, int d0, int dims, bool in0, bool in1) {
+  const int lane = threadIdx.x & 31, flip = (lane >> 2 & 3) * 8, tig = lane & 3;
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i)
+    if (32 * i >= d0 && 32 * i < d0 + dims) {
+      const int c = (32 * i + 8 * tig - d0) ^ flip;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (in0)
+          *reinterpret_cast<float4*>(row0 + c + 4 * k) = make_float4(x.o[4 * i][k], x.o[4 * i + 1][k], x.o[4 * i + 2][k], x.o[4 * i + 3][k]);
+        if (in1)
+          *reinterpret_cast<float4*>(row8 + c + 4 * k) =
+              make_float4(x.o[4 * i][2 + k], x.o[4 * i + 1][2 + k], x.o[4 * i + 2][2 + k], x.o[4 * i + 3][2 + k]);
+      }
+    }
+}
+// byte offsets of 16-byte chunk c of a tile's row r: keys and values, free of bank conflicts
+// as mm_tile reads them
+template <typename T, int HD>
+__device__ __forceinline__ uint32_t mm_key(int r, int c) {
+  if constexpr (sizeof(T) == 2) return mm_swz<HD>(r, c);
+  return static_cast<uint32_t>(r * HD * 4 + ((c ^ (r & 1) << 2) << 4));
+}
+template <typename T, int HD>
+__device__ __forceinline__ uint32_t mm_value(int r, int c) {
+  if constexpr (sizeof(T) == 2) return mm_swz<HD>(r, c);
+  return static_cast<uint32_t>(r * HD * 4 + ((c ^ (r >> 1 & 3) << 1) << 4));
+}
+// Asks for a tile's keys and their values, which lie one after the other from element `at`
+// on; rows past `keys` are zero.
+template <typename T, int HD>
+__device__ __forceinline__ void mm_load_tile(const PagedArgs& a, uint32_t sk, size_t at, int keys) {
+  using C = MmCfg<T, HD>;
+  constexpr int E = 16 / sizeof(T), CH = HD / E, STEP = 32 / CH;  // elements of a chunk, chunks per row, rows per round
+  const int lane = threadIdx.x & 31, c = lane % CH;
+  const uint32_t sv = sk + C::TILE;
+#pragma unroll
+  for (int i = 0; i < C::KEYS / STEP; ++i) {
     const int r = lane / CH + i * STEP;
-    const size_t from = at + static_cast<size_t>(r < keys ? r : 0) * HD + c * 8;
-    cp_async16(sk + mm_swz<HD>(r, c), static_cast<const bf16*>(a.k) + from, r < keys);
-    cp_async16(sv + mm_swz<HD>(r, c), static_cast<const bf16*>(a.v) + from, r < keys);
+    const size_t from = at + static_cast<size_t>(r < keys ? r : 0) * HD + c * E;
+    cp_async16(sk + mm_key<T, HD>(r, c), static_cast<const T*>(a.k) + from, r < keys);
+    cp_async16(sv + mm_value<T, HD>(r, c), static_cast<const T*>(a.v) + from, r < keys);
   }
 }
 // 16 keys (the first `keys` count) and their values at sk
 template <int HD>
-__device__ __forceinline__ void mm_tile(MmRows<HD>& x, uint32_t sk, int keys, float scale) {
+__device__ __forceinline__ void mm_tile(MmRows<bf16, HD>& x, uint32_t sk, int keys, float scale) {
   const int lane = threadIdx.x & 31, tig = lane & 3, mi = lane >> 3;
-  const uint32_t sv = sk + MmCfg<HD>::TILE;
+  const uint32_t sv = sk + MmCfg<bf16, HD>::TILE;
   float s[2][4] = {};
 #pragma unroll
   for (int kk = 0; kk < HD / 16; ++kk) {
@@ -149,10 +237,105 @@ __device__ __forceinline__ void mm_tile(MmRows<HD>& x, uint32_t sk, int keys, fl
   }
 }
 
+__device__ __forceinline__ void mma_tf32_1688(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mm_lds4(uint32_t at, float (&x)[4]) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(at) : "memory");
+}
+// 8 keys (the first `keys` count) and their values at sk
 template <int HD>
-__global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
+__device__ __forceinline__ void mm_tile(MmRows<float, HD>& x, uint32_t sk, int keys, float scale) {
+  const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+  const uint32_t sv = sk + MmCfg<float, HD>::TILE;
+  float s[4] = {}, hl[4] = {}, lh[4] = {};
+#pragma unroll
+  for (int j0 = 0; j0 < HD / 16; j0 += 2) {
+    float hh[4] = {};
+#pragma unroll
+    for (int j = j0; j < j0 + 2; ++j) {
+      float y[4];
+      uint32_t h[4], l[4];
+      mm_lds4(sk + mm_key<float, HD>(gid, 4 * j + tig), y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mm_split(y[e], h[e], l[e]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        mma_tf32_1688(hh, x.qh[2 * j + t], h[2 * t], h[2 * t + 1]);
+        mma_tf32_1688(hl, x.qh[2 * j + t], l[2 * t], l[2 * t + 1]);
+        mma_tf32_1688(lh, x.ql[2 * j + t], h[2 * t], h[2 * t + 1]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += hh[e];
+  }
+  float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    s[e] = 2 * tig + (e & 1) < keys ? (s[e] + (hl[e] + lh[e])) * scale : -INFINITY;
+    mx[e >> 1] = fmaxf(mx[e >> 1], s[e]);
+  }
+  bool need = false;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+    need |= mx[i] > x.m[i] + MM_RESCALE_LOG2;
+  }
+  if (__any_sync(0xffffffffu, need)) {
+    float f[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float mn = fmaxf(x.m[i], mx[i]);
+      f[i] = mn == -INFINITY ? 1.f : exp2f(x.m[i] - mn);
+      x.m[i] = mn;
+      x.l[i] *= f[i];
+    }
+#pragma unroll
+    for (int i = 0; i < HD / 8; ++i) {
+      x.o[i][0] *= f[0];
+      x.o[i][1] *= f[0];
+      x.o[i][2] *= f[1];
+      x.o[i][3] *= f[1];
+    }
+  }
+  uint32_t ph[4], pl[4];  // keys 2 tig and 2 tig + 1 as terms tig and tig + 4 of the product
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float base = x.m[i] == -INFINITY ? 0.f : x.m[i];
+    const float p0 = exp2f(s[2 * i] - base), p1 = exp2f(s[2 * i + 1] - base);
+    x.l[i] += p0 + p1;
+    mm_split(p0, ph[i], pl[i]);
+    mm_split(p1, ph[2 + i], pl[2 + i]);
+  }
+#pragma unroll
+  for (int i = 0; i < HD / 32; ++i) {
+    float v0[4], v1[4];
+    mm_lds4(sv + mm_value<float, HD>(2 * tig, 8 * i + gid), v0);
+    mm_lds4(sv + mm_value<float, HD>(2 * tig + 1, 8 * i + gid), v1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t h0, l0, h1, l1;
+      mm_split(v0[k], h0, l0);
+      mm_split(v1[k], h1, l1);
+      float y[4] = {};
+      mma_tf32_1688(y, pl, h0, h1);
+      mma_tf32_1688(y, ph, l0, l1);
+      mma_tf32_1688(y, ph, h0, h1);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.o[4 * i + k][e] += y[e];
+    }
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(MM_THREADS, MmCfg<T, HD>::CTAS)
     paged_mma_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
-  using C = MmCfg<HD>;
+  using C = MmCfg<T, HD>;
+  auto ex2 = [](float v) { return sizeof(T) == 4 ? exp2f(v) : ex2_fast(v); };
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_m[MM_WARPS][MM_ROWS], s_l[MM_WARPS][MM_ROWS];
   float* join = reinterpret_cast<float*>(smem + MM_WARPS * C::RING);  // [warps][MM_JOIN]
@@ -163,8 +346,8 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   pdl_wait();
   __shared__ PagedSpan told;
   PagedSpan span;
-  if (!paged_plan<MM_ROWS, MM_KEYS>(a, w, told, span)) return;
-  const bf16* q = static_cast<const bf16*>(a.q);
+  if (!paged_plan<MM_ROWS, C::BLOCK>(a, w, told, span)) return;
+  const T* q = static_cast<const T*>(a.q);
 
   // the tile to load next; its page number is looked at when it is loaded, a tile later
   PagedSpan ls = span;
@@ -174,19 +357,19 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   bool more = true;
   auto find = [&](bool next_part) {
     if (next_part) {
-      more = paged_next<MM_ROWS, MM_KEYS>(a, w, ls, lp);
+      more = paged_next<MM_ROWS, C::BLOCK>(a, w, ls, lp);
       lb = lp.b0;
       row = paged_row(a, lp);
     }
-    const int k0 = lb * MM_KEYS + 16 * warp;
+    const int k0 = lb * C::BLOCK + C::KEYS * warp;
     if (more && k0 < lp.x.keys) lpage = row[k0 >> a.page_shift];
   };
   auto load = [&](int stage) {
     if (more) {
-      const int k0 = lb * MM_KEYS + 16 * warp, keys = lp.x.keys - k0;
+      const int k0 = lb * C::BLOCK + C::KEYS * warp, keys = lp.x.keys - k0;
       if (keys > 0) {
         const size_t at = paged_at<HD>(a, paged_sound(a, lpage), lp.h, k0);
-        mm_load_tile<HD>(a, ring + stage * (2 * C::TILE), at, keys);
+        mm_load_tile<T, HD>(a, ring + stage * (2 * C::TILE), at, keys);
       }
       ++lb;
       find(lb >= lp.b1);
@@ -194,8 +377,8 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
     cp_async_commit();
   };
   PagedPart p;
-  bool have = paged_next<MM_ROWS, MM_KEYS>(a, w, span, p);
-  MmRows<HD> x;
+  bool have = paged_next<MM_ROWS, C::BLOCK>(a, w, span, p);
+  MmRows<T, HD> x;
   auto load_q = [&]() {
     const int r0 = p.r * MM_ROWS + gid;
     const bool in0 = r0 < p.x.rows, in1 = r0 + 8 < p.x.rows;
@@ -209,19 +392,19 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
   int use = 0, fill = MM_STAGES - 1;  // stages
   while (have) {
     const int rows = min(MM_ROWS, p.x.rows - p.r * MM_ROWS), all = p.x.keys, b1 = p.b1, slot = p.slot;
-    mm_clear<HD>(x);
+    mm_clear<T, HD>(x);
     for (int b = p.b0; b < b1; ++b) {
       load(fill);
       cp_async_wait<MM_STAGES - 1>();
       __syncwarp();
-      const int keys = all - (b * MM_KEYS + 16 * warp);
+      const int keys = all - (b * C::BLOCK + C::KEYS * warp);
       if (keys > 0) mm_tile<HD>(x, ring + use * (2 * C::TILE), keys, a.scale_log2);
       __syncwarp();  // the stage is read: the next load may fill it
       use = use + 1 == MM_STAGES ? 0 : use + 1;
       fill = fill + 1 == MM_STAGES ? 0 : fill + 1;
     }
     // the next part's queries are on their way while this one's results are joined
-    have = paged_next<MM_ROWS, MM_KEYS>(a, w, span, p);
+    have = paged_next<MM_ROWS, C::BLOCK>(a, w, span, p);
     if (have) load_q();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -233,17 +416,11 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
       }
     }
     // The part's result from the four warps', all dims at once for up to 8 rows (more rows
-    // of 128 dims: half of the dims at a time).  A row's groups of 8 floats are XORed by its
-    // number, which keeps stores and loads clear of bank conflicts.
+    // of 128 dims: half of the dims at a time)
     const int dims = rows > 8 ? min(64, HD) : HD;
     for (int d0 = 0; d0 < HD; d0 += dims) {
-#pragma unroll
-      for (int i = 0; i < HD / 8; ++i)
-        if (8 * i >= d0 && 8 * i < d0 + dims) {
-          float* j0 = join + warp * MM_JOIN + gid * dims + ((8 * i - d0) ^ ((gid & 3) * 8)) + 2 * tig;
-          if (gid < rows) *reinterpret_cast<float2*>(j0) = make_float2(x.o[i][0], x.o[i][1]);
-          if (gid + 8 < rows) *reinterpret_cast<float2*>(j0 + 8 * dims) = make_float2(x.o[i][2], x.o[i][3]);
-        }
+      float* j0 = join + warp * MM_JOIN + gid * dims;
+      mm_put<HD>(x, j0, j0 + 8 * dims, d0, dims, gid < rows, gid + 8 < rows);
       __syncthreads();
       const int quads = dims / 4;
       for (int i = tid; i < rows * quads; i += MM_THREADS) {
@@ -256,7 +433,7 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
         float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int k = 0; k < MM_WARPS; ++k) {
-          const float f = ex2_fast(s_m[k][r] - base);
+          const float f = ex2(s_m[k][r] - base);
           const float4 y = *reinterpret_cast<const float4*>(join + k * MM_JOIN + r * dims + (c ^ ((r & 3) * 8)));
           sum = fmaf(f, s_l[k][r], sum);
           z.x = fmaf(f, y.x, z.x), z.y = fmaf(f, y.y, z.y), z.z = fmaf(f, y.z, z.z), z.w = fmaf(f, y.w, z.w);
@@ -277,10 +454,12 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<HD>::CTAS)
 // results, one launch.  The prefix is read once for every sequence, in L2.
 // PARTS: the prefixes' partial results are in w already (the 128-row tiles'), and this
 // launch has the sequences' own entries and joins.
-template <int HD, int W, bool PARTS>
+template <typename T, int HD, int W, bool PARTS>
 __global__ void __launch_bounds__(32 * W, 8 / W)
     paged_direct_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
-  using C = MmCfg<HD>;
+  using C = MmCfg<T, HD>;
+  constexpr int LOG = C::KEYS == 16 ? 4 : 3;
+  auto ex2 = [](float v) { return sizeof(T) == 4 ? exp2f(v) : ex2_fast(v); };
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float s_m[W][MM_ROWS], s_l[W][MM_ROWS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
@@ -290,14 +469,14 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   const int rows = min(MM_ROWS, n_rows - r0);
   pdl_trigger();
   pdl_wait();
-  MmRows<HD> x;
+  MmRows<T, HD> x;
   auto q_row = [&](int r) {  // row r of the sequence and KV head
     const size_t tok = static_cast<size_t>(s) * a.n_q + r / a.per;
-    return static_cast<const bf16*>(a.q) + (tok * (static_cast<size_t>(a.Hkv) * a.per) + static_cast<size_t>(g) * a.per + r % a.per) * HD;
+    return static_cast<const T*>(a.q) + (tok * (static_cast<size_t>(a.Hkv) * a.per) + static_cast<size_t>(g) * a.per + r % a.per) * HD;
   };
   const bool in0 = gid < rows, in1 = gid + 8 < rows;
   mm_load_q<HD>(x, q_row(in0 ? r0 + gid : 0), q_row(in1 ? r0 + gid + 8 : 0), in0, in1);
-  mm_clear<HD>(x);
+  mm_clear<T, HD>(x);
   const int own = max(0, min(a.lens[s], a.cols << a.page_shift) - (a.n_q - 1));
   const int32_t *shared_row = nullptr, *own_row = a.table + static_cast<size_t>(s) * a.cols;
   int shared = 0, per = 0;
@@ -313,19 +492,19 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
     shared = e.keys;
     shared_row = a.ptable + static_cast<size_t>(e.g) * a.pcols;
   }
-  // tiles of 16 keys, those of the prefix first: warp w has w, w + W, ...; the pages of
+  // tiles of keys, those of the prefix first: warp w has w, w + W, ...; the pages of
   // its next 32 tiles are asked for together
-  const int n_shared = (shared + 15) >> 4, n = n_shared + ((own + 15) >> 4), mine = n > warp ? (n - warp + W - 1) / W : 0;
+  const int n_shared = (shared + C::KEYS - 1) >> LOG, n = n_shared + ((own + C::KEYS - 1) >> LOG), mine = n > warp ? (n - warp + W - 1) / W : 0;
   int pages = 0;
   auto load = [&](int i) {  // the warp's i-th tile into stage i % MM_STAGES
     if (i < mine) {
       if ((i & 31) == 0) {
         const int t = warp + W * (i + lane);
-        pages = t < n_shared ? shared_row[t << 4 >> a.page_shift] : t < n ? own_row[(t - n_shared) << 4 >> a.page_shift] : 0;
+        pages = t < n_shared ? shared_row[t << LOG >> a.page_shift] : t < n ? own_row[(t - n_shared) << LOG >> a.page_shift] : 0;
       }
-      const int t = warp + W * i, k0 = (t < n_shared ? t : t - n_shared) << 4;
+      const int t = warp + W * i, k0 = (t < n_shared ? t : t - n_shared) << LOG;
       const int page = paged_sound(a, __shfl_sync(0xffffffffu, pages, i & 31));
-      mm_load_tile<HD>(a, ring + i % MM_STAGES * (2 * C::TILE), paged_at<HD>(a, page, g, k0), (t < n_shared ? shared : own) - k0);
+      mm_load_tile<T, HD>(a, ring + i % MM_STAGES * (2 * C::TILE), paged_at<HD>(a, page, g, k0), (t < n_shared ? shared : own) - k0);
     }
     cp_async_commit();
   };
@@ -336,7 +515,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
     cp_async_wait<MM_STAGES - 1>();
     __syncwarp();
     const int t = warp + W * i;
-    mm_tile<HD>(x, ring + i % MM_STAGES * (2 * C::TILE), t < n_shared ? shared - (t << 4) : own - ((t - n_shared) << 4), a.scale_log2);
+    mm_tile<HD>(x, ring + i % MM_STAGES * (2 * C::TILE), t < n_shared ? shared - (t << LOG) : own - ((t - n_shared) << LOG), a.scale_log2);
     __syncwarp();  // the stage is read: the next load may fill it
   }
   cp_async_wait<0>();
@@ -349,15 +528,11 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
       s_l[warp][gid + 8 * i] = x.l[i];
     }
   }
-  // the warps' results in the ring's place, a row's groups of 8 floats XORed by its number
+  // the warps' results in the ring's place
   __syncthreads();
   float* join = reinterpret_cast<float*>(smem);  // [W][rows][HD]
-#pragma unroll
-  for (int i = 0; i < HD / 8; ++i) {
-    float* j0 = join + (warp * MM_ROWS + gid) * HD + ((8 * i) ^ ((gid & 3) * 8)) + 2 * tig;
-    if (in0) *reinterpret_cast<float2*>(j0) = make_float2(x.o[i][0], x.o[i][1]);
-    if (in1) *reinterpret_cast<float2*>(j0 + 8 * HD) = make_float2(x.o[i][2], x.o[i][3]);
-  }
+  float* j0 = join + (warp * MM_ROWS + gid) * HD;
+  mm_put<HD>(x, j0, j0 + 8 * HD, 0, HD, in0, in1);
   __syncthreads();
   constexpr int DPL = HD / 32;
   constexpr int R = MM_ROWS / W;
@@ -376,7 +551,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
     if (r >= rows) continue;
 #pragma unroll
     for (int k = 0; k < W; ++k) {
-      const float f = ex2_fast(s_m[k][r] - base);
+      const float f = ex2(s_m[k][r] - base);
       const float* z = join + (k * MM_ROWS + r) * HD + ((lane * DPL) ^ ((r & 3) * 8));
       y.l[i] = fmaf(f, s_l[k][r], y.l[i]);
 #pragma unroll
@@ -388,48 +563,56 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
 #pragma unroll
     for (int i = 0; i < R; ++i)
       pre[i] = y.rr[i] < 0 ? JoinParts{nullptr, nullptr, 0, 0} : join_prefix(a, w, e, per, s, g, y.rr[i], HD);
-    paged_add_parts<bf16, HD, R, 16 / R>(y, pre, none);
+    paged_add_parts<T, HD, R, 16 / R>(y, pre, none);
   }
-  paged_finish<bf16, HD, R>(a, s, g, y);
+  paged_finish<T, HD, R>(a, s, g, y);
 }
 
 }  // namespace
 
-PagedTiles paged_mma_tiles(int hd, int sms) {
-  return PagedTiles{MM_ROWS, MM_KEYS, (hd == 128 ? MmCfg<128>::CTAS : MmCfg<64>::CTAS) * sms, 1};
-}
-
-template <int HD>
+template <typename T, int HD>
 static cudaError_t run_mma(const PagedArgs& a, const PagedWork& w, int ctas, cudaStream_t s) {
   static OncePerDevice once;
-  const cudaError_t e = set_smem_limit_once(once, paged_mma_kernel<HD>, MmCfg<HD>::SMEM);
+  const cudaError_t e = set_smem_limit_once(once, paged_mma_kernel<T, HD>, MmCfg<T, HD>::SMEM);
   if (e != cudaSuccess) return e;
-  ZSAA_LAUNCH(paged_mma_kernel<HD>, dim3(ctas), dim3(MM_THREADS), MmCfg<HD>::SMEM, s, a, w);
+  ZSAA_LAUNCH(paged_mma_kernel<T, HD>, dim3(ctas), dim3(MM_THREADS), MmCfg<T, HD>::SMEM, s, a, w);
   return cudaSuccess;
 }
 
-template <int HD, int W, bool PARTS>
+template <typename T, int HD, int W, bool PARTS>
 static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream_t s) {
   static OncePerDevice once;
-  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<HD, W, PARTS>, W * MmCfg<HD>::RING);
+  const int smem = std::max(W * MmCfg<T, HD>::RING, W * MM_ROWS * HD * 4);  // (the ring, then the warps' results)
+  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<T, HD, W, PARTS>, smem);
   if (e != cudaSuccess) return e;
   const int tiles = (a.n_q * a.per + MM_ROWS - 1) / MM_ROWS;
-  ZSAA_LAUNCH(paged_direct_kernel<HD, W, PARTS>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), W * MmCfg<HD>::RING, s, a, w);
+  ZSAA_LAUNCH(paged_direct_kernel<T, HD, W, PARTS>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), smem, s, a, w);
   return cudaSuccess;
 }
 
-cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int hd, bool wide, cudaStream_t s) {
-  const PagedWork w = prefixes != nullptr ? *prefixes : PagedWork{};
-  if (prefixes != nullptr) {
-    if (hd == 64) return wide ? run_direct<64, 8, true>(a, w, s) : run_direct<64, 4, true>(a, w, s);
-    return wide ? run_direct<128, 8, true>(a, w, s) : run_direct<128, 4, true>(a, w, s);
-  }
-  if (hd == 64) return wide ? run_direct<64, 8, false>(a, w, s) : run_direct<64, 4, false>(a, w, s);
-  return wide ? run_direct<128, 8, false>(a, w, s) : run_direct<128, 4, false>(a, w, s);
+template <typename T, int HD>
+static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, bool wide, cudaStream_t s) {
+  if constexpr (sizeof(T) == 2)
+    if (w != nullptr) return wide ? run_direct<T, HD, 8, true>(a, *w, s) : run_direct<T, HD, 4, true>(a, *w, s);
+  return wide ? run_direct<T, HD, 8, false>(a, PagedWork{}, s) : run_direct<T, HD, 4, false>(a, PagedWork{}, s);
 }
 
-cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s) {
-  return hd == 64 ? run_mma<64>(a, w, ctas, s) : run_mma<128>(a, w, ctas, s);
+PagedTiles paged_mma_tiles(int dtype, int hd, int sms) {
+  const bool bf = dtype == ZSAA_BF16;
+  const int ctas = hd == 128 ? MmCfg<bf16, 128>::CTAS : hd == 64 ? MmCfg<bf16, 64>::CTAS : MmCfg<float, 32>::CTAS;
+  return PagedTiles{MM_ROWS, bf ? MmCfg<bf16, 128>::BLOCK : MmCfg<float, 128>::BLOCK, ctas * sms, 1};
+}
+
+cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, bool wide, cudaStream_t s) {
+  if (dtype == ZSAA_BF16) return hd == 64 ? run_direct<bf16, 64>(a, prefixes, wide, s) : run_direct<bf16, 128>(a, prefixes, wide, s);
+  if (hd == 32) return run_direct<float, 32>(a, nullptr, wide, s);
+  return hd == 64 ? run_direct<float, 64>(a, nullptr, wide, s) : run_direct<float, 128>(a, nullptr, wide, s);
+}
+
+cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int dtype, int hd, int ctas, cudaStream_t s) {
+  if (dtype == ZSAA_BF16) return hd == 64 ? run_mma<bf16, 64>(a, w, ctas, s) : run_mma<bf16, 128>(a, w, ctas, s);
+  if (hd == 32) return run_mma<float, 32>(a, w, ctas, s);
+  return hd == 64 ? run_mma<float, 64>(a, w, ctas, s) : run_mma<float, 128>(a, w, ctas, s);
 }
 
 }  // namespace zsaa

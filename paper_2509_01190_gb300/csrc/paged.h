@@ -47,16 +47,12 @@ struct PagedWork {
 struct PagedTiles {
   int mt, bn, ctas, min_blocks;
 };
-// bf16, tiles of 16 rows (k_paged_mma.cu)
-PagedTiles paged_mma_tiles(int hd, int sms);
-cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);
-// bf16, all of a sequence and KV head's keys in one CTA (of 8 warps, wide, or 4); prefixes:
-// the launch that has left the prefixes' partial results, or null
-cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int hd, bool wide, cudaStream_t s);
-// float32, tiles of 16 rows (k_paged_f32.cu), and all of a sequence and KV head's keys in one CTA
-PagedTiles paged_f32_tiles(int sms);
-cudaError_t launch_paged_f32(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);
-cudaError_t launch_paged_f32_direct(const PagedArgs& a, int hd, cudaStream_t s);
+// tiles of 16 rows (k_paged_mma.cu)
+PagedTiles paged_mma_tiles(int dtype, int hd, int sms);
+cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int dtype, int hd, int ctas, cudaStream_t s);
+// all of a sequence and KV head's keys in one CTA (of 8 warps, wide, or 4); prefixes: the
+// launch that has left the prefixes' partial results (bf16), or null
+cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, bool wide, cudaStream_t s);
 // bf16, tiles of 128 rows (k_paged_tc.cu)
 PagedTiles paged_tc_tiles(int sms);
 cudaError_t launch_paged_tc(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);
