@@ -223,10 +223,10 @@ long long items_of(const PagedArgs& a, int mt, bool prefixes, bool sequences) {
   if (sequences) n += static_cast<long long>(a.S) * ((row + mt - 1) / mt) * a.Hkv;
   return n;
 }
-long long blocks_of(const PagedArgs& a, int mt, int bn) {
+long long units_of(const PagedArgs& a, int mt, int bn, int lead) {
   const long long row = static_cast<long long>(a.n_q) * a.per;
-  const long long pk = (static_cast<long long>(a.pcols) << a.page_shift) / bn + 1;
-  const long long sk = (static_cast<long long>(a.cols) << a.page_shift) / bn + 1;
+  const long long pk = (static_cast<long long>(a.pcols) << a.page_shift) / bn + 1 + lead;
+  const long long sk = (static_cast<long long>(a.cols) << a.page_shift) / bn + 1 + lead;
   return (a.S * row / mt + a.G) * a.Hkv * pk + a.S * ((row + mt - 1) / mt) * a.Hkv * sk;
 }
 
@@ -240,7 +240,8 @@ PagedWork work_share(const PagedArgs& a, const PagedTiles& t, bool prefixes, boo
   PagedWork w{};
   w.e0 = prefixes ? 0 : a.G;
   w.e1 = sequences ? a.G + a.S : a.G;
-  w.min_blocks = t.min_blocks;
+  w.min_units = t.min_units;
+  w.lead = t.lead;
   while ((1 << w.mt_shift) < t.mt) ++w.mt_shift;
   while ((1 << w.bn_shift) < t.bn) ++w.bn_shift;
   const size_t slots = static_cast<size_t>(t.ctas) + static_cast<size_t>(items_of(a, t.mt, prefixes, sequences));
@@ -261,7 +262,7 @@ struct Launches {
   PagedTiles tiles[2];
   PagedWork work[2];
   size_t bytes;
-  long long most;  // items and blocks that number the slots and the line
+  long long most;  // items and units that number the slots and the line
 };
 
 // The 128-row tiles take entries whose 16-row tiles would have more than `blocks` blocks of
@@ -333,8 +334,8 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
     r.tiles[i] = r.tc[i] ? paged_tc_tiles(sms) : paged_mma_tiles(dtype, hd, sms);
     r.work[i] = work_share(a, r.tiles[i], pre, seq, hd, &at);
     const long long slots = items_of(a, r.tiles[i].mt, pre, seq) + r.tiles[i].ctas;
-    const long long blocks = blocks_of(a, r.tiles[i].mt, r.tiles[i].bn);
-    r.most = std::max(r.most, std::max(slots, blocks));
+    const long long units = units_of(a, r.tiles[i].mt, r.tiles[i].bn, r.tiles[i].lead);
+    r.most = std::max(r.most, std::max(slots, units));
   }
   r.bytes = at - reinterpret_cast<uintptr_t>(ws);
   return r;

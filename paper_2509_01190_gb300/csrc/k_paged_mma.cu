@@ -347,17 +347,20 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<T, HD>::CTAS)
   __shared__ PagedSpan told;
   PagedSpan span;
   if (!paged_plan<MM_ROWS, C::BLOCK>(a, w, told, span)) return;
+  PagedSpan ls = span;
+  PagedPart p;
+  bool have = paged_next<MM_ROWS, C::BLOCK>(a, w, span, p);
+  if (!have) return;  // no block of an item, its lead alone
   const T* q = static_cast<const T*>(a.q);
 
   // the tile to load next; its page number is looked at when it is loaded, a tile later
-  PagedSpan ls = span;
   PagedPart lp;
   const int32_t* row = nullptr;
   int lb = 0, lpage = 0;
   bool more = true;
   auto find = [&](bool next_part) {
     if (next_part) {
-      more = paged_next<MM_ROWS, C::BLOCK>(a, w, ls, lp);
+      more = paged_next<MM_ROWS, C::BLOCK>(a, w, ls, lp);  // (there is a first one)
       lb = lp.b0;
       row = paged_row(a, lp);
     }
@@ -376,8 +379,6 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<T, HD>::CTAS)
     }
     cp_async_commit();
   };
-  PagedPart p;
-  bool have = paged_next<MM_ROWS, C::BLOCK>(a, w, span, p);
   MmRows<T, HD> x;
   auto load_q = [&]() {
     const int r0 = p.r * MM_ROWS + gid;
@@ -600,7 +601,7 @@ static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, bool wide,
 PagedTiles paged_mma_tiles(int dtype, int hd, int sms) {
   const bool bf = dtype == ZSAA_BF16;
   const int ctas = hd == 128 ? MmCfg<bf16, 128>::CTAS : hd == 64 ? MmCfg<bf16, 64>::CTAS : MmCfg<float, 32>::CTAS;
-  return PagedTiles{MM_ROWS, bf ? MmCfg<bf16, 128>::BLOCK : MmCfg<float, 128>::BLOCK, ctas * sms, 1};
+  return PagedTiles{MM_ROWS, bf ? MmCfg<bf16, 128>::BLOCK : MmCfg<float, 128>::BLOCK, ctas * sms, 1, 2};
 }
 
 cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, bool wide, cudaStream_t s) {

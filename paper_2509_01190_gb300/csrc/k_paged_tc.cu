@@ -200,8 +200,10 @@ __global__ void __launch_bounds__(TC_THREADS, 2)
         ++parts;
       }
       // every MMA issued has finished before the CTA frees TMEM
-      tc_commit(mma_done);
-      mbar_wait(mma_done, 0, a.status);
+      if (parts > 0) {
+        tc_commit(mma_done);
+        mbar_wait(mma_done, 0, a.status);
+      }
     }
     __syncwarp();
   } else if (work) {
@@ -394,7 +396,7 @@ cudaError_t run_tc(const PagedArgs& a, const PagedWork& w, int ctas, cudaStream_
 
 }  // namespace
 
-PagedTiles paged_tc_tiles(int sms) { return PagedTiles{TC_ROWS, TC_KEYS, 2 * sms, 2}; }
+PagedTiles paged_tc_tiles(int sms) { return PagedTiles{TC_ROWS, TC_KEYS, 2 * sms, 2, 1}; }
 
 cudaError_t launch_paged_tc(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s) {
   return hd == 64 ? run_tc<64>(a, w, ctas, s) : run_tc<128>(a, w, ctas, s);

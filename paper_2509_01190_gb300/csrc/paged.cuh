@@ -6,7 +6,9 @@
 // last n_q - 1 are hidden from some of them and belong to the joining kernel).  So
 // no key of an entry is masked.  For each KV head the rows of an entry are cut into
 // tiles of MT rows and its keys into blocks of BN; a tile's walk over its entry's
-// blocks is an item.  All blocks of all items stand in one line, entry by entry,
+// blocks is an item.  All blocks of all items stand in one line, entry by entry, each
+// item's behind `lead` units that stand for its start and end (which cost some blocks'
+// time: without them the CTAs with the many short items would finish last by far),
 // and every CTA takes an equal stretch of it, whatever the lengths are.  A stretch
 // covers whole items or parts of them; for each it leaves one partial result
 // (normalised rows and their log2 sums) in a slot, and the joining kernel adds a
@@ -61,10 +63,10 @@ __device__ __forceinline__ PagedEntry paged_entry(const PagedArgs& a, const Page
   x.keys = max(0, min(len, (shared ? a.pcols : a.cols) << a.page_shift) - (shared ? 0 : a.n_q - 1));
   return x;
 }
-// blocks of an entry for one tile of rows
+// units of an entry for one tile of rows
 template <int BN>
-__device__ __forceinline__ int paged_blocks(const PagedEntry& x) {
-  return x.rows > 0 ? (x.keys + BN - 1) / BN : 0;
+__device__ __forceinline__ int paged_units(const PagedWork& w, const PagedEntry& x) {
+  return x.rows > 0 && x.keys > 0 ? (x.keys + BN - 1) / BN + w.lead : 0;
 }
 template <int MT>
 __device__ __forceinline__ int paged_tiles(const PagedEntry& x) { return (x.rows + MT - 1) / MT; }
@@ -78,48 +80,48 @@ __device__ __forceinline__ int paged_first_item(const PagedArgs& a, const PagedW
   return prefixes + x.seq0 * ((row + MT - 1) / MT) * a.Hkv;
 }
 
-// This CTA's stretch [t, end) of the line; t lies in entry e, whose first block is
+// This CTA's stretch [t, end) of the line; t lies in entry e, whose first unit is
 // number t0.  The first warp works it out (its lanes over the entries; sums stop growing
-// at kMostBlocks, since group bounds that run backwards could pass any number) and tells
+// at kMostUnits, since group bounds that run backwards could pass any number) and tells
 // the others; more warps would only queue for the same lines of L2.  CTA 0 also leaves
 // what the joining kernel needs: the stretch length (0: nothing is done) and every entry's
-// first block.  All threads; false: no work.
+// first unit.  All threads; false: no work.
 struct PagedSpan {
   int t, end, e, t0;
   PagedLive live;
 };
-constexpr int kMostBlocks = 0x3fffffff;
+constexpr int kMostUnits = 0x3fffffff;
 template <int MT, int BN>
 __device__ __forceinline__ bool paged_plan(const PagedArgs& a, const PagedWork& w, PagedSpan& told, PagedSpan& s) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x, n = w.e1 - w.e0, q = (n + 31) / 32;
     const int lo = min(n, lane * q), hi = min(n, lo + q), grid = static_cast<int>(gridDim.x);
     const PagedLive live = paged_live(a);
-    auto blocks = [&](int i) {
+    auto units = [&](int i) {
       const PagedEntry x = paged_entry(a, live, w.e0 + i);
-      return paged_blocks<BN>(x) * paged_tiles<MT>(x) * a.Hkv;
+      return paged_units<BN>(w, x) * paged_tiles<MT>(x) * a.Hkv;
     };
     int sum = 0;
 #pragma unroll 2
-    for (int i = lo; i < hi; ++i) sum = min(sum + blocks(i), kMostBlocks);
+    for (int i = lo; i < hi; ++i) sum = min(sum + units(i), kMostUnits);
     int upto = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto = min(upto + v, kMostBlocks);
+      if (lane >= o) upto = min(upto + v, kMostUnits);
     }
     const int total = __shfl_sync(0xffffffffu, upto, 31);
-    const int per = max(w.min_blocks, static_cast<int>(static_cast<unsigned>(total + grid - 1) / static_cast<unsigned>(grid)));
+    const int per = max(w.min_units, static_cast<int>(static_cast<unsigned>(total + grid - 1) / static_cast<unsigned>(grid)));
     const int start = static_cast<int>(blockIdx.x) * per;
-    const bool work = total < kMostBlocks && start < total;
+    const bool work = total < kMostUnits && start < total;
     int at = upto - sum;
     if (lane == 0) told.end = work ? min(start + per, total) : -1;
     if (work && start >= at && start < at + sum) {
       int i = lo;
       for (; i + 1 < hi; ++i) {
-        const int b = blocks(i);
-        if (start < at + b) break;
-        at += b;
+        const int n = units(i);
+        if (start < at + n) break;
+        at += n;
       }
       told.t = start;
       told.e = w.e0 + i;
@@ -130,11 +132,11 @@ __device__ __forceinline__ bool paged_plan(const PagedArgs& a, const PagedWork& 
       at = upto - sum;
       for (int i = lo; i < hi; ++i) {
         w.head[1 + i] = at;
-        at = min(at + blocks(i), kMostBlocks);
+        at = min(at + units(i), kMostUnits);
       }
       if (lane == 0) {
-        w.head[0] = total < kMostBlocks ? per : 0;
-        if (total >= kMostBlocks) atomicOr(a.status, kStatusBadIndex);
+        w.head[0] = total < kMostUnits ? per : 0;
+        if (total >= kMostUnits) atomicOr(a.status, kStatusBadIndex);
       }
     }
   }
@@ -152,27 +154,28 @@ struct PagedPart {
 };
 template <int MT, int BN>
 __device__ __forceinline__ bool paged_next(const PagedArgs& a, const PagedWork& w, PagedSpan& s, PagedPart& p) {
-  if (s.t >= s.end) return false;
-  int nb, rt;
-  while (true) {
+  while (s.t < s.end) {
     p.x = paged_entry(a, s.live, s.e);
-    nb = paged_blocks<BN>(p.x);
-    rt = paged_tiles<MT>(p.x);
-    const int all = nb * rt * a.Hkv;
-    if (s.t < s.t0 + all) break;
-    s.t0 += all;
-    ++s.e;
+    const int nu = paged_units<BN>(w, p.x), rt = paged_tiles<MT>(p.x), all = nu * rt * a.Hkv;
+    if (s.t >= s.t0 + all) {
+      s.t0 += all;
+      ++s.e;
+      continue;
+    }
+    const unsigned u = static_cast<unsigned>(s.t - s.t0), item = u / static_cast<unsigned>(nu);
+    const int u0 = static_cast<int>(u - item * static_cast<unsigned>(nu)), u1 = min(nu, u0 + s.end - s.t);
+    s.t += u1 - u0;
+    p.b0 = max(0, u0 - w.lead);
+    p.b1 = u1 - w.lead;
+    if (p.b0 >= p.b1) continue;  // no block of the item
+    p.e = s.e;
+    p.shared = s.e < a.G;
+    p.h = rt == 1 ? item : item / static_cast<unsigned>(rt);
+    p.r = static_cast<int>(item) - p.h * rt;
+    p.slot = blockIdx.x + paged_first_item<MT>(a, w, p.x, s.e) + static_cast<int>(item);
+    return true;
   }
-  const unsigned u = static_cast<unsigned>(s.t - s.t0), item = u / static_cast<unsigned>(nb);
-  p.e = s.e;
-  p.shared = s.e < a.G;
-  p.h = rt == 1 ? item : item / static_cast<unsigned>(rt);
-  p.r = static_cast<int>(item) - p.h * rt;
-  p.b0 = static_cast<int>(u - item * static_cast<unsigned>(nb));
-  p.b1 = min(nb, p.b0 + s.end - s.t);
-  p.slot = blockIdx.x + paged_first_item<MT>(a, w, p.x, s.e) + static_cast<int>(item);
-  s.t += p.b1 - p.b0;
-  return true;
+  return false;
 }
 
 // A page number out of range is reported, and page 0 read instead.
@@ -196,7 +199,7 @@ __device__ __forceinline__ size_t paged_at(const PagedArgs& a, int page, int h, 
   return (((static_cast<size_t>(page) * a.Hkv + h) << a.page_shift) + (i & ((1 << a.page_shift) - 1))) * HD;
 }
 // The group of sequence s (the last one that starts at or before it): a lane per group, so
-// one round trip for up to 32 groups; t0: first blocks of the entries, or null.  Whole warps.
+// one round trip for up to 32 groups; t0: first units of the entries, or null.  Whole warps.
 struct PagedGroup {
   int g, seq0, end, keys, t0;  // g < 0: the sequence is padding
   bool beyond;                 // the prefix is longer than its table
@@ -261,17 +264,17 @@ struct JoinParts {
   int n;
 };
 // rr: the row's number among its entry's rows for KV head g; per, t_entry: the stretch
-// length and the entry's first block
+// length and the entry's first unit
 __device__ __forceinline__ JoinParts join_parts(const PagedArgs& a, const PagedWork& w, int e, const PagedEntry& x,
                                                 int per, int t_entry, int g, int rr, int hd) {
   if (per == 0 || x.keys == 0) return JoinParts{nullptr, nullptr, 0, 0};
   const int ms = w.mt_shift, up = (1 << ms) - 1;
-  const int nb = (x.keys + (1 << w.bn_shift) - 1) >> w.bn_shift, rt = (x.rows + up) >> ms;
+  const int nu = ((x.keys + (1 << w.bn_shift) - 1) >> w.bn_shift) + w.lead, rt = (x.rows + up) >> ms;
   const int item = g * rt + (rr >> ms), row = a.n_q * a.per;
-  const unsigned t0 = static_cast<unsigned>(t_entry + item * nb);
+  const unsigned t0 = static_cast<unsigned>(t_entry + item * nu);
   const int first = e < a.G ? (((x.seq0 * row) >> ms) + e) * a.Hkv
                             : (w.e0 < a.G ? (((a.S * row) >> ms) + a.G) * a.Hkv : 0) + x.seq0 * ((row + up) >> ms) * a.Hkv;
-  const unsigned c0 = t0 / static_cast<unsigned>(per), c1 = (t0 + nb - 1) / static_cast<unsigned>(per);
+  const unsigned c0 = (t0 + w.lead) / static_cast<unsigned>(per), c1 = (t0 + nu - 1) / static_cast<unsigned>(per);  // (of its blocks)
   const size_t at = (static_cast<size_t>(static_cast<int>(c0) + first + item) << ms) + (rr & up);
   return JoinParts{w.o + at * hd, w.lse2 + at, static_cast<size_t>(1) << ms, static_cast<int>(c1 - c0) + 1};
 }

@@ -37,15 +37,17 @@ struct PagedArgs {
 // One attention launch's entries and its part of the workspace (paged.cuh).
 struct PagedWork {
   int e0, e1;      // entries [e0, e1) of the groups' prefixes, then the sequences
-  int min_blocks;  // a CTA's stretch is at least this long
+  int min_units;   // a CTA's stretch is at least this long
+  int lead;        // units of an item before its blocks
   int mt_shift, bn_shift;  // rows of a tile, keys of a block: powers of two
   int* head;       // [1 + entries]
   float* o;        // [slots][rows of a tile][hd]
   float* lse2;     // [slots][rows of a tile]
 };
-// A kernel's tiles, the CTAs it is launched with, and the least blocks a CTA takes.
+// A kernel's tiles, the CTAs it is launched with, the least units a CTA takes, and the blocks
+// that an item's start and end take the time of.
 struct PagedTiles {
-  int mt, bn, ctas, min_blocks;
+  int mt, bn, ctas, min_units, lead;
 };
 // tiles of 16 rows (k_paged_mma.cu)
 PagedTiles paged_mma_tiles(int dtype, int hd, int sms);
