@@ -268,31 +268,32 @@ struct Launches {
 // The 128-row tiles take entries whose 16-row tiles would have more than `blocks` blocks of
 // 64 keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64, by the tables' sizes).
 // Up to 16 rows there is one 16-row tile and nothing to gain.  Six blocks where that saves
-// or costs no launch: 128 rows to a prefix without own entries (us, 16-row and 128-row
-// tiles, 8 heads of 128 dims) 512 keys 16 and 22, 1024 20 and 23, 2048 27 and 24, 8192 79
-// and 34; 24 sequences of 4 queries in 3 groups with 300 own entries 512 keys 30 and 29,
-// 1024 38 and 31, 2048 53 and 35; with 64 dims 19 and 19, 23 and 22, 30 and 23.  Forty where
-// the sequences' own entries, too many for the joining launch, then need a launch of their
-// own: those sequences with 1500 entries 1024 keys 49 and 62, 2048 58 and 67, 4096 80 and
-// 75, 8192 117 and 85; with 64 dims 4096 51 and 48, 8192 72 and 56.
+// or costs no launch (us, 16-row and 128-row tiles, 8 heads of 128 dims): 24 sequences of 4
+// queries in 3 groups with 300 own entries, 512 keys 24 and 26, 1024 31 and 29, 2048 37 and 32,
+// 8192 104 and 56; 62 of 5 in one group, 512 58 and 43, 2048 93 and 50; 128 of one in 4 groups
+// and 300 own, which the joining launch then has, 512 46 and 54, 2048 58 and 60, 8192 131 and
+// 84; with 64 dims the first 21 and 21 at 1024, 24 and 22, 60 and 40.  Forty where the
+// sequences' own entries, too many for the joining launch, then need a launch of their own:
+// the first with 1500 own 2048 keys 48 and 59, 4096 63 and 64, 8192 106 and 81; with 64 dims
+// 31 and 37, 40 and 43, 66 and 55.  None where the sequences take 128-row tiles: 10 of 5 with
+// 1200 own, 64 dims, 2048 keys 28 and 18.
 bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int heads, int blocks) {
   return rows > 16 && row_tiles * heads * (keys / 64) > blocks * (hd == 128 ? 304 : 456);
 }
 
 // Calls that one CTA for each sequence, KV head and tile of 16 rows does at once, without
 // a plan and partial results.  Measured by the tables' sizes against the split over all SMs
-// (us, 8 KV heads of 128 dims, up to 16 rows to a head): 1 sequence of 512 keys 6.0 and 7.8,
-// of 1024 9.2 and 8.7, of 2048 15 and 11; 16 of 1024 14 and 21; 64 of 1024 47 and 52, of
-// 2048 86 and 92; 256 of 2048 311 and 338.  32 rows: 16 sequences of 1024 23 and 28, of
-// 2048 36 and 40; 128 of 1024 147 and 147, of 2048 263 and 227.  64 rows, 16 sequences of
-// 256: 41 and 35, with 64 dims 28 and 33; of 1024 46 and 38.  A shared prefix is read again
-// for every sequence: 64 sequences in 8 groups, 512 keys 20 and 23, 1024 33 and 27; with
-// 32 rows 62 and 78, 91 and 87.
-// In float32, 4 sequences and 4 heads of 32, 64 and 128 dims: 128 keys 3.7 and 6.5, 4.5 and
-// 7.0, 6.6 and 9.0, 512 7.3 and 8.0, 10.2 and 8.9, 17 and 10.5; 16 sequences and 8 heads: 1024
-// 12 and 17, 19 and 32, 33 and 41; 64: 43 and 41, 62 and 64, 112 and 120.  64 in 8 groups: 128
-// 11 and 12, 14 and 17, 23 and 25, 256 16 and 15, 22 and 20, 36 and 34, 512 25 and 20, 35 and
-// 26, 62 and 49.
+// (us, 8 KV heads of 128 dims, bf16, 4 rows to a head): 4 sequences of 512 keys 6.3 and 9.2, of
+// 1024 9.5 and 9.6, of 2048 16 and 12; 16 of 1024 14 and 19; 64 of 1024 47 and 52, of 2048 86
+// and 90; 256 of 2048 311 and 338.  20 rows: 8 of 1024 12 and 16, 62 of 1024 73 and 68.  32 rows:
+// 16 of 1024 23 and 28, 128 of 1024 147 and 147, of 2048 263 and 227.  64 rows, 16 of 256: 41 and
+// 35, with 64 dims 28 and 33; of 1024 46 and 38.  A shared prefix is read again for every
+// sequence: 16 in 4 groups, 1024 keys 11 and 13, 2048 18 and 16; 64 in 8, 256 14 and 19, 512 21
+// and 18, 1024 34 and 24; 62 of 20 rows in 8, 512 45 and 45, 1024 73 and 53.
+// In float32: 4 sequences of 256 keys 10 and 12, 512 17 and 12, with 32 dims 7.3 and 8.6 and at
+// 1024 12 and 9.8; 16 of 1024 33 and 41; 64 of 1024 112 and 121, with 32 dims 43 and 41; 62 of 20
+// rows 208 and 238.  With groups: 16 in 4, 256 12 and 16, 512 19 and 18; 64 in 8, 128 23 and 26,
+// 256 36 and 26, with 32 dims 16 and 15, 25 and 17 at 512; 62 of 20 rows in 8, 256 74 and 88.
 long long direct_ctas(const PagedArgs& a) {
   return static_cast<long long>(a.S) * a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16);
 }
@@ -322,9 +323,9 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
   const bool bf = dtype == ZSAA_BF16;
   const bool own = bf && a.G > 0 && own_in_one(a, hd);
   const bool tc_seq = bf && many_rows(hd, a.S * ((row + 15) / 16), row, static_cast<long long>(a.cols) << a.page_shift, a.Hkv, 6);
-  const bool tc_pre = a.G == 0 ? tc_seq
-                               : bf && many_rows(hd, std::max(a.S * row / 16, static_cast<long long>(a.G)), a.S * row / a.G,
-                                                 static_cast<long long>(a.pcols) << a.page_shift, a.Hkv, own || tc_seq ? 6 : 40);
+  const bool tc_pre = tc_seq || (bf && a.G > 0 &&
+                                 many_rows(hd, std::max(a.S * row / 16, static_cast<long long>(a.G)), a.S * row / a.G,
+                                           static_cast<long long>(a.pcols) << a.page_shift, a.Hkv, own ? 6 : 40));
   r.own = own && tc_pre;
   r.n = tc_seq == tc_pre || r.own ? 1 : 2;
   uintptr_t at = reinterpret_cast<uintptr_t>(ws);

@@ -396,6 +396,9 @@ cudaError_t run_tc(const PagedArgs& a, const PagedWork& w, int ctas, cudaStream_
 
 }  // namespace
 
+// Lead: with 0, 1 and 4 units to an item (us): 128 sequences in 20 groups of 3000, 64 dims, 52, 53
+// and 55; 64 dims and 24 sequences in 6 groups of 1500, 31, 30 and 32; a prefix of 32000, 128
+// dims, 96, 93 and 92.
 PagedTiles paged_tc_tiles(int sms) { return PagedTiles{TC_ROWS, TC_KEYS, 2 * sms, 2, 1}; }
 
 cudaError_t launch_paged_tc(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s) {
