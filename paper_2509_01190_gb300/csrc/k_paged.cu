@@ -345,15 +345,14 @@ Launches launches_of(const PagedArgs& a, int dtype, int hd, int sms, void* ws) {
 template <typename T, int HD>
 cudaError_t run_paged_attention(const PagedArgs& a, void* ws, int sms, cudaStream_t s) {
   constexpr int dtype = sizeof(T) == 4 ? ZSAA_F32 : ZSAA_BF16;
-  const bool wide = direct_ctas(a) <= 152;  // eight warps a CTA where four would leave SMs empty
-  if (direct_call(a, dtype == ZSAA_BF16, HD)) return launch_paged_direct(a, nullptr, dtype, HD, wide, s);
+  if (direct_call(a, dtype == ZSAA_BF16, HD)) return launch_paged_direct(a, nullptr, dtype, HD, s);
   const Launches r = launches_of(a, dtype, HD, std::min(sms, kMostSms), ws);
   for (int i = 0; i < r.n; ++i) {
     const cudaError_t e = r.tc[i] ? launch_paged_tc(a, r.work[i], HD, r.tiles[i].ctas, s)
                                   : launch_paged_mma(a, r.work[i], dtype, HD, r.tiles[i].ctas, s);
     if (e != cudaSuccess) return e;
   }
-  if (r.own) return launch_paged_direct(a, &r.work[0], dtype, HD, wide, s);
+  if (r.own) return launch_paged_direct(a, &r.work[0], dtype, HD, s);
   const int heads = a.Hkv * a.per, per_cta = kJoinThreads / 32;
   ZSAA_LAUNCH(paged_join_kernel<T, HD>, dim3(a.S * a.n_q, (heads + per_cta - 1) / per_cta), dim3(kJoinThreads), 0, s, a, r.work[0], r.work[r.n - 1]);
   return cudaSuccess;

@@ -596,11 +596,19 @@ static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream
   return cudaSuccess;
 }
 
+// Warps of a CTA: eight where CTAs of four would leave SMs empty, two where more than two of
+// four would be asked of an SM, so that one's start and end run under the others' loads (us,
+// four and two, 64 sequences, 8 heads of 128 dims: 32 keys 6.6 and 4.3, 256 17.7 and 15.0, 512
+// 27.5 and 25.3, float32 9.2 and 7.2, 36 and 33, 61 and 59; 64 dims 5.4 and 4.4, 8.8 and 9.6, 18
+// and 17; 30 sequences, 256 keys 6.6 and 9.9).  Four after partial results, whose joining has
+// more for a warp to wait for (24 sequences of 4 drafts 22 and 28).
 template <typename T, int HD>
-static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, bool wide, cudaStream_t s) {
+static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, cudaStream_t s) {
+  const long long ctas = static_cast<long long>(a.S) * a.Hkv * ((a.n_q * a.per + MM_ROWS - 1) / MM_ROWS);
   if constexpr (sizeof(T) == 2)
-    if (w != nullptr) return wide ? run_direct<T, HD, 8, true>(a, *w, s) : run_direct<T, HD, 4, true>(a, *w, s);
-  return wide ? run_direct<T, HD, 8, false>(a, PagedWork{}, s) : run_direct<T, HD, 4, false>(a, PagedWork{}, s);
+    if (w != nullptr) return ctas <= 152 ? run_direct<T, HD, 8, true>(a, *w, s) : run_direct<T, HD, 4, true>(a, *w, s);
+  if (ctas <= 152) return run_direct<T, HD, 8, false>(a, PagedWork{}, s);
+  return ctas <= 304 ? run_direct<T, HD, 4, false>(a, PagedWork{}, s) : run_direct<T, HD, 2, false>(a, PagedWork{}, s);
 }
 
 // Lead: without, with 2 and with 8 units to an item (us): 60 sequences of 160 entries on 57
@@ -612,10 +620,10 @@ PagedTiles paged_mma_tiles(int dtype, int hd, int sms) {
   return PagedTiles{MM_ROWS, bf ? MmCfg<bf16, 128>::BLOCK : MmCfg<float, 128>::BLOCK, ctas * sms, 1, 2};
 }
 
-cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, bool wide, cudaStream_t s) {
-  if (dtype == ZSAA_BF16) return hd == 64 ? run_direct<bf16, 64>(a, prefixes, wide, s) : run_direct<bf16, 128>(a, prefixes, wide, s);
-  if (hd == 32) return run_direct<float, 32>(a, nullptr, wide, s);
-  return hd == 64 ? run_direct<float, 64>(a, nullptr, wide, s) : run_direct<float, 128>(a, nullptr, wide, s);
+cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, cudaStream_t s) {
+  if (dtype == ZSAA_BF16) return hd == 64 ? run_direct<bf16, 64>(a, prefixes, s) : run_direct<bf16, 128>(a, prefixes, s);
+  if (hd == 32) return run_direct<float, 32>(a, nullptr, s);
+  return hd == 64 ? run_direct<float, 64>(a, nullptr, s) : run_direct<float, 128>(a, nullptr, s);
 }
 
 cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int dtype, int hd, int ctas, cudaStream_t s) {

@@ -52,9 +52,9 @@ struct PagedTiles {
 // tiles of 16 rows (k_paged_mma.cu)
 PagedTiles paged_mma_tiles(int dtype, int hd, int sms);
 cudaError_t launch_paged_mma(const PagedArgs& a, const PagedWork& w, int dtype, int hd, int ctas, cudaStream_t s);
-// all of a sequence and KV head's keys in one CTA (of 8 warps, wide, or 4); prefixes: the
-// launch that has left the prefixes' partial results (bf16), or null
-cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, bool wide, cudaStream_t s);
+// all of a sequence and KV head's keys in one CTA; prefixes: the launch that has left the
+// prefixes' partial results (bf16), or null
+cudaError_t launch_paged_direct(const PagedArgs& a, const PagedWork* prefixes, int dtype, int hd, cudaStream_t s);
 // bf16, tiles of 128 rows (k_paged_tc.cu)
 PagedTiles paged_tc_tiles(int sms);
 cudaError_t launch_paged_tc(const PagedArgs& a, const PagedWork& w, int hd, int ctas, cudaStream_t s);

@@ -122,6 +122,11 @@ CASES = [
     ("bf16", 5, 1, 64, 64, 3, [70, 3, 2], None, None),
     ("bf16", 8, 1, 64, 16, 3, [5, 40], [0, 2], [12000]),                 # more than 32 partial results to a row
     ("bf16", 20, 1, 128, 16, 1, [3] * 70, list(range(71)), [17] * 70),  # more than 32 groups
+    ("bf16", 10, 5, 64, 16, 1, [33, 0, 1, 90, 16] * 14, None, None),     # more CTAs than the SMs hold
+    ("bf16", 10, 5, 128, 16, 3, [40, 1, 0, 17, 66] * 14, [0, 30, 70], [50, 0]),
+    ("f32", 10, 5, 32, 16, 1, [33, 0, 1, 90, 16] * 14, None, None),
+    ("f32", 10, 5, 64, 16, 2, [40, 1, 0, 17, 66] * 14, [2, 70], [35]),
+    ("f32", 10, 5, 128, 16, 1, [33, 0, 1, 90, 16] * 14, [0, 40, 70], [0, 21]),
     ("f32", 4, 4, 32, 16, 1, [1, 0, 50], None, None),
     ("f32", 2, 1, 64, 16, 1, [3] * 40, list(range(41)), [17] * 40),
     ("f32", 4, 4, 32, 16, 3, [77, 3, 12, 40], [0, 1, 4], [413, 100]),
