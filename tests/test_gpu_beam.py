@@ -60,7 +60,8 @@ def draw(B, W, V, seed, scale=3.0):
 
 @pytest.mark.parametrize("B,W,V,K", [
     (1, 1, 1, 1), (1, 1, 3, 3), (2, 3, 2, 6), (1, 4, 1000, 8), (3, 5, 2047, 5), (2, 8, 2049, 16), (1, 1, 40001, 64),
-    (1, 64, 333, 64), (5, 2, 8192, 4), (1, 4, 128256, 8), (4, 2, 50257, 2), (90, 4, 8193, 3), (1, 3, 8188, 64)])
+    (1, 64, 333, 64), (5, 2, 8192, 4), (1, 4, 128256, 8), (4, 2, 50257, 2), (90, 4, 8193, 3), (1, 3, 8188, 64),
+    (1, 1, 600001, 64), (1, 12, 300000, 20), (2, 16, 5000, 32), (3, 9, 700, 64), (30, 16, 4100, 8), (1, 32, 20000, 33)])
 def test_select(zlib, B, W, V, K):
     logits, scores, _ = draw(B, W, V, B + W + V + K)
     check_select(zlib, logits, scores, None, -1, K)
@@ -115,6 +116,29 @@ def test_select_values_that_crowd_one_warp(zlib):
         check_select(zlib, np.ascontiguousarray(logits), None, None, -1, K)
     many = np.ascontiguousarray(np.repeat(logits, 90, axis=0))  # enough rows for the long chunks
     check_select(zlib, many, None, None, -1, 64)
+
+
+def test_select_long_rows_with_the_best_in_few_stretches(zlib):
+    """Lists of more than 63 stretches are merged in rounds; the best values lie in the
+    first stretch, in the last, and in one of the second round."""
+    V = 600000
+    logits = np.full((3, 1, V), -30, np.float32) + (np.arange(V) % 977).astype(np.float32) * 1e-4
+    best = np.arange(200, dtype=np.float32) * 1e-2
+    logits[0, 0, 17:217] = best
+    logits[1, 0, -200:] = -best
+    logits[2, 0, 400000:400200] = best[::-1]
+    for row in logits:  # (one row: as many stretches as there are)
+        for K in (1, 9, 64):
+            check_select(zlib, row[None], None, None, -1, K)
+
+
+def test_select_many_beams_some_ended(zlib):
+    logits, scores, r = draw(3, 20, 4000, 21)
+    done = r.random((3, 20)) < 0.4
+    done[1, 8:] = True
+    logits[2, 11] = -INF
+    for K in (5, 30):
+        check_select(zlib, logits, scores, done, 3, K)
 
 
 @pytest.mark.parametrize("level", [-3e4, 1e4, 80.0])
