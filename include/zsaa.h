@@ -506,12 +506,13 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  *            normaliser as zsaa_op_attention gives it
  * A query that sees no entry gets zeros and lse -inf.  Entries that a query does not
  * see never touch its result, whatever they hold.  (An entry that it sees has to be
- * finite, in float32 below 2^127: an infinity among them can make its row NaN.)  But for short tables the prefix of a
- * group is read once for all of its queries.  Results do not depend on timing.  The
- * lengths stay on the device, so a call is planned by the widths of its tables, cols and
- * prefix_cols: rows much wider than the lengths cost time.  At most 65536 heads.  ws:
- * 16-byte aligned, ws_bytes at least what zsaa_op_paged_attention_workspace returns for
- * these sizes (host only; prefix_cols is ignored with G = 0). */
+ * finite, in float32 below 2^127: an infinity among them can make its row NaN.)  But for
+ * short tables the prefix of a group is read once for all of its queries.  Results do not
+ * depend on timing.  The lengths stay on the device, so a call is planned by the widths of
+ * its tables, cols and prefix_cols: rows much wider than the lengths cost time.  At most
+ * 65536 heads.  ws: 16-byte aligned, ws_bytes at least what
+ * zsaa_op_paged_attention_workspace returns for these sizes (host only; prefix_cols is
+ * ignored with G = 0). */
 zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
                                               int cols, int prefix_cols, size_t* bytes);
 zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, int n_q, int Hq,
