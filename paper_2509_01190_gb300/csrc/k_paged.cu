@@ -6,11 +6,11 @@
 // keys are written once and the projection needs no position.
 //
 // Attention: sequence s of group g has n_q new entries, its last; query j sees the
-// group's prefix and the sequence's entries i <= len - n_q + j.  The prefix is read
-// once for all queries of the group (paged.cuh has the decomposition); the joining
-// kernel adds the partial results and the at most n_q - 1 entries that only some of
-// the queries see, one by one and so without a mask: a value hidden from a query,
-// finite or not, never enters its sums.
+// group's prefix and the sequence's entries i <= len - n_q + j.  Short tables take one launch
+// (k_paged_mma.cu).  Else the prefix is read once for all queries of the group (paged.cuh has
+// the decomposition), and the launch that joins adds the partial results.  The at most n_q - 1
+// entries that only some of the queries see are added at the end of a query row, one by one
+// and so without a mask: a value hidden from a query, finite or not, never enters its sums.
 #include <algorithm>
 #include <cmath>
 

@@ -17,9 +17,10 @@
 // float32 operands are split into pairs of tf32: x = hi + lo, hi the nearest number of 11
 // significant bits, lo the rest rounded to 11, which leaves 2^-24 |x| at most, the rounding of
 // a float32; the products hi hi, hi lo and lo hi are taken and lo lo, below 2^-24 of the
-// product, is not.  The tensor cores' own sums may be rounded towards zero, so none is longer
-// than four products of a kind: scores are put together from such sums, and a tile's P V is
-// added to the output, in float32 additions.
+// product, is not.  The tensor cores' own sums may be rounded towards zero, so no sum of hi hi
+// is longer than four of them (32 dims): scores are put together from such sums, and a tile's
+// P V is added to the output, in float32 additions.  (The sums of the other two, 2^-11 of those,
+// run over all dims.)
 //
 // 48 sequences of 2000 to 4000 bf16 entries, 8 heads of 128 dims: 95 us for 576 MB, 90% of the
 // copy rate.  float32, 64 sequences of 2048: 214 us for 1.07 GB, 74%; with more rows than 16 to a
