@@ -461,7 +461,7 @@ __global__ void __launch_bounds__(MM_THREADS, MmCfg<T, HD>::CTAS)
 // results, one launch.  The prefix is read once for every sequence, in L2.
 // PARTS: the prefixes' partial results are in w already (the 128-row tiles'), and this
 // launch has the sequences' own entries and joins.
-template <typename T, int HD, int W, bool PARTS>
+template <typename T, int HD, int W, int R, bool PARTS>
 __global__ void __launch_bounds__(32 * W, 8 / W)
     paged_direct_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ PagedWork w) {
   using C = MmCfg<T, HD>;
@@ -542,8 +542,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   mm_put<HD>(x, j0, j0 + 8 * HD, 0, HD, in0, in1);
   __syncthreads();
   constexpr int DPL = HD / 32;
-  constexpr int R = MM_ROWS / W;
-  PagedRows<HD, R> y;
+  PagedRows<HD, R> y;  // (rows warp, warp + W, ...: R W rows or fewer)
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     const int r = warp + i * W;
@@ -586,15 +585,25 @@ static cudaError_t run_mma(const PagedArgs& a, const PagedWork& w, int ctas, cud
   return cudaSuccess;
 }
 
-template <typename T, int HD, int W, bool PARTS>
+template <typename T, int HD, int W, int R, bool PARTS>
 static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream_t s) {
   static OncePerDevice once;
   const int smem = std::max(W * MmCfg<T, HD>::RING, W * MM_ROWS * HD * 4);  // (the ring, then the warps' results)
-  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<T, HD, W, PARTS>, smem);
+  const cudaError_t e = set_smem_limit_once(once, paged_direct_kernel<T, HD, W, R, PARTS>, smem);
   if (e != cudaSuccess) return e;
   const int tiles = (a.n_q * a.per + MM_ROWS - 1) / MM_ROWS;
-  ZSAA_LAUNCH(paged_direct_kernel<T, HD, W, PARTS>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), smem, s, a, w);
+  ZSAA_LAUNCH(paged_direct_kernel<T, HD, W, R, PARTS>, dim3(a.S, a.Hkv * tiles), dim3(32 * W), smem, s, a, w);
   return cudaSuccess;
+}
+
+// R: the rows that a warp finishes together.  With 4 rows to a head (us, R of 4 and of 1): 64
+// sequences of 600 entries after a prefix of 32000, 128 dims, 93.1 and 86.4; of 150 after 16000,
+// 64 dims, 35.8 and 30.9: a row that is not there still takes its turns in the reductions.
+template <typename T, int HD, int W, bool PARTS>
+static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream_t s) {
+  constexpr int FEW = W == 2 ? 2 : 1;
+  if (a.n_q * a.per <= FEW * W) return run_direct<T, HD, W, FEW, PARTS>(a, w, s);
+  return run_direct<T, HD, W, MM_ROWS / W, PARTS>(a, w, s);
 }
 
 // Warps of a CTA: eight where CTAs of four would leave SMs empty, two where more than two of
