@@ -608,10 +608,11 @@ static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream
 
 // Warps of a CTA: eight where CTAs of four would leave SMs empty, two where more than two of
 // four would be asked of an SM, so that one's start and end run under the others' loads (us,
-// four and two, 64 sequences, 8 heads of 128 dims: 32 keys 6.6 and 4.3, 256 17.7 and 15.0, 512
-// 27.5 and 25.3, float32 9.2 and 7.2, 36 and 33, 61 and 59; 64 dims 5.4 and 4.4, 8.8 and 9.6, 18
-// and 17; 30 sequences, 256 keys 6.6 and 9.9).  Four after partial results, whose joining has
-// more for a warp to wait for (24 sequences of 4 drafts 22 and 28).
+// four and two, 64 sequences, 8 heads of 128 dims: 32 keys 6.1 and 3.9, 256 17.0 and 14.4, 512
+// 27.3 and 24.7, float32 8.5 and 6.6, 35 and 32, 61 and 58; 64 dims 4.8 and 3.7, 8.3 and 8.8, 18
+// and 16; 62 of 5 queries, 256 keys 32 and 27, 64 dims 18 and 19; 30 of one 6.2 and 9.2).  Four
+// after partial results: with 600 own entries after 16000, 128 dims, 64 sequences 61 and 59, 30
+// 38 and 45; 24 of 4 drafts 22 and 28.
 template <typename T, int HD>
 static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, cudaStream_t s) {
   const long long ctas = static_cast<long long>(a.S) * a.Hkv * ((a.n_q * a.per + MM_ROWS - 1) / MM_ROWS);
