@@ -524,7 +524,8 @@ zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, 
 /* zsaa_op_beam_select: the K best continuations of each of B batch elements with W
  * beams over a vocabulary of V tokens.  Continuation (w, v) has the total
  * scores[w] + logits[w, v] - log sum_u exp(logits[w, u]), in 64 bits from the stored
- * float32 logits (the sum of exponentials in parts of 32 bits, joined in 64).
+ * float32 logits of any size, the row's maximum taken off first (the exponentials and the
+ * factors that join their sums are float32's, the sums 64-bit integers).
  *   logits : float32 [B*W, ld], ld >= V (not read past V);  V <= 2^26
  *   scores : float32 [B, W] or NULL (all 0);  1 <= W <= 64, 1 <= K <= 64, K <= W*V
  *   done   : uint8 [B, W] or NULL; a beam with a flag other than 0 has ended: its logits

@@ -22,14 +22,15 @@
 // where more values than the list holds reach the bound all the same, the K-th best is
 // found bit by bit instead.
 //
-// Sums are taken against c, the float next to n ln 2 with n the maximum of a warp's first
-// values in the log2 domain rounded up, and are then brought to the power of two at the
-// last maximum by exact steps and the factor exp(c - n ln 2), so that warps and stretches
-// are put together by shifts and a beam needs one logarithm.  (Logits are taken off c
-// before the product with log2(e): the other way around a logit of 1000 would be off by
-// 1e-4.)  A thread's terms are added in 32 bits and everything after that as 64-bit
-// integers of 2^-36: FP64 runs at a sixty-fourth of FP32 here, and is left to a beam's
-// logarithm and the totals of its K tokens.
+// Sums are taken against a logit: a warp's against the maximum of its first values, brought
+// to its last maximum at the end; warps and stretches are put together against the larger of
+// their maxima, by the factor exp(their own - the larger).  A reference that is itself a
+// float32 logit makes x - reference exact where it matters, next to the maximum, at every
+// size of the logits, and a maximum's own term 1.  (Differences are taken before the product
+// with log2(e): the other way around a logit of 1000 would be off by 1e-4.)  A thread's
+// terms are added in 32 bits and everything after that as 64-bit integers of 2^-36: FP64
+// runs at a sixty-fourth of FP32 here, and is left to a beam's logarithm and the totals of
+// its K tokens.
 #include <algorithm>
 
 #include "common.cuh"
@@ -47,11 +48,6 @@ constexpr int kMergeThreads = 512;
 constexpr int kMergeWarps = kMergeThreads / 32;
 constexpr int kMergeDepth = 8;  // elements of each list that the merge holds in shared memory
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.69314718055994530942;
-constexpr float kLn2Hi = static_cast<float>(kLn2), kLn2Lo = static_cast<float>(kLn2 - static_cast<double>(kLn2Hi));
-// logits of this size and more have no neighbours within reach of exp: a maximum is
-// then its own reference, and its sum counts the values equal to it
-constexpr float kHuge = 0x1p100f;
 constexpr float kSumUnit = 0x1p36f;  // (2^26 terms of up to 1 fit)
 
 // Order-preserving map of a float (no NaN) to unsigned; -0 equals +0, -inf is 0x007fffff.
@@ -93,22 +89,17 @@ __device__ __forceinline__ float fmin3(float a, float b, float c) {
   return y;
 }
 
-// c of x: the reference of sums whose maximum is x, and its n (a huge x is its own)
-__device__ __forceinline__ bool is_huge(float x) { return !(fabsf(x) < kHuge); }
-__device__ __forceinline__ float log2_ceil(float x) { return is_huge(x) ? x : ceilf(x * kLog2e); }
-__device__ __forceinline__ float reference(float x) {
-  const float n = log2_ceil(x);
-  return !is_huge(x) ? fmaf(n, kLn2Hi, n * kLn2Lo) : x == -INFINITY ? 0.f : x;
-}
-
 // A value (no NaN) at a place: the higher value, then the lower place, is the larger.
 __device__ __forceinline__ uint64_t value_at(float x, int place) {
   return static_cast<uint64_t>(float_key(x)) << 32 | static_cast<uint32_t>(~place);
 }
 
-// sum / 2^steps; steps: 0 or a positive whole number, or NaN (two maxima of -inf)
-__device__ __forceinline__ uint64_t down_by(uint64_t sum, float steps) {
-  return steps < 64.f ? sum >> static_cast<int>(steps) : 0;
+// A sum against the maximum `own` as one against `top`, which is as large or larger; below
+// e^-64 nothing of 2^62 is left.  (NaN, of two maxima of -inf, whose sums are 0: 0.)
+__device__ __forceinline__ uint64_t sum_against(uint64_t sum, float own, float top) {
+  const float d = own - top;
+  if (d == 0.f) return sum;
+  return d > -64.f ? __float2ull_rn(__ull2float_rn(sum) * expf(d)) : 0;
 }
 
 // One stretch: `tiles` steps of 4096 values.  A value's place is its token; a collected
@@ -126,7 +117,7 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   __shared__ uint64_t list[kListCap], s_bound, s_sum[kScanWarps];
   __shared__ int s_count, s_bad[kScanWarps], s_n[kScanWarps];
   __shared__ uint32_t s_least[kScanWarps];
-  __shared__ float s_n2[kScanWarps];
+  __shared__ float s_top[kScanWarps];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x / chunks, c = blockIdx.x % chunks;
   pdl_trigger();
@@ -169,7 +160,7 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   };
   auto max_of = [](const float4& f, float m) { return fmax3_nan(fmax3_nan(f.x, f.y, f.z), f.w, m); };
 
-  float best = -INFINITY, least = INFINITY, n2 = -INFINITY, ref = 0.f;
+  float best = -INFINITY, least = INFINITY, first = -INFINITY, ref = 0.f;
   float s4[4] = {0.f, 0.f, 0.f, 0.f};
   auto add = [&](const float4& f) {
     s4[0] += ex2_fast((f.x - ref) * kLog2e);
@@ -187,10 +178,9 @@ __global__ void __launch_bounds__(kScanThreads, 4)
       best = max_of(f[i], best);
       least = fmin3(fmin3(f[i].x, f[i].y, f[i].z), f[i].w, least);
     }
-    if (n2 == -INFINITY) {  // (warp-uniform) the reference: the first finite maximum
-      const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(fmaxf(best, -INFINITY))));
-      n2 = log2_ceil(m);
-      ref = reference(m);
+    if (first == -INFINITY) {  // (warp-uniform) the reference: the first finite maximum
+      first = key_float(__reduce_max_sync(0xffffffffu, float_key(fmaxf(best, -INFINITY))));
+      ref = first == -INFINITY ? 0.f : first;
     }
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
@@ -208,10 +198,9 @@ __global__ void __launch_bounds__(kScanThreads, 4)
       for (int i = 0; i < GROUPS; ++i) best = fmaxf(best, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
     }
   }
-  const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(best))), last = log2_ceil(m);
-  if (m > ref + 40.f && n2 != -INFINITY) {  // (warp-uniform) the first values were far below: the sum again
-    n2 = last;
-    ref = reference(m);
+  const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(best)));
+  if (m - ref > 40.f && first != -INFINITY) {  // (warp-uniform) the first values were far below: the sum again
+    ref = m;
     s4[0] = s4[1] = s4[2] = s4[3] = 0.f;
     for (int t = 0; t < n_tiles; ++t) {
       load(t, f);
@@ -219,9 +208,9 @@ __global__ void __launch_bounds__(kScanThreads, 4)
       for (int i = 0; i < GROUPS; ++i) add(f[i]);
     }
   }
-  // to the power of two at the last maximum (at most 58 steps up), as integers
+  // against the last maximum, as integers
   bad = __any_sync(0xffffffffu, bad);
-  const float step = is_huge(m) ? 1.f : __int_as_float((127 + static_cast<int>(n2 - last)) << 23);
+  const float step = m > ref ? expf(ref - m) : 1.f;  // (e^-40 or more, but for a maximum of +inf)
   uint64_t sum = __float2ull_rn(((s4[0] + s4[1]) + (s4[2] + s4[3])) * step * kSumUnit);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -235,9 +224,8 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   }
   const uint32_t low = __reduce_min_sync(0xffffffffu, float_key(least));
   if (lane == 0) {
-    const float d = is_huge(m) ? 0.f : -(fmaf(n2, kLn2Hi, -ref) + n2 * kLn2Lo);  // c - n ln 2
-    s_sum[warp] = sum + __float2ll_rn(__ull2float_rn(sum) * (d + d * d * (0.5f + d * (1.f / 6.f))));
-    s_n2[warp] = last;
+    s_sum[warp] = sum;
+    s_top[warp] = m;
     s_bad[warp] = bad;
     s_least[warp] = low;
   }
@@ -253,16 +241,6 @@ __global__ void __launch_bounds__(kScanThreads, 4)
       }
     }
     if (r == K - 1) s_bound = x;
-  } else if (tid == kScanThreads - 1) {
-    BeamChunk x{0, s_n2[0], s_bad[0]};
-#pragma unroll
-    for (int w = 1; w < kScanWarps; ++w) {
-      x.n2 = fmaxf(x.n2, s_n2[w]);
-      x.bad |= s_bad[w];
-    }
-#pragma unroll
-    for (int w = 0; w < kScanWarps; ++w) x.sum += down_by(s_sum[w], x.n2 - s_n2[w]);
-    stat[blockIdx.x] = x;
   }
   __syncthreads();
   uint64_t bound = s_bound;
@@ -332,6 +310,15 @@ __global__ void __launch_bounds__(kScanThreads, 4)
     __syncthreads();
     n = s_count;
   }
+  if (warp == kScanWarps - 1) {  // (few lists reach this warp) the warps' sums, one a lane
+    const bool in = lane < kScanWarps;
+    const float own = in ? s_top[lane] : -INFINITY, top = warp_max(own);
+    const bool any_bad = __any_sync(0xffffffffu, in && s_bad[lane] != 0);
+    uint64_t x = in ? sum_against(s_sum[lane], own, top) : 0;
+#pragma unroll
+    for (int o = kScanWarps / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (lane == 0) stat[blockIdx.x] = BeamChunk{x, top, any_bad};
+  }
   for (int i = tid; i < n; i += kScanThreads) {  // (at least K: a step has more places than that)
     const uint64_t x = list[i];
     int r = 0;
@@ -370,8 +357,8 @@ __global__ void __launch_bounds__(kMergeThreads)
   uint2* merged = best + W * K;                           // [list warps][2][K] lists of the chunks merged so far
   uint2* cache = merged + list_warps * 2 * K;             // [list warps][depth][64] the lists' next elements
   __shared__ uint64_t s_sum[kBeamMaxBeams];
-  __shared__ float s_n2[kBeamMaxBeams];
-  __shared__ double s_lse[kBeamMaxBeams], s_score[kBeamMaxBeams];
+  __shared__ float s_top[kBeamMaxBeams];
+  __shared__ double s_log[kBeamMaxBeams], s_score[kBeamMaxBeams];  // log of the sum against s_top
   __shared__ uint8_t s_done[kBeamMaxBeams], s_bad[kBeamMaxBeams];
   __shared__ int rank[kRankPairs];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -455,22 +442,22 @@ __global__ void __launch_bounds__(kMergeThreads)
       BeamChunk first = lane < chunks ? st[lane] : BeamChunk{0, -INFINITY, 0};
       const bool over = done != nullptr && done[b * W + w] != 0;
       const float score = scores == nullptr ? 0.f : scores[b * W + w];
-      float top = first.n2;
+      float top = first.top;
       int bad = first.bad;
       for (int c = lane + 32; c < chunks; c += 32) {
         const BeamChunk x = st[c];
-        top = fmaxf(top, x.n2);
+        top = fmaxf(top, x.top);
         bad |= x.bad;
       }
       top = warp_max(top);
       bad = __any_sync(0xffffffffu, bad);
-      uint64_t sum = down_by(first.sum, top - first.n2);
-      for (int c = lane + 32; c < chunks; c += 32) sum += down_by(st[c].sum, top - st[c].n2);
+      uint64_t sum = sum_against(first.sum, first.top, top);
+      for (int c = lane + 32; c < chunks; c += 32) sum += sum_against(st[c].sum, st[c].top, top);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       if (lane == 0) {
         s_sum[w] = sum;
-        s_n2[w] = top;
+        s_top[w] = top;
         s_bad[w] = bad;
         s_done[w] = over;
         s_score[w] = static_cast<double>(score);
@@ -478,19 +465,16 @@ __global__ void __launch_bounds__(kMergeThreads)
     }
     asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
     if (tid < W) {  // (a logarithm is a long chain of FP64: all beams' at once, while the lists are merged)
-      const float n2 = s_n2[tid];
-      double lse;
-      if (s_done[tid])
-        lse = 0.0;
-      else if (s_bad[tid])
-        lse = __longlong_as_double(0x7ff8000000000000ll);  // every total NaN
-      else if (n2 == -INFINITY)
-        lse = 0.0;  // no allowed token: every total is -inf - 0
-      else if (!(fabsf(n2) < 2.f * kHuge))  // (in the log2 domain a maximum below 2^100 is below 2^101)
-        lse = static_cast<double>(n2);
-      else
-        lse = (static_cast<double>(n2) + log2(static_cast<double>(s_sum[tid]) * (1.0 / kSumUnit))) * kLn2;
-      s_lse[tid] = lse;
+      double l;
+      if (s_done[tid] || (!s_bad[tid] && s_top[tid] == -INFINITY)) {
+        l = 0.0;  // eos at no cost; no allowed token: every total is -inf
+        s_top[tid] = 0.f;
+      } else if (s_bad[tid]) {
+        l = __longlong_as_double(0x7ff8000000000000ll);  // every total NaN
+      } else {
+        l = log(static_cast<double>(s_sum[tid]) * (1.0 / kSumUnit));
+      }
+      s_log[tid] = l;
     }
     __syncwarp();
     for (int w = kSumWarps + warp; w < W; w += kMergeWarps) merge_lists(w, kSumWarps + warp);
@@ -498,8 +482,10 @@ __global__ void __launch_bounds__(kMergeThreads)
     for (int w = warp - kSumWarps; w < W; w += list_warps) merge_lists(w, warp - kSumWarps);
   }
   __syncthreads();
-  for (int i = tid; i < n; i += kMergeThreads)
-    total[i] = double_key(s_score[i / K] + (static_cast<double>(key_float(best[i].x)) - s_lse[i / K]));
+  for (int i = tid; i < n; i += kMergeThreads) {  // (the maximum off first: of floats, all but always exact)
+    const double x = static_cast<double>(key_float(best[i].x)) - static_cast<double>(s_top[i / K]);
+    total[i] = double_key(s_score[i / K] + (x - s_log[i / K]));
+  }
   __syncthreads();
   auto put = [&](int r, int w, int i, uint64_t x) {  // total x of element i, beam w's, has rank r
     const size_t o = static_cast<size_t>(b) * K + r;

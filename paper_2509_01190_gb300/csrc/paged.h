@@ -66,8 +66,8 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* 
 constexpr int kBeamMaxBeams = 64, kBeamMaxKept = 64, kBeamMaxVocab = 1 << 26;
 constexpr int kReorderMaxLayers = 64;
 struct BeamChunk {
-  unsigned long long sum;  // sum of exp(x) / 2^n2 in units of 2^-36
-  float n2;                // the maximum in the log2 domain, rounded up (a huge one: itself)
+  unsigned long long sum;  // sum of exp(x - top) in units of 2^-36
+  float top;               // the maximum
   int bad;                 // a NaN or +inf among the logits
 };
 // Stretches that a beam's logits are scanned in, at most, on any device.

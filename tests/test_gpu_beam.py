@@ -149,6 +149,71 @@ def test_select_logits_far_from_zero(zlib, level):
     check_select(zlib, logits, scores, None, -1, 8)
 
 
+def ulps(level, steps):
+    """float32 numbers `steps` units of the last place above `level`."""
+    x = np.float32(level)
+    return x + np.asarray(steps, np.float32) * np.spacing(np.abs(x))
+
+
+def check_levels(z, logits, scores, K):
+    """As check_select, with totals that take the maximum off first, so that 64 bits hold
+    what they are at any level: score + ((x - max) - log sum exp(x - max))."""
+    B, W, V = logits.shape
+    top = logits.max(-1, keepdims=True).astype(np.float64)
+    gap = logits - top
+    total = scores[..., None] + (gap - np.log(np.exp(gap).sum(-1, keepdims=True)))
+    want = []
+    for b in range(B):
+        w, v = np.meshgrid(np.arange(W), np.arange(V), indexing="ij")
+        order = np.lexsort((v.ravel(), -logits[b].ravel().astype(np.float64), w.ravel(), -total[b].ravel()))[:K + 1]
+        t, w, v = total[b].ravel()[order], w.ravel()[order], v.ravel()[order]
+        apart = (t[:-1] - t[1:])[(w[:-1] != w[1:]) & (t[:-1] != t[1:])]
+        assert apart.size == 0 or apart.min() > 2e-6, "two totals are too close to be told apart"
+        want.append((t[:K], w[:K], v[:K]))
+    got = select(z, logits, scores, None, -1, K)
+    for b, (t, w, v) in enumerate(want):
+        np.testing.assert_array_equal(got[1][b], w)
+        np.testing.assert_array_equal(got[2][b], v)
+        # as in check_select
+        assert np.all(np.abs(got[0][b] - t) <= 2.0 ** -19 + R.F32_HALF * np.abs(t)), (got[0][b], t)
+
+
+@pytest.mark.parametrize("V", [4096, 70001])
+@pytest.mark.parametrize("level", [1e6, -1e6, 1e7, -1e7, 3e7, -3e7, 1e8, -1e8, 1e9, -1.5e9, 1e10, -1e10, 1e12, -1e12, 1e30,
+                                   -1e30, 3e38, -3e38])
+def test_select_logits_of_any_size(zlib, level, V):
+    """Rows far from zero as a whole or in part: masks of a large finite number, forced
+    tokens, values a few units of the last place apart."""
+    ordinary, scores, r = draw(5, 3, V, 17)
+    logits = ordinary.copy()
+    logits[0] = ulps(level, r.integers(-3, 4, (3, V)))   # all beams
+    logits[1, 0] = np.float32(level)                     # one beam, all of it the same
+    logits[2, :, V - 2] = ulps(level, [0, 1, 2])         # one token in the last stretch
+    logits[3, :, 5] = ulps(level, [2, 0, 1])             # one in the first
+    keep = r.permutation(V)[:5]                          # all but five
+    logits[4] = np.float32(level)
+    logits[4][:, keep] = ordinary[4][:, keep]
+    for K in (1, 8, 64):
+        check_levels(zlib, logits, scores, K)
+
+
+@pytest.mark.parametrize("low,high", [(0.9 * 2.0 ** 100, 2.0 ** 100), (-(2.0 ** 100), -0.9 * 2.0 ** 100), (2.0 ** 23 - 1, 2.0 ** 23 + 1),
+                                      (1.0, 2.0 ** 100), (-(2.0 ** 100), 1.0), (-30.0, 9.5), (-41.0, 0.0), (-80.0, 7.0)])
+def test_select_maxima_of_different_warps_and_stretches(zlib, low, high):
+    """Warps and stretches whose own maxima lie far below the row's, or next to it."""
+    V = 50000
+    logits, scores, r = draw(4, 2, V, 23, scale=0.5)
+    at = np.arange(V)
+    logits[0] = np.where((at % 1024) // 128 == 3, np.float32(high), np.float32(low))  # one warp of eight
+    logits[1] = np.where(at // 4096 == 6, np.float32(high), np.float32(low))          # one step
+    logits[2] = np.where(at < 4096, np.float32(low), np.float32(high))                # rising
+    logits[3] = np.where(at < V - 4096, np.float32(high), np.float32(low))            # falling
+    for K in (1, 9, 64):
+        check_levels(zlib, logits, scores, K)
+    many = np.ascontiguousarray(np.repeat(logits, 90, axis=0))  # stretches of several steps
+    check_levels(zlib, many, np.repeat(scores, 90, axis=0), 4)
+
+
 def test_select_in_a_graph(zlib):
     logits, scores, _ = draw(2, 4, 6000, 3)
     x, s = torch.from_numpy(logits).cuda(), torch.from_numpy(scores).cuda()
