@@ -18,9 +18,9 @@
 // all, so only the threads whose maximum reaches it look at their values again (in L2),
 // and the few values that do are ranked by counting.  Values are compared together with
 // their place, lower place first; where the bound is the stretch's minimum (a banned
-// vocabulary, whatever number marks it) the first 2 K places hold the K best or more, and
-// where more values than the list holds reach the bound all the same, the K-th best is
-// found bit by bit instead.
+// vocabulary, whatever number marks it; a NaN counts as -inf) the first 2 K places hold the
+// K best or more, and where more values than the list holds reach the bound all the same,
+// the K-th best is found bit by bit instead.
 //
 // Sums are taken against a logit: a warp's against the maximum of its first values, brought
 // to its last maximum at the end; warps and stretches are put together against the larger of
@@ -190,12 +190,16 @@ __global__ void __launch_bounds__(kScanThreads, 4)
   }
   // what few stretches need
   bool bad = !(best < INFINITY);
-  if (bad) {  // a NaN or +inf: the maximum of the numbers
+  if (bad) {  // a NaN or +inf: the maximum of the numbers; a NaN is a -inf among them
     best = -INFINITY;
     for (int t = 0; t < n_tiles; ++t) {
       load(t, f);
 #pragma unroll
-      for (int i = 0; i < GROUPS; ++i) best = fmaxf(best, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
+      for (int i = 0; i < GROUPS; ++i) {
+        const float m = max_of(f[i], -INFINITY);
+        if (m != m) least = -INFINITY;
+        best = fmaxf(best, fmaxf(fmaxf(f[i].x, f[i].y), fmaxf(f[i].z, f[i].w)));
+      }
     }
   }
   const float m = key_float(__reduce_max_sync(0xffffffffu, float_key(best)));

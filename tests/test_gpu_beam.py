@@ -214,6 +214,27 @@ def test_select_maxima_of_different_warps_and_stretches(zlib, low, high):
     check_levels(zlib, many, np.repeat(scores, 90, axis=0), 4)
 
 
+@pytest.mark.parametrize("K", [1, 8, 64])
+@pytest.mark.parametrize("V", [4096, 4097, 20480])
+def test_select_nan_ahead_of_equal_logits(zlib, K, V):
+    """A NaN counts as -inf among its row's logits, also where all the others are equal."""
+    logits = np.zeros((6, 2, V), np.float32)
+    logits[0, :, :16] = NAN
+    logits[1, :, :200] = NAN
+    logits[2, 0, :16] = NAN
+    logits[2, 0, V - 3:] = 2.0
+    logits[2, 1, 100] = 1.0
+    logits[3, 1, ::2] = NAN
+    logits[4, 0, :16] = NAN
+    logits[4, 0, 16:18] = INF
+    logits[4, 1, V - 1] = NAN
+    logits[5, :, :8] = NAN
+    logits[5, :, 8:] = -3e4
+    scores = np.array([[-1, -2]] * 6, np.float32)
+    check_select(zlib, logits, scores, None, -1, K)
+    check_select(zlib, np.ascontiguousarray(logits[:, :1]), None, None, -1, K)  # one beam fills the selection
+
+
 def test_select_in_a_graph(zlib):
     logits, scores, _ = draw(2, 4, 6000, 3)
     x, s = torch.from_numpy(logits).cuda(), torch.from_numpy(scores).cuda()
