@@ -505,8 +505,9 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  *   out    : as q (must not overlap it);  lse: float32 [S, n_q, Hq] or NULL, log2 of the
  *            normaliser as zsaa_op_attention gives it
  * A query that sees no entry gets zeros and lse -inf.  Entries that a query does not
- * see never touch its result, whatever they hold.  (An entry that it sees has to be
- * finite, in float32 below 2^127: an infinity among them can make its row NaN.)  But for
+ * see never touch its result, whatever they hold.  (An entry that it sees and the query have
+ * to be finite, in float32 below 2^127: an infinity among them can make its row NaN.  A NaN
+ * does: in a query or a key the whole row, in a value its dim.)  But for
  * short tables the prefix of a group is read once for all of its queries.  Results do not
  * depend on timing.  The lengths stay on the device, so a call is planned by the widths of
  * its tables, cols and prefix_cols: rows much wider than the lengths cost time.  At most

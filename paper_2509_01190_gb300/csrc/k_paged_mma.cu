@@ -15,12 +15,12 @@
 // 0.1% in every output).
 //
 // float32 operands are split into pairs of tf32: x = hi + lo, hi the nearest number of 11
-// significant bits, lo the rest rounded to 11, which leaves 2^-24 |x| at most, the rounding of
-// a float32; the products hi hi, hi lo and lo hi are taken and lo lo, below 2^-24 of the
-// product, is not.  The tensor cores' own sums may be rounded towards zero, so no sum of hi hi
-// is longer than four of them (32 dims): scores are put together from such sums, and a tile's
-// P V is added to the output, in float32 additions.  (The sums of the other two, 2^-11 of those,
-// run over all dims.)
+// significant bits, lo the rest cut to 11.  The rest has a sign and 12 bits, so at most the last
+// bit of x is lost, 2^-23 |x| (a rounding to 11 would lose no less).  A NaN stays one in lo.  The
+// products hi hi, hi lo and lo hi are taken and lo lo, at most 2^-22 of the product, is not.  The
+// tensor cores' own sums may be rounded towards zero, so no sum of hi hi is longer than four
+// of them (32 dims): scores are put together from such sums, and a tile's P V is added to the
+// output, in float32 additions.  (The sums of the other two, 2^-11 of those, run over all dims.)
 //
 // 48 sequences of 2000 to 4000 bf16 entries, 8 heads of 128 dims: 95 us for 576 MB, 90% of the
 // copy rate.  float32, 64 sequences of 2048: 214 us for 1.07 GB, 74%; with more rows than 16 to a
@@ -95,8 +95,8 @@ __device__ __forceinline__ void mm_load_q(MmRows<bf16, HD>& x, const bf16* q0, c
   }
 }
 __device__ __forceinline__ void mm_split(float x, uint32_t& hi, uint32_t& lo) {
-  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
-  lo = (__float_as_uint(x - __uint_as_float(hi)) + 0x1000u) & 0xffffe000u;
+  hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;  // (the carry makes a zero of some NaNs)
+  lo = __float_as_uint(x - __uint_as_float(hi)) & 0xffffe000u;  // (cut: 0x7fffffff, the NaN of a difference, stays NaN)
 }
 template <int HD>
 __device__ __forceinline__ void mm_load_q(MmRows<float, HD>& x, const float* q0, const float* q1, bool in0, bool in1) {

@@ -198,6 +198,38 @@ def test_a_later_draft_that_is_not_finite_stays_out_of_earlier_ones(zlib, dtype,
     check(p, q[:, :-1].contiguous(), table, clean, out[:, :-1].contiguous(), lse[:, :-1].contiguous(), [0, 3], ptable, [50])
 
 
+NAN_BITS = {"f32": (0x7fffffff, -1, 0x7fc00000, 0x7f800001), "bf16": (0x7fff, -1, 0x7fc0, 0x7f81)}
+
+
+@pytest.mark.parametrize("dtype,hd,cols", [("f32", 32, 0), ("f32", 32, 300), ("f32", 64, 0), ("f32", 64, 300), ("f32", 128, 0),
+                                           ("f32", 128, 300), ("bf16", 64, 0), ("bf16", 128, 300), ("bf16", 64, 5000),
+                                           ("bf16", 128, 5000)])
+@pytest.mark.parametrize("place", ["query", "own key", "own value", "prefix key", "prefix value"])
+def test_a_nan_that_a_query_sees_reaches_its_result(zlib, dtype, hd, cols, place):
+    """Any NaN, CUDA's own 0x7fffffff among them; rows that do not see it keep their bits."""
+    lens, plens, groups = [23, 9, 30], [40, 18], [0, 2, 3]
+    p, q, table, ptable = build(zlib, dtype, 12, 2, hd, 16, lens, 3, groups, plens)
+    table, ptable = widened(table, cols), widened(ptable, cols)
+    clean, clean_lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
+    bits = torch.int32 if dtype == "f32" else torch.int16
+    for nan in NAN_BITS[dtype]:
+        rows = (ptable[0] if place.startswith("prefix") else table[2])[0]
+        if place == "query":
+            word = q.view(bits)[1, 2, 7:8, hd - 3]
+        else:
+            word = (p.k if place.endswith("key") else p.v).view(bits)[rows, 1, 5:6, 11]
+        before = word.clone()
+        word.fill_(nan)
+        out, lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
+        k, v = p.np()
+        ref, ref_lse = R.attention(k, v, np64(q), table, lens, groups, ptable, plens)
+        hit, hit_lse = torch.from_numpy(np.isnan(ref)).cuda(), torch.from_numpy(np.isnan(ref_lse)).cuda()
+        assert hit.any() and not hit.all()
+        assert torch.equal(torch.isnan(out), hit) and torch.equal(torch.isnan(lse), hit_lse), hex(nan)
+        assert torch.equal(out[~hit], clean[~hit]) and torch.equal(lse[~hit_lse], clean_lse[~hit_lse])
+        word.copy_(before)
+
+
 @pytest.mark.parametrize("dtype,hd", [("bf16", 64), ("bf16", 128), ("f32", 64)])
 def test_large_scores(zlib, dtype, hd):
     """Scores far apart, rising and falling along the keys: the running maximum moves
