@@ -451,9 +451,10 @@ zsaa_status zsaa_op_colmass_ex(const void* qkv, const float* lse, int B, int N, 
  * A table row lists a sequence's pages in order (device int32, `cols` to a row): entry
  * i lies in page row[i / page_size].  Entries of a row past the last page in use are
  * not read.  lens[s] counts the entries of sequence s, the ones that the current step
- * appends included.  A page number outside [0, n_pages) or a length beyond the row is
- * reported by zsaa_device_status as ZSAA_ERR_INVALID_ARG: nothing out of range is read
- * or written, and what the sequence got is unspecified.
+ * appends included; a negative one counts as 0.  A page number outside [0, n_pages) or a
+ * length beyond the row (for zsaa_op_beam_reorder a negative one too) is reported by
+ * zsaa_device_status as ZSAA_ERR_INVALID_ARG: nothing out of range is read or written, and
+ * what the sequence got is unspecified.
  *
  * All pointers are device pointers on the current device unless stated; every call
  * may be captured into a graph (call one once before, outside capture: the status word

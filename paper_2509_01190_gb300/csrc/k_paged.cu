@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kAppendThreads, RPC == 1 ? 1 : 8)
     }
     long long at = -1;
     if (s >= 0 && back > 0) {  // not a row before the first sequence or behind the last
-      const int e = after_wait(a.lens)[s] - back;
+      const int e = max(after_wait(a.lens)[s], 0) - back;  // (of a negative length: below 0 as well)
       if (e >= 0) {
         if (e >> a.page_shift < a.cols) {
           const int page = after_wait(a.table)[static_cast<size_t>(s) * a.cols + (e >> a.page_shift)];
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4)
   if (h >= Hq) return;
   const int s = token / a.n_q, j = token - s * a.n_q, g = h / a.per;
   pdl_wait();
-  const int len = min(a.lens[s], a.cols << a.page_shift);
+  const int len = paged_len(a.lens[s], a.cols << a.page_shift);
   const int own_per = ws.head[0], own_t = ws.head[1 + a.G + s - ws.e0];
   JoinParts shared{nullptr, nullptr, 0, 0};
   if (a.G > 0) {

@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(32 * W, 8 / W)
   const bool in0 = gid < rows, in1 = gid + 8 < rows;
   mm_load_q<HD>(x, q_row(in0 ? r0 + gid : 0), q_row(in1 ? r0 + gid + 8 : 0), in0, in1);
   mm_clear<T, HD>(x);
-  const int own = max(0, min(a.lens[s], a.cols << a.page_shift) - (a.n_q - 1));
+  const int own = max(0, paged_len(a.lens[s], a.cols << a.page_shift) - (a.n_q - 1));
   const int32_t *shared_row = nullptr, *own_row = a.table + static_cast<size_t>(s) * a.cols;
   int shared = 0, per = 0;
   PagedGroup e{};

@@ -43,6 +43,10 @@ __device__ __forceinline__ PagedLive paged_live(const PagedArgs& a) {
   return PagedLive{paged_group_at(a, 0), paged_group_at(a, a.G)};
 }
 
+// `given` entries of a table row with `cap` of them: a negative length counts as 0 (and nothing
+// is taken off it that its type cannot hold)
+__device__ __forceinline__ int paged_len(int given, int cap) { return min(max(given, 0), cap); }
+
 struct PagedEntry {
   int keys, rows;  // keys of the entry, query rows per KV head
   int seq0;        // first sequence
@@ -60,7 +64,7 @@ __device__ __forceinline__ PagedEntry paged_entry(const PagedArgs& a, const Page
   PagedEntry x;
   x.seq0 = shared ? c0 : s;
   x.rows = (shared ? max(0, c1 - c0) : s >= live.lo && s < live.hi ? 1 : 0) * a.n_q * a.per;
-  x.keys = max(0, min(len, (shared ? a.pcols : a.cols) << a.page_shift) - (shared ? 0 : a.n_q - 1));
+  x.keys = max(0, paged_len(len, (shared ? a.pcols : a.cols) << a.page_shift) - (shared ? 0 : a.n_q - 1));
   return x;
 }
 // units of an entry for one tile of rows
@@ -221,7 +225,7 @@ __device__ __forceinline__ PagedGroup paged_group_of(const PagedArgs& a, int s, 
     r.t0 = __shfl_sync(0xffffffffu, pt, src);
   }
   if (s >= end) r.g = -1;
-  r.keys = min(max(len, 0), most);
+  r.keys = paged_len(len, most);
   r.beyond = len > most;
   return r;
 }
@@ -354,7 +358,7 @@ template <typename T, int HD, int R>
 __device__ __forceinline__ void paged_finish(const PagedArgs& a, int s, int g, PagedRows<HD, R>& x) {
   constexpr int DPL = HD / 32;
   auto ex2 = [](float v) { return sizeof(T) == 4 ? exp2f(v) : ex2_fast(v); };
-  const int lane = threadIdx.x & 31, cap = a.cols << a.page_shift, given = a.lens[s], len = min(given, cap);
+  const int lane = threadIdx.x & 31, cap = a.cols << a.page_shift, given = a.lens[s], len = paged_len(given, cap);
   if (lane == 0 && given > cap) atomicOr(a.status, kStatusBadIndex);
   size_t row[R];
 #pragma unroll

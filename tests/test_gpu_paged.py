@@ -354,6 +354,28 @@ def test_bad_pages_and_lengths_are_reported(zlib, cols):
         assert torch.equal(changed, want)
 
 
+@pytest.mark.parametrize("dtype,cols", [("bf16", 4), ("bf16", 100), ("bf16", 5000), ("f32", 4), ("f32", 100)])
+@pytest.mark.parametrize("n_q", [1, 4, 16])
+def test_negative_lengths_count_as_none(zlib, dtype, cols, n_q):
+    lens, plens = [-1, 40, -2 ** 31, 5, -2 ** 31 + n_q, -2 ** 31 + 15], [30, 0]
+    p, q, table, ptable = build(zlib, dtype, 40, 2, 64, 16, [max(n, 0) for n in lens], n_q, [0, 3, 6], plens)
+    table, ptable = widened(table, cols), widened(ptable, cols)
+    out, lse = attend(zlib, p, q, table, lens, [0, 3, 6], ptable, plens)
+    check(p, q, table, lens, out, lse, [0, 3, 6], ptable, plens)
+    out, lse = attend(zlib, p, q, table, lens)
+    check(p, q, table, lens, out, lse)
+    out, lse = attend(zlib, p, q, table, lens, [0, 3, 6], ptable, [-2 ** 31, -7])
+    check(p, q, table, lens, out, lse)  # (a prefix of a negative length is none)
+
+
+@pytest.mark.parametrize("rows,pad", [([1, 1, 1], 0), ([1, 1, 1], 1), ([3, 20, 1], 2)])
+def test_append_writes_nothing_for_negative_lengths(zlib, rows, pad):
+    p = Pool(zlib, "bf16", 2, 64, 16, 9)
+    table = [p.row(40, 3, fill=False) for _ in range(3)]
+    _, _, q_out = append_rows(zlib, p, table, [-1, -2 ** 31, -2 ** 31 + 7], rows, pad=pad)
+    assert (q_out == 7.0).all() and torch.isnan(p.k).all() and torch.isnan(p.v).all()
+
+
 @pytest.mark.parametrize("dtype,cols", [("bf16", 3), ("bf16", 100), ("bf16", 3000), ("f32", 3), ("f32", 100)])
 def test_group_bounds_that_run_backwards_stay_in_bounds(zlib, dtype, cols):
     p, q, table, ptable = build(zlib, dtype, 40, 2, 64, 16, [20] * 4, 1, [0, 4], [40, 40, 40])
