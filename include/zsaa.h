@@ -448,8 +448,8 @@ zsaa_status zsaa_op_colmass_ex(const void* qkv, const float* lse, int B, int N, 
  * page_size: 16, 32, 64, 128 or 256 entries.  head_dim 64 or 128 (bf16), 32, 64 or 128
  * (float32).  n_pages * n_kv_heads * page_size < 2^31.
  *
- * A table row lists a sequence's pages in order (device int32, `cols` to a row): entry
- * i lies in page row[i / page_size].  Entries of a row past the last page in use are
+ * A table row lists a sequence's pages in order (device int32, `cols` to a row, cols *
+ * page_size < 2^31): entry i lies in page row[i / page_size].  Entries of a row past the last page in use are
  * not read.  lens[s] counts the entries of sequence s, the ones that the current step
  * appends included; a negative one counts as 0.  A page number outside [0, n_pages) or a
  * length beyond the row (for zsaa_op_beam_reorder a negative one too) is reported by
@@ -512,7 +512,7 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  * short tables the prefix of a group is read once for all of its queries.  Results do not
  * depend on timing.  The lengths stay on the device, so a call is planned by the widths of
  * its tables, cols and prefix_cols: rows much wider than the lengths cost time.  At most
- * 65536 heads.  ws: 16-byte aligned, ws_bytes at least what
+ * 65536 heads, and 2^31 - 256 entries to a table row.  ws: 16-byte aligned, ws_bytes at least what
  * zsaa_op_paged_attention_workspace returns for these sizes (host only; prefix_cols is
  * ignored with G = 0). */
 zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,

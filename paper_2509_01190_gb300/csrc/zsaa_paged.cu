@@ -106,6 +106,9 @@ zsaa_status attention_sizes(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
   if (G < 0) return bad("G must be >= 0");
   ZTRY(check_cols(cols, kv->page_size));
   if (G > 0) ZTRY(check_cols(prefix_cols, kv->page_size));
+  // (the kernels round a row's entries up to blocks of keys, the largest of 128)
+  if (cols > (kMostInt - 255) / kv->page_size || (G > 0 && prefix_cols > (kMostInt - 255) / kv->page_size))
+    return bad("a table row of an attention call holds at most 2^31 - 256 entries");
   if (static_cast<long long>(S) * n_q > kMostInt / 32 / Hq || G > kMostInt / 2 - S)
     return bad("too many query rows or groups");
   *a = PagedArgs{};

@@ -106,6 +106,23 @@ def test_attention_workspace_needs_no_device_and_covers_smaller_calls(zlib):
     assert zlib.lib().zsaa_op_paged_attention_workspace(None, 1, 1, 1, 0, 1, 0, None) == zlib.ZSAA_ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_attention_refuses_rows_whose_blocks_pass_31_bits(zlib, page):
+    """Entries are walked in blocks of up to 128 keys, and the numbers of a row's last block
+    still have to fit an int32."""
+    kv = pages(zlib, page_size=page, n_kv_heads=1)
+    most = (2 ** 31 - 256) // page
+    for dtype in (zlib.ZSAA_BF16, zlib.ZSAA_F32):
+        kv.dtype = dtype
+        assert zlib.zsaa_op_paged_attention_workspace(kv, 1, 1, 1, 0, most, 0) > 0
+        assert zlib.zsaa_op_paged_attention_workspace(kv, 1, 1, 1, 1, 1, most) > 0
+        for cols in range(most + 1, (2 ** 31 - 1) // page + 2):
+            refused(zlib, lambda: zlib.zsaa_op_paged_attention_workspace(kv, 1, 1, 1, 0, cols, 0))
+            refused(zlib, lambda: zlib.zsaa_op_paged_attention_workspace(kv, 1, 1, 1, 1, 1, cols))
+            refused(zlib, lambda: attention(zlib, kv, cols=cols, Hq=1))
+            refused(zlib, lambda: attention(zlib, kv, pcols=cols, Hq=1))
+
+
 @pytest.mark.parametrize("kw", [
     dict(logits=None), dict(scores_out=None), dict(parent=None), dict(token=None), dict(ws=None), dict(B=0), dict(W=0),
     dict(W=65), dict(V=0), dict(V=(1 << 26) + 1, ld=1 << 27), dict(K=0), dict(K=65), dict(V=3, W=1, K=4, eos=1),
