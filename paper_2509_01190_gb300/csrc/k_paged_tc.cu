@@ -103,13 +103,16 @@ __global__ void __launch_bounds__(TC_THREADS, 2)
     prefetch_tmap(&tm_k);
     prefetch_tmap(&tm_v);
   }
+  // TMEM is taken between the wait and the trigger.  An allocation blocks: columns taken before
+  // the wait could be those that a CTA of the kernel before still waits for, and a kernel let
+  // in before the allocation could take those that this one's CTAs need, and then wait for them.
+  pdl_wait();
   if (warp == 1) tmem_alloc(tmem_slot, TC_TMEM_COLS);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_wait();
-  pdl_trigger();  // after the wait: a kernel that starts now may read what came before this one
+  pdl_trigger();
 
   __shared__ PagedSpan told;
   PagedSpan span;

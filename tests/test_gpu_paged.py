@@ -290,6 +290,51 @@ def test_attention_without_lse_on_another_stream_and_as_two_graphs(zlib, dtype, 
     check(p, q, table, [12, 1, 50], runs[0][1], runs[0][2], groups, ptable, plens)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+def test_128_row_tiles_between_other_tensor_core_kernels(zlib, hd):
+    """Projections and attention launched one behind the other, as a layer has them: each
+    kernel may start before the one ahead has ended, and all of them take tensor memory."""
+    lens, plens, groups, Hq, Hkv, d = [20] * 24, [2100, 1500], [0, 9, 24], 16, 2, 256
+    p, q, table, ptable = build(zlib, "bf16", Hq, Hkv, hd, 16, lens, 1, groups, plens)
+    table, ptable = widened(table, 4), widened(ptable, 4000)
+    want, want_lse = attend(zlib, p, q, table, lens, groups, ptable, plens)
+    check(p, q, table, lens, want, want_lse, groups, ptable, plens)
+    t, l, g, pt, pl = ints(table), ints(lens), ints(groups), ints(ptable), ints(plens)
+    W = (0.05 * torch.randn(d, Hq * hd, generator=p.g, device="cuda")).to(torch.bfloat16)
+    n = zlib.zsaa_op_paged_attention_workspace(p.pages, 24, 1, Hq, 2, 4, 4000)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    rows = q.view(24, -1)
+    before, after, other = (torch.empty(24, d, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    out = torch.empty_like(q)
+
+    def linear(x, y):
+        zlib.zsaa_op_linear(x, W, None, None, y, 24, d, Hq * hd, zlib.ZSAA_BF16, zlib.EPI_STORE)
+
+    def layer():
+        linear(rows, before)
+        zlib.zsaa_op_paged_attention(p.pages, q, 24, 1, Hq, t, 4, l, g, 2, pt, 4000, pl, out, None, ws, n)
+        linear(out.view(24, -1), after)
+
+    layer()
+    torch.cuda.synchronize()
+    linear(rows, other)
+    torch.cuda.synchronize()
+    assert torch.equal(before, other) and torch.equal(out, want)
+    linear(want.view(24, -1), other)
+    torch.cuda.synchronize()
+    assert torch.equal(after, other)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for _ in range(20):
+            layer()
+    for _ in range(10):
+        out.zero_()
+        after.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(after, other)
+
+
 def test_pages_beyond_32_bit_offsets(zlib):
     """The sequence's pages lie past element 2^31 of the pools."""
     page, Hkv, hd = 256, 8, 128
