@@ -513,9 +513,8 @@ def _at(t, dtype, n, name, dev):
 
 def _flags(t, n, name, dev):
     """_at for flags: uint8 or bool."""
-    if t is not None and not isinstance(t, int) and t.element_size() == 1 and not t.dtype.is_signed:
-        return _at(t, t.dtype, n, name, dev)
-    return _at(t, _types()[2], n, name, dev)
+    u8, flag = _types()[2], _types()[6]
+    return _at(t, flag if getattr(t, "dtype", u8) is flag else u8, n, name, dev)
 
 
 _TORCH = None
@@ -523,7 +522,7 @@ _TORCH = None
 
 def _types():
     """(float32, int32, uint8, bfloat16, the current device's number, the current
-    stream's handle by device number); torch is imported with the first call."""
+    stream's handle by device number, bool); torch is imported with the first call."""
     global _TORCH
     if _TORCH is None:
         import torch
@@ -534,7 +533,7 @@ def _types():
         # the same two in one call each, where torch has them
         device = getattr(torch._C, "_cuda_getDevice", device) if torch.cuda.is_available() else device
         stream = getattr(torch._C, "_cuda_getCurrentRawStream", stream) if torch.cuda.is_available() else stream
-        _TORCH = (torch.float32, torch.int32, torch.uint8, torch.bfloat16, device, stream)
+        _TORCH = (torch.float32, torch.int32, torch.uint8, torch.bfloat16, device, stream, torch.bool)
     return _TORCH
 
 
@@ -576,7 +575,7 @@ def _pools_here(kv, dev):
 
 def zsaa_op_paged_append(kv: zsaa_pages, qkv, ld: int, qkv_dtype: int, T: int, Hq: int, pos, rope_theta: float, cu_rows,
                          S: int, table, cols: int, lens, q_out=None, stream=None):
-    f32, i32, _, bf16, device, current = _types()
+    f32, i32, _, bf16, device, current, _ = _types()
     dev = device()
     _pools_here(kv, dev)
     hd = kv.head_dim
@@ -597,7 +596,7 @@ def zsaa_op_paged_attention_workspace(kv: zsaa_pages, S: int, n_q: int, Hq: int,
 
 def zsaa_op_paged_attention(kv: zsaa_pages, q, S: int, n_q: int, Hq: int, table, cols: int, lens, cu_seqs, G: int,
                             prefix_table, prefix_cols: int, prefix_lens, out, lse, ws, ws_bytes: int, stream=None):
-    f32, i32, u8, bf16, device, current = _types()
+    f32, i32, u8, bf16, device, current, _ = _types()
     dev = device()
     _pools_here(kv, dev)
     own, rows = bf16 if kv.dtype == ZSAA_BF16 else f32, S * n_q * Hq
@@ -623,7 +622,7 @@ def zsaa_op_beam_select_workspace(B: int, W: int, V: int, K: int) -> int:
 def zsaa_op_beam_select(logits, ld: int, B: int, W: int, V: int, scores, done, eos: int, K: int, scores_out, parent,
                         token, done_out, ws, ws_bytes: int, stream=None):
     """done, done_out: uint8 or bool."""
-    f32, i32, u8, _, device, current = _types()
+    f32, i32, u8, _, device, current, _ = _types()
     dev = device()
     n = B * K
     _check(lib().zsaa_op_beam_select(
@@ -636,7 +635,7 @@ def zsaa_op_beam_select(logits, ld: int, B: int, W: int, V: int, scores, done, e
 def zsaa_op_beam_reorder(layers, B: int, W: int, K: int, parent, table, table_out, cols: int, lens, lens_out, fresh,
                          stream=None):
     """layers: what make_pages_list returns (or a ctypes array of zsaa_pages)."""
-    _, i32, _, _, device, current = _types()
+    _, i32, _, _, device, current, _ = _types()
     dev = device()
     _pools_here(layers, dev)
     _check(lib().zsaa_op_beam_reorder(

@@ -168,6 +168,19 @@ def test_the_binding_refuses_tensors_of_another_kind(zlib):
     refused(zlib, lambda: zlib.make_pages_list([], []))
 
 
+@pytest.mark.parametrize("flags", [[0] * 8, np.zeros(8, np.uint8), np.zeros(8, bool), "01010101", (0, 1)])
+@pytest.mark.parametrize("name", ["done", "done_out"])
+def test_the_binding_refuses_flags_that_are_no_tensor(zlib, name, flags):
+    refused(zlib, lambda: select(zlib, **{name: flags}))
+
+
+@pytest.mark.parametrize("dtype", ["int8", "int32", "float32", "uint8", "bool"])
+def test_the_binding_refuses_flags_of_other_types_or_on_the_host(zlib, dtype):
+    import torch
+    for name in ("done", "done_out"):
+        refused(zlib, lambda: select(zlib, **{name: torch.zeros(8, dtype=getattr(torch, dtype))}))
+
+
 def test_plain_forms_agree_with_closed_ones():
     """The oracle itself: one key gives its value, equal keys the mean, a rotation keeps
     scores relative, and selection orders ties as stated."""
