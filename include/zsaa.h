@@ -438,8 +438,8 @@ zsaa_status zsaa_op_colmass_ex(const void* qkv, const float* lse, int B, int N, 
  *
  * A decode step of zsaa_decode_step keeps one cache per sequence.  These calls are
  * the steps of a generation in which several sequences continue one prompt (beams,
- * samples, drafted tokens): the prompt's entries are kept and read once, and each
- * sequence has pages of its own for what it adds.  The prompt may be pruned: entry i
+ * samples, drafted tokens): the prompt's entries are kept once and read for several
+ * sequences together, and each sequence has pages of its own for what it adds.  The prompt may be pruned: entry i
  * of a layer's cache need not be position i (Sec. 3.3 removes rows), so positions are
  * given apart from entries, and every layer has its own prefix lengths.
  *
@@ -508,13 +508,14 @@ zsaa_status zsaa_op_paged_append(const zsaa_pages* kv, const void* qkv, int64_t 
  * A query that sees no entry gets zeros and lse -inf.  Entries that a query does not
  * see never touch its result, whatever they hold.  (An entry that it sees and the query have
  * to be finite, in float32 below 2^127: an infinity among them can make its row NaN.  A NaN
- * does: in a query or a key the whole row, in a value its dim.)  But for
- * short tables the prefix of a group is read once for all of its queries.  Results do not
- * depend on timing.  The lengths stay on the device, so a call is planned by the widths of
- * its tables, cols and prefix_cols: rows much wider than the lengths cost time.  At most
- * 65536 heads, and 2^31 - 256 entries to a table row.  ws: 16-byte aligned, ws_bytes at least what
- * zsaa_op_paged_attention_workspace returns for these sizes (host only; prefix_cols is
- * ignored with G = 0). */
+ * does: in a query or a key the whole row, in a value its dim.)  The rows of a KV head that
+ * share a prefix (its group's queries times Hq / n_kv_heads) go through it 16 or 128 at a
+ * time, as a rule in L2 after the first; over short tables each sequence goes through it.
+ * Results do not depend on timing.  The lengths stay on the device, so a call is planned by
+ * the widths of its tables, cols and prefix_cols: rows much wider than the lengths cost time.
+ * At most 65536 heads, and 2^31 - 256 entries to a table row.  ws: 16-byte aligned, ws_bytes
+ * at least what zsaa_op_paged_attention_workspace returns for these sizes (host only;
+ * prefix_cols is ignored with G = 0). */
 zsaa_status zsaa_op_paged_attention_workspace(const zsaa_pages* kv, int S, int n_q, int Hq, int G,
                                               int cols, int prefix_cols, size_t* bytes);
 zsaa_status zsaa_op_paged_attention(const zsaa_pages* kv, const void* q, int S, int n_q, int Hq,

@@ -107,7 +107,7 @@ __device__ __forceinline__ uint64_t sum_against(uint64_t sum, float own, float t
 // ordered as -inf (their row's totals are all NaN).  Places before the row or past its end
 // hold -inf and come after every real one: as unsigned, their ~token is smaller.
 // Bound by its loads on large batches, and then by the end of the stretches: 192 beams of
-// 128256 logits in 24 us from HBM, 4.1 TB/s, 60% of the copy rate (29 with a bound and a list kept
+// 128256 logits in 25 us from HBM, 3.9 TB/s, 58% of the copy rate (29 with a bound and a list kept
 // up from step to step, whose barriers and rare branches then were most of the time).
 __global__ void __launch_bounds__(kScanThreads, 4)
     beam_scan_kernel(const float* __restrict__ logits, long long ld, int V, int K, int chunks, int tiles,
@@ -339,8 +339,8 @@ constexpr int kSumWarps = kMergeWarps / 2;
 
 // An element and another beam: up to so many such pairs are ranked by counting, more take a
 // merge of the beams' lists by one warp (us of 24 selections from 32000 logits a beam, counting
-// and merge: 8 beams with 8 tokens, 512 pairs, 11.7 and 12.7; with 16, 1024, 15.7 and 17.4; 16
-// beams with 16, 4096, 30.9 and 27.2).
+// and merge: 8 beams with 8 tokens, 512 pairs, 12.0 and 12.9; with 16, 1024, 15.8 and 17.6; 16
+// beams with 16, 4096, 31.3 and 27.4).
 constexpr int kRankPairs = 1024;
 
 // 8 bytes from device memory to this thread's place in shared memory
@@ -617,9 +617,9 @@ cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, 
                                cudaStream_t s) {
   // Long stretches save most of a stretch's fixed work, short ones keep the SMs even: one
   // round of the resident CTAs (four to an SM) while that is up to four steps each, else two.
-  // 128256 logits, us by steps: 64 beams (4 are one round) 18.4 with one, 14.3 with two,
-  // 13.9 with four, 15.5 with eight; 192 (11 and 6 steps) 28.4 with five, 27.6 with six, 29.0
-  // with 11; 256 (16 and 8) 30.7 with five, 31.1 with eight, 32.2 with 16.
+  // 128256 logits, us by steps: 64 beams (4 are one round) 18.1 with one, 14.5 with two,
+  // 13.3 with four, 15.0 with eight; 192 (11 and 6 steps) 28.0 with five, 27.6 with six, 28.9
+  // with 11; 256 (16 and 8) 31.6 with five, 31.7 with eight, 32.7 with 16.
   const int rows = B * W, total = beam_chunks_most(V);
   auto steps = [&](int rounds) {
     const int c = std::max(1, std::min(total, rounds * 4 * sms / rows));

@@ -7,8 +7,9 @@
 //
 // Attention: sequence s of group g has n_q new entries, its last; query j sees the
 // group's prefix and the sequence's entries i <= len - n_q + j.  Short tables take one launch
-// (k_paged_mma.cu).  Else the prefix is read once for all queries of the group (paged.cuh has
-// the decomposition), and the launch that joins adds the partial results.  The at most n_q - 1
+// (k_paged_mma.cu).  Else a prefix is read once for each tile of 16 or 128 of its group's query
+// rows, in L2 as a rule after the first (paged.cuh has the decomposition), and the launch that
+// joins adds the partial results.  The at most n_q - 1
 // entries that only some of the queries see are added at the end of a query row, one by one
 // and so without a mask: a value hidden from a query, finite or not, never enters its sums.
 #include <algorithm>
@@ -26,8 +27,9 @@ namespace {
 // and cosines (one set for all heads) go through shared memory.  A thread's first loads are
 // out before the sines and the lookup of the entries.
 // Angle: the position times the frequency in 2^-64 turns, modulo a turn, is one 64-bit
-// product: exact for every 32-bit position.  The nearest quarter turn is taken off
-// before the conversion to float, so sine and cosine are good to about 1e-7.
+// product, exact for every 32-bit position.  The nearest quarter turn is taken off
+// before the conversion to float, so sine and cosine are good to about 1e-7; to that the
+// frequency's own rounding to 53 bits adds 2^-53 of the angle, 2^-22 at the farthest positions.
 // Bound by bytes on prompts (8411 rows of 6144 bf16: 35 us, 5.8 TB/s; more units a thread in
 // flight cost occupancy and up to twice that), by the chain table -> address -> store on
 // single tokens (8 rows: 2.5 us).
@@ -266,7 +268,8 @@ struct Launches {
 };
 
 // The 128-row tiles take entries whose 16-row tiles would have more than `blocks` blocks of
-// 64 keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64, by the tables' sizes).
+// 64 keys to a CTA (304 CTAs with heads of 128 dims, 456 with 64: two and three to each of the
+// 152 SMs the rules were measured on; by the tables' sizes).
 // Up to 16 rows there is one 16-row tile and nothing to gain.  Six blocks where that saves
 // or costs no launch (us, 16-row and 128-row tiles, 8 heads of 128 dims): 24 sequences of 4
 // queries in 3 groups with 300 own entries, 512 keys 24 and 26, 1024 31 and 29, 2048 37 and 32,
@@ -290,10 +293,13 @@ bool many_rows(int hd, long long row_tiles, long long rows, long long keys, int 
 // 35, with 64 dims 28 and 33; of 1024 46 and 38.  A shared prefix is read again for every
 // sequence: 16 in 4 groups, 1024 keys 11 and 13, 2048 18 and 16; 64 in 8, 256 14 and 19, 512 21
 // and 18, 1024 34 and 24; 62 of 20 rows in 8, 512 45 and 45, 1024 73 and 53.
-// In float32: 4 sequences of 256 keys 10 and 12, 512 17 and 12, with 32 dims 7.3 and 8.6 and at
-// 1024 12 and 9.8; 16 of 1024 33 and 41; 64 of 1024 112 and 121, with 32 dims 43 and 41; 62 of 20
-// rows 208 and 238.  With groups: 16 in 4, 256 12 and 16, 512 19 and 18; 64 in 8, 128 23 and 26,
-// 256 36 and 26, with 32 dims 16 and 15, 25 and 17 at 512; 62 of 20 rows in 8, 256 74 and 88.
+// In float32: 4 sequences of 256 keys 9.5 and 12, 512 16 and 12, with 32 dims 4.9 and 8.0 and at
+// 1024 12 and 9.8; 16 of 1024 31 and 40; 64 of 1024 105 and 118, with 32 dims 49 and 40; 62 of 20
+// rows 213 and 232.  With groups: 16 in 4, 256 11 and 16, 512 17 and 18; 64 in 8, 128 18 and 26,
+// 256 30 and 26, with 32 dims 16 and 14, 27 and 17 at 512; 62 of 20 rows in 8, 256 68 and 86.
+// The rules are coarser than these figures and give some of them away: 4% at 64 sequences of
+// 2048 (split), 7% at 62 of 20 rows and 1024 keys (direct), and most, a fifth, at 64 float32
+// sequences of 1024 with 32 dims (direct).
 long long direct_ctas(const PagedArgs& a) {
   return static_cast<long long>(a.S) * a.Hkv * ((static_cast<long long>(a.n_q) * a.per + 15) / 16);
 }

@@ -23,7 +23,7 @@
 // output, in float32 additions.  (The sums of the other two, 2^-11 of those, run over all dims.)
 //
 // 48 sequences of 2000 to 4000 bf16 entries, 8 heads of 128 dims: 95 us for 576 MB, 90% of the
-// copy rate.  float32, 64 sequences of 2048: 214 us for 1.07 GB, 74%; with more rows than 16 to a
+// copy rate.  float32, 64 sequences of 2048: 216 us for 1.07 GB, 73%; with more rows than 16 to a
 // head it is bound by the chain of a warp's tile (96 products for 8 keys at 128 dims), 1 us
 // with two warps on an SM's quarter.
 #include <algorithm>
@@ -609,7 +609,7 @@ static cudaError_t run_direct(const PagedArgs& a, const PagedWork& w, cudaStream
 // Warps of a CTA: eight where CTAs of four would leave SMs empty, two where more than two of
 // four would be asked of an SM, so that one's start and end run under the others' loads (us,
 // four and two, 64 sequences, 8 heads of 128 dims: 32 keys 6.1 and 3.9, 256 17.0 and 14.4, 512
-// 27.3 and 24.7, float32 8.5 and 6.6, 35 and 32, 61 and 58; 64 dims 4.8 and 3.7, 8.3 and 8.8, 18
+// 27.3 and 24.7, float32 8.2 and 6.5, 34 and 31, 58 and 55; 64 dims 4.8 and 3.7, 8.3 and 8.8, 18
 // and 16; 62 of 5 queries, 256 keys 32 and 27, 64 dims 18 and 19; 30 of one 6.2 and 9.2).  Four
 // after partial results: with 600 own entries after 16000, 128 dims, 64 sequences 61 and 59, 30
 // 38 and 45; 24 of 4 drafts 22 and 28.
@@ -623,8 +623,9 @@ static cudaError_t run_direct(const PagedArgs& a, const PagedWork* w, cudaStream
 }
 
 // Lead: without, with 2 and with 8 units to an item (us): 60 sequences of 160 entries on 57
-// prefixes of 1700, 128 dims, 78, 64 and 67, float32 194, 153 and 176; 62 sequences of 5 queries
-// on one prefix of 1024, float32, 316, 158 and 186; 32 in 8 groups, prefix 1204, 20, 20 and 24.
+// prefixes of 850 to 1700, 128 dims, 79, 64 and 66, float32 189, 149 and 171; 62 sequences of 5
+// queries on one prefix of 1024, float32, 356, 174 and 209; 32 in 8 groups, prefix 1204, 20, 20
+// and 24.
 PagedTiles paged_mma_tiles(int dtype, int hd, int sms) {
   const bool bf = dtype == ZSAA_BF16;
   const int ctas = hd == 128 ? MmCfg<bf16, 128>::CTAS : hd == 64 ? MmCfg<bf16, 64>::CTAS : MmCfg<float, 32>::CTAS;

@@ -10,8 +10,11 @@
 //   O += P_hi V + P_lo V  (A = P from TMEM, B = V as it lies in its pages, MN-major)
 // While one CTA's softmax runs, the other's products do.  Tensor work for a block is
 // 1.0 us at the measured rate however few of the 128 rows are in use, its keys and values
-// (64 KB) take 1.4 us of an SM's share of HBM: up to 128 rows to a prefix the kernel is
-// bound by HBM, beyond by the tensor pipe, the tiles of a prefix sharing its keys in L2.
+// (64 KB) take 1.4 us of an SM's share of HBM, which the tiles of a prefix share in L2.  Beyond
+// 128 rows to a prefix neither is the bound: with 256 rows to a head and a prefix of 32000 (58
+// us) the tensor pipe is active for 38% of the cycles and HBM gives 2.3 TB/s, while the thread
+// that issues is busy for 83%: a switch between the operand forms of S (A from shared memory)
+// and of P V (A from TMEM) costs the pipe some 500 clocks.
 //
 // Roles (192 threads): warp 0 TMA producer (K and V in rings of their own, a lane per
 // page), warp 1 MMA issuer, warps 2-5 softmax, Q and results (warp w has TMEM lanes
