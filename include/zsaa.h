@@ -439,9 +439,13 @@ zsaa_status zsaa_op_colmass_ex(const void* qkv, const float* lse, int B, int N, 
  * A decode step of zsaa_decode_step keeps one cache per sequence.  These calls are
  * the steps of a generation in which several sequences continue one prompt (beams,
  * samples, drafted tokens): the prompt's entries are kept once and read for several
- * sequences together, and each sequence has pages of its own for what it adds.  The prompt may be pruned: entry i
- * of a layer's cache need not be position i (Sec. 3.3 removes rows), so positions are
- * given apart from entries, and every layer has its own prefix lengths.
+ * sequences together, and each sequence has pages of its own for what it adds.  The
+ * prompt may be pruned: entry i of a layer's cache need not be position i (Sec. 3.3
+ * removes rows), so positions are given apart from entries, and every layer has its own
+ * prefix lengths.  (No call moves a prompt that zsaa_prefill has put into a zsaa_cache: its
+ * keys are rotated already, and page i of a sequence is the slice [n_kv_heads, page_size,
+ * head_dim] from entry i page_size on of what zsaa_cache_layer points to, one 2-D copy each
+ * for k and v.)
  *
  * zsaa_pages: one layer's cache as a pool of pages (device memory of the caller's),
  * k and v each [n_pages, n_kv_heads, page_size, head_dim] of `dtype`, 16-byte aligned.

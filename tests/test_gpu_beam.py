@@ -235,6 +235,59 @@ def test_select_nan_ahead_of_equal_logits(zlib, K, V):
     check_select(zlib, np.ascontiguousarray(logits[:, :1]), None, None, -1, K)  # one beam fills the selection
 
 
+def test_select_takes_bool_flags(zlib):
+    logits, scores, r = draw(3, 4, 900, 31)
+    done = r.random((3, 4)) < 0.4
+    want = R.select(logits, scores, done, 2, 6)
+    n = zlib.zsaa_op_beam_select_workspace(3, 4, 900, 6)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    s_out, d_out = torch.empty(3, 6, device="cuda"), torch.empty(3, 6, dtype=torch.bool, device="cuda")
+    parent, token = (torch.empty(3, 6, dtype=torch.int32, device="cuda") for _ in range(2))
+    zlib.zsaa_op_beam_select(torch.from_numpy(logits).cuda(), 900, 3, 4, 900, torch.from_numpy(scores).cuda(),
+                             torch.from_numpy(done).cuda(), 2, 6, s_out, parent, token, d_out, ws, n)
+    for got, ref in zip((parent, token, d_out), want[1:4]):
+        np.testing.assert_array_equal(got.cpu().numpy(), ref)
+
+
+def test_append_and_reorder_in_a_graph(zlib):
+    """Captured calls read the lengths, pages and parents that are there at the replay."""
+    p = Pool(zlib, "bf16", 2, 64, 16, 12)
+    table = ints([p.row(40, 4, fill=False), p.row(40, 4, fill=False)])
+    fresh = ints([p.free.pop() for _ in range(2)])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    qkv = torch.randn(2, 8 * 64, generator=g, device="cuda").to(torch.bfloat16)
+    pos, lens, parent = ints([5, 9]), ints([3, 4]), ints([[0, 1]])
+    q, out, out_lens = torch.empty(2, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.empty_like(table), torch.empty_like(lens)
+    layers = (zlib.zsaa_pages * 1)(p.pages)
+
+    def step():
+        zlib.zsaa_op_paged_append(p.pages, qkv, 512, zlib.ZSAA_BF16, 2, 4, pos, 1e4, None, 2, table, 4, lens, q)
+        zlib.zsaa_op_beam_reorder(layers, 1, 2, 2, parent, table, out, 4, lens, out_lens, fresh)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    want = []
+    for replay in (False, True):
+        p.k.fill_(float("nan"))
+        p.v.fill_(float("nan"))
+        qkv.copy_(torch.arange(qkv.numel(), device="cuda").view_as(qkv) % 7 - 3)
+        pos.copy_(ints([100, 7]))
+        lens.copy_(ints([19, 32]))
+        parent.copy_(ints([[0, 0]]))
+        out.fill_(-9)
+        graph.replay() if replay else step()
+        torch.cuda.synchronize()
+        want.append([torch.nan_to_num(t.float(), nan=-77.0) for t in (p.k, p.v, q, out, out_lens)])
+    for a, b in zip(*want):
+        assert torch.equal(a, b)
+    assert out_lens.tolist() == [19, 19] and out[1, 1] == fresh[1] and out[0, 1] == table[0, 1]
+    assert torch.isfinite(p.v[table[0, 1], :, 2]).all() and torch.equal(p.v[table[0, 1], :, 2], p.v[fresh[1], :, 2])
+
+
 def test_select_in_a_graph(zlib):
     logits, scores, _ = draw(2, 4, 6000, 3)
     x, s = torch.from_numpy(logits).cuda(), torch.from_numpy(scores).cuda()
