@@ -573,6 +573,98 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
                                  int cols, const int32_t* lens, int32_t* lens_out,
                                  const int32_t* fresh, zsaa_stream stream);
 
+/* ---- Pages counted by reference, and drafted tokens.
+ *
+ * refs (device int32 [n_pages]) counts for every page of a pool how many table entries name
+ * it; a page with 0 is free, and there is no other list of free pages.  The caller sets refs
+ * to 0 (and to 1 or more for pages that it keeps for itself); the calls below keep it from
+ * then on, and with lengths and counts on the device a generation loop needs no host between
+ * its steps.  Every call takes the free pages of the lowest numbers, in the order of its rows
+ * and their columns, so results do not depend on timing.  Calls that share refs or tables are
+ * ordered by the caller (one stream, or events).  Tables, lengths, captures and page numbers
+ * or lengths out of range as above; at most 16384 rows to a call that takes pages, and
+ * fewer than 2^31 entries to a table.
+ *
+ * zsaa_op_paged_resize: S sequences from lens to want entries (negative: 0).  First every
+ * sequence that shrinks gives up the pages past ceil(want / page_size), then those that grow
+ * get pages, sequence by sequence, pages just given up among them.  Contents are not moved.
+ *   table   : int32 [S, cols], changed in place: entries of pages given up stay, unused
+ *   lens_out: int32 [S], the lengths reached: want, or what the pages suffice for where
+ *             they run out (no error: lens_out < want tells).  Must not overlap lens or want
+ *   n_free  : int32 [1], the free pages left, or NULL
+ * want = 0 ends a sequence.  A page given up that nothing refers to is reported as a page
+ * number out of range is.  page_size as zsaa_pages', n_pages <= 2^30. */
+zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int S, int32_t* table, int cols,
+                                 const int32_t* lens, const int32_t* want, int32_t* lens_out, int32_t* n_free,
+                                 zsaa_stream stream);
+
+/* zsaa_op_paged_fork: N new sequences that continue others.  Child i takes the first
+ * m = min(at[i], lens[p]) entries of sequence p = parent[i] (at NULL: all; negative: 0): it
+ * shares the m / page_size whole pages (their refs go up), and of a partly filled page it
+ * gets the entries copied, in every layer, into a page of its own that the call takes.
+ *   layers : HOST array of n_layers pools (1..64) of the same sizes and dtype; one table
+ *            serves them all
+ *   table, lens: int32 [S, cols] and [S]
+ *   parent : int32 [N] in [0, S), or -1 for no child (its lens_out is 0);  at: int32 [N] or NULL
+ *   table_out, lens_out: int32 [N, cols] and [N], overwritten: rows that held pages give them
+ *            up first (zsaa_op_paged_resize to 0).  Must not overlap the inputs; entries of
+ *            table_out past a child's last page stay as they were
+ *   n_free : as above
+ * Where pages run out a child keeps its whole pages: lens_out = m / page_size * page_size. */
+zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* refs, int S, const int32_t* table, int cols,
+                               const int32_t* lens, int N, const int32_t* parent, const int32_t* at, int32_t* table_out,
+                               int32_t* lens_out, int32_t* n_free, zsaa_stream stream);
+
+/* zsaa_op_paged_compact: chosen entries of each sequence moved together, in every layer: a
+ * cache pruned after the prompt (keep from zsaa_score_select), or the accepted path of a tree
+ * of drafts.  Entry start[s] + j of the result is entry keep[s, j]; entries below start[s] are
+ * not touched.
+ *   keep   : int32 [S, keep_cols], row s has n_keep[s] entries, strictly ascending, in
+ *            [start[s], lens[s]);  n_keep: int32 [S];  start: int32 [S] or NULL (0)
+ *   table, lens: int32 [S, cols] and [S], the entries as they are
+ *   table_out: int32 [S, out_cols], the pages that the result is written to (not changed):
+ *            `table` itself for a move in place, or another.  A page that is written may be
+ *            in use for nothing else but the same column of the same sequence's row of table
+ *   refs   : the pool's counts or NULL; with them a page that is to be written and does not
+ *            have a count of 1 is reported as a page number out of range is, and not written
+ *   lens_out: int32 [S], start + n_keep.  Must not overlap lens, start or n_keep
+ * Pages past lens_out are given up by zsaa_op_paged_resize.  An entry out of range or not
+ * above the one before it is reported, and not moved. */
+zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const int32_t* refs, int S, const int32_t* table,
+                                  int cols, const int32_t* lens, const int32_t* start, const int32_t* keep, int keep_cols,
+                                  const int32_t* n_keep, const int32_t* table_out, int out_cols, int32_t* lens_out,
+                                  zsaa_stream stream);
+
+/* zsaa_op_draft_verify: which of n drafted tokens stand against the target's probabilities,
+ * and the token that follows them.  With p_j and q_j the softmax of target row j and draft row
+ * j over the temperature, draft x_j stands where all before it do and u_j q_j(x_j) < p_j(x_j).
+ * At a refused draft the next token is drawn from max(p_j - q_j, 0), behind the last draft from
+ * p: the first token t whose running sum over tokens 0..t exceeds u_n times the whole sum.  So
+ * tokens are distributed as the target's.  n = 0 draws one token from the target.
+ *   target   : [S, n+1, ld] logits of `dtype` (ZSAA_F32 or ZSAA_BF16; any alignment of the
+ *              type), ld >= V (not read past V), V <= 2^26;  0 <= n <= 15
+ *   draft    : [S, n, draft_ld], or NULL: drafts without probabilities (looked up; q_j is 1 at x_j)
+ *   drafts   : int32 [S, n]; a sequence's drafts end before the first that is no token (a -1)
+ *              or whose draft row has no distribution
+ *   temperature: float32 [S] or NULL (1).  0, and what is below 2^-64: all probability on
+ *              the first of the largest logits, draft rows not read.  At most 2^64
+ *   uniform  : float32 [S, n+1] in [0, 1), u_0 .. u_n (a NaN counts as 0, others as the nearest)
+ *   accepted : int32 [S], how many drafts stand
+ *   tokens   : int32 [S, n+1], those drafts, the next token, then -1 (must not overlap drafts)
+ *   logp     : float32 [S, n+1] or NULL, log p_j of each token of `tokens`, 0 where there is none
+ *   lens, lens_out: int32 [S], both or neither: lens - (n - accepted), not below 0: the entries
+ *              that remain of a cache to which a token and n drafts were appended.  lens_out
+ *              may be lens
+ * A row has no distribution where it holds a NaN or +inf or nothing above -inf, or its
+ * temperature is negative, NaN or above 2^64.  A target row without one ends the sequence's
+ * tokens: the next one is -1.  Sums that a token is picked by are good to about 2^-36.  ws:
+ * 16-byte aligned, of at least the bytes that zsaa_op_draft_verify_workspace returns (host only). */
+zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes);
+zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* draft, int64_t draft_ld, int dtype, int S, int n,
+                                 int V, const int32_t* drafts, const float* temperature, const float* uniform,
+                                 int32_t* accepted, int32_t* tokens, float* logp, const int32_t* lens, int32_t* lens_out,
+                                 void* ws, size_t ws_bytes, zsaa_stream stream);
+
 /* Per-kernel timing of the forward pass.  After zsaa_trace_begin every
  * kernel the model launches is bracketed by CUDA events recorded on the launch
  * stream (this adds a small gap between launches, so traced forwards are not

@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(kMergeThreads)
 // with the parent's first child, and a later child gets its entries copied into its
 // own fresh page.
 struct ReorderArgs {
-  void* pool[2 * kReorderMaxLayers];  // K and V of each layer
+  PoolList pools;
   const int32_t *parent, *table, *lens, *fresh;
   int32_t *table_out, *lens_out;
   int W, K, cols, n_pages, page_shift, Hkv, row_vecs;  // row_vecs: 16-byte vectors of one entry of one head
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(256) beam_reorder_kernel(const __grid_constant
   }
   if (!copy || bad) return;
   const int n = part * a.row_vecs, stride = a.row_vecs << a.page_shift;  // vectors to copy, and of a page, per head
-  uint4* pool = static_cast<uint4*>(a.pool[blockIdx.y]);
+  uint4* pool = static_cast<uint4*>(a.pools.p[blockIdx.y]);
   const uint4* s = pool + static_cast<size_t>(from) * a.Hkv * stride;
   uint4* d = pool + static_cast<size_t>(to) * a.Hkv * stride;
   for (int h = 0; h < a.Hkv; ++h)
@@ -640,21 +640,18 @@ cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, 
   return cudaSuccess;
 }
 
-cudaError_t launch_beam_reorder(const void* const* k, const void* const* v, int n_layers, int n_pages, int page_shift,
-                                int Hkv, int entry_bytes, int B, int W, int K, const int32_t* parent,
-                                const int32_t* table, int32_t* table_out, int cols, const int32_t* lens,
-                                int32_t* lens_out, const int32_t* fresh, int* status, cudaStream_t s) {
+cudaError_t launch_beam_reorder(const PoolList& pools, int n_pages, int page_shift, int Hkv, int entry_bytes, int B,
+                                int W, int K, const int32_t* parent, const int32_t* table, int32_t* table_out,
+                                int cols, const int32_t* lens, int32_t* lens_out, const int32_t* fresh, int* status,
+                                cudaStream_t s) {
   ReorderArgs a{};
-  for (int l = 0; l < n_layers; ++l) {
-    a.pool[2 * l] = const_cast<void*>(k[l]);
-    a.pool[2 * l + 1] = const_cast<void*>(v[l]);
-  }
+  a.pools = pools;
   a.parent = parent, a.table = table, a.lens = lens, a.fresh = fresh;
   a.table_out = table_out, a.lens_out = lens_out;
   a.W = W, a.K = K, a.cols = cols, a.n_pages = n_pages, a.page_shift = page_shift, a.Hkv = Hkv;
   a.row_vecs = entry_bytes / 16;
   a.status = status;
-  ZSAA_LAUNCH(beam_reorder_kernel, dim3(B * K, 2 * n_layers), dim3(256), 0, s, a);
+  ZSAA_LAUNCH(beam_reorder_kernel, dim3(B * K, pools.n), dim3(256), 0, s, a);
   return cudaSuccess;
 }
 

@@ -65,6 +65,10 @@ cudaError_t launch_paged_attention(const PagedArgs& a, int dtype, int hd, void* 
 // ---- beam search (k_beam.cu)
 constexpr int kBeamMaxBeams = 64, kBeamMaxKept = 64, kBeamMaxVocab = 1 << 26;
 constexpr int kReorderMaxLayers = 64;
+struct PoolList {
+  void* p[2 * kReorderMaxLayers];  // k and v of each layer
+  int n;
+};
 struct BeamChunk {
   unsigned long long sum;  // sum of exp(x - top) in units of 2^-36
   float top;               // the maximum
@@ -76,10 +80,58 @@ cudaError_t launch_beam_select(const float* logits, long long ld, int B, int W, 
                                const uint8_t* done, int eos, int K, float* scores_out, int32_t* parent,
                                int32_t* token, uint8_t* done_out, BeamChunk* stat, uint2* cand, int sms,
                                cudaStream_t s);
-cudaError_t launch_beam_reorder(const void* const* k, const void* const* v, int n_layers, int n_pages, int page_shift,
-                                int Hkv, int entry_bytes, int B, int W, int K, const int32_t* parent,
-                                const int32_t* table, int32_t* table_out, int cols, const int32_t* lens,
-                                int32_t* lens_out, const int32_t* fresh, int* status, cudaStream_t s);
+cudaError_t launch_beam_reorder(const PoolList& pools, int n_pages, int page_shift, int Hkv, int entry_bytes, int B,
+                                int W, int K, const int32_t* parent, const int32_t* table, int32_t* table_out,
+                                int cols, const int32_t* lens, int32_t* lens_out, const int32_t* fresh, int* status,
+                                cudaStream_t s);
+
+// ---- pages counted by reference (k_pages.cu)
+constexpr int kPagesMaxRows = 16384;  // rows of a table whose pages one call takes
+// A call that takes free pages for the rows of a table: resize (parent null), or fork.
+struct PagesArgs {
+  int32_t* refs;         // [n_pages], 0: free
+  const int32_t *table;  // resize: the table itself; fork: the parents'
+  int32_t *table_out;    // resize: the same
+  const int32_t *lens, *want;   // want: resize alone
+  const int32_t *parent, *at;   // fork alone; at or null
+  int32_t *lens_out, *n_free;   // n_free or null
+  int rows, cols, n_pages, page_shift;
+  int parents;  // fork: rows of `table`
+  int* status;
+};
+cudaError_t launch_paged_resize(const PagesArgs& a, cudaStream_t s);
+// row_vecs: 16-byte vectors of one entry of one head
+cudaError_t launch_paged_fork(const PagesArgs& a, const PoolList& pools, int Hkv, int row_vecs, cudaStream_t s);
+struct CompactArgs {
+  const int32_t *table, *lens, *start, *keep, *n_keep;  // start or null
+  const int32_t *table_out, *refs;                      // refs or null
+  int32_t* lens_out;
+  int S, cols, out_cols, keep_cols, n_pages, page_shift, Hkv, row_vecs;
+  int* status;
+};
+cudaError_t launch_paged_compact(const CompactArgs& a, const PoolList& pools, cudaStream_t s);
+
+// ---- verification of drafted tokens (k_verify.cu)
+constexpr int kVerifyMaxDrafts = 15, kVerifyMaxVocab = 1 << 26;
+struct VerifyChunk {
+  double sum;  // sum of exp((x - top) / T)
+  float top;   // the maximum
+  int first;   // its first place (where a temperature of 0 asks for it)
+  int bad;     // a NaN or +inf among the logits
+  int pad;
+};
+struct VerifyArgs {
+  const void *target, *draft;  // draft or null
+  long long ld, draft_ld;
+  int S, n, V, chunks;
+  const int32_t *drafts, *lens;             // lens or null
+  const float *temperature, *uniform;       // temperature or null
+  int32_t *accepted, *tokens, *lens_out;    // lens_out or null
+  float* logp;                              // or null
+  VerifyChunk* stat;                        // [S][n + 1 target rows, n draft rows][chunks]
+};
+int verify_chunks(int V);
+cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, cudaStream_t s);
 
 // ---- status word of the calls without a model (zsaa_api.cu): the current device's, or null
 int* shared_status_word();

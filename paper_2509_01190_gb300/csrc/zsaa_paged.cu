@@ -1,4 +1,4 @@
-// C ABI of the paged-cache and beam-search calls: argument checks and launches.
+// C ABI of the paged-cache, beam-search and draft-verification calls: argument checks and launches.
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -48,6 +48,7 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
 }
 
 constexpr long long kMostInt = 0x7fffffff;
+constexpr int kMostPages = 1 << 30;
 
 size_t element(int dtype) { return dtype == ZSAA_BF16 ? 2 : 4; }
 
@@ -137,6 +138,43 @@ zsaa_status select_sizes(int B, int W, int V, int K, size_t* stat, size_t* cand)
   if (static_cast<long long>(B) * W > kMostInt / 64 / chunks) return bad("B*W*V too large");
   *stat = (static_cast<size_t>(B) * W * chunks * sizeof(BeamChunk) + 255) & ~static_cast<size_t>(255);
   *cand = static_cast<size_t>(B) * W * chunks * K * sizeof(uint2);
+  return ZSAA_OK;
+}
+
+// the layers' pools of a call that moves entries in all of them
+zsaa_status check_layers(const zsaa_pages* layers, int n_layers, PoolList* pools) {
+  if (layers == nullptr) return bad("null layers");
+  if (n_layers < 1 || n_layers > kReorderMaxLayers) return refuse(ZSAA_ERR_INVALID_ARG, "n_layers=%d outside [1, 64]", n_layers);
+  for (int l = 0; l < n_layers; ++l) {
+    const zsaa_pages& p = layers[l];
+    ZTRY(check_pages(&p));
+    ZTRY(check_pool(&p));
+    if (p.n_pages != layers[0].n_pages || p.page_size != layers[0].page_size || p.n_kv_heads != layers[0].n_kv_heads ||
+        p.head_dim != layers[0].head_dim || p.dtype != layers[0].dtype)
+      return bad("the layers' pools must have the same sizes and dtype");
+    pools->p[2 * l] = p.k;
+    pools->p[2 * l + 1] = p.v;
+  }
+  pools->n = 2 * n_layers;
+  return ZSAA_OK;
+}
+
+// rows of a table whose pages a call takes
+zsaa_status check_taking(int rows, int cols, int page) {
+  if (rows < 1) return bad("a table needs 1 or more rows");
+  if (rows > kPagesMaxRows) return refuse(ZSAA_ERR_UNSUPPORTED, "%d rows of pages, the most are %d", rows, kPagesMaxRows);
+  ZTRY(check_cols(cols, page));
+  if (static_cast<long long>(rows) * cols > kMostInt) return bad("a table must have fewer than 2^31 entries");
+  return ZSAA_OK;
+}
+
+zsaa_status verify_sizes(int S, int n, int V, size_t* bytes) {
+  if (S < 1 || V < 1) return bad("S and V must be >= 1");
+  if (n < 0 || n > kVerifyMaxDrafts) return refuse(ZSAA_ERR_UNSUPPORTED, "n=%d drafts outside [0, %d]", n, kVerifyMaxDrafts);
+  if (V > kVerifyMaxVocab) return bad("V must be at most 2^26");
+  const long long items = static_cast<long long>(2 * n + 1) * verify_chunks(V);
+  if (S > kMostInt / 16 / items) return bad("S*n*V too large");
+  *bytes = static_cast<size_t>(S) * items * sizeof(VerifyChunk);
   return ZSAA_OK;
 }
 
@@ -258,18 +296,8 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
       lens_out == nullptr || fresh == nullptr)
     return bad("null argument");
   if (!words(parent, table, table_out, lens, lens_out, fresh)) return bad("int32 arrays must be 4-byte aligned");
-  if (n_layers < 1 || n_layers > kReorderMaxLayers) return refuse(ZSAA_ERR_INVALID_ARG, "n_layers=%d outside [1, 64]", n_layers);
-  const void *k[kReorderMaxLayers], *v[kReorderMaxLayers];
-  for (int l = 0; l < n_layers; ++l) {
-    const zsaa_pages& p = layers[l];
-    ZTRY(check_pages(&p));
-    ZTRY(check_pool(&p));
-    if (p.n_pages != layers[0].n_pages || p.page_size != layers[0].page_size || p.n_kv_heads != layers[0].n_kv_heads ||
-        p.head_dim != layers[0].head_dim || p.dtype != layers[0].dtype)
-      return bad("the layers' pools must have the same sizes and dtype");
-    k[l] = p.k;
-    v[l] = p.v;
-  }
+  PoolList pools{};
+  ZTRY(check_layers(layers, n_layers, &pools));
   if (B < 1) return bad("B must be >= 1");
   if (W < 1 || W > kBeamMaxBeams || K < 1 || K > kBeamMaxKept)
     return refuse(ZSAA_ERR_INVALID_ARG, "W=%d or K=%d outside [1, 64]", W, K);
@@ -282,10 +310,123 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
   int* status = nullptr;
   ZTRY(status_word(&status));
   return launched("zsaa_op_beam_reorder",
-                  launch_beam_reorder(k, v, n_layers, p.n_pages, page_shift(p.page_size), p.n_kv_heads,
+                  launch_beam_reorder(pools, p.n_pages, page_shift(p.page_size), p.n_kv_heads,
                                       static_cast<int>(p.head_dim * element(p.dtype)), B, W, K, parent, table,
                                       table_out, cols, lens, lens_out, fresh, status,
                                       reinterpret_cast<cudaStream_t>(stream)));
+}
+
+zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int S, int32_t* table, int cols,
+                                 const int32_t* lens, const int32_t* want, int32_t* lens_out, int32_t* n_free,
+                                 zsaa_stream stream) {
+  if (refs == nullptr || table == nullptr || lens == nullptr || want == nullptr || lens_out == nullptr)
+    return bad("null argument");
+  if (!words(refs, table, lens, want, lens_out, n_free)) return bad("int32 arrays must be 4-byte aligned");
+  if (n_pages < 1 || n_pages > kMostPages) return bad("n_pages must be in [1, 2^30]");
+  if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0)
+    return refuse(ZSAA_ERR_UNSUPPORTED, "page_size %d is not 16, 32, 64, 128 or 256", page_size);
+  ZTRY(check_taking(S, cols, page_size));
+  const size_t row = 4 * static_cast<size_t>(S);
+  if (overlap(lens, row, lens_out, row) || overlap(want, row, lens_out, row))
+    return bad("lens_out overlaps lens or want");
+  PagesArgs a{};
+  ZTRY(status_word(&a.status));
+  a.refs = refs, a.table = a.table_out = table, a.lens = lens, a.want = want, a.lens_out = lens_out, a.n_free = n_free;
+  a.rows = S, a.cols = cols, a.n_pages = n_pages, a.page_shift = page_shift(page_size);
+  return launched("zsaa_op_paged_resize", launch_paged_resize(a, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* refs, int S, const int32_t* table, int cols,
+                               const int32_t* lens, int N, const int32_t* parent, const int32_t* at, int32_t* table_out,
+                               int32_t* lens_out, int32_t* n_free, zsaa_stream stream) {
+  PoolList pools{};
+  ZTRY(check_layers(layers, n_layers, &pools));
+  if (refs == nullptr || table == nullptr || lens == nullptr || parent == nullptr || table_out == nullptr ||
+      lens_out == nullptr)
+    return bad("null argument");
+  if (!words(refs, table, lens, parent, at, table_out, lens_out, n_free)) return bad("int32 arrays must be 4-byte aligned");
+  const zsaa_pages& p = layers[0];
+  if (S < 1) return bad("S must be >= 1");
+  ZTRY(check_taking(N, cols, p.page_size));
+  if (static_cast<long long>(S) * cols > kMostInt) return bad("a table must have fewer than 2^31 entries");
+  const size_t in = 4 * static_cast<size_t>(S), out = 4 * static_cast<size_t>(N);
+  if (overlap(table, in * cols, table_out, out * cols)) return bad("table_out overlaps table");
+  if (overlap(lens, in, lens_out, out) || overlap(parent, out, lens_out, out) || (at != nullptr && overlap(at, out, lens_out, out)))
+    return bad("lens_out overlaps lens, parent or at");
+  PagesArgs a{};
+  ZTRY(status_word(&a.status));
+  a.refs = refs, a.table = table, a.table_out = table_out, a.lens = lens, a.parent = parent, a.at = at;
+  a.lens_out = lens_out, a.n_free = n_free;
+  a.rows = N, a.cols = cols, a.n_pages = p.n_pages, a.page_shift = page_shift(p.page_size), a.parents = S;
+  return launched("zsaa_op_paged_fork",
+                  launch_paged_fork(a, pools, p.n_kv_heads, static_cast<int>(p.head_dim * element(p.dtype) / 16),
+                                    reinterpret_cast<cudaStream_t>(stream)));
+}
+
+zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const int32_t* refs, int S, const int32_t* table,
+                                  int cols, const int32_t* lens, const int32_t* start, const int32_t* keep, int keep_cols,
+                                  const int32_t* n_keep, const int32_t* table_out, int out_cols, int32_t* lens_out,
+                                  zsaa_stream stream) {
+  PoolList pools{};
+  ZTRY(check_layers(layers, n_layers, &pools));
+  if (table == nullptr || lens == nullptr || keep == nullptr || n_keep == nullptr || table_out == nullptr ||
+      lens_out == nullptr)
+    return bad("null argument");
+  if (!words(refs, table, lens, start, keep, n_keep, table_out, lens_out)) return bad("int32 arrays must be 4-byte aligned");
+  const zsaa_pages& p = layers[0];
+  if (S < 1 || keep_cols < 1) return bad("S and keep_cols must be >= 1");
+  if (p.n_kv_heads > 65535) return bad("more than 65535 KV heads");  // (a grid's third dimension)
+  ZTRY(check_cols(cols, p.page_size));
+  ZTRY(check_cols(out_cols, p.page_size));
+  const size_t row = 4 * static_cast<size_t>(S);
+  if (overlap(lens, row, lens_out, row) || overlap(n_keep, row, lens_out, row) ||
+      (start != nullptr && overlap(start, row, lens_out, row)))
+    return bad("lens_out overlaps lens, start or n_keep");
+  CompactArgs a{};
+  ZTRY(status_word(&a.status));
+  a.table = table, a.lens = lens, a.start = start, a.keep = keep, a.n_keep = n_keep, a.table_out = table_out, a.refs = refs;
+  a.lens_out = lens_out;
+  a.S = S, a.cols = cols, a.out_cols = out_cols, a.keep_cols = keep_cols, a.n_pages = p.n_pages;
+  a.page_shift = page_shift(p.page_size), a.Hkv = p.n_kv_heads;
+  a.row_vecs = static_cast<int>(p.head_dim * element(p.dtype) / 16);
+  return launched("zsaa_op_paged_compact", launch_paged_compact(a, pools, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes) {
+  if (bytes == nullptr) return bad("null bytes");
+  *bytes = 0;
+  return verify_sizes(S, n, V, bytes);
+}
+
+zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* draft, int64_t draft_ld, int dtype, int S, int n,
+                                 int V, const int32_t* drafts, const float* temperature, const float* uniform,
+                                 int32_t* accepted, int32_t* tokens, float* logp, const int32_t* lens, int32_t* lens_out,
+                                 void* ws, size_t ws_bytes, zsaa_stream stream) {
+  size_t need = 0;
+  ZTRY(verify_sizes(S, n, V, &need));
+  if (dtype != ZSAA_F32 && dtype != ZSAA_BF16) return bad("bad dtype");
+  if (n == 0) drafts = nullptr, draft = nullptr;
+  if (target == nullptr || (n > 0 && drafts == nullptr) || uniform == nullptr || accepted == nullptr || tokens == nullptr ||
+      ws == nullptr)
+    return bad("null argument");
+  if ((lens == nullptr) != (lens_out == nullptr)) return bad("lens and lens_out: both or neither");
+  if (ld < V || ld > (1LL << 40)) return bad("ld is shorter than V");
+  if (draft != nullptr && (draft_ld < V || draft_ld > (1LL << 40))) return bad("draft_ld is shorter than V");
+  if (!aligned(target, element(dtype)) || !aligned(draft, element(dtype))) return bad("logits must be aligned to their type");
+  if (!words(drafts, temperature, uniform, accepted, tokens, logp, lens, lens_out))
+    return bad("int32 and float32 arrays must be 4-byte aligned");
+  if (!aligned(ws, 16)) return bad("ws must be 16-byte aligned");
+  if (ws_bytes < need) return refuse(ZSAA_ERR_INVALID_ARG, "ws_bytes %zu, needs %zu", ws_bytes, need);
+  const size_t row = 4 * static_cast<size_t>(S);
+  if (drafts != nullptr && overlap(drafts, row * n, tokens, row * (n + 1))) return bad("tokens overlap drafts");
+  if (lens != nullptr && lens != lens_out && overlap(lens, row, lens_out, row)) return bad("lens_out overlaps lens");
+  VerifyArgs a{};
+  a.target = target, a.draft = draft, a.ld = ld, a.draft_ld = draft_ld;
+  a.S = S, a.n = n, a.V = V, a.chunks = verify_chunks(V);
+  a.drafts = drafts, a.lens = lens, a.temperature = temperature, a.uniform = uniform;
+  a.accepted = accepted, a.tokens = tokens, a.lens_out = lens_out, a.logp = logp;
+  a.stat = static_cast<VerifyChunk*>(ws);
+  return launched("zsaa_op_draft_verify", launch_draft_verify(a, dtype, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -33,6 +33,8 @@ EXPORTED = [
     "zsaa_forward_varlen", "zsaa_forward_masked", "zsaa_forward_marked", "zsaa_selftest_wait_timeout",
     "zsaa_gemm_schedule", "zsaa_op_paged_append", "zsaa_op_paged_attention_workspace",
     "zsaa_op_paged_attention", "zsaa_op_beam_select_workspace", "zsaa_op_beam_select", "zsaa_op_beam_reorder",
+    "zsaa_op_paged_resize", "zsaa_op_paged_fork", "zsaa_op_paged_compact", "zsaa_op_draft_verify_workspace",
+    "zsaa_op_draft_verify",
 ]
 
 
@@ -131,6 +133,12 @@ def lib():
             "zsaa_op_beam_select_workspace": ([_I, _I, _I, _I, C.POINTER(C.c_size_t)], _I),
             "zsaa_op_beam_select": ([_P, C.c_int64, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, C.c_size_t, _P], _I),
             "zsaa_op_beam_reorder": ([_P, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _P, _P], _I),
+            "zsaa_op_paged_resize": ([_P, _I, _I, _I, _P, _I, _P, _P, _P, _P, _P], _I),
+            "zsaa_op_paged_fork": ([_P, _I, _P, _I, _P, _I, _P, _I, _P, _P, _P, _P, _P, _P], _I),
+            "zsaa_op_paged_compact": ([_P, _I, _P, _I, _P, _I, _P, _P, _P, _I, _P, _P, _I, _P, _P], _I),
+            "zsaa_op_draft_verify_workspace": ([_I, _I, _I, C.POINTER(C.c_size_t)], _I),
+            "zsaa_op_draft_verify": ([_P, C.c_int64, _P, C.c_int64, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                      C.c_size_t, _P], _I),
         }
         for name, (args, res) in sig.items():
             f = getattr(L, name)
@@ -556,7 +564,7 @@ def make_pages(k, v) -> zsaa_pages:
 
 
 def make_pages_list(ks, vs):
-    """Array of zsaa_pages, one per layer, for zsaa_op_beam_reorder."""
+    """Array of zsaa_pages, one per layer, for the calls that move entries in all of them."""
     pages = [make_pages(k, v) for k, v in zip(ks, vs)]
     if not pages or len(ks) != len(vs):
         raise ZsaaError(ZSAA_ERR_INVALID_ARG, "one key and one value pool for each layer")
@@ -643,6 +651,64 @@ def zsaa_op_beam_reorder(layers, B: int, W: int, K: int, parent, table, table_ou
         _at(table, i32, B * W * cols, "table", dev), _at(table_out, i32, B * K * cols, "table_out", dev), cols,
         _at(lens, i32, B * W, "lens", dev), _at(lens_out, i32, B * K, "lens_out", dev),
         _at(fresh, i32, B * K, "fresh", dev), _here(stream, dev, current)))
+
+
+def zsaa_op_paged_resize(refs, n_pages: int, page_size: int, S: int, table, cols: int, lens, want, lens_out, n_free=None,
+                         stream=None):
+    _, i32, _, _, device, current, _ = _types()
+    dev = device()
+    _check(lib().zsaa_op_paged_resize(
+        _at(refs, i32, n_pages, "refs", dev), n_pages, page_size, S, _at(table, i32, S * cols, "table", dev), cols,
+        _at(lens, i32, S, "lens", dev), _at(want, i32, S, "want", dev), _at(lens_out, i32, S, "lens_out", dev),
+        _at(n_free, i32, 1, "n_free", dev), _here(stream, dev, current)))
+
+
+def zsaa_op_paged_fork(layers, refs, S: int, table, cols: int, lens, N: int, parent, at, table_out, lens_out, n_free=None,
+                       stream=None):
+    """layers: what make_pages_list returns (or a ctypes array of zsaa_pages)."""
+    _, i32, _, _, device, current, _ = _types()
+    dev = device()
+    _pools_here(layers, dev)
+    _check(lib().zsaa_op_paged_fork(
+        C.addressof(layers), len(layers), _at(refs, i32, layers[0].n_pages, "refs", dev), S,
+        _at(table, i32, S * cols, "table", dev), cols, _at(lens, i32, S, "lens", dev), N, _at(parent, i32, N, "parent", dev),
+        _at(at, i32, N, "at", dev), _at(table_out, i32, N * cols, "table_out", dev), _at(lens_out, i32, N, "lens_out", dev),
+        _at(n_free, i32, 1, "n_free", dev), _here(stream, dev, current)))
+
+
+def zsaa_op_paged_compact(layers, refs, S: int, table, cols: int, lens, start, keep, keep_cols: int, n_keep, table_out,
+                          out_cols: int, lens_out, stream=None):
+    """layers: what make_pages_list returns (or a ctypes array of zsaa_pages)."""
+    _, i32, _, _, device, current, _ = _types()
+    dev = device()
+    _pools_here(layers, dev)
+    _check(lib().zsaa_op_paged_compact(
+        C.addressof(layers), len(layers), _at(refs, i32, layers[0].n_pages, "refs", dev), S,
+        _at(table, i32, S * cols, "table", dev), cols, _at(lens, i32, S, "lens", dev), _at(start, i32, S, "start", dev),
+        _at(keep, i32, S * keep_cols, "keep", dev), keep_cols, _at(n_keep, i32, S, "n_keep", dev),
+        _at(table_out, i32, S * out_cols, "table_out", dev), out_cols, _at(lens_out, i32, S, "lens_out", dev),
+        _here(stream, dev, current)))
+
+
+def zsaa_op_draft_verify_workspace(S: int, n: int, V: int) -> int:
+    b = C.c_size_t()
+    _check(lib().zsaa_op_draft_verify_workspace(S, n, V, C.byref(b)))
+    return b.value
+
+
+def zsaa_op_draft_verify(target, ld: int, draft, draft_ld: int, dtype: int, S: int, n: int, V: int, drafts, temperature,
+                         uniform, accepted, tokens, logp, lens, lens_out, ws, ws_bytes: int, stream=None):
+    f32, i32, u8, bf16, device, current, _ = _types()
+    dev = device()
+    kind, rows = bf16 if dtype == ZSAA_BF16 else f32, S * (n + 1)
+    if n == 0:
+        draft = drafts = None
+    _check(lib().zsaa_op_draft_verify(
+        _at(target, kind, (rows - 1) * ld + V, "target", dev), ld, _at(draft, kind, (S * n - 1) * draft_ld + V, "draft", dev),
+        draft_ld, dtype, S, n, V, _at(drafts, i32, S * n, "drafts", dev), _at(temperature, f32, S, "temperature", dev),
+        _at(uniform, f32, rows, "uniform", dev), _at(accepted, i32, S, "accepted", dev), _at(tokens, i32, rows, "tokens", dev),
+        _at(logp, f32, rows, "logp", dev), _at(lens, i32, S, "lens", dev), _at(lens_out, i32, S, "lens_out", dev),
+        _at(ws, u8, ws_bytes, "ws", dev), ws_bytes, _here(stream, dev, current)))
 
 
 def zsaa_device_status():
