@@ -9,13 +9,21 @@
 //
 //   verify_scan_kernel    one stretch of one row per CTA: its maximum and the sum of its
 //                         exponentials.  Bound by the logits' bytes.
-//   verify_sample_kernel  one cluster per sequence: which drafts stand, then the token.
+//   verify_finish_kernel  which drafts stand; then the rows at which a sequence stops again, a
+//                         slice per CTA, and its last CTA finds the token.
 //
 // What decides a draft is one comparison of two quotients, off by about 1e-8 with sums of
 // float32 exponentials.  What decides a token is where u_n falls among V borders, some 1e-5
 // apart and closer: a running sum that is off by 1e-9 picks the wrong token every few thousand
 // calls.  So the rows at which a sequence stops are gone through again with exponentials as
 // pairs of floats, good to about 2^-37, and sums in pairs and in 64 bits.
+//
+// One pass does it, although the residual needs the sums of both rows: with E the exponentials,
+// Z their exact sums and c0 the quotient Z_p / Z_q as the scan has it, the pass adds up
+//   D_i = E_p,i - c0 E_q,i        over all tokens, and
+//   A = sum D_i, B = sum E_q,i    over a group's tokens with D_i > 0.
+// The exact quotient is c0 + k with k = sum D / Z_q, some 2^-24 of it, so a group's residual is
+// A - k B; tokens whose D_i changes its sign with k are off by 2^-24 of a 2^-24th of them.
 #include <algorithm>
 #include <cmath>
 
@@ -42,6 +50,8 @@ __device__ __forceinline__ Temperature temperature_of(const VerifyArgs& a, int s
   const float t = after_wait(a.temperature)[s];
   return Temperature{t, t >= 0.f && t < kMinTemperature, !(t >= 0.f && t <= kMaxTemperature)};
 }
+
+__device__ __forceinline__ float log2e_over(float t) { return 1.44269504088896340736f / t; }
 
 // drafts of sequence s before the first that is no token
 // (whole warps)
@@ -73,11 +83,22 @@ __device__ __forceinline__ const T* row_of(const VerifyArgs& a, int s, int r) {
   return after_wait(static_cast<const T*>(a.draft)) + (static_cast<long long>(s) * a.n + (r - a.n - 1)) * a.draft_ld;
 }
 
+// (64-bit floats are left out of both kernels: the SM does two of their operations a clock.)
+constexpr float kSumScale = 0x1p36f;  // a stretch's sum, at most 2^13, in units of 2^-36
+
+// Sum over the warp of values in [0, 2^50) (two 32-bit reductions of 25 bits each).
+__device__ __forceinline__ unsigned long long warp_sum_u50(unsigned long long v) {
+  const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & 0x1ffffffu);
+  const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 25));
+  return (static_cast<unsigned long long>(hi) << 25) + lo;
+}
+
+// Every warp takes its sum against its own maximum, so the warps meet once, at the end.
 template <typename T>
 __global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __grid_constant__ VerifyArgs a, int rows) {
   constexpr int VEC = 16 / sizeof(T), VECS = kScanValues / VEC;
   __shared__ float s_top[kScanThreads / 32];
-  __shared__ double s_sum[kScanThreads / 32];
+  __shared__ unsigned long long s_sum[kScanThreads / 32];
   __shared__ int s_first[kScanThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -85,6 +106,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __gr
   const unsigned item = blockIdx.x / static_cast<unsigned>(a.chunks);
   const int chunk = static_cast<int>(blockIdx.x - item * a.chunks);
   const int s = static_cast<int>(item / static_cast<unsigned>(rows)), r = static_cast<int>(item - s * static_cast<unsigned>(rows));
+  if (r == 0 && chunk == 0 && tid == 0) a.done[s] = 0;
   const Temperature t = temperature_of(a, s);
   const bool is_draft = r > a.n;
   if (t.bad || (t.greedy && is_draft)) return;  // rows that decide nothing
@@ -116,11 +138,8 @@ __global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __gr
     bad |= !(x[k] < INFINITY);
   }
   top = warp_max(top);
-  if (lane == 0) s_top[warp] = top;
-  bad = __syncthreads_or(bad) != 0;
-#pragma unroll
-  for (int w = 0; w < kScanThreads / 32; ++w) top = fmaxf(top, s_top[w]);
-  double total = 0.0;
+  const float c = log2e_over(t.t);
+  unsigned long long total = 0;
   int first = a.V;
   if (t.greedy) {
 #pragma unroll
@@ -130,28 +149,26 @@ __global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __gr
     }
     first = __reduce_min_sync(0xffffffffu, first);
   } else {
-    const float c = static_cast<float>(1.4426950408889634 / static_cast<double>(t.t));
     const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kScanValues; ++k) sum += ex2((x[k] - ref) * c);
-    total = sum;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    for (int k = 0; k < kScanValues; ++k) sum[k & 3] += ex2((x[k] - ref) * c);
+    // (bad rows have any sum)
+    total = warp_sum_u50(static_cast<unsigned long long>(fminf((sum[0] + sum[1]) + (sum[2] + sum[3]), 64.f) * kSumScale));
   }
-  if (lane == 0) s_sum[warp] = total, s_first[warp] = first;
-  __syncthreads();
-  if (tid == 0) {
-    VerifyChunk out{};
-#pragma unroll
-    for (int w = 0; w < kScanThreads / 32; ++w) {
-      out.sum += s_sum[w];
-      first = min(first, s_first[w]);
-    }
-    out.top = top;
-    out.first = first;
-    out.bad = bad;
-    a.stat[(static_cast<size_t>(s) * rows + r) * a.chunks + chunk] = out;
+  if (lane == 0) s_top[warp] = top, s_sum[warp] = total, s_first[warp] = first;
+  bad = __syncthreads_or(bad) != 0;
+  if (warp == 0) {
+    const bool in = lane < kScanThreads / 32;
+    top = in ? s_top[lane] : -INFINITY;
+    const float all = warp_max(top);
+    total = in && top > -INFINITY ? static_cast<unsigned long long>(static_cast<float>(s_sum[lane]) * ex2((top - all) * c)) : 0;
+    VerifyChunk out;
+    out.sum = static_cast<long long>(warp_sum_u50(total));
+    out.top = all;
+    out.first = __reduce_min_sync(0xffffffffu, in && top == all ? s_first[lane] : a.V);
+    if (bad) out.first = -1;
+    if (lane == 0) a.stat[(static_cast<size_t>(s) * rows + r) * a.chunks + chunk] = out;
   }
 }
 
@@ -169,9 +186,10 @@ struct MassRow {
   float m, ch, cl;  // the row's maximum; log2(e) / T
 };
 __device__ __forceinline__ MassRow mass_row(float m, float t) {
-  const double c = 1.4426950408889634074 / static_cast<double>(t);
-  const float ch = static_cast<float>(c);
-  return MassRow{m, ch, static_cast<float>(c - static_cast<double>(ch))};
+  constexpr float kLog2eH = 1.44269502162933349609375f;
+  constexpr float kLog2eL = static_cast<float>(1.4426950408889634074 - static_cast<double>(kLog2eH));
+  const float ch = kLog2eH / t;
+  return MassRow{m, ch, (fmaf(-ch, t, kLog2eH) + kLog2eL) / t};
 }
 __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* table_h, const float* table_l) {
   constexpr float kLn2H = 0.693147182464599609375f;  // ln 2 rounded to float, and what that leaves
@@ -195,15 +213,41 @@ __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* tab
   return y > -125.f ? Pair{h * scale, l * scale} : Pair{0.f, 0.f};
 }
 
-// running sums of pairs
+// arithmetic of pairs (products whose rounding is kept are not fused into what follows)
 __device__ __forceinline__ void add(Pair& s, float h, float l) {
   const float t = s.h + h, b = t - s.h;
   s.l += ((s.h - (t - b)) + (h - b)) + l;
   s.h = t;
 }
-__device__ __forceinline__ double value(const Pair& s) { return static_cast<double>(s.h) + static_cast<double>(s.l); }
-
-__device__ __forceinline__ double warp_sum64(double v) {
+__device__ __forceinline__ Pair mul(const Pair& a, const Pair& b) {
+  const float h = __fmul_rn(a.h, b.h);
+  return Pair{h, fmaf(a.h, b.h, -h) + fmaf(a.h, b.l, a.l * b.h)};
+}
+__device__ __forceinline__ Pair sub(const Pair& a, const Pair& b) {
+  const float h = a.h - b.h, c = h - a.h;
+  return Pair{h, ((a.h - (h - c)) + (-b.h - c)) + (a.l - b.l)};
+}
+__device__ __forceinline__ Pair div(const Pair& a, const Pair& b) {
+  const float h = a.h / b.h;
+  return Pair{h, (fmaf(-h, b.h, a.h) + fmaf(-h, b.l, a.l)) / b.h};
+}
+__device__ __forceinline__ Pair warp_sum_pair(Pair v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float h = __shfl_xor_sync(0xffffffffu, v.h, o), l = __shfl_xor_sync(0xffffffffu, v.l, o);
+    add(v, h, l);
+  }
+  return v;
+}
+__device__ __forceinline__ Pair pair_of(long long v, float unit) {
+  const float h = __ll2float_rn(v);
+  return Pair{h * unit, __ll2float_rn(v - __float2ll_rn(h)) * unit};
+}
+// in units of 1 / scale
+__device__ __forceinline__ long long fixed(const Pair& v, float scale) {
+  return __float2ll_rn(v.h * scale) + __float2ll_rn(v.l * scale);
+}
+__device__ __forceinline__ long long warp_sum_ll(long long v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
@@ -211,101 +255,143 @@ __device__ __forceinline__ double warp_sum64(double v) {
 
 // ---------------------------------------------------------------- decisions and the token
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleCtas = 8;
-constexpr int kGroups = 4;  // a warp's tokens in so many groups, each with its sum
-constexpr int kSums = kSampleCtas * kSampleWarps * kGroups;
+constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
+constexpr int kGroupLeast = 128, kGroupMost = 1024;  // tokens of a warp, whose sums are kept
 
 enum { kFromTarget = 0, kWithout = 1, kResidual = 2 };  // r = p; p without token x; max(p - q, 0)
 
 struct RowStat {
-  double sum;
+  Pair sum;
   float top;
   int first;
   int ok;  // the row has a distribution
 };
 
-__device__ __forceinline__ void st_cluster_f64(uint32_t saddr, uint32_t rank, double v) {
-  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(map_rank(saddr, rank)), "d"(v) : "memory");
+// u q(x) < p(x) from the logits alone, where the exponentials are too small for float pairs
+__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const RowStat& p, const RowStat& q) {
+  auto log_of = [t](float x, const RowStat& r) {
+    return (static_cast<double>(x) - static_cast<double>(r.top)) / t - log(static_cast<double>(r.sum.h) + static_cast<double>(r.sum.l));
+  };
+  const double lp = log_of(xp, p), lq = log_of(xq, q);
+  return lp > -INFINITY && (lq == -INFINITY || u < exp(lp - lq));
+}
+
+__device__ __forceinline__ VerifyGroup load_group(const VerifyGroup* p) {
+  const longlong2 x = __ldcg(reinterpret_cast<const longlong2*>(p));
+  VerifyGroup g;
+  g.a = x.x;
+  g.d = x.y;
+  g.b = __ldcg(&p->b);
+  return g;
+}
+
+// floor(u total), u in [0, 1)
+__device__ __forceinline__ long long goal_of(float u, long long total) {
+  int e;
+  const float m = frexpf(u, &e);  // u = m 2^e, m 2^24 a whole number
+  const unsigned __int128 v = static_cast<unsigned __int128>(static_cast<unsigned>(m * 0x1p24f)) * static_cast<unsigned long long>(total);
+  return 24 - e > 127 ? 0 : static_cast<long long>(v >> (24 - e));
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads, 1) verify_sample_kernel(const __grid_constant__ VerifyArgs a, int rows) {
+__global__ void __launch_bounds__(kFinishThreads, 4)
+    verify_finish_kernel(const __grid_constant__ VerifyArgs a, int rows, int ctas, int group, float unit) {
   __shared__ float table_h[32], table_l[32];
   __shared__ RowStat stat[2 * kVerifyMaxDrafts + 1];
   __shared__ int s_stands[kVerifyMaxDrafts + 1];
-  __shared__ double part[2][kSampleWarps];
-  __shared__ double norm[2][kSampleCtas];
-  __shared__ double sums[2][kSums];
-  __shared__ int s_segment;
-  __shared__ double s_before;
+  __shared__ long long s_part[kFinishWarps], s_before;
+  __shared__ int s_first[kFinishWarps], s_some[kFinishWarps], s_group, s_last;
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int ctas = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
-  const int s = static_cast<int>(blockIdx.x) / ctas;
+  const int s = static_cast<int>(blockIdx.x) / ctas, cta = static_cast<int>(blockIdx.x) - s * ctas;
   if (tid < 32) {
     const double e = exp2(tid / 32.0);
     table_h[tid] = static_cast<float>(e);
     table_l[tid] = static_cast<float>(e - static_cast<double>(table_h[tid]));
   }
-  cluster_sync_all();  // every CTA of the cluster runs before another writes into it
+  __syncthreads();
   pdl_wait();
   const Temperature t = temperature_of(a, s);
   const int n = drafts_of(a, s);
-  const bool lookup = a.draft == nullptr;
-  const VerifyChunk* chunks = after_wait(a.stat) + static_cast<size_t>(s) * rows * a.chunks;
-  const double inv_t = t.greedy || t.bad ? 1.0 : 1.0 / static_cast<double>(t.t);
+  const bool lookup = a.draft == nullptr, soft = !t.greedy && !t.bad;
+  const int4* chunks = after_wait(reinterpret_cast<const int4*>(a.stat)) + static_cast<size_t>(s) * rows * a.chunks;
+  auto chunk_at = [&](int r, int i) {
+    const int4 v = chunks[static_cast<size_t>(r) * a.chunks + i];
+    VerifyChunk c;
+    c.sum = static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(v.y)) << 32 | static_cast<unsigned>(v.x));
+    c.top = __int_as_float(v.z);
+    c.first = v.w;
+    return c;
+  };
 
   // every row that may decide something: its maximum and its sum
-  for (int r = warp; r < rows; r += kSampleWarps) {
+  for (int r = warp; r < rows; r += kFinishWarps) {
     const bool is_draft = r > a.n;
-    RowStat out{0.0, -INFINITY, a.V, 0};
+    RowStat out{{0.f, 0.f}, -INFINITY, a.V, 0};
     if (!t.bad && (is_draft ? !t.greedy && r - a.n - 1 < n : r <= n)) {
-      const VerifyChunk* c = chunks + static_cast<size_t>(r) * a.chunks;
-      int bad = 0;
+      bool bad = false;
       for (int i = lane; i < a.chunks; i += 32) {
-        out.top = fmaxf(out.top, c[i].top);
-        bad |= c[i].bad;
+        const VerifyChunk c = chunk_at(r, i);
+        out.top = fmaxf(out.top, c.top);
+        bad |= c.first < 0;
       }
       out.top = warp_max(out.top);
-      double sum = 0.0;
-      for (int i = lane; i < a.chunks; i += 32) {
-        if (c[i].top == -INFINITY) continue;
-        if (t.greedy) {
-          if (c[i].top == out.top) out.first = min(out.first, c[i].first);
-        } else {
-          sum += c[i].sum * exp((static_cast<double>(c[i].top) - static_cast<double>(out.top)) * inv_t);
+      if (soft) {
+        const MassRow m = mass_row(out.top, t.t);
+        for (int i = lane; i < a.chunks; i += 32) {
+          const VerifyChunk c = chunk_at(r, i);
+          const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, m, table_h, table_l));
+          if (c.top > -INFINITY) add(out.sum, v.h, v.l);
         }
+        out.sum = warp_sum_pair(out.sum);
+      } else {
+        for (int i = lane; i < a.chunks; i += 32) {
+          const VerifyChunk c = chunk_at(r, i);
+          if (c.top == out.top) out.first = min(out.first, c.first);
+        }
+        out.first = __reduce_min_sync(0xffffffffu, out.first);
       }
-      out.sum = warp_sum64(sum);
-      out.first = __reduce_min_sync(0xffffffffu, out.first);
-      out.ok = __reduce_or_sync(0xffffffffu, bad) == 0 && out.top > -INFINITY;
+      out.ok = !__any_sync(0xffffffffu, bad) && out.top > -INFINITY;
     }
     if (lane == 0) stat[r] = out;
   }
   __syncthreads();
-  auto log_p = [&](int r, int x) {  // of token x in row r, natural
-    const double d = static_cast<double>(to_f<T>(row_of<T>(a, s, r)[x])) - static_cast<double>(stat[r].top);
-    return d * inv_t - log(stat[r].sum);
+  auto logit = [&](int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); };
+  // log p of a token of row r with the logit x: (x - top) / t - log(sum), the rounding errors of
+  // each kept: log(sum) = g + log(sum exp(-g)) with g near it, and the latter is its argument less 1
+  auto log_p = [&](int r, float x) {
+    const RowStat& row = stat[r];
+    const float g = logf(row.sum.h);
+    const Pair e = mul(row.sum, mass(-g, mass_row(0.f, 1.f), table_h, table_l));
+    const float d = x - row.top, b = d - x, de = (x - (d - b)) + (-row.top - b);
+    const float h = d / t.t, l = (fmaf(-h, t.t, d) + de) / t.t;
+    const Pair z = sub(Pair{h, l}, Pair{g, (e.h - 1.f) + e.l});
+    return h > -INFINITY ? z.h + z.l : h;
   };
   const int32_t* drafts = after_wait(a.drafts) + static_cast<size_t>(s) * a.n;
   const float* uniform = after_wait(a.uniform) + static_cast<size_t>(s) * (a.n + 1);
   // numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
-  auto number = [&](int j) { return static_cast<double>(fminf(fmaxf(uniform[j], 0.f), 0x1.fffffep-1f)); };
+  auto number = [&](int j) { return fminf(fmaxf(uniform[j], 0.f), 0x1.fffffep-1f); };
   enum { kStands, kRefused, kNoDraft, kNoTarget };
   if (tid <= a.n) {
     int what = kNoDraft;
-    if (!stat[tid].ok && tid <= n) {
+    const RowStat p = stat[tid];
+    if (!p.ok && tid <= n) {
       what = kNoTarget;
     } else if (tid < n) {
       const int x = drafts[tid];
       if (t.greedy) {
-        what = stat[tid].first == x ? kStands : kRefused;
-      } else if (lookup) {
-        what = number(tid) < exp(log_p(tid, x)) ? kStands : kRefused;
-      } else if (stat[a.n + 1 + tid].ok) {
-        const double lq = log_p(a.n + 1 + tid, x), lp = log_p(tid, x);
-        // (q(x) = 0: it stands where p(x) > 0)
-        what = lp > -INFINITY && (lq == -INFINITY || number(tid) < exp(lp - lq)) ? kStands : kRefused;
+        what = p.first == x ? kStands : kRefused;
+      } else {
+        // u q(x) < p(x); where q(x) = 0: 0 < p(x)
+        const RowStat q = lookup ? RowStat{{1.f, 0.f}, 0.f, 0, 1} : stat[a.n + 1 + tid];
+        if (q.ok) {
+          const float xp = logit(tid, x), xq = lookup ? q.top : logit(a.n + 1 + tid, x), u = number(tid);
+          const Pair ep = mass(xp, mass_row(p.top, t.t), table_h, table_l), eq = mass(xq, mass_row(q.top, t.t), table_h, table_l);
+          const Pair z = sub(mul(Pair{u, 0.f}, mul(eq, p.sum)), mul(ep, q.sum));
+          const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && u > 0x1p-30f;
+          what = (near ? z.h + z.l < 0.f : stands_far(u, xp, xq, t.t, p, q)) ? kStands : kRefused;
+        }
       }
     }
     s_stands[tid] = what;
@@ -316,10 +402,10 @@ __global__ void __launch_bounds__(kSampleThreads, 1) verify_sample_kernel(const 
   const int why = s_stands[stop];
   int32_t* tokens = a.tokens + static_cast<size_t>(s) * (a.n + 1);
   float* logp = a.logp != nullptr ? a.logp + static_cast<size_t>(s) * (a.n + 1) : nullptr;
-  if (rank == 0) {
+  if (cta == 0) {
     if (tid <= a.n && tid != stop) {
       tokens[tid] = tid < stop ? drafts[tid] : -1;
-      if (logp != nullptr) logp[tid] = tid < stop && !t.greedy ? static_cast<float>(log_p(tid, drafts[tid])) : 0.f;
+      if (logp != nullptr) logp[tid] = tid < stop && soft ? log_p(tid, logit(tid, drafts[tid])) : 0.f;
     }
     if (tid == 0) {
       a.accepted[s] = stop;
@@ -330,157 +416,188 @@ __global__ void __launch_bounds__(kSampleThreads, 1) verify_sample_kernel(const 
       }
     }
   }
-  if (why == kNoTarget || t.greedy) return;  // (the same for the whole cluster)
+  if (why == kNoTarget || t.greedy) return;  // (the same for all CTAs of the sequence)
 
+  const int kind = why == kNoDraft ? kFromTarget : lookup ? kWithout : kResidual;
   const T* row_p = row_of<T>(a, s, stop);
-  int kind = why == kNoDraft ? kFromTarget : lookup ? kWithout : kResidual;
   const T* row_q = kind == kResidual ? row_of<T>(a, s, a.n + 1 + stop) : row_p;
   const int refused = kind == kFromTarget ? -1 : drafts[stop];
   const MassRow mp = mass_row(stat[stop].top, t.t);
   const MassRow mq = kind == kResidual ? mass_row(stat[a.n + 1 + stop].top, t.t) : mp;
-  // tokens of a warp: kGroups groups of `group`, a multiple of 32
-  const int warps = ctas * kSampleWarps, gw = rank * kSampleWarps + warp;
-  const int group = ((a.V + warps * kGroups - 1) / (warps * kGroups) + 31) & ~31;
-  const long long w0 = static_cast<long long>(gw) * kGroups * group;
-
-  Pair ratio{0.f, 0.f};  // sum_p / sum_q
-  if (kind == kResidual) {
-    Pair sp{0.f, 0.f}, sq{0.f, 0.f};
-#pragma unroll 2
-    for (int i = lane; i < kGroups * group; i += 32) {
-      if (w0 + i >= a.V) break;
-      const Pair p = mass(to_f<T>(row_p[w0 + i]), mp, table_h, table_l), q = mass(to_f<T>(row_q[w0 + i]), mq, table_h, table_l);
-      add(sp, p.h, p.l);
-      add(sq, q.h, q.l);
-    }
-    const double p = warp_sum64(value(sp)), q = warp_sum64(value(sq));
-    if (lane == 0) part[0][warp] = p, part[1][warp] = q;
-    __syncthreads();
-    if (tid < 2) {
-      double v = 0.0;
-      for (int w = 0; w < kSampleWarps; ++w) v += part[tid][w];
-      for (int r = 0; r < ctas; ++r) st_cluster_f64(smem_u32(&norm[tid][rank]), r, v);
-    }
-    cluster_sync_all();
-    double np = 0.0, nq = 0.0;
-    for (int r = 0; r < ctas; ++r) np += norm[0][r], nq += norm[1][r];
-    const double x = np / nq;
-    ratio.h = static_cast<float>(x);
-    ratio.l = static_cast<float>(x - static_cast<double>(ratio.h));
-  }
-
-  // r of a token, times the sum of p's exponentials
-  auto left = [&](long long i) {
-    const Pair p = mass(to_f<T>(row_p[i]), mp, table_h, table_l);
-    if (kind == kFromTarget) return p;
-    if (kind == kWithout) return i == refused ? Pair{0.f, 0.f} : p;
-    const Pair q = mass(to_f<T>(row_q[i]), mq, table_h, table_l);
-    const float qh = __fmul_rn(q.h, ratio.h), ql = fmaf(q.h, ratio.h, -qh) + fmaf(q.h, ratio.l, q.l * ratio.h);
-    const float h = p.h - qh, b = h - p.h;
-    const float l = ((p.h - (h - b)) + (-qh - b)) + (p.l - ql);
-    return h + l > 0.f ? Pair{h, l} : Pair{0.f, 0.f};
+  const Pair ratio = kind == kResidual ? div(stat[stop].sum, stat[a.n + 1 + stop].sum) : Pair{0.f, 0.f};
+  // D of a token and its E_q; without a draft row p's exponential
+  auto left = [&](float xp, float xq, int at, float& eq) {
+    const Pair p = mass(xp, mp, table_h, table_l);
+    eq = 0.f;
+    if (kind != kResidual) return at == refused ? Pair{0.f, 0.f} : p;
+    const Pair q = mass(xq, mq, table_h, table_l);
+    eq = q.h;
+    return sub(p, mul(q, ratio));
   };
-  int turn = 0;
-  double total = 0.0;
-  for (;;) {
-    for (int g = 0; g < kGroups; ++g) {
-      Pair sum{0.f, 0.f};
-      for (int i = lane; i < group; i += 32) {
-        const long long at = w0 + static_cast<long long>(g) * group + i;
-        if (at >= a.V) break;
-        const Pair r = left(at);
-        add(sum, r.h, r.l);
-      }
-      const double v = warp_sum64(value(sum));
-      if (lane < ctas) st_cluster_f64(smem_u32(&sums[turn][gw * kGroups + g]), lane, v);
-    }
-    cluster_sync_all();
-    total = 0.0;
-    if (warp == 0) {  // running sums, a lane per stretch of them
-      const int all = warps * kGroups, each = all / 32;
-      double mine = 0.0;
-      for (int i = 0; i < each; ++i) mine += sums[turn][lane * each + i];
-      double run = mine;
+
+  // this CTA's slice, a group of tokens per warp
+  const int groups = ctas * kFinishWarps;
+  VerifyGroup* sums = a.groups + static_cast<size_t>(s) * groups;
+  {
+    const long long g0 = (static_cast<long long>(cta) * kFinishWarps + warp) * group;
+    Pair plus{0.f, 0.f}, all{0.f, 0.f};
+    float b = 0.f;
+    for (int i0 = 0; i0 < group; i0 += 128) {
+      float xp[4], xq[4];
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double x = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += x;
+      for (int k = 0; k < 4; ++k) {
+        const long long at = g0 + i0 + 32 * k + lane;
+        xp[k] = at < a.V ? to_f<T>(row_p[at]) : -INFINITY;
+        xq[k] = kind == kResidual && at < a.V ? to_f<T>(row_q[at]) : -INFINITY;
       }
-      total = __shfl_sync(0xffffffffu, run, 31);
-      const double goal = number(a.n) * total;
-      const unsigned above = __ballot_sync(0xffffffffu, run > goal);
-      const int who = above != 0 ? __ffs(above) - 1 : 31;
-      if (lane == who) {
-        // (its own sums may round otherwise than the running one: then its last with any)
-        double before = run - mine;
-        int at = -1;
-        double at_before = before;
-        for (int i = 0; i < each; ++i) {
-          const double v = sums[turn][lane * each + i];
-          if (v > 0.0) at = lane * each + i, at_before = before;
-          before += v;
-          if (before > goal && v > 0.0) break;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float eq;
+        const Pair d = left(xp[k], xq[k], static_cast<int>(g0) + i0 + 32 * k + lane, eq);
+        const bool some = d.h + d.l > 0.f;
+        add(plus, some ? d.h : 0.f, some ? d.l : 0.f);
+        if (kind == kResidual) {
+          add(all, d.h, d.l);
+          b += some ? eq : 0.f;
         }
-        s_segment = at;
-        s_before = at_before;
       }
-      if (lane == 0) part[0][0] = total;
     }
-    __syncthreads();
-    total = part[0][0];
-    if (total > 0.0 || kind == kFromTarget) break;
-    kind = kFromTarget;  // p = q as far as can be told: nothing is left of p - q
-    turn = 1;
+    VerifyGroup out;
+    out.a = warp_sum_ll(fixed(plus, unit));
+    out.d = kind == kResidual ? warp_sum_ll(fixed(all, unit)) : 0;
+    out.b = warp_sum(b);
+    if (lane == 0) sums[cta * kFinishWarps + warp] = out;
   }
-  // the segment's warp finds the token
-  const int segment = s_segment;
-  if (segment < 0 || segment / kGroups != gw) return;
-  const double goal = number(a.n) * total;
-  double before = s_before;
-  int token = -1;
-  for (int i = lane; i - lane < group; i += 32) {
-    const long long at = static_cast<long long>(segment) * group + i;
-    double r = 0.0;
-    if (at < a.V) r = value(left(at));
-    double run = r;
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) {
+    s_last = atomicAdd(a.done + s, 1u) == static_cast<unsigned>(ctas) - 1;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!s_last) return;
+
+  // The last CTA: k, the running sums of the groups, the group that holds the number, its token.
+  // Of values in the order of the threads: the thread where the running sum, on top of
+  // `offset`, first exceeds the goal (u times the whole sum where it is below 0).  Groups and
+  // tokens are rounded apart: where none exceeds it, the last one with any.
+  struct Pick {
+    int who;  // or -1
+    long long before, goal;
+  };
+  const float u = number(a.n);
+  auto pick = [&](long long mine, long long offset, long long goal) {
+    long long run = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const double x = __shfl_up_sync(0xffffffffu, run, o);
+      const long long x = __shfl_up_sync(0xffffffffu, run, o);
       if (lane >= o) run += x;
     }
-    const unsigned some = __ballot_sync(0xffffffffu, r > 0.0);
-    const unsigned above = __ballot_sync(0xffffffffu, r > 0.0 && before + run > goal);
-    if (above != 0) {
-      token = static_cast<int>(at - lane) + __ffs(above) - 1;
-      break;
+    __syncthreads();  // (what the last pick left has been read)
+    if (lane == 31) s_part[warp] = run;
+    __syncthreads();
+    long long total = 0, base = offset;
+    for (int w = 0; w < kFinishWarps; ++w) {
+      if (w < warp) base += s_part[w];
+      total += s_part[w];
     }
-    if (some != 0) token = static_cast<int>(at - lane) + 31 - __clz(some);
-    before += __shfl_sync(0xffffffffu, run, 31);
+    if (goal < 0) goal = goal_of(u, total);
+    const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
+    const unsigned above = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
+    if (lane == 0) s_first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1, s_some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
+    __syncthreads();
+    int who = -1, last = -1;
+    for (int w = kFinishWarps - 1; w >= 0; --w) {
+      if (s_first[w] >= 0) who = s_first[w];
+      if (last < 0) last = s_some[w];
+    }
+    who = who >= 0 ? who : last;
+    if (tid == who) s_before = base + (run - mine);
+    __syncthreads();
+    return Pick{who, s_before, goal};
+  };
+  const int each = (groups + kFinishThreads - 1) / kFinishThreads;
+  const int first = min(tid * each, groups), end = min(first + each, groups);
+  long long sa = 0, sd = 0;
+  float sb = 0.f;
+  for (int g = first; g < end; ++g) {
+    const VerifyGroup x = load_group(sums + g);
+    sa += x.a, sd += x.d, sb += x.b;
   }
-  if (lane == 0) {
+  float k = 0.f;
+  if (kind == kResidual) {
+    sd = warp_sum_ll(sd);
+    if (lane == 0) s_part[warp] = sd;
+    __syncthreads();
+    sd = 0;
+    for (int w = 0; w < kFinishWarps; ++w) sd += s_part[w];
+    k = static_cast<float>(sd) / unit / stat[a.n + 1 + stop].sum.h;
+  }
+  Pick at = pick(max(sa - __float2ll_rn(k * sb * unit), 0ll), 0, -1);
+  // nothing is left of p - q, as far as can be told: the token is drawn from p, by this CTA alone
+  const bool plain = at.who < 0;
+  long long lo = 0;
+  int count = a.V;
+  if (!plain) {
+    if (tid == at.who) {
+      long long before = at.before;
+      for (int g = first; g < end; ++g) {
+        const VerifyGroup x = load_group(sums + g);
+        const long long v = x.a - __float2ll_rn(k * x.b * unit);
+        if (v <= 0) continue;
+        s_group = g;
+        s_before = before;
+        before += v;
+        if (before > at.goal) break;
+      }
+    }
+    __syncthreads();
+    lo = static_cast<long long>(s_group) * group;
+    count = static_cast<int>(min(static_cast<long long>(group), a.V - lo));
+    at.before = s_before;
+  }
+  auto token_left = [&](long long i, float& x) {
+    float eq;
+    x = to_f<T>(row_p[i]);
+    if (plain) return fixed(mass(x, mp, table_h, table_l), unit);
+    Pair d = left(x, kind == kResidual ? to_f<T>(row_q[i]) : 0.f, static_cast<int>(i), eq);
+    d.l -= k * eq;
+    return max(fixed(d, unit), 0ll);
+  };
+  const int per = (count + kFinishThreads - 1) / kFinishThreads, t0 = min(tid * per, count), t1 = min(t0 + per, count);
+  long long mine = 0;
+  float x = 0.f;
+  for (int i = t0; i < t1; ++i) mine += token_left(lo + i, x);
+  at = plain ? pick(mine, 0, -1) : pick(mine, at.before, at.goal);
+  if (tid == max(at.who, 0)) {
+    long long before = at.before;
+    int token = -1;
+    float chosen = 0.f;
+    for (int i = t0; i < t1; ++i) {
+      const long long v = token_left(lo + i, x);
+      if (v <= 0) continue;
+      token = static_cast<int>(lo + i);
+      chosen = x;
+      before += v;
+      if (before > at.goal) break;
+    }
+    // (a group whose sum is more than 0 only by rounding: its last token)
+    if (token < 0) token = static_cast<int>(lo) + count - 1, chosen = to_f<T>(row_p[token]);
     tokens[stop] = token;
-    if (logp != nullptr) logp[stop] = static_cast<float>(log_p(stop, token));
+    if (logp != nullptr) logp[stop] = log_p(stop, chosen);
   }
 }
 
 template <typename T>
-cudaError_t run_verify(const VerifyArgs& a, cudaStream_t s) {
+cudaError_t run_verify(const VerifyArgs& a, const VerifySlices& c, cudaStream_t s) {
   const int rows = a.n + 1 + (a.draft != nullptr ? a.n : 0);
   const unsigned grid = static_cast<unsigned>(a.S) * rows * a.chunks;
   ZSAA_LAUNCH(verify_scan_kernel<T>, dim3(grid), dim3(kScanThreads), 0, s, a, rows);
-  cudaLaunchAttribute attr[2];
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.S) * kSampleCtas);
-  cfg.blockDim = dim3(kSampleThreads);
-  cfg.stream = s;
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kSampleCtas;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_sample_kernel<T>, a, rows);
+  int bits = 0;  // units in which sums of up to V exponentials stay below 2^62
+  while ((1 << bits) < a.V) ++bits;
+  ZSAA_LAUNCH(verify_finish_kernel<T>, dim3(static_cast<unsigned>(a.S) * c.ctas), dim3(kFinishThreads), 0, s, a, rows, c.ctas,
+              c.group, std::ldexp(1.f, 62 - std::max(bits, 10)));
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -488,8 +605,17 @@ cudaError_t run_verify(const VerifyArgs& a, cudaStream_t s) {
 // one more than the tokens fill: a row may start inside a 16-byte block
 int verify_chunks(int V) { return (V + 7 + kScanTokens - 1) / kScanTokens; }
 
-cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, cudaStream_t s) {
-  return dtype == ZSAA_F32 ? run_verify<float>(a, s) : run_verify<bf16>(a, s);
+VerifySlices verify_slices(int S, int V, int sms) {
+  int group = kGroupLeast;
+  auto ctas = [&] { return (V + group * kFinishWarps - 1) / (group * kFinishWarps); };
+  while (group < kGroupMost && static_cast<long long>(S) * ctas() > 4 * sms) group *= 2;
+  return VerifySlices{ctas(), group};
+}
+int verify_groups_most(int V) { return (V + kGroupLeast * kFinishWarps - 1) / (kGroupLeast * kFinishWarps) * kFinishWarps; }
+
+cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s) {
+  const VerifySlices c = verify_slices(a.S, a.V, sms);
+  return dtype == ZSAA_F32 ? run_verify<float>(a, c, s) : run_verify<bf16>(a, c, s);
 }
 
 }  // namespace zsaa

@@ -113,12 +113,18 @@ cudaError_t launch_paged_compact(const CompactArgs& a, const PoolList& pools, cu
 
 // ---- verification of drafted tokens (k_verify.cu)
 constexpr int kVerifyMaxDrafts = 15, kVerifyMaxVocab = 1 << 26;
-struct VerifyChunk {
-  double sum;  // sum of exp((x - top) / T)
-  float top;   // the maximum
-  int first;   // its first place (where a temperature of 0 asks for it)
-  int bad;     // a NaN or +inf among the logits
-  int pad;
+struct alignas(16) VerifyChunk {
+  long long sum;  // sum of exp((x - top) / T) in units of 2^-36
+  float top;      // the maximum
+  int first;      // its first place (where a temperature of 0 asks for it), or -1: a NaN or +inf among the logits
+};
+// A warp's tokens in the pass over the rows at which a sequence stops.
+struct alignas(16) VerifyGroup {
+  long long a, d;
+  float b;
+};
+struct VerifySlices {
+  int ctas, group;  // CTAs of a sequence, tokens of a warp
 };
 struct VerifyArgs {
   const void *target, *draft;  // draft or null
@@ -129,9 +135,12 @@ struct VerifyArgs {
   int32_t *accepted, *tokens, *lens_out;    // lens_out or null
   float* logp;                              // or null
   VerifyChunk* stat;                        // [S][n + 1 target rows, n draft rows][chunks]
+  VerifyGroup* groups;                      // [S][CTAs of a sequence][warps]
+  unsigned* done;                           // [S] CTAs that have finished
 };
 int verify_chunks(int V);
-cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, cudaStream_t s);
+int verify_groups_most(int V);  // groups of a sequence, at most
+cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s);
 
 // ---- status word of the calls without a model (zsaa_api.cu): the current device's, or null
 int* shared_status_word();
