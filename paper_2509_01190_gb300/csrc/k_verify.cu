@@ -191,9 +191,10 @@ __device__ __forceinline__ MassRow mass_row(float m, float t) {
   const float ch = kLog2eH / t;
   return MassRow{m, ch, (fmaf(-ch, t, kLog2eH) + kLog2eL) / t};
 }
+constexpr float kLn2H = 0.693147182464599609375f;  // ln 2 rounded to float, and what that leaves
+constexpr float kLn2L = static_cast<float>(0.69314718055994530942 - static_cast<double>(kLn2H));
+
 __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* table_h, const float* table_l) {
-  constexpr float kLn2H = 0.693147182464599609375f;  // ln 2 rounded to float, and what that leaves
-  constexpr float kLn2L = static_cast<float>(0.69314718055994530942 - static_cast<double>(kLn2H));
   const float d = x - r.m, b = d - x;
   const float de = (x - (d - b)) + (-r.m - b);  // what rounding took off x - m
   const float y = __fmul_rn(d, r.ch);  // (products whose rounding is kept are not fused into what follows)
@@ -211,6 +212,58 @@ __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* tab
   const float h = th + ph, l = (ph - (h - th)) + pl;
   const float scale = __int_as_float((max(k >> 5, -126) + 127) << 23);
   return y > -125.f ? Pair{h * scale, l * scale} : Pair{0.f, 0.f};
+}
+
+// The same of two tokens at once, in packed arithmetic (whose products are never fused into
+// what follows).  Negated products come from negated factors.
+struct Pair2 {
+  uint64_t h, l;
+};
+struct MassRow2 {
+  uint64_t m, nm, ch, nch, cl;
+};
+__device__ __forceinline__ uint64_t both(float x) { return f2pack(x, x); }
+__device__ __forceinline__ MassRow2 mass_row2(const MassRow& r) {
+  return MassRow2{both(r.m), both(-r.m), both(r.ch), both(-r.ch), both(r.cl)};
+}
+__device__ __forceinline__ Pair2 mass2(float x0, float x1, const MassRow2& r, const float* table_h, const float* table_l) {
+  const uint64_t x = f2pack(x0, x1);
+  const uint64_t d = fsub2(x, r.m), b = fsub2(d, x);
+  const uint64_t de = fadd2(fsub2(x, fsub2(d, b)), fsub2(r.nm, b));
+  const uint64_t ny = fmul2(d, r.nch);
+  const uint64_t ye = fadd2(ffma2(d, r.ch, ny), ffma2(d, r.cl, fmul2(de, r.ch)));
+  const uint64_t magic = ffma2(ny, both(-32.f), both(0x1.8p23f));
+  const uint64_t nf = ffma2(fsub2(magic, both(0x1.8p23f)), both(0.03125f), ny);
+  const uint64_t g = fmul2(nf, both(-kLn2H)), ng = fmul2(nf, both(kLn2H));
+  const uint64_t ge = fadd2(ffma2(nf, both(-kLn2H), ng), ffma2(nf, both(-kLn2L), fmul2(ye, both(kLn2H))));
+  const uint64_t w = fadd2(g, ge);
+  const uint64_t rest = ffma2(fmul2(w, w), ffma2(w, ffma2(w, both(1.f / 24.f), both(1.f / 6.f)), both(0.5f)), ge);
+  float magic0, magic1, ny0, ny1;
+  f2unpack(magic, magic0, magic1);
+  f2unpack(ny, ny0, ny1);
+  const int k0 = __float_as_int(magic0) - __float_as_int(0x1.8p23f), k1 = __float_as_int(magic1) - __float_as_int(0x1.8p23f);
+  const uint64_t th = f2pack(table_h[k0 & 31], table_h[k1 & 31]), tl = f2pack(table_l[k0 & 31], table_l[k1 & 31]);
+  const uint64_t ph = fmul2(th, g), nph = fmul2(th, ng);
+  const uint64_t pl = fadd2(ffma2(th, g, nph), ffma2(th, rest, ffma2(tl, g, tl)));
+  const uint64_t h = fadd2(th, ph), l = fadd2(fsub2(ph, fsub2(h, th)), pl);
+  // (2^(k/32 whole) where y > -125; elsewhere whatever it is, it is not taken)
+  const uint64_t scale = f2pack(__int_as_float(((k0 & ~31) << 18) + 0x3f800000), __int_as_float(((k1 & ~31) << 18) + 0x3f800000));
+  float h0, h1, l0, l1;
+  f2unpack(fmul2(h, scale), h0, h1);
+  f2unpack(fmul2(l, scale), l0, l1);
+  return Pair2{f2pack(ny0 < 125.f ? h0 : 0.f, ny1 < 125.f ? h1 : 0.f), f2pack(ny0 < 125.f ? l0 : 0.f, ny1 < 125.f ? l1 : 0.f)};
+}
+__device__ __forceinline__ void add2(Pair2& s, uint64_t h, uint64_t l) {
+  const uint64_t t = fadd2(s.h, h), b = fsub2(t, s.h);
+  s.l = fadd2(s.l, fadd2(fadd2(fsub2(s.h, fsub2(t, b)), fsub2(h, b)), l));
+  s.h = t;
+}
+// a - c b with the pair c (nh, l: its negated first part and its second)
+__device__ __forceinline__ Pair2 less2(const Pair2& a, const Pair2& b, uint64_t ch, uint64_t nch, uint64_t cl) {
+  const uint64_t nh = fmul2(b.h, nch), e = ffma2(b.h, ch, nh);  // -(b c) and what rounding took off
+  const uint64_t cb = fadd2(e, ffma2(b.h, cl, fmul2(b.l, ch)));
+  const uint64_t h = fadd2(a.h, nh), c = fsub2(h, a.h);
+  return Pair2{h, fadd2(fadd2(fsub2(a.h, fsub2(h, c)), fsub2(nh, c)), fsub2(a.l, cb))};
 }
 
 // arithmetic of pairs (products whose rounding is kept are not fused into what follows)
@@ -231,14 +284,6 @@ __device__ __forceinline__ Pair div(const Pair& a, const Pair& b) {
   const float h = a.h / b.h;
   return Pair{h, (fmaf(-h, b.h, a.h) + fmaf(-h, b.l, a.l)) / b.h};
 }
-__device__ __forceinline__ Pair warp_sum_pair(Pair v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float h = __shfl_xor_sync(0xffffffffu, v.h, o), l = __shfl_xor_sync(0xffffffffu, v.l, o);
-    add(v, h, l);
-  }
-  return v;
-}
 __device__ __forceinline__ Pair pair_of(long long v, float unit) {
   const float h = __ll2float_rn(v);
   return Pair{h * unit, __ll2float_rn(v - __float2ll_rn(h)) * unit};
@@ -256,7 +301,9 @@ __device__ __forceinline__ long long warp_sum_ll(long long v) {
 // ---------------------------------------------------------------- decisions and the token
 
 constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
-constexpr int kGroupLeast = 128, kGroupMost = 1024;  // tokens of a warp, whose sums are kept
+constexpr int kFinishPerSm = 3;
+constexpr int kGroupStep = 128;    // a group, the tokens of a warp, is a multiple of it
+constexpr int kGroupsMost = 1024;  // groups of a sequence, at most
 
 enum { kFromTarget = 0, kWithout = 1, kResidual = 2 };  // r = p; p without token x; max(p - q, 0)
 
@@ -294,11 +341,11 @@ __device__ __forceinline__ long long goal_of(float u, long long total) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kFinishThreads, 4)
+__global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     verify_finish_kernel(const __grid_constant__ VerifyArgs a, int rows, int ctas, int group, float unit) {
   __shared__ float table_h[32], table_l[32];
   __shared__ RowStat stat[2 * kVerifyMaxDrafts + 1];
-  __shared__ int s_stands[kVerifyMaxDrafts + 1];
+  __shared__ int s_stop, s_why;
   __shared__ long long s_part[kFinishWarps], s_before;
   __shared__ int s_first[kFinishWarps], s_some[kFinishWarps], s_group, s_last;
   pdl_trigger();
@@ -311,9 +358,24 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
   }
   __syncthreads();
   pdl_wait();
+  // one round trip: temperature, drafts, numbers, the rows' stretches; then the drafts' logits
   const Temperature t = temperature_of(a, s);
   const int n = drafts_of(a, s);
   const bool lookup = a.draft == nullptr, soft = !t.greedy && !t.bad;
+  const int32_t* drafts = after_wait(a.drafts) + static_cast<size_t>(s) * a.n;
+  const float* uniform = after_wait(a.uniform) + static_cast<size_t>(s) * (a.n + 1);
+  // numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
+  auto number = [&](int j) { return fminf(fmaxf(uniform[j], 0.f), 0x1.fffffep-1f); };
+  auto logit = [&](int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); };
+  const float u = number(a.n);
+  float my_u = 0.f, xp = 0.f, xq = 0.f;
+  int my_draft = -1;
+  if (tid < n) {
+    my_draft = drafts[tid];
+    my_u = number(tid);
+    xp = logit(tid, my_draft);
+    if (!lookup && soft) xq = logit(a.n + 1 + tid, my_draft);
+  }
   const int4* chunks = after_wait(reinterpret_cast<const int4*>(a.stat)) + static_cast<size_t>(s) * rows * a.chunks;
   auto chunk_at = [&](int r, int i) {
     const int4 v = chunks[static_cast<size_t>(r) * a.chunks + i];
@@ -324,39 +386,41 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     return c;
   };
 
-  // every row that may decide something: its maximum and its sum
-  for (int r = warp; r < rows; r += kFinishWarps) {
-    const bool is_draft = r > a.n;
-    RowStat out{{0.f, 0.f}, -INFINITY, a.V, 0};
-    if (!t.bad && (is_draft ? !t.greedy && r - a.n - 1 < n : r <= n)) {
-      bool bad = false;
-      for (int i = lane; i < a.chunks; i += 32) {
-        const VerifyChunk c = chunk_at(r, i);
-        out.top = fmaxf(out.top, c.top);
-        bad |= c.first < 0;
-      }
-      out.top = warp_max(out.top);
-      if (soft) {
-        const MassRow m = mass_row(out.top, t.t);
-        for (int i = lane; i < a.chunks; i += 32) {
-          const VerifyChunk c = chunk_at(r, i);
-          const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, m, table_h, table_l));
-          if (c.top > -INFINITY) add(out.sum, v.h, v.l);
-        }
-        out.sum = warp_sum_pair(out.sum);
-      } else {
-        for (int i = lane; i < a.chunks; i += 32) {
-          const VerifyChunk c = chunk_at(r, i);
-          if (c.top == out.top) out.first = min(out.first, c.first);
-        }
-        out.first = __reduce_min_sync(0xffffffffu, out.first);
-      }
-      out.ok = !__any_sync(0xffffffffu, bad) && out.top > -INFINITY;
+  // every row's maximum and sum, of 16 or 32 lanes (rows that the scan left out: anything)
+  const int lanes = a.chunks <= 16 ? 16 : 32, per_warp = 32 / lanes;
+  for (int r0 = warp * per_warp; r0 < rows; r0 += kFinishWarps * per_warp) {
+    const int r = min(r0 + lane / lanes, rows - 1), l = lane & (lanes - 1);
+    float top = -INFINITY;
+    int bad = 0;
+    for (int i = l; i < a.chunks; i += lanes) {
+      const VerifyChunk c = chunk_at(r, i);
+      top = fmaxf(top, c.top);
+      bad |= c.first < 0;
     }
-    if (lane == 0) stat[r] = out;
+    for (int o = lanes / 2; o > 0; o >>= 1) {
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+    }
+    Pair sum{0.f, 0.f};
+    int first = a.V;
+    const MassRow m = mass_row(top, t.t);
+    for (int i = l; i < a.chunks; i += lanes) {
+      const VerifyChunk c = chunk_at(r, i);
+      if (t.greedy) {
+        if (c.top == top) first = min(first, c.first);
+      } else {
+        const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, m, table_h, table_l));
+        if (c.top > -INFINITY) add(sum, v.h, v.l);
+      }
+    }
+    for (int o = lanes / 2; o > 0; o >>= 1) {
+      const float h = __shfl_xor_sync(0xffffffffu, sum.h, o), e = __shfl_xor_sync(0xffffffffu, sum.l, o);
+      add(sum, h, e);
+      first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
+    }
+    if (l == 0 && r0 + lane / lanes < rows) stat[r] = RowStat{sum, top, first, !t.bad && bad == 0 && top > -INFINITY};
   }
   __syncthreads();
-  auto logit = [&](int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); };
   // log p of a token of row r with the logit x: (x - top) / t - log(sum), the rounding errors of
   // each kept: log(sum) = g + log(sum exp(-g)) with g near it, and the latter is its argument less 1
   auto log_p = [&](int r, float x) {
@@ -368,44 +432,38 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     const Pair z = sub(Pair{h, l}, Pair{g, (e.h - 1.f) + e.l});
     return h > -INFINITY ? z.h + z.l : h;
   };
-  const int32_t* drafts = after_wait(a.drafts) + static_cast<size_t>(s) * a.n;
-  const float* uniform = after_wait(a.uniform) + static_cast<size_t>(s) * (a.n + 1);
-  // numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
-  auto number = [&](int j) { return fminf(fmaxf(uniform[j], 0.f), 0x1.fffffep-1f); };
   enum { kStands, kRefused, kNoDraft, kNoTarget };
-  if (tid <= a.n) {
+  if (warp == 0) {  // (lane j: draft j)
     int what = kNoDraft;
-    const RowStat p = stat[tid];
-    if (!p.ok && tid <= n) {
+    const RowStat p = stat[min(lane, a.n)];
+    if (!p.ok) {
       what = kNoTarget;
-    } else if (tid < n) {
-      const int x = drafts[tid];
+    } else if (lane < n) {
       if (t.greedy) {
-        what = p.first == x ? kStands : kRefused;
+        what = p.first == my_draft ? kStands : kRefused;
       } else {
         // u q(x) < p(x); where q(x) = 0: 0 < p(x)
-        const RowStat q = lookup ? RowStat{{1.f, 0.f}, 0.f, 0, 1} : stat[a.n + 1 + tid];
+        const RowStat q = lookup ? RowStat{{1.f, 0.f}, 0.f, 0, 1} : stat[a.n + 1 + lane];
         if (q.ok) {
-          const float xp = logit(tid, x), xq = lookup ? q.top : logit(a.n + 1 + tid, x), u = number(tid);
           const Pair ep = mass(xp, mass_row(p.top, t.t), table_h, table_l), eq = mass(xq, mass_row(q.top, t.t), table_h, table_l);
-          const Pair z = sub(mul(Pair{u, 0.f}, mul(eq, p.sum)), mul(ep, q.sum));
-          const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && u > 0x1p-30f;
-          what = (near ? z.h + z.l < 0.f : stands_far(u, xp, xq, t.t, p, q)) ? kStands : kRefused;
+          const Pair z = sub(mul(Pair{my_u, 0.f}, mul(eq, p.sum)), mul(ep, q.sum));
+          const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && my_u > 0x1p-30f;
+          what = (near ? z.h + z.l < 0.f : stands_far(my_u, xp, xq, t.t, p, q)) ? kStands : kRefused;
         }
       }
     }
-    s_stands[tid] = what;
+    const int stop = __ffs(__ballot_sync(0xffffffffu, what != kStands || lane >= a.n)) - 1;
+    what = __shfl_sync(0xffffffffu, what, stop);
+    if (lane == 0) s_stop = stop, s_why = what;
   }
   __syncthreads();
-  int stop = 0;
-  while (stop < a.n && s_stands[stop] == kStands) ++stop;
-  const int why = s_stands[stop];
+  const int stop = s_stop, why = s_why;
   int32_t* tokens = a.tokens + static_cast<size_t>(s) * (a.n + 1);
   float* logp = a.logp != nullptr ? a.logp + static_cast<size_t>(s) * (a.n + 1) : nullptr;
   if (cta == 0) {
     if (tid <= a.n && tid != stop) {
-      tokens[tid] = tid < stop ? drafts[tid] : -1;
-      if (logp != nullptr) logp[tid] = tid < stop && soft ? log_p(tid, logit(tid, drafts[tid])) : 0.f;
+      tokens[tid] = tid < stop ? my_draft : -1;
+      if (logp != nullptr) logp[tid] = tid < stop && soft ? log_p(tid, xp) : 0.f;
     }
     if (tid == 0) {
       a.accepted[s] = stop;
@@ -425,46 +483,71 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
   const MassRow mp = mass_row(stat[stop].top, t.t);
   const MassRow mq = kind == kResidual ? mass_row(stat[a.n + 1 + stop].top, t.t) : mp;
   const Pair ratio = kind == kResidual ? div(stat[stop].sum, stat[a.n + 1 + stop].sum) : Pair{0.f, 0.f};
-  // D of a token and its E_q; without a draft row p's exponential
-  auto left = [&](float xp, float xq, int at, float& eq) {
-    const Pair p = mass(xp, mp, table_h, table_l);
-    eq = 0.f;
-    if (kind != kResidual) return at == refused ? Pair{0.f, 0.f} : p;
-    const Pair q = mass(xq, mq, table_h, table_l);
-    eq = q.h;
-    return sub(p, mul(q, ratio));
-  };
 
   // this CTA's slice, a group of tokens per warp
   const int groups = ctas * kFinishWarps;
   VerifyGroup* sums = a.groups + static_cast<size_t>(s) * groups;
   {
     const long long g0 = (static_cast<long long>(cta) * kFinishWarps + warp) * group;
-    Pair plus{0.f, 0.f}, all{0.f, 0.f};
+    const MassRow2 p2 = mass_row2(mp);
+    Pair2 plus{0, 0}, all{0, 0};
     float b = 0.f;
-    for (int i0 = 0; i0 < group; i0 += 128) {
-      float xp[4], xq[4];
+    auto load = [&](const T* row, int i0, float (&x)[4]) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const long long at = g0 + i0 + 32 * k + lane;
-        xp[k] = at < a.V ? to_f<T>(row_p[at]) : -INFINITY;
-        xq[k] = kind == kResidual && at < a.V ? to_f<T>(row_q[at]) : -INFINITY;
+        x[k] = i0 < group && at < a.V ? to_f<T>(row[at]) : -INFINITY;
       }
+    };
+    float x[4], next[4];
+    load(row_p, 0, x);
+    if (kind == kResidual) {
+      const MassRow2 q2 = mass_row2(mq);
+      const uint64_t ch = both(ratio.h), nch = both(-ratio.h), cl = both(ratio.l);
+      float y[4], next_y[4];
+      load(row_q, 0, y);
+      for (int i0 = 0; i0 < group; i0 += 128) {
+        load(row_p, i0 + 128, next);
+        load(row_q, i0 + 128, next_y);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float eq;
-        const Pair d = left(xp[k], xq[k], static_cast<int>(g0) + i0 + 32 * k + lane, eq);
-        const bool some = d.h + d.l > 0.f;
-        add(plus, some ? d.h : 0.f, some ? d.l : 0.f);
-        if (kind == kResidual) {
-          add(all, d.h, d.l);
-          b += some ? eq : 0.f;
+        for (int k = 0; k < 4; k += 2) {
+          const Pair2 q = mass2(y[k], y[k + 1], q2, table_h, table_l);
+          const Pair2 d = less2(mass2(x[k], x[k + 1], p2, table_h, table_l), q, ch, nch, cl);
+          add2(all, d.h, d.l);
+          float s0, s1, h0, h1, l0, l1, q0, q1;
+          f2unpack(fadd2(d.h, d.l), s0, s1);
+          f2unpack(d.h, h0, h1);
+          f2unpack(d.l, l0, l1);
+          f2unpack(q.h, q0, q1);
+          add2(plus, f2pack(s0 > 0.f ? h0 : 0.f, s1 > 0.f ? h1 : 0.f), f2pack(s0 > 0.f ? l0 : 0.f, s1 > 0.f ? l1 : 0.f));
+          b += (s0 > 0.f ? q0 : 0.f) + (s1 > 0.f ? q1 : 0.f);
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = next[k], y[k] = next_y[k];
+      }
+    } else {
+      for (int i0 = 0; i0 < group; i0 += 128) {
+        load(row_p, i0 + 128, next);
+#pragma unroll
+        for (int k = 0; k < 4; k += 2) {
+          const long long at = g0 + i0 + 32 * k + lane;
+          const Pair2 p = mass2(at == refused ? -INFINITY : x[k], at + 32 == refused ? -INFINITY : x[k + 1], p2, table_h, table_l);
+          add2(plus, p.h, p.l);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = next[k];
       }
     }
+    // the two tokens' sums, in units
+    auto joined = [&](const Pair2& v) {
+      float h0, h1, l0, l1;
+      f2unpack(v.h, h0, h1);
+      f2unpack(v.l, l0, l1);
+      return warp_sum_ll(fixed(Pair{h0, l0}, unit) + fixed(Pair{h1, l1}, unit));
+    };
     VerifyGroup out;
-    out.a = warp_sum_ll(fixed(plus, unit));
-    out.d = kind == kResidual ? warp_sum_ll(fixed(all, unit)) : 0;
+    out.a = joined(plus);
+    out.d = kind == kResidual ? joined(all) : 0;
     out.b = warp_sum(b);
     if (lane == 0) sums[cta * kFinishWarps + warp] = out;
   }
@@ -485,7 +568,6 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     int who;  // or -1
     long long before, goal;
   };
-  const float u = number(a.n);
   auto pick = [&](long long mine, long long offset, long long goal) {
     long long run = mine;
 #pragma unroll
@@ -497,6 +579,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     if (lane == 31) s_part[warp] = run;
     __syncthreads();
     long long total = 0, base = offset;
+#pragma unroll
     for (int w = 0; w < kFinishWarps; ++w) {
       if (w < warp) base += s_part[w];
       total += s_part[w];
@@ -507,6 +590,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     if (lane == 0) s_first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1, s_some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
     __syncthreads();
     int who = -1, last = -1;
+#pragma unroll
     for (int w = kFinishWarps - 1; w >= 0; --w) {
       if (s_first[w] >= 0) who = s_first[w];
       if (last < 0) last = s_some[w];
@@ -516,24 +600,34 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     __syncthreads();
     return Pick{who, s_before, goal};
   };
-  const int each = (groups + kFinishThreads - 1) / kFinishThreads;
-  const int first = min(tid * each, groups), end = min(first + each, groups);
-  long long sa = 0, sd = 0;
-  float sb = 0.f;
-  for (int g = first; g < end; ++g) {
-    const VerifyGroup x = load_group(sums + g);
-    sa += x.a, sd += x.d, sb += x.b;
+  constexpr int EACH = kGroupsMost / kFinishThreads;  // groups of a thread
+  const int each = (groups + kFinishThreads - 1) / kFinishThreads, g0 = tid * each;
+  VerifyGroup mine_g[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    mine_g[i] = VerifyGroup{0, 0, 0.f};
+    if (i < each && g0 + i < groups) mine_g[i] = load_group(sums + g0 + i);
   }
   float k = 0.f;
   if (kind == kResidual) {
+    long long sd = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sd += mine_g[i].d;
     sd = warp_sum_ll(sd);
     if (lane == 0) s_part[warp] = sd;
     __syncthreads();
     sd = 0;
+#pragma unroll
     for (int w = 0; w < kFinishWarps; ++w) sd += s_part[w];
     k = static_cast<float>(sd) / unit / stat[a.n + 1 + stop].sum.h;
   }
-  Pick at = pick(max(sa - __float2ll_rn(k * sb * unit), 0ll), 0, -1);
+  long long mine = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    mine_g[i].a = max(mine_g[i].a - __float2ll_rn(k * mine_g[i].b * unit), 0ll);
+    mine += mine_g[i].a;
+  }
+  Pick at = pick(mine, 0, -1);
   // nothing is left of p - q, as far as can be told: the token is drawn from p, by this CTA alone
   const bool plain = at.who < 0;
   long long lo = 0;
@@ -541,14 +635,14 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
   if (!plain) {
     if (tid == at.who) {
       long long before = at.before;
-      for (int g = first; g < end; ++g) {
-        const VerifyGroup x = load_group(sums + g);
-        const long long v = x.a - __float2ll_rn(k * x.b * unit);
-        if (v <= 0) continue;
-        s_group = g;
+      bool found = false;
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        if (found || mine_g[i].a == 0) continue;
+        s_group = g0 + i;
         s_before = before;
-        before += v;
-        if (before > at.goal) break;
+        before += mine_g[i].a;
+        found = before > at.goal;
       }
     }
     __syncthreads();
@@ -556,16 +650,18 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     count = static_cast<int>(min(static_cast<long long>(group), a.V - lo));
     at.before = s_before;
   }
+  // a token's share of the sum
   auto token_left = [&](long long i, float& x) {
-    float eq;
     x = to_f<T>(row_p[i]);
-    if (plain) return fixed(mass(x, mp, table_h, table_l), unit);
-    Pair d = left(x, kind == kResidual ? to_f<T>(row_q[i]) : 0.f, static_cast<int>(i), eq);
-    d.l -= k * eq;
+    const Pair p = mass(x, mp, table_h, table_l);
+    if (plain || kind != kResidual) return !plain && i == refused ? 0ll : fixed(p, unit);
+    const Pair q = mass(to_f<T>(row_q[i]), mq, table_h, table_l);
+    Pair d = sub(p, mul(q, ratio));
+    d.l -= k * q.h;
     return max(fixed(d, unit), 0ll);
   };
   const int per = (count + kFinishThreads - 1) / kFinishThreads, t0 = min(tid * per, count), t1 = min(t0 + per, count);
-  long long mine = 0;
+  mine = 0;
   float x = 0.f;
   for (int i = t0; i < t1; ++i) mine += token_left(lo + i, x);
   at = plain ? pick(mine, 0, -1) : pick(mine, at.before, at.goal);
@@ -605,16 +701,17 @@ cudaError_t run_verify(const VerifyArgs& a, const VerifySlices& c, cudaStream_t 
 // one more than the tokens fill: a row may start inside a 16-byte block
 int verify_chunks(int V) { return (V + 7 + kScanTokens - 1) / kScanTokens; }
 
-VerifySlices verify_slices(int S, int V, int sms) {
-  int group = kGroupLeast;
-  auto ctas = [&] { return (V + group * kFinishWarps - 1) / (group * kFinishWarps); };
-  while (group < kGroupMost && static_cast<long long>(S) * ctas() > 4 * sms) group *= 2;
-  return VerifySlices{ctas(), group};
+// CTAs of a sequence: as many as there are at once for it, each with 128 tokens a warp or more.
+static VerifySlices verify_slices(int V, long long at_once) {
+  const int tokens = kGroupStep * kFinishWarps, most = std::min((V + tokens - 1) / tokens, kGroupsMost / kFinishWarps);
+  const int ctas = static_cast<int>(std::max(1ll, std::min(static_cast<long long>(most), at_once)));
+  const int group = ((V + ctas * kFinishWarps - 1) / (ctas * kFinishWarps) + kGroupStep - 1) / kGroupStep * kGroupStep;
+  return VerifySlices{(V + group * kFinishWarps - 1) / (group * kFinishWarps), group};
 }
-int verify_groups_most(int V) { return (V + kGroupLeast * kFinishWarps - 1) / (kGroupLeast * kFinishWarps) * kFinishWarps; }
+int verify_groups_most(int V) { return verify_slices(V, kGroupsMost).ctas * kFinishWarps; }
 
 cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s) {
-  const VerifySlices c = verify_slices(a.S, a.V, sms);
+  const VerifySlices c = verify_slices(a.V, kFinishPerSm * sms / a.S);
   return dtype == ZSAA_F32 ? run_verify<float>(a, c, s) : run_verify<bf16>(a, c, s);
 }
 
