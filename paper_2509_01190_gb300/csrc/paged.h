@@ -109,7 +109,7 @@ struct CompactArgs {
   int S, cols, out_cols, keep_cols, n_pages, page_shift, Hkv, row_vecs;
   int* status;
 };
-cudaError_t launch_paged_compact(const CompactArgs& a, const PoolList& pools, cudaStream_t s);
+cudaError_t launch_paged_compact(const CompactArgs& a, const PoolList& pools, int sms, cudaStream_t s);
 
 // ---- verification of drafted tokens (k_verify.cu)
 constexpr int kVerifyMaxDrafts = 15, kVerifyMaxVocab = 1 << 26;

@@ -385,6 +385,8 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   if (overlap(lens, row, lens_out, row) || overlap(n_keep, row, lens_out, row) ||
       (start != nullptr && overlap(start, row, lens_out, row)))
     return bad("lens_out overlaps lens, start or n_keep");
+  int sms = 0;
+  ZTRY(device_sms(&sms));
   CompactArgs a{};
   ZTRY(status_word(&a.status));
   a.table = table, a.lens = lens, a.start = start, a.keep = keep, a.n_keep = n_keep, a.table_out = table_out, a.refs = refs;
@@ -392,7 +394,7 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   a.S = S, a.cols = cols, a.out_cols = out_cols, a.keep_cols = keep_cols, a.n_pages = p.n_pages;
   a.page_shift = page_shift(p.page_size), a.Hkv = p.n_kv_heads;
   a.row_vecs = static_cast<int>(p.head_dim * element(p.dtype) / 16);
-  return launched("zsaa_op_paged_compact", launch_paged_compact(a, pools, reinterpret_cast<cudaStream_t>(stream)));
+  return launched("zsaa_op_paged_compact", launch_paged_compact(a, pools, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes) {
