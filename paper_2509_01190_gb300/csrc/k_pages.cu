@@ -92,23 +92,83 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t saddr, uint32_t rank, ui
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(saddr, rank)), "r"(v) : "memory");
 }
 
+// The row of place k, at or behind row `lo`: the last with base[row] <= k (a whole warp).
+__device__ __forceinline__ int row_of_place(const int* base, int lo, int rows, int k) {
+  const int lane = threadIdx.x & 31;
+  int n = rows - lo;
+  while (n > 1) {
+    const int step = (n + 31) >> 5, i = lane * step;
+    const int at = (__popc(__ballot_sync(0xffffffffu, i < n && base[lo + i] <= k)) - 1) * step;
+    lo += at;
+    n = min(step, n - at);
+  }
+  return lo;
+}
+
+// Warp gw of `warps` gives up or shares its part of the rows' pages, each row's columns
+// [touch(i), end(i)).
+template <bool FORK, typename Touch>
+__device__ __forceinline__ void touch_pages(const PagesArgs& a, int gw, int warps, Touch&& columns) {
+  const int lane = threadIdx.x & 31, blocks = (a.cols + kTakeBlock - 1) / kTakeBlock;
+  const long long units = static_cast<long long>(a.rows) * blocks;
+#pragma unroll 2
+  for (long long u = gw; u < units; u += warps) {
+    const int i = static_cast<int>(u / blocks), c0 = static_cast<int>(u - static_cast<long long>(i) * blocks) * kTakeBlock;
+    const int2 t = columns(i);
+    if (t.x >= c0 + kTakeBlock || t.y <= c0) continue;
+    const int32_t* row = a.table + static_cast<size_t>(FORK ? a.parent[i] : i) * a.cols;
+    int page[kTakeBlock / 32];
+#pragma unroll
+    for (int k = 0; k < kTakeBlock / 32; ++k) {
+      const int c = c0 + 32 * k + lane;
+      page[k] = c >= t.x && c < t.y ? row[c] : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kTakeBlock / 32; ++k) {
+      const int c = c0 + 32 * k + lane;
+      if (c < t.x || c >= t.y) continue;
+      if (FORK) a.table_out[static_cast<size_t>(i) * a.cols + c] = page[k];
+      if (page[k] < 0 || page[k] >= a.n_pages) atomicOr(a.status, kStatusBadIndex);
+      else atomicAdd(a.refs + page[k], FORK ? 1 : -1);
+    }
+  }
+}
+
 template <bool FORK>
-__global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __grid_constant__ PagesArgs given) {
+__device__ __forceinline__ PagesArgs args_after_wait(const PagesArgs& given) {
+  PagesArgs a = given;
+  a.refs = after_wait(a.refs), a.table = after_wait(a.table), a.lens = after_wait(a.lens);
+  if (FORK) a.parent = after_wait(a.parent), a.at = after_wait(a.at);
+  else a.want = after_wait(a.want);
+  return a;
+}
+
+// The pages given up or shared, on the whole device (calls that touch many).
+template <bool FORK>
+__global__ void __launch_bounds__(256) pages_touch_kernel(const __grid_constant__ PagesArgs given) {
+  pdl_trigger();
+  pdl_wait();
+  const PagesArgs a = args_after_wait<FORK>(given);
+  touch_pages<FORK>(a, static_cast<int>(blockIdx.x * 8 + (threadIdx.x >> 5)), static_cast<int>(gridDim.x) * 8, [&](int i) {
+    const TakeRow r = take_row<FORK>(a, i);
+    return make_int2(r.touch0, r.touch1);
+  });
+}
+
+template <bool FORK>
+__global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __grid_constant__ PagesArgs given, bool touched) {
   extern __shared__ int dynamic[];
   __shared__ int warp_sum[kTakeWarps], warp_free[kTakeWarps], cta_free[kTakeCtas];
   pdl_trigger();
-  PagesArgs a = given;
   int* base = dynamic;             // [rows + 1]: pages that earlier rows need
-  int* touch = base + a.rows + 1;  // [rows]: first column given up or shared
-  int* end = touch + a.rows;       // [rows]: the column behind the last; the first that gets a page
-  unsigned* masks = reinterpret_cast<unsigned*>(end + a.rows);  // free pages of a warp's part, 32 to a word
+  int* touch = base + given.rows + 1;  // [rows]: first column given up or shared
+  int* end = touch + given.rows;    // [rows]: the column behind the last; the first that gets a page
+  unsigned* masks = reinterpret_cast<unsigned*>(end + given.rows);  // free pages of a warp's part, 32 to a word
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = static_cast<int>(cluster_rank()), ctas = static_cast<int>(cluster_size());
   const int gw = rank * kTakeWarps + warp, warps = ctas * kTakeWarps;
   pdl_wait();
-  a.refs = after_wait(a.refs), a.table = after_wait(a.table), a.lens = after_wait(a.lens);
-  if (FORK) a.parent = after_wait(a.parent), a.at = after_wait(a.at);
-  else a.want = after_wait(a.want);
+  const PagesArgs a = args_after_wait<FORK>(given);
 
   // the rows, every CTA for itself: what each gives up or shares, and the pages needed before it
   const int own = rank * kTakeThreads + tid;  // the row whose length this thread writes (the first one)
@@ -146,30 +206,10 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   if (tid == 0) base[a.rows] = total_need;
 
   // pages given up or shared.  (A count that falls below 0 is found with the free pages.)
-  const int blocks = (a.cols + kTakeBlock - 1) / kTakeBlock;
-  const long long units = static_cast<long long>(a.rows) * blocks;
-#pragma unroll 2
-  for (long long u = gw; u < units; u += warps) {
-    const int i = static_cast<int>(u / blocks), c0 = static_cast<int>(u - static_cast<long long>(i) * blocks) * kTakeBlock;
-    const int t0 = touch[i], t1 = end[i];
-    if (t0 >= c0 + kTakeBlock || t1 <= c0) continue;
-    const int32_t* row = a.table + static_cast<size_t>(FORK ? a.parent[i] : i) * a.cols;
-    int page[kTakeBlock / 32];
-#pragma unroll
-    for (int k = 0; k < kTakeBlock / 32; ++k) {
-      const int c = c0 + 32 * k + lane;
-      page[k] = c >= t0 && c < t1 ? row[c] : -1;
-    }
-#pragma unroll
-    for (int k = 0; k < kTakeBlock / 32; ++k) {
-      const int c = c0 + 32 * k + lane;
-      if (c < t0 || c >= t1) continue;
-      if (FORK) a.table_out[static_cast<size_t>(i) * a.cols + c] = page[k];
-      if (page[k] < 0 || page[k] >= a.n_pages) atomicOr(a.status, kStatusBadIndex);
-      else atomicAdd(a.refs + page[k], FORK ? 1 : -1);
-    }
+  if (!touched) {
+    touch_pages<FORK>(a, gw, warps, [&](int i) { return make_int2(touch[i], end[i]); });
+    __threadfence();
   }
-  __threadfence();
   cluster_sync_all();
 
   // the free pages of this warp's part of the pool
@@ -178,22 +218,27 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   const long long p0 = static_cast<long long>(gw) * part;
   const int q0 = static_cast<int>(min(p0, static_cast<long long>(a.n_pages)));
   const int q1 = static_cast<int>(min(p0 + part, static_cast<long long>(a.n_pages)));
-  auto free_of = [&](int q) {
-    const int c = q + lane < q1 ? __ldcg(a.refs + q + lane) : 1;
+  auto free_of = [&](int q, int c) {  // of the 32 pages from q on, with the count c at this lane's
     if (c < 0) {  // more given up than there were
       a.refs[q + lane] = 0;
       atomicOr(a.status, kStatusBadIndex);
     }
     return __ballot_sync(0xffffffffu, c <= 0);
   };
+  auto count_at = [&](int q) { return q + lane < q1 ? __ldcg(a.refs + q + lane) : 1; };
   int n_free = 0;
-#pragma unroll 8
-  for (int w = 0; w < words; ++w) {
-    const int q = q0 + 32 * w;
-    if (q >= q1) break;
-    const unsigned m = free_of(q);
-    if (kept && lane == 0) masks[warp * words + w] = m;
-    n_free += __popc(m);
+  for (int w0 = 0; w0 < words && q0 + 32 * w0 < q1; w0 += 16) {
+    int c[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k)
+      if (w0 + k < words) c[k] = count_at(q0 + 32 * (w0 + k));
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      if (w0 + k >= words) break;
+      const unsigned m = free_of(q0 + 32 * (w0 + k), c[k]);
+      if (kept && lane == 0) masks[warp * words + w0 + k] = m;
+      n_free += __popc(m);
+    }
   }
   if (lane == 0) warp_free[warp] = n_free;
   __syncthreads();
@@ -211,22 +256,30 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
     free_total += cta_free[r];
   }
 
-  // the free page of rank k goes to the k-th place that needs one
-#pragma unroll 2
+  // The free page of rank k goes to the k-th place that needs one.  A word's pages mostly go to
+  // one row, so the rows of its first and its last page are looked for by the whole warp.
+  int lo = 0;
+  bool found = false;
   for (int w = 0; w < words; ++w) {
     const int q = q0 + 32 * w;
     if (q >= q1 || free_before >= total_need) break;
-    const unsigned mask = kept ? masks[warp * words + w] : free_of(q);
-    const int k = free_before + __popc(mask & ((1u << lane) - 1));
+    const unsigned mask = kept ? masks[warp * words + w] : free_of(q, count_at(q));
+    if (mask == 0) continue;
+    const int k = free_before + __popc(mask & ((1u << lane) - 1)), last = min(free_before + __popc(mask), total_need) - 1;
+    if (!found || base[lo + 1] <= free_before) lo = row_of_place(base, lo, a.rows, free_before);
+    found = true;
+    const int hi = base[lo + 1] > last ? lo : row_of_place(base, lo, a.rows, last);
     free_before += __popc(mask);
-    if ((mask >> lane & 1) == 0 || k >= total_need) continue;
-    int lo = 0, hi = a.rows;  // base[lo] <= k < base[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (base[mid] <= k) lo = mid; else hi = mid;
+    if ((mask >> lane & 1) != 0 && k < total_need) {
+      int row = lo, n = hi - lo + 1;  // base[row] <= k < base[row + n]
+      while (n > 1) {
+        const int half = n >> 1;
+        if (base[row + half] <= k) row += half, n -= half; else n = half;
+      }
+      a.table_out[static_cast<size_t>(row) * a.cols + end[row] + (k - base[row])] = q + lane;
+      a.refs[q + lane] = 1;
     }
-    a.table_out[static_cast<size_t>(lo) * a.cols + end[lo] + (k - base[lo])] = q + lane;
-    a.refs[q + lane] = 1;
+    lo = hi;
   }
   for (int i = own; i < a.rows; i += ctas * kTakeThreads) {
     const TakeRow r = i == own ? own_row : take_row<FORK>(a, i);
@@ -245,7 +298,10 @@ cudaError_t run_take(const PagesArgs& a, cudaStream_t s) {
   const cudaError_t e = set_smem_limit_once(once, pages_take_kernel<FORK>,
                                             static_cast<int>(sizeof(int)) * (3 * kPagesMaxRows + 1 + kTakeMasks * kTakeWarps));
   if (e != cudaSuccess) return e;
-  return launch_cluster(pages_take_kernel<FORK>, dim3(kTakeCtas), dim3(kTakeThreads), kTakeCtas, smem, s, a);
+  const long long units = static_cast<long long>(a.rows) * ((a.cols + kTakeBlock - 1) / kTakeBlock);
+  const bool many = units > kTakeCtas * kTakeWarps;
+  if (many) ZSAA_LAUNCH(pages_touch_kernel<FORK>, dim3(static_cast<unsigned>(std::min((units + 7) / 8, 1024ll))), dim3(256), 0, s, a);
+  return launch_cluster(pages_take_kernel<FORK>, dim3(kTakeCtas), dim3(kTakeThreads), kTakeCtas, smem, s, a, many);
 }
 
 // ---------------------------------------------------------------- fork: the partly filled pages
@@ -274,8 +330,13 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(const __grid_constant__ 
   uint4* pool = static_cast<uint4*>(a.pools.p[blockIdx.y]);
   const uint4* s = pool + static_cast<size_t>(from) * a.Hkv * stride;
   uint4* d = pool + static_cast<size_t>(to) * a.Hkv * stride;
-  for (int h = 0; h < a.Hkv; ++h)
-    for (int v = tid; v < n; v += blockDim.x) d[static_cast<size_t>(h) * stride + v] = s[static_cast<size_t>(h) * stride + v];
+  const int all = n * a.Hkv;
+#pragma unroll 4
+  for (int v = tid; v < all; v += blockDim.x) {
+    const int h = v / n;
+    const size_t at = static_cast<size_t>(h) * stride + (v - h * n);
+    d[at] = s[at];
+  }
 }
 
 // ---------------------------------------------------------------- compact
@@ -286,22 +347,28 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(const __grid_constant__ 
 // place is as right as into other pages.  While a tile's values are on their way the next tile's
 // places are looked up (keep -> table -> page, three round trips), so a tile costs about one
 // round trip.
+constexpr int kCompactPerSm = 3;
 constexpr int kCompactThreads = 256, kCompactUnroll = 8, kCompactVecs = kCompactThreads * kCompactUnroll;
 
 struct CompactPlan {
-  int heads;  // of a CTA
-  int tile;   // entries of a CTA's share of a tile: heads * tile * row_vecs <= kCompactVecs
-  int ctas;   // of a cluster
+  int heads;   // of a CTA
+  int slices;  // CTAs of a head, each with a part of its dims (heads is 1 then)
+  int vecs;    // 16-byte vectors of a CTA's part of an entry: a power of two, 8 or more
+  int tile;    // entries of a CTA's share of a tile: heads * tile * vecs <= kCompactVecs
+  int ctas;    // of a cluster
+  int clusters;
 };
 
-__global__ void __launch_bounds__(kCompactThreads, 3)
+__global__ void __launch_bounds__(kCompactThreads, kCompactPerSm)
     compact_kernel(const __grid_constant__ CompactArgs a, const __grid_constant__ PoolList pools, const __grid_constant__ CompactPlan plan) {
-  __shared__ int s_from[2][kCompactVecs / 8], s_to[2][kCompactVecs / 8];  // entries in the pool (of head 0), or -1
+  __shared__ int s_from[2][kCompactThreads], s_to[2][kCompactThreads];  // entries in the pool (of head 0), or -1
   pdl_trigger();
   pdl_wait();
-  const int rank = static_cast<int>(blockIdx.x) % plan.ctas, s = static_cast<int>(blockIdx.x) / plan.ctas, tid = threadIdx.x;
-  const int h0 = blockIdx.z * plan.heads, heads = min(plan.heads, a.Hkv - h0);
-  const bool first_cta = blockIdx.y == 0 && h0 == 0;
+  const int shares = plan.ctas * plan.clusters, s = static_cast<int>(blockIdx.x) / shares, tid = threadIdx.x;
+  const int rank = static_cast<int>(blockIdx.x) - s * shares;
+  const int part = static_cast<int>(blockIdx.z) / plan.slices, slice = static_cast<int>(blockIdx.z) - part * plan.slices;
+  const int h0 = part * plan.heads, heads = min(plan.heads, a.Hkv - h0);
+  const bool first_cta = blockIdx.y == 0 && blockIdx.z == 0;
   const int given = after_wait(a.lens)[s], cap = a.cols << a.page_shift, out_cap = a.out_cols << a.page_shift;
   const int len = min(max(given, 0), cap);
   const int begin = a.start != nullptr ? after_wait(a.start)[s] : 0, start = min(max(begin, 0), len);
@@ -314,65 +381,91 @@ __global__ void __launch_bounds__(kCompactThreads, 3)
   const int32_t* keep = after_wait(a.keep) + static_cast<size_t>(s) * a.keep_cols;
   const int32_t* from_row = after_wait(a.table) + static_cast<size_t>(s) * a.cols;
   const int32_t* to_row = after_wait(a.table_out) + static_cast<size_t>(s) * a.out_cols;
-  const int mask = (1 << a.page_shift) - 1, step = plan.tile * plan.ctas;
-  // this CTA's entries of the tile from j0 on
-  auto look_up = [&](unsigned j0, int slot) {  // (j0 may pass 2^31)
-    for (int i = tid; i < plan.tile; i += kCompactThreads) {
-      const unsigned j = j0 + rank * plan.tile + i;
-      int from = -1, to = -1;
-      if (j < static_cast<unsigned>(n)) {
-        const int e = keep[j], d = start + static_cast<int>(j);
-        const int before = j > 0 ? keep[j - 1] : -1, q = to_row[d >> a.page_shift];
-        bool ok = e >= d && e < len && before < e;
-        const int p = ok ? from_row[e >> a.page_shift] : -1;
-        ok = p >= 0 && p < a.n_pages && q >= 0 && q < a.n_pages;
-        const bool stays = p == q && e == d;
-        if (ok && !stays && a.refs != nullptr) ok = after_wait(a.refs)[q] == 1;  // no other sequence's page
-        if (!ok && first_cta) atomicOr(a.status, kStatusBadIndex);
-        if (ok && !stays) {
-          from = ((p * a.Hkv) << a.page_shift) + (e & mask);
-          to = ((q * a.Hkv) << a.page_shift) + (d & mask);
-        }
-      }
-      s_from[slot][i] = from;
-      s_to[slot][i] = to;
+  const int mask = (1 << a.page_shift) - 1;
+  // Where no page is both read and written all shares go at once, each for itself; else one
+  // cluster's do, tile by tile.
+  bool in_place = a.table_out == a.table;
+  if (!in_place) {
+    bool same = false;
+    for (int c = (start >> a.page_shift) + tid; n > 0 && c <= (start + n - 1) >> a.page_shift; c += kCompactThreads)
+      same |= c < a.cols && to_row[c] == from_row[c];
+    in_place = __syncthreads_or(same) != 0;
+  }
+  if (in_place && rank >= plan.ctas) return;  // (whole clusters)
+  const unsigned step = plan.tile * (in_place ? plan.ctas : shares), end = n;
+  // thread i < tile looks entry i of this CTA's share up: first its list entry, a tile later its pages
+  const unsigned mine = rank * plan.tile + tid;
+  int e = -1, before = -1;
+  auto look = [&](unsigned j0) {  // (j0 may pass 2^31)
+    const unsigned j = j0 + mine;
+    if (tid < plan.tile && j < end) {
+      e = keep[j];
+      before = j > 0 ? keep[j - 1] : -1;
     }
   };
-  uint4* pool = static_cast<uint4*>(pools.p[blockIdx.y]);
-  const int row_shift = 31 - __clz(a.row_vecs), vec = tid & (a.row_vecs - 1);
-  const int at = tid >> row_shift, rows = kCompactThreads >> row_shift;  // (head, entry) pairs of a round
-  look_up(0, 0);
+  auto place = [&](unsigned j0, int slot) {
+    const unsigned j = j0 + mine;
+    if (tid >= plan.tile) return;
+    int from = -1, to = -1;
+    if (j < end) {
+      const int d = start + static_cast<int>(j), q = to_row[d >> a.page_shift];
+      bool ok = e >= d && e < len && before < e;
+      const int p = ok ? from_row[e >> a.page_shift] : -1;
+      ok = p >= 0 && p < a.n_pages && q >= 0 && q < a.n_pages;
+      const bool stays = p == q && e == d;
+      if (ok && !stays && a.refs != nullptr) ok = after_wait(a.refs)[q] == 1;  // no other sequence's page
+      if (!ok && first_cta) atomicOr(a.status, kStatusBadIndex);
+      if (ok && !stays) {
+        from = ((p * a.Hkv) << a.page_shift) + (e & mask);
+        to = ((q * a.Hkv) << a.page_shift) + (d & mask);
+      }
+    }
+    s_from[slot][tid] = from;
+    s_to[slot][tid] = to;
+  };
+  const int row_shift = 31 - __clz(a.row_vecs), part_shift = 31 - __clz(plan.vecs);
+  uint4* pool = static_cast<uint4*>(pools.p[blockIdx.y]) + slice * plan.vecs + (tid & (plan.vecs - 1));
+  const int at = tid >> part_shift, rows = kCompactThreads >> part_shift;  // (head, entry) pairs of a round
+  look(0);
+  place(0, 0);
+  look(step);
   __syncthreads();
   int slot = 0;
-  for (unsigned j0 = 0; j0 < static_cast<unsigned>(n); j0 += step, slot ^= 1) {
+  for (unsigned j0 = 0; j0 < end; j0 += step, slot ^= 1) {
     uint4 x[kCompactUnroll];
     int to[kCompactUnroll];
 #pragma unroll
     for (int k = 0; k < kCompactUnroll; ++k) {
-      const int i = k * rows + at, h = i / plan.tile, e = i - h * plan.tile;
+      const int i = k * rows + at, h = i / plan.tile, r = i - h * plan.tile;
       to[k] = -1;
       if (h >= heads) continue;
-      const int from = s_from[slot][e], head = (h0 + h) << a.page_shift;
+      const int from = s_from[slot][r], head = (h0 + h) << a.page_shift;
       if (from < 0) continue;
-      x[k] = pool[(static_cast<size_t>(from + head) << row_shift) + vec];
-      to[k] = s_to[slot][e] + head;
+      x[k] = pool[static_cast<size_t>(from + head) << row_shift];
+      to[k] = s_to[slot][r] + head;
     }
-    if (j0 + step < static_cast<unsigned>(n)) look_up(j0 + step, slot ^ 1);
-    if (plan.ctas > 1) cluster_sync_all(); else __syncthreads();
+    place(j0 + step, slot ^ 1);
+    look(j0 + 2 * step);
+    if (in_place && plan.ctas > 1) cluster_sync_all(); else __syncthreads();
 #pragma unroll
     for (int k = 0; k < kCompactUnroll; ++k)
-      if (to[k] >= 0) pool[(static_cast<size_t>(to[k]) << row_shift) + vec] = x[k];
+      if (to[k] >= 0) pool[static_cast<size_t>(to[k]) << row_shift] = x[k];
   }
 }
 
-// A CTA takes as many heads as its registers hold of the longest list, and clusters split a list
-// where its CTAs would not fill the SMs.
+// A CTA takes as many heads as its registers hold of the longest list.  Where the CTAs would not
+// fill the SMs the list is split over a cluster; a move in place splits a head's dims first (down to
+// 128 bytes), one into another table takes as many clusters as run at once.
 CompactPlan compact_plan(const CompactArgs& a, int pools, int sms) {
-  CompactPlan p{1, kCompactVecs / a.row_vecs, 1};
-  p.tile = std::min(p.tile, a.keep_cols);
-  p.heads = std::max(1, std::min(a.Hkv, kCompactVecs / (a.row_vecs * p.tile)));
+  CompactPlan p{1, 1, a.row_vecs, 0, 1, 1};
+  const bool in_place = a.table_out == a.table;
+  p.heads = std::max(1, std::min(a.Hkv, kCompactVecs / (a.row_vecs * std::min(a.keep_cols, kCompactVecs / a.row_vecs))));
   const long long ctas = static_cast<long long>(a.S) * pools * ((a.Hkv + p.heads - 1) / p.heads);
-  while (p.ctas < 8 && ctas * p.ctas < 2 * sms && p.tile * p.ctas < a.keep_cols) p.ctas *= 2;
+  while (in_place && p.heads == 1 && p.vecs > 8 && ctas * p.slices < 2 * sms) p.slices *= 2, p.vecs /= 2;
+  p.tile = std::min(kCompactVecs / (p.heads * p.vecs), a.keep_cols);
+  while (p.ctas < 8 && ctas * p.slices * p.ctas < 2 * sms && p.tile * p.ctas < a.keep_cols) p.ctas *= 2;
+  if (!in_place && p.ctas == 8)
+    p.clusters = static_cast<int>(std::max(1ll, std::min<long long>(kCompactPerSm * sms / (8 * ctas), (a.keep_cols + 8ll * p.tile - 1) / (8 * p.tile))));
   return p;
 }
 
@@ -394,7 +487,7 @@ cudaError_t launch_paged_fork(const PagesArgs& a, const PoolList& pools, int Hkv
 
 cudaError_t launch_paged_compact(const CompactArgs& a, const PoolList& pools, int sms, cudaStream_t s) {
   const CompactPlan p = compact_plan(a, pools.n, sms);
-  return launch_cluster(compact_kernel, dim3(a.S * p.ctas, pools.n, (a.Hkv + p.heads - 1) / p.heads), dim3(kCompactThreads),
+  return launch_cluster(compact_kernel, dim3(a.S * p.ctas * p.clusters, pools.n, (a.Hkv + p.heads - 1) / p.heads * p.slices), dim3(kCompactThreads),
                         p.ctas, 0, s, a, pools, p);
 }
 

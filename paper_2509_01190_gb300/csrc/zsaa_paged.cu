@@ -378,7 +378,7 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   if (!words(refs, table, lens, start, keep, n_keep, table_out, lens_out)) return bad("int32 arrays must be 4-byte aligned");
   const zsaa_pages& p = layers[0];
   if (S < 1 || keep_cols < 1) return bad("S and keep_cols must be >= 1");
-  if (p.n_kv_heads > 65535) return bad("more than 65535 KV heads");  // (a grid's third dimension)
+  if (p.n_kv_heads > 16383) return bad("more than 16383 KV heads");  // (a grid's third dimension, 4 CTAs to a head)
   ZTRY(check_cols(cols, p.page_size));
   ZTRY(check_cols(out_cols, p.page_size));
   const size_t row = 4 * static_cast<size_t>(S);
