@@ -9,8 +9,13 @@
 //
 //   verify_scan_kernel    one stretch of one row per CTA: its maximum and the sum of its
 //                         exponentials.  Bound by the logits' bytes.
-//   verify_finish_kernel  which drafts stand; then the rows at which a sequence stops again, a
-//                         slice per CTA, and its last CTA finds the token.
+//   verify_finish_kernel  the rows at which a sequence stops again, a group of tokens per CTA;
+//                         a sequence's last CTA finds the token.
+//
+// Small calls scan all rows at once, and every CTA of the second kernel works out which drafts
+// stand.  Large calls scan draft 0's rows of all sequences first, then draft 1's, and so on; the
+// CTA that ends a draft's rows decides it, and rows behind a refused draft, which nothing depends
+// on, are left out as far as that is known when their turn comes.
 //
 // What decides a draft is one comparison of two quotients, off by about 1e-8 with sums of
 // float32 exponentials.  What decides a token is where u_n falls among V borders, some 1e-5
@@ -61,10 +66,6 @@ __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int s) {
   return __ffs(__ballot_sync(0xffffffffu, x < 0 || x >= a.V)) - 1;  // (lane 31 has no draft)
 }
 
-// ---------------------------------------------------------------- the rows' maxima and sums
-
-constexpr int kScanThreads = 256, kScanValues = 32, kScanTokens = kScanThreads * kScanValues;
-
 template <typename T>
 __device__ __forceinline__ void load16(const T* p, float* x) {
   const uint4 u = *reinterpret_cast<const uint4*>(p);
@@ -83,100 +84,29 @@ __device__ __forceinline__ const T* row_of(const VerifyArgs& a, int s, int r) {
   return after_wait(static_cast<const T*>(a.draft)) + (static_cast<long long>(s) * a.n + (r - a.n - 1)) * a.draft_ld;
 }
 
-// (64-bit floats are left out of both kernels: the SM does two of their operations a clock.)
 constexpr float kSumScale = 0x1p36f;  // a stretch's sum, at most 2^13, in units of 2^-36
-
-// Sum over the warp of values in [0, 2^50) (two 32-bit reductions of 25 bits each).
-__device__ __forceinline__ unsigned long long warp_sum_u50(unsigned long long v) {
-  const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & 0x1ffffffu);
-  const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 25));
-  return (static_cast<unsigned long long>(hi) << 25) + lo;
-}
-
-// Every warp takes its sum against its own maximum, so the warps meet once, at the end.
-template <typename T>
-__global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __grid_constant__ VerifyArgs a, int rows) {
-  constexpr int VEC = 16 / sizeof(T), VECS = kScanValues / VEC;
-  __shared__ float s_top[kScanThreads / 32];
-  __shared__ unsigned long long s_sum[kScanThreads / 32];
-  __shared__ int s_first[kScanThreads / 32];
-  pdl_trigger();
-  pdl_wait();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const unsigned item = blockIdx.x / static_cast<unsigned>(a.chunks);
-  const int chunk = static_cast<int>(blockIdx.x - item * a.chunks);
-  const int s = static_cast<int>(item / static_cast<unsigned>(rows)), r = static_cast<int>(item - s * static_cast<unsigned>(rows));
-  if (r == 0 && chunk == 0 && tid == 0) a.done[s] = 0;
-  const Temperature t = temperature_of(a, s);
-  const bool is_draft = r > a.n;
-  if (t.bad || (t.greedy && is_draft)) return;  // rows that decide nothing
-  const int j = is_draft ? r - a.n - 1 : r;
-  if (j > 0 || is_draft) {
-    const int have = drafts_of(a, s);
-    if (j > have || (is_draft && j == have)) return;
-  }
-  const T* row = row_of<T>(a, s, r);
-  // the stretch starts on a 16-byte boundary, before the row's first token for the first one
-  const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-  const int t0 = chunk * kScanTokens - lead;
-  float x[kScanValues];
-#pragma unroll
-  for (int k = 0; k < VECS; ++k) {
-    const int at = t0 + (k * kScanThreads + tid) * VEC;
-    if (at >= 0 && at <= a.V - VEC) {
-      load16(row + at, x + k * VEC);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) x[k * VEC + i] = at + i >= 0 && at + i < a.V ? to_f<T>(row[at + i]) : -INFINITY;
-    }
-  }
-  float top = -INFINITY;
-  bool bad = false;
-#pragma unroll
-  for (int k = 0; k < kScanValues; ++k) {
-    top = fmaxf(top, x[k]);
-    bad |= !(x[k] < INFINITY);
-  }
-  top = warp_max(top);
-  const float c = log2e_over(t.t);
-  unsigned long long total = 0;
-  int first = a.V;
-  if (t.greedy) {
-#pragma unroll
-    for (int k = kScanValues - 1; k >= 0; --k) {
-      const int at = t0 + ((k / VEC) * kScanThreads + tid) * VEC + k % VEC;
-      if (x[k] == top && at >= 0 && at < a.V) first = at;
-    }
-    first = __reduce_min_sync(0xffffffffu, first);
-  } else {
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < kScanValues; ++k) sum[k & 3] += ex2((x[k] - ref) * c);
-    // (bad rows have any sum)
-    total = warp_sum_u50(static_cast<unsigned long long>(fminf((sum[0] + sum[1]) + (sum[2] + sum[3]), 64.f) * kSumScale));
-  }
-  if (lane == 0) s_top[warp] = top, s_sum[warp] = total, s_first[warp] = first;
-  bad = __syncthreads_or(bad) != 0;
-  if (warp == 0) {
-    const bool in = lane < kScanThreads / 32;
-    top = in ? s_top[lane] : -INFINITY;
-    const float all = warp_max(top);
-    total = in && top > -INFINITY ? static_cast<unsigned long long>(static_cast<float>(s_sum[lane]) * ex2((top - all) * c)) : 0;
-    VerifyChunk out;
-    out.sum = static_cast<long long>(warp_sum_u50(total));
-    out.top = all;
-    out.first = __reduce_min_sync(0xffffffffu, in && top == all ? s_first[lane] : a.V);
-    if (bad) out.first = -1;
-    if (lane == 0) a.stat[(static_cast<size_t>(s) * rows + r) * a.chunks + chunk] = out;
-  }
-}
 
 // ---------------------------------------------------------------- exponentials as pairs of floats
 
 struct Pair {
   float h, l;
 };
+
+// 2^(i/32) as pairs of floats, all first parts, then all second parts
+struct Powers {
+  float v[64];
+};
+constexpr Powers powers() {
+  Powers p{};
+  double x = 1.0;
+  for (int i = 0; i < 32; ++i) {
+    p.v[i] = static_cast<float>(x);
+    p.v[32 + i] = static_cast<float>(x - static_cast<double>(p.v[i]));
+    x *= 1.02189714865411667823;  // 2^(1/32)
+  }
+  return p;
+}
+__constant__ Powers kPowers = powers();
 
 // exp((x - m) / T) = 2^y: y = (x - m) log2(e) / T with its rounding errors kept, cut into
 // k / 32 and a rest f of at most 1/64; 2^(k/32) from a table of pairs, 2^f by its series, whose
@@ -185,16 +115,16 @@ struct Pair {
 struct MassRow {
   float m, ch, cl;  // the row's maximum; log2(e) / T
 };
-__device__ __forceinline__ MassRow mass_row(float m, float t) {
+__device__ __forceinline__ MassRow mass_row(float t) {  // without its maximum
   constexpr float kLog2eH = 1.44269502162933349609375f;
   constexpr float kLog2eL = static_cast<float>(1.4426950408889634074 - static_cast<double>(kLog2eH));
   const float ch = kLog2eH / t;
-  return MassRow{m, ch, (fmaf(-ch, t, kLog2eH) + kLog2eL) / t};
+  return MassRow{0.f, ch, (fmaf(-ch, t, kLog2eH) + kLog2eL) / t};
 }
 constexpr float kLn2H = 0.693147182464599609375f;  // ln 2 rounded to float, and what that leaves
 constexpr float kLn2L = static_cast<float>(0.69314718055994530942 - static_cast<double>(kLn2H));
 
-__device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* table_h, const float* table_l) {
+__device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* table) {
   const float d = x - r.m, b = d - x;
   const float de = (x - (d - b)) + (-r.m - b);  // what rounding took off x - m
   const float y = __fmul_rn(d, r.ch);  // (products whose rounding is kept are not fused into what follows)
@@ -206,7 +136,7 @@ __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* tab
   const float ge = fmaf(f, kLn2H, -g) + fmaf(f, kLn2L, ye * kLn2H);
   const float w = g + ge;
   const float rest = ge + w * w * fmaf(w, fmaf(w, 1.f / 24.f, 1.f / 6.f), 0.5f);
-  const float th = table_h[k & 31], tl = table_l[k & 31];
+  const float th = table[k & 31], tl = table[32 + (k & 31)];
   const float ph = __fmul_rn(th, g);
   const float pl = fmaf(th, g, -ph) + fmaf(th, rest, fmaf(tl, g, tl));
   const float h = th + ph, l = (ph - (h - th)) + pl;
@@ -219,17 +149,19 @@ __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* tab
 struct Pair2 {
   uint64_t h, l;
 };
-struct MassRow2 {
-  uint64_t m, nm, ch, nch, cl;
+struct Factor2 {
+  uint64_t ch, nch, cl;
 };
 __device__ __forceinline__ uint64_t both(float x) { return f2pack(x, x); }
-__device__ __forceinline__ MassRow2 mass_row2(const MassRow& r) {
-  return MassRow2{both(r.m), both(-r.m), both(r.ch), both(-r.ch), both(r.cl)};
+__device__ __forceinline__ MassRow with_top(MassRow r, float top) {
+  r.m = top;
+  return r;
 }
-__device__ __forceinline__ Pair2 mass2(float x0, float x1, const MassRow2& r, const float* table_h, const float* table_l) {
+__device__ __forceinline__ Factor2 factor2(const MassRow& r) { return Factor2{both(r.ch), both(-r.ch), both(r.cl)}; }
+__device__ __forceinline__ Pair2 mass2(float x0, float x1, uint64_t m, const Factor2& r, const float* table) {
   const uint64_t x = f2pack(x0, x1);
-  const uint64_t d = fsub2(x, r.m), b = fsub2(d, x);
-  const uint64_t de = fadd2(fsub2(x, fsub2(d, b)), fsub2(r.nm, b));
+  const uint64_t d = fsub2(x, m), b = fsub2(d, x);
+  const uint64_t de = fsub2(fsub2(x, fsub2(d, b)), fadd2(m, b));
   const uint64_t ny = fmul2(d, r.nch);
   const uint64_t ye = fadd2(ffma2(d, r.ch, ny), ffma2(d, r.cl, fmul2(de, r.ch)));
   const uint64_t magic = ffma2(ny, both(-32.f), both(0x1.8p23f));
@@ -242,7 +174,7 @@ __device__ __forceinline__ Pair2 mass2(float x0, float x1, const MassRow2& r, co
   f2unpack(magic, magic0, magic1);
   f2unpack(ny, ny0, ny1);
   const int k0 = __float_as_int(magic0) - __float_as_int(0x1.8p23f), k1 = __float_as_int(magic1) - __float_as_int(0x1.8p23f);
-  const uint64_t th = f2pack(table_h[k0 & 31], table_h[k1 & 31]), tl = f2pack(table_l[k0 & 31], table_l[k1 & 31]);
+  const uint64_t th = f2pack(table[k0 & 31], table[k1 & 31]), tl = f2pack(table[32 + (k0 & 31)], table[32 + (k1 & 31)]);
   const uint64_t ph = fmul2(th, g), nph = fmul2(th, ng);
   const uint64_t pl = fadd2(ffma2(th, g, nph), ffma2(th, rest, ffma2(tl, g, tl)));
   const uint64_t h = fadd2(th, ph), l = fadd2(fsub2(ph, fsub2(h, th)), pl);
@@ -298,39 +230,318 @@ __device__ __forceinline__ long long warp_sum_ll(long long v) {
   return v;
 }
 
-// ---------------------------------------------------------------- decisions and the token
+// Adds to a count on the device, ordered after what the warp has stored (and __syncwarp) and before
+// what it loads from L2; returns the old count.
+__device__ __forceinline__ unsigned add_acq_rel(unsigned* p, unsigned v) {
+  unsigned old;
+  asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+  return old;
+}
 
-constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32;
-constexpr int kFinishPerSm = 3;
-constexpr int kGroupStep = 128;    // a group, the tokens of a warp, is a multiple of it
-constexpr int kGroupsMost = 1024;  // groups of a sequence, at most
+// ---------------------------------------------------------------- decisions
 
-enum { kFromTarget = 0, kWithout = 1, kResidual = 2 };  // r = p; p without token x; max(p - q, 0)
-
-struct RowStat {
-  Pair sum;
-  float top;
-  int first;
-  int ok;  // the row has a distribution
-};
+enum { kStands, kRefused, kNoDraft, kNoTarget };
 
 // u q(x) < p(x) from the logits alone, where the exponentials are too small for float pairs
-__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const RowStat& p, const RowStat& q) {
-  auto log_of = [t](float x, const RowStat& r) {
-    return (static_cast<double>(x) - static_cast<double>(r.top)) / t - log(static_cast<double>(r.sum.h) + static_cast<double>(r.sum.l));
+__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const VerifyRow& p, const VerifyRow& q) {
+  auto log_of = [t](float x, const VerifyRow& r) {
+    return (static_cast<double>(x) - static_cast<double>(r.top)) / t - log(static_cast<double>(r.sum_h) + static_cast<double>(r.sum_l));
   };
   const double lp = log_of(xp, p), lq = log_of(xq, q);
   return lp > -INFINITY && (lq == -INFINITY || u < exp(lp - lq));
 }
 
-__device__ __forceinline__ VerifyGroup load_group(const VerifyGroup* p) {
-  const longlong2 x = __ldcg(reinterpret_cast<const longlong2*>(p));
-  VerifyGroup g;
-  g.a = x.x;
-  g.d = x.y;
-  g.b = __ldcg(&p->b);
-  return g;
+// What a sequence's rows have in common.
+struct Sequence {
+  Temperature t;
+  MassRow factor;
+  bool soft, lookup;  // a temperature above 0; no draft rows
+  int s, n;           // n: drafts before the first that is no token
+};
+__device__ __forceinline__ Sequence sequence_with(const VerifyArgs& a, int s, const Temperature& t, int n) {
+  return Sequence{t, mass_row(t.t), !t.greedy && !t.bad, a.draft == nullptr, s, n};
 }
+// numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
+__device__ __forceinline__ float number_at(const VerifyArgs& a, int s, int j) {
+  return fminf(fmaxf(after_wait(a.uniform)[static_cast<size_t>(s) * (a.n + 1) + j], 0.f), 0x1.fffffep-1f);
+}
+template <typename T>
+__device__ __forceinline__ float logit_at(const VerifyArgs& a, int s, int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); }
+
+// What becomes of draft j < q.n (or kNoDraft, kNoTarget), with the logits of its token.
+__device__ __forceinline__ int verdict(const Sequence& q, int j, int draft, float u, float xp, float xq, const VerifyRow& p,
+                                       const VerifyRow& draft_row, const float* table) {
+  if (!p.ok) return kNoTarget;
+  if (j >= q.n) return kNoDraft;
+  if (q.t.greedy) return p.first == draft ? kStands : kRefused;
+  // u q(x) < p(x); where q(x) = 0: 0 < p(x)
+  const VerifyRow r = q.lookup ? VerifyRow{1.f, 0.f, 0.f, 0, 1} : draft_row;
+  if (!r.ok) return kNoDraft;
+  if (q.lookup) xq = r.top;
+  const Pair ep = mass(xp, with_top(q.factor, p.top), table), eq = mass(xq, with_top(q.factor, r.top), table);
+  const Pair z = sub(mul(Pair{u, 0.f}, mul(eq, Pair{p.sum_h, p.sum_l})), mul(ep, Pair{r.sum_h, r.sum_l}));
+  const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && u > 0x1p-30f;
+  return (near ? z.h + z.l < 0.f : stands_far(u, xp, xq, q.t.t, p, r)) ? kStands : kRefused;
+}
+
+// A row from its stretches, by `lanes` lanes (16 or 32) of a warp, the same in all of them.
+__device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, int n, int lanes, const Sequence& q, int V, const float* table) {
+  const int l = threadIdx.x & (lanes - 1);
+  auto chunk_at = [&](int i) {
+    const int4 v = __ldcg(reinterpret_cast<const int4*>(chunks) + i);
+    VerifyChunk c;
+    c.sum = static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(v.y)) << 32 | static_cast<unsigned>(v.x));
+    c.top = __int_as_float(v.z);
+    c.first = v.w;
+    return c;
+  };
+  VerifyChunk mine{0, -INFINITY, V};
+  if (l < n) mine = chunk_at(l);
+  float top = mine.top;
+  int bad = mine.first < 0;
+  for (int i = l + lanes; i < n; i += lanes) {
+    const VerifyChunk c = chunk_at(i);
+    top = fmaxf(top, c.top);
+    bad |= c.first < 0;
+  }
+  for (int o = lanes / 2; o > 0; o >>= 1) {
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    bad |= __shfl_xor_sync(0xffffffffu, bad, o);
+  }
+  Pair sum{0.f, 0.f};
+  int first = V;
+  for (int i = l; i < n; i += lanes) {
+    const VerifyChunk c = i == l ? mine : chunk_at(i);
+    if (q.t.greedy) {
+      if (c.top == top) first = min(first, c.first);
+    } else {
+      const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, with_top(q.factor, top), table));
+      if (c.top > -INFINITY) add(sum, v.h, v.l);
+    }
+  }
+  for (int o = lanes / 2; o > 0; o >>= 1) {
+    const float h = __shfl_xor_sync(0xffffffffu, sum.h, o), e = __shfl_xor_sync(0xffffffffu, sum.l, o);
+    add(sum, h, e);
+    first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
+  }
+  return VerifyRow{sum.h, sum.l, top, first, !q.t.bad && bad == 0 && top > -INFINITY};
+}
+
+// ---------------------------------------------------------------- the rows' maxima and sums
+
+constexpr int kScanThreads = 256, kScanValues = 32, kScanTokens = kScanThreads * kScanValues;
+
+// (64-bit floats are left out: the SM does two of their operations a clock.)
+// Sum over the warp of values in [0, 2^50) (two 32-bit reductions of 25 bits each).
+__device__ __forceinline__ unsigned long long warp_sum_u50(unsigned long long v) {
+  const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & 0x1ffffffu);
+  const unsigned hi = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v >> 25));
+  return (static_cast<unsigned long long>(hi) << 25) + lo;
+}
+
+// One stretch of a row.  Every warp takes its sum against its own maximum, so the warps meet
+// once; warp 0 then has the stretch.
+struct StretchParts {
+  float top[kScanThreads / 32];
+  unsigned long long sum[kScanThreads / 32];
+  int first[kScanThreads / 32];
+};
+template <typename T>
+__device__ __forceinline__ void load_stretch(const T* row, int chunk, int V, float (&x)[kScanValues]) {
+  constexpr int VEC = 16 / sizeof(T);
+  // the stretch starts on a 16-byte boundary, before the row's first token for the first one
+  const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+  const int t0 = chunk * kScanTokens - lead;
+#pragma unroll
+  for (int k = 0; k < kScanValues / VEC; ++k) {
+    const int at = t0 + (k * kScanThreads + static_cast<int>(threadIdx.x)) * VEC;
+    if (at >= 0 && at <= V - VEC) {
+      load16(row + at, x + k * VEC);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[k * VEC + i] = at + i >= 0 && at + i < V ? to_f<T>(row[at + i]) : -INFINITY;
+    }
+  }
+}
+// (returns whether the CTA has seen a NaN or +inf)
+template <typename T>
+__device__ __forceinline__ bool scan_stretch(const T* row, int chunk, int V, bool greedy, float c, const float (&x)[kScanValues],
+                                             StretchParts& parts) {
+  constexpr int VEC = 16 / sizeof(T);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float top = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < kScanValues; ++k) {
+    top = fmaxf(top, x[k]);
+    bad |= !(x[k] < INFINITY);
+  }
+  top = warp_max(top);
+  unsigned long long total = 0;
+  int first = V;
+  if (greedy) {
+    const int t0 = chunk * kScanTokens - static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+#pragma unroll
+    for (int k = kScanValues - 1; k >= 0; --k) {
+      const int at = t0 + ((k / VEC) * kScanThreads + tid) * VEC + k % VEC;
+      if (x[k] == top && at >= 0 && at < V) first = at;
+    }
+    first = __reduce_min_sync(0xffffffffu, first);
+  } else {
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kScanValues; ++k) sum[k & 3] += ex2((x[k] - ref) * c);
+    // (bad rows have any sum)
+    total = warp_sum_u50(static_cast<unsigned long long>(fminf((sum[0] + sum[1]) + (sum[2] + sum[3]), 64.f) * kSumScale));
+  }
+  if (lane == 0) parts.top[warp] = top, parts.sum[warp] = total, parts.first[warp] = first;
+  return __syncthreads_or(bad) != 0;
+}
+__device__ __forceinline__ VerifyChunk joined_stretch(const StretchParts& parts, bool bad, float c, int V) {  // warp 0
+  const int lane = threadIdx.x & 31;
+  const bool in = lane < kScanThreads / 32;
+  VerifyChunk out;
+  const float top = in ? parts.top[lane] : -INFINITY;
+  out.top = warp_max(top);
+  const unsigned long long total =
+      in && top > -INFINITY ? static_cast<unsigned long long>(static_cast<float>(parts.sum[lane]) * ex2((top - out.top) * c)) : 0;
+  out.sum = static_cast<long long>(warp_sum_u50(total));
+  out.first = __reduce_min_sync(0xffffffffu, in && top == out.top ? parts.first[lane] : V);
+  if (bad) out.first = -1;
+  return out;
+}
+
+// All rows at once.
+template <typename T>
+__global__ void __launch_bounds__(kScanThreads, 4) verify_scan_kernel(const __grid_constant__ VerifyArgs a) {
+  __shared__ StretchParts parts;
+  pdl_trigger();
+  pdl_wait();
+  const unsigned item = blockIdx.x / static_cast<unsigned>(a.chunks);
+  const int chunk = static_cast<int>(blockIdx.x - item * a.chunks);
+  const int s = static_cast<int>(item / static_cast<unsigned>(a.rows)), r = static_cast<int>(item - s * static_cast<unsigned>(a.rows));
+  if (r == 0 && chunk == 0 && threadIdx.x == 0) a.state[s].done = 0;
+  const Temperature t = temperature_of(a, s);
+  const bool is_draft = r > a.n;
+  if (t.bad || (t.greedy && is_draft)) return;  // rows that decide nothing
+  const int j = is_draft ? r - a.n - 1 : r;
+  if (j > 0 || is_draft) {
+    const int have = drafts_of(a, s);
+    if (j > have || (is_draft && j == have)) return;
+  }
+  const T* row = row_of<T>(a, s, r);
+  const float c = log2e_over(t.t);
+  float x[kScanValues];
+  load_stretch(row, chunk, a.V, x);
+  const bool bad = scan_stretch(row, chunk, a.V, t.greedy, c, x, parts);
+  if (threadIdx.x >= 32) return;
+  const VerifyChunk out = joined_stretch(parts, bad, c, a.V);
+  if (threadIdx.x == 0) a.stat[(static_cast<size_t>(s) * a.rows + r) * a.chunks + chunk] = out;
+}
+
+// Draft by draft over all sequences: a CTA takes one stretch of draft j's rows, the target's and the
+// draft's.  Warp 0 of the CTA that ends draft j decides it; what does not stand lowers the
+// sequence's stop.  A row is left out only where the stop lies before it, so the rows up to the
+// first draft that does not stand are all scanned, whatever the order in which CTAs run.
+template <typename T>
+__global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(const __grid_constant__ VerifyArgs a) {
+  __shared__ float table[64];
+  __shared__ StretchParts parts[2];
+  __shared__ int4 s_state;
+  pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31;
+  const unsigned level = static_cast<unsigned>(a.S) * a.chunks;
+  const int j = static_cast<int>(blockIdx.x / level);
+  const unsigned at = blockIdx.x - j * level;
+  const int s = static_cast<int>(at / a.chunks), chunk = static_cast<int>(at - s * a.chunks);
+  pdl_wait();
+  VerifyState* state = after_wait(a.state) + s;
+  if (tid == 0) s_state = __ldcg(reinterpret_cast<const int4*>(state));  // (one thread looks: the stop may fall meanwhile)
+  __syncthreads();
+  const int4 v = s_state;
+  if (v.x < j) return;
+  const int n = v.y;
+  const bool soft = v.z != 0, two = soft && a.draft != nullptr && j < n;
+  const float temperature = __int_as_float(v.w), c = log2e_over(temperature);
+  const T *row = row_of<T>(a, s, j), *draft_row = two ? row_of<T>(a, s, a.n + 1 + j) : row;
+  float x[kScanValues], y[kScanValues];
+  load_stretch(row, chunk, a.V, x);
+  if (two) load_stretch(draft_row, chunk, a.V, y);
+  if (tid < 64) table[tid] = kPowers.v[tid];
+  const bool bad = scan_stretch(row, chunk, a.V, !soft, c, x, parts[0]);
+  const bool draft_bad = two && scan_stretch(draft_row, chunk, a.V, false, c, y, parts[1]);
+  if (tid >= 32) return;
+  VerifyChunk* stat = a.stat + static_cast<size_t>(s) * a.rows * a.chunks;
+  VerifyChunk *p_stat = stat + static_cast<size_t>(j) * a.chunks, *d_stat = stat + static_cast<size_t>(a.n + 1 + j) * a.chunks;
+  const VerifyChunk p_out = joined_stretch(parts[0], bad, c, a.V);
+  VerifyChunk d_out{};
+  if (two) d_out = joined_stretch(parts[1], draft_bad, c, a.V);
+  int last = 0;
+  if (lane == 0) {
+    p_stat[chunk] = p_out;
+    if (two) d_stat[chunk] = d_out;
+    last = add_acq_rel(&state->scanned[j], 1u) == static_cast<unsigned>(a.chunks) - 1;
+  }
+  __syncwarp();
+  if (__shfl_sync(0xffffffffu, last, 0) == 0) return;
+  // this stretch was draft j's last
+  const Sequence q = sequence_with(a, s, Temperature{temperature, !soft, false}, n);
+  VerifyRow p, d{0.f, 0.f, 0.f, 0, 0};
+  int draft = 0;
+  float u = 0.f, xp = 0.f, xq = 0.f;
+  if (j < n) {
+    draft = after_wait(a.drafts)[static_cast<size_t>(s) * a.n + j];
+    u = number_at(a, s, j);
+    xp = to_f<T>(row[draft]);
+    if (two) xq = to_f<T>(draft_row[draft]);
+  }
+  if (two && a.chunks <= 16) {  // (the warp's halves take a row each)
+    const VerifyRow mine = row_total(lane < 16 ? p_stat : d_stat, a.chunks, 16, q, a.V, table);
+    auto from = [&](int at) {
+      return VerifyRow{__shfl_sync(0xffffffffu, mine.sum_h, at), __shfl_sync(0xffffffffu, mine.sum_l, at),
+                       __shfl_sync(0xffffffffu, mine.top, at), __shfl_sync(0xffffffffu, mine.first, at), __shfl_sync(0xffffffffu, mine.ok, at)};
+    };
+    p = from(0);
+    d = from(16);
+  } else {
+    p = row_total(p_stat, a.chunks, 32, q, a.V, table);
+    if (two) d = row_total(d_stat, a.chunks, 32, q, a.V, table);
+  }
+  const int what = verdict(q, j, draft, u, xp, xq, p, d, table);
+  if (lane == 0) {
+    state->target[j] = p;
+    state->draft[j] = d;
+    state->why[j] = what;
+    if (what != kStands) atomicMin(&state->stop, j);
+  }
+}
+
+__global__ void verify_start_kernel(const __grid_constant__ VerifyArgs a) {
+  pdl_trigger();
+  pdl_wait();
+  const int s = static_cast<int>(blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5));
+  if (s >= a.S) return;
+  const Temperature t = temperature_of(a, s);
+  const int n = drafts_of(a, s), lane = threadIdx.x & 31;
+  VerifyState* state = a.state + s;
+  if (lane <= kVerifyMaxDrafts) state->scanned[lane] = 0;
+  if (lane != 0) return;
+  state->stop = t.bad ? -1 : n;
+  state->n = n;
+  state->soft = !t.greedy;
+  state->temperature = t.t;
+  state->done = 0;
+}
+
+// ---------------------------------------------------------------- the token
+
+constexpr int kFinishWarps = kVerifyWarps, kFinishThreads = 32 * kFinishWarps, kFinishPerSm = 4;
+constexpr int kWarpStep = 128, kGroupStep = kFinishWarps * kWarpStep;  // a group, the tokens of a CTA, is a multiple of it
+constexpr int kGroupsMost = 128;                // groups of a sequence, at most
+
+enum { kFromTarget = 0, kWithout = 1, kResidual = 2 };  // r = p; p without token x; max(p - q, 0)
+
 
 // floor(u total), u in [0, 1)
 __device__ __forceinline__ long long goal_of(float u, long long total) {
@@ -340,202 +551,164 @@ __device__ __forceinline__ long long goal_of(float u, long long total) {
   return 24 - e > 127 ? 0 : static_cast<long long>(v >> (24 - e));
 }
 
-template <typename T>
+__device__ __forceinline__ long long running_sum(long long v) {  // over the warp's lanes, own one included
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+
+// Rows by draft in the calls that scan in turn (decided there), else worked out here.
+template <typename T, bool DECIDED>
 __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
-    verify_finish_kernel(const __grid_constant__ VerifyArgs a, int rows, int ctas, int group, float unit) {
-  __shared__ float table_h[32], table_l[32];
-  __shared__ RowStat stat[2 * kVerifyMaxDrafts + 1];
-  __shared__ int s_stop, s_why;
-  __shared__ long long s_part[kFinishWarps], s_before;
-  __shared__ int s_first[kFinishWarps], s_some[kFinishWarps], s_group, s_last;
+    verify_finish_kernel(const __grid_constant__ VerifyArgs a, int ctas, int group, float unit) {
+  __shared__ float table[64];
+  __shared__ VerifyRow target[kVerifyMaxDrafts + 1], draft_rows[kVerifyMaxDrafts + 1];
+  __shared__ int s_stop, s_why, s_last, s_first[kFinishWarps], s_some[kFinishWarps];
+  __shared__ long long s_part[2][kFinishWarps];
+  __shared__ float s_b[kFinishWarps];
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int s = static_cast<int>(blockIdx.x) / ctas, cta = static_cast<int>(blockIdx.x) - s * ctas;
-  if (tid < 32) {
-    const double e = exp2(tid / 32.0);
-    table_h[tid] = static_cast<float>(e);
-    table_l[tid] = static_cast<float>(e - static_cast<double>(table_h[tid]));
-  }
+  if (tid < 64) table[tid] = kPowers.v[tid];
   __syncthreads();
   pdl_wait();
-  // one round trip: temperature, drafts, numbers, the rows' stretches; then the drafts' logits
-  const Temperature t = temperature_of(a, s);
-  const int n = drafts_of(a, s);
-  const bool lookup = a.draft == nullptr, soft = !t.greedy && !t.bad;
-  const int32_t* drafts = after_wait(a.drafts) + static_cast<size_t>(s) * a.n;
-  const float* uniform = after_wait(a.uniform) + static_cast<size_t>(s) * (a.n + 1);
-  // numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
-  auto number = [&](int j) { return fminf(fmaxf(uniform[j], 0.f), 0x1.fffffep-1f); };
-  auto logit = [&](int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); };
-  const float u = number(a.n);
-  float my_u = 0.f, xp = 0.f, xq = 0.f;
+  VerifyState* state = after_wait(a.state) + s;
+  const float u = number_at(a, s, a.n);
+  Temperature t;
+  int n, stop, why;
+  if constexpr (DECIDED) {
+    const int4 v = *reinterpret_cast<const int4*>(state);
+    if (tid <= a.n) target[tid] = state->target[tid], draft_rows[tid] = state->draft[tid];  // (rows left out: anything)
+    t = Temperature{__int_as_float(v.w), v.z == 0, v.x < 0};
+    n = v.y;
+    stop = max(v.x, 0);
+    why = t.bad ? kNoTarget : state->why[stop];
+  } else {
+    t = temperature_of(a, s);
+    n = drafts_of(a, s);
+  }
+  const Sequence q = sequence_with(a, s, t, n);
   int my_draft = -1;
-  if (tid < n) {
-    my_draft = drafts[tid];
-    my_u = number(tid);
-    xp = logit(tid, my_draft);
-    if (!lookup && soft) xq = logit(a.n + 1 + tid, my_draft);
+  if (tid < q.n) my_draft = after_wait(a.drafts)[static_cast<size_t>(s) * a.n + tid];
+  if constexpr (DECIDED) {
+    __syncthreads();
+  } else {
+    float my_u = 0.f, xp = 0.f, xq = 0.f;
+    if (tid < q.n) {
+      my_u = number_at(a, s, tid);
+      xp = logit_at<T>(a, s, tid, my_draft);
+      if (!q.lookup && q.soft) xq = logit_at<T>(a, s, a.n + 1 + tid, my_draft);
+    }
+    const VerifyChunk* stat = after_wait(a.stat) + static_cast<size_t>(s) * a.rows * a.chunks;
+    const int lanes = a.chunks <= 16 ? 16 : 32, per_warp = 32 / lanes;
+    for (int r0 = warp * per_warp; r0 < a.rows; r0 += kFinishWarps * per_warp) {
+      const int r = min(r0 + lane / lanes, a.rows - 1);
+      const VerifyRow row = row_total(stat + static_cast<size_t>(r) * a.chunks, a.chunks, lanes, q, a.V, table);
+      if ((lane & (lanes - 1)) == 0) (r <= a.n ? target[r] : draft_rows[r - a.n - 1]) = row;
+    }
+    __syncthreads();
+    if (warp == 0) {  // (lane j: draft j)
+      const int j = min(lane, a.n);
+      int what = verdict(q, j, my_draft, my_u, xp, xq, target[j], draft_rows[j], table);
+      const int first = __ffs(__ballot_sync(0xffffffffu, what != kStands || lane >= a.n)) - 1;
+      what = __shfl_sync(0xffffffffu, what, first);
+      if (lane == 0) s_stop = first, s_why = what;
+    }
+    __syncthreads();
+    stop = s_stop;
+    why = s_why;
   }
-  const int4* chunks = after_wait(reinterpret_cast<const int4*>(a.stat)) + static_cast<size_t>(s) * rows * a.chunks;
-  auto chunk_at = [&](int r, int i) {
-    const int4 v = chunks[static_cast<size_t>(r) * a.chunks + i];
-    VerifyChunk c;
-    c.sum = static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(v.y)) << 32 | static_cast<unsigned>(v.x));
-    c.top = __int_as_float(v.z);
-    c.first = v.w;
-    return c;
-  };
-
-  // every row's maximum and sum, of 16 or 32 lanes (rows that the scan left out: anything)
-  const int lanes = a.chunks <= 16 ? 16 : 32, per_warp = 32 / lanes;
-  for (int r0 = warp * per_warp; r0 < rows; r0 += kFinishWarps * per_warp) {
-    const int r = min(r0 + lane / lanes, rows - 1), l = lane & (lanes - 1);
-    float top = -INFINITY;
-    int bad = 0;
-    for (int i = l; i < a.chunks; i += lanes) {
-      const VerifyChunk c = chunk_at(r, i);
-      top = fmaxf(top, c.top);
-      bad |= c.first < 0;
-    }
-    for (int o = lanes / 2; o > 0; o >>= 1) {
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      bad |= __shfl_xor_sync(0xffffffffu, bad, o);
-    }
-    Pair sum{0.f, 0.f};
-    int first = a.V;
-    const MassRow m = mass_row(top, t.t);
-    for (int i = l; i < a.chunks; i += lanes) {
-      const VerifyChunk c = chunk_at(r, i);
-      if (t.greedy) {
-        if (c.top == top) first = min(first, c.first);
-      } else {
-        const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, m, table_h, table_l));
-        if (c.top > -INFINITY) add(sum, v.h, v.l);
-      }
-    }
-    for (int o = lanes / 2; o > 0; o >>= 1) {
-      const float h = __shfl_xor_sync(0xffffffffu, sum.h, o), e = __shfl_xor_sync(0xffffffffu, sum.l, o);
-      add(sum, h, e);
-      first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
-    }
-    if (l == 0 && r0 + lane / lanes < rows) stat[r] = RowStat{sum, top, first, !t.bad && bad == 0 && top > -INFINITY};
-  }
-  __syncthreads();
   // log p of a token of row r with the logit x: (x - top) / t - log(sum), the rounding errors of
   // each kept: log(sum) = g + log(sum exp(-g)) with g near it, and the latter is its argument less 1
   auto log_p = [&](int r, float x) {
-    const RowStat& row = stat[r];
-    const float g = logf(row.sum.h);
-    const Pair e = mul(row.sum, mass(-g, mass_row(0.f, 1.f), table_h, table_l));
+    const VerifyRow& row = target[r];
+    const float g = logf(row.sum_h);
+    const Pair e = mul(Pair{row.sum_h, row.sum_l}, mass(-g, mass_row(1.f), table));
     const float d = x - row.top, b = d - x, de = (x - (d - b)) + (-row.top - b);
-    const float h = d / t.t, l = (fmaf(-h, t.t, d) + de) / t.t;
+    const float h = d / q.t.t, l = (fmaf(-h, q.t.t, d) + de) / q.t.t;
     const Pair z = sub(Pair{h, l}, Pair{g, (e.h - 1.f) + e.l});
     return h > -INFINITY ? z.h + z.l : h;
   };
-  enum { kStands, kRefused, kNoDraft, kNoTarget };
-  if (warp == 0) {  // (lane j: draft j)
-    int what = kNoDraft;
-    const RowStat p = stat[min(lane, a.n)];
-    if (!p.ok) {
-      what = kNoTarget;
-    } else if (lane < n) {
-      if (t.greedy) {
-        what = p.first == my_draft ? kStands : kRefused;
-      } else {
-        // u q(x) < p(x); where q(x) = 0: 0 < p(x)
-        const RowStat q = lookup ? RowStat{{1.f, 0.f}, 0.f, 0, 1} : stat[a.n + 1 + lane];
-        if (q.ok) {
-          const Pair ep = mass(xp, mass_row(p.top, t.t), table_h, table_l), eq = mass(xq, mass_row(q.top, t.t), table_h, table_l);
-          const Pair z = sub(mul(Pair{my_u, 0.f}, mul(eq, p.sum)), mul(ep, q.sum));
-          const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && my_u > 0x1p-30f;
-          what = (near ? z.h + z.l < 0.f : stands_far(my_u, xp, xq, t.t, p, q)) ? kStands : kRefused;
-        }
-      }
-    }
-    const int stop = __ffs(__ballot_sync(0xffffffffu, what != kStands || lane >= a.n)) - 1;
-    what = __shfl_sync(0xffffffffu, what, stop);
-    if (lane == 0) s_stop = stop, s_why = what;
-  }
-  __syncthreads();
-  const int stop = s_stop, why = s_why;
   int32_t* tokens = a.tokens + static_cast<size_t>(s) * (a.n + 1);
   float* logp = a.logp != nullptr ? a.logp + static_cast<size_t>(s) * (a.n + 1) : nullptr;
   if (cta == 0) {
     if (tid <= a.n && tid != stop) {
       tokens[tid] = tid < stop ? my_draft : -1;
-      if (logp != nullptr) logp[tid] = tid < stop && soft ? log_p(tid, xp) : 0.f;
+      if (logp != nullptr) logp[tid] = tid < stop && q.soft ? log_p(tid, logit_at<T>(a, s, tid, my_draft)) : 0.f;
     }
     if (tid == 0) {
       a.accepted[s] = stop;
       if (a.lens_out != nullptr) a.lens_out[s] = max(after_wait(a.lens)[s] - (a.n - stop), 0);
-      if (why == kNoTarget || t.greedy) {
-        tokens[stop] = why == kNoTarget ? -1 : stat[stop].first;
+      if (why == kNoTarget || q.t.greedy) {
+        tokens[stop] = why == kNoTarget ? -1 : target[stop].first;
         if (logp != nullptr) logp[stop] = 0.f;
       }
     }
   }
-  if (why == kNoTarget || t.greedy) return;  // (the same for all CTAs of the sequence)
+  if (why == kNoTarget || q.t.greedy) return;  // (the same for all CTAs of the sequence)
 
-  const int kind = why == kNoDraft ? kFromTarget : lookup ? kWithout : kResidual;
+  const int kind = why == kNoDraft ? kFromTarget : q.lookup ? kWithout : kResidual;
+  const VerifyRow row = target[stop], other = draft_rows[stop];
   const T* row_p = row_of<T>(a, s, stop);
   const T* row_q = kind == kResidual ? row_of<T>(a, s, a.n + 1 + stop) : row_p;
-  const int refused = kind == kFromTarget ? -1 : drafts[stop];
-  const MassRow mp = mass_row(stat[stop].top, t.t);
-  const MassRow mq = kind == kResidual ? mass_row(stat[a.n + 1 + stop].top, t.t) : mp;
-  const Pair ratio = kind == kResidual ? div(stat[stop].sum, stat[a.n + 1 + stop].sum) : Pair{0.f, 0.f};
+  const int refused = kind == kFromTarget ? -1 : after_wait(a.drafts)[static_cast<size_t>(s) * a.n + stop];
+  const MassRow mp = with_top(q.factor, row.top), mq = with_top(q.factor, other.top);
+  const Pair ratio = kind == kResidual ? div(Pair{row.sum_h, row.sum_l}, Pair{other.sum_h, other.sum_l}) : Pair{0.f, 0.f};
 
-  // this CTA's slice, a group of tokens per warp
-  const int groups = ctas * kFinishWarps;
-  VerifyGroup* sums = a.groups + static_cast<size_t>(s) * groups;
+  // this CTA's group of tokens
+  VerifyGroup* sums = a.groups + static_cast<size_t>(s) * ctas;
   {
-    const long long g0 = (static_cast<long long>(cta) * kFinishWarps + warp) * group;
-    const MassRow2 p2 = mass_row2(mp);
+    // (a warp has neighbouring tokens, a lane every 32nd of them)
+    const int share = group / kFinishWarps;
+    const long long g0 = static_cast<long long>(cta) * group + static_cast<long long>(warp) * share + lane;
+    const int left = static_cast<int>(min(static_cast<long long>(share), a.V - g0));  // (from this lane's first token on)
+    const Factor2 f2 = factor2(q.factor);
+    const uint64_t m2 = both(row.top);
     Pair2 plus{0, 0}, all{0, 0};
     float b = 0.f;
-    auto load = [&](const T* row, int i0, float (&x)[4]) {
+    auto load = [&](const T* from, int i0, float (&x)[4]) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const long long at = g0 + i0 + 32 * k + lane;
-        x[k] = i0 < group && at < a.V ? to_f<T>(row[at]) : -INFINITY;
+        const int i = i0 + k * 32;
+        x[k] = i < left ? to_f<T>(from[g0 + i]) : -INFINITY;
       }
     };
-    float x[4], next[4];
-    load(row_p, 0, x);
     if (kind == kResidual) {
-      const MassRow2 q2 = mass_row2(mq);
-      const uint64_t ch = both(ratio.h), nch = both(-ratio.h), cl = both(ratio.l);
-      float y[4], next_y[4];
-      load(row_q, 0, y);
-      for (int i0 = 0; i0 < group; i0 += 128) {
-        load(row_p, i0 + 128, next);
-        load(row_q, i0 + 128, next_y);
+      const uint64_t mq2 = both(other.top), ch = both(ratio.h), nch = both(-ratio.h), cl = both(ratio.l);
+      for (int i0 = 0; i0 < share; i0 += kWarpStep) {
+        float x[4], y[4];
+        load(row_p, i0, x);
+        load(row_q, i0, y);
 #pragma unroll
         for (int k = 0; k < 4; k += 2) {
-          const Pair2 q = mass2(y[k], y[k + 1], q2, table_h, table_l);
-          const Pair2 d = less2(mass2(x[k], x[k + 1], p2, table_h, table_l), q, ch, nch, cl);
+          const Pair2 e = mass2(y[k], y[k + 1], mq2, f2, table);
+          const Pair2 d = less2(mass2(x[k], x[k + 1], m2, f2, table), e, ch, nch, cl);
           add2(all, d.h, d.l);
           float s0, s1, h0, h1, l0, l1, q0, q1;
           f2unpack(fadd2(d.h, d.l), s0, s1);
           f2unpack(d.h, h0, h1);
           f2unpack(d.l, l0, l1);
-          f2unpack(q.h, q0, q1);
+          f2unpack(e.h, q0, q1);
           add2(plus, f2pack(s0 > 0.f ? h0 : 0.f, s1 > 0.f ? h1 : 0.f), f2pack(s0 > 0.f ? l0 : 0.f, s1 > 0.f ? l1 : 0.f));
           b += (s0 > 0.f ? q0 : 0.f) + (s1 > 0.f ? q1 : 0.f);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = next[k], y[k] = next_y[k];
       }
     } else {
-      for (int i0 = 0; i0 < group; i0 += 128) {
-        load(row_p, i0 + 128, next);
+      const long long skip = refused - g0;  // the refused token among this thread's
+      for (int i0 = 0; i0 < share; i0 += kWarpStep) {
+        float x[4];
+        load(row_p, i0, x);
 #pragma unroll
         for (int k = 0; k < 4; k += 2) {
-          const long long at = g0 + i0 + 32 * k + lane;
-          const Pair2 p = mass2(at == refused ? -INFINITY : x[k], at + 32 == refused ? -INFINITY : x[k + 1], p2, table_h, table_l);
-          add2(plus, p.h, p.l);
+          const int i = i0 + k * 32;
+          const Pair2 e = mass2(i == skip && refused >= 0 ? -INFINITY : x[k],
+                                i + 32 == skip && refused >= 0 ? -INFINITY : x[k + 1], m2, f2, table);
+          add2(plus, e.h, e.l);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = next[k];
       }
     }
     // the two tokens' sums, in units
@@ -545,128 +718,127 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
       f2unpack(v.l, l0, l1);
       return warp_sum_ll(fixed(Pair{h0, l0}, unit) + fixed(Pair{h1, l1}, unit));
     };
-    VerifyGroup out;
-    out.a = joined(plus);
-    out.d = kind == kResidual ? joined(all) : 0;
-    out.b = warp_sum(b);
-    if (lane == 0) sums[cta * kFinishWarps + warp] = out;
+    const long long sum_a = joined(plus), sum_d = kind == kResidual ? joined(all) : 0;
+    b = warp_sum(b);
+    if (lane == 0) s_part[0][warp] = sum_a, s_part[1][warp] = sum_d, s_b[warp] = b;
   }
-  __threadfence();
   __syncthreads();
-  if (tid == 0) {
-    s_last = atomicAdd(a.done + s, 1u) == static_cast<unsigned>(ctas) - 1;
-    __threadfence();
+  if (warp == 0) {
+    const bool in = lane < kFinishWarps;
+    const long long part_a = in ? s_part[0][lane] : 0;
+    const float part_b = in ? s_b[lane] : 0.f;
+    const long long sum_a = warp_sum_ll(part_a), sum_d = warp_sum_ll(in ? s_part[1][lane] : 0);
+    const float b = warp_sum(part_b);
+    VerifyGroup* g = sums + cta;
+    if (in) g->warp_a[lane] = part_a, g->warp_b[lane] = part_b;
+    if (lane == 0) g->a = sum_a, g->d = sum_d, g->b = b;
+    __syncwarp();
+    if (lane == 0) s_last = add_acq_rel(&state->done, 1u) == static_cast<unsigned>(ctas) - 1;
   }
   __syncthreads();
   if (!s_last) return;
 
-  // The last CTA: k, the running sums of the groups, the group that holds the number, its token.
-  // Of values in the order of the threads: the thread where the running sum, on top of
-  // `offset`, first exceeds the goal (u times the whole sum where it is below 0).  Groups and
-  // tokens are rounded apart: where none exceeds it, the last one with any.
-  struct Pick {
-    int who;  // or -1
-    long long before, goal;
-  };
-  auto pick = [&](long long mine, long long offset, long long goal) {
-    long long run = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xffffffffu, run, o);
-      if (lane >= o) run += x;
-    }
-    __syncthreads();  // (what the last pick left has been read)
-    if (lane == 31) s_part[warp] = run;
-    __syncthreads();
-    long long total = 0, base = offset;
-#pragma unroll
-    for (int w = 0; w < kFinishWarps; ++w) {
-      if (w < warp) base += s_part[w];
-      total += s_part[w];
-    }
-    if (goal < 0) goal = goal_of(u, total);
-    const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
-    const unsigned above = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
-    if (lane == 0) s_first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1, s_some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
-    __syncthreads();
-    int who = -1, last = -1;
-#pragma unroll
-    for (int w = kFinishWarps - 1; w >= 0; --w) {
-      if (s_first[w] >= 0) who = s_first[w];
-      if (last < 0) last = s_some[w];
-    }
-    who = who >= 0 ? who : last;
-    if (tid == who) s_before = base + (run - mine);
-    __syncthreads();
-    return Pick{who, s_before, goal};
-  };
-  constexpr int EACH = kGroupsMost / kFinishThreads;  // groups of a thread
-  const int each = (groups + kFinishThreads - 1) / kFinishThreads, g0 = tid * each;
-  VerifyGroup mine_g[EACH];
+  // The last CTA: k, the running sums of the groups (each warp for itself, neighbouring groups to
+  // a lane), the group that holds the number, the warp's share of it that does, its token.  The
+  // place looked for is the first whose running sum exceeds u times the whole.  Groups, shares and
+  // tokens are rounded apart: where none does, it is the last one with any.
+  constexpr int EACH = kGroupsMost / 32;
+  long long group_a[EACH], sd = 0, mine = 0;
+  float group_b[EACH];
+  const int each = (ctas + 31) / 32, first_g = lane * each;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    mine_g[i] = VerifyGroup{0, 0, 0.f};
-    if (i < each && g0 + i < groups) mine_g[i] = load_group(sums + g0 + i);
+    group_a[i] = 0;
+    group_b[i] = 0.f;
+    if (i < each && first_g + i < ctas) {
+      const VerifyGroup* g = sums + first_g + i;
+      const longlong2 x = __ldcg(reinterpret_cast<const longlong2*>(g));
+      group_a[i] = x.x;
+      sd += x.y;
+      group_b[i] = __ldcg(&g->b);
+    }
   }
-  float k = 0.f;
-  if (kind == kResidual) {
-    long long sd = 0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) sd += mine_g[i].d;
-    sd = warp_sum_ll(sd);
-    if (lane == 0) s_part[warp] = sd;
-    __syncthreads();
-    sd = 0;
-#pragma unroll
-    for (int w = 0; w < kFinishWarps; ++w) sd += s_part[w];
-    k = static_cast<float>(sd) / unit / stat[a.n + 1 + stop].sum.h;
-  }
-  long long mine = 0;
+  const float k = kind == kResidual ? __ll2float_rn(warp_sum_ll(sd)) / (unit * other.sum_h) : 0.f;
+  auto corrected = [&](long long part, float b) { return max(part - __float2ll_rn(k * b * unit), 0ll); };
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
-    mine_g[i].a = max(mine_g[i].a - __float2ll_rn(k * mine_g[i].b * unit), 0ll);
-    mine += mine_g[i].a;
+    group_a[i] = corrected(group_a[i], group_b[i]);
+    mine += group_a[i];
   }
-  Pick at = pick(mine, 0, -1);
-  // nothing is left of p - q, as far as can be told: the token is drawn from p, by this CTA alone
-  const bool plain = at.who < 0;
+  long long run = running_sum(mine), goal = goal_of(u, __shfl_sync(0xffffffffu, run, 31)), before = 0;
+  // the lane of the place looked for, among lanes with running sums `sum` that end with `part` of their own
+  auto lane_of = [&](long long part, long long sum) {
+    const unsigned some = __ballot_sync(0xffffffffu, part > 0), above = __ballot_sync(0xffffffffu, part > 0 && sum > goal);
+    return above != 0 ? __ffs(above) - 1 : 31 - __clz(some);
+  };
+  // (nothing is left of p - q, as far as can be told: the token is drawn from p, by this CTA alone)
+  int who = lane_of(mine, run);
+  const bool plain = who < 0;
   long long lo = 0;
   int count = a.V;
   if (!plain) {
-    if (tid == at.who) {
-      long long before = at.before;
-      bool found = false;
+    int at = 0;
+    before = run - mine;
+    long long at_before = before;
+    bool found = false;
 #pragma unroll
-      for (int i = 0; i < EACH; ++i) {
-        if (found || mine_g[i].a == 0) continue;
-        s_group = g0 + i;
-        s_before = before;
-        before += mine_g[i].a;
-        found = before > at.goal;
-      }
+    for (int i = 0; i < EACH; ++i) {
+      if (found || group_a[i] == 0) continue;
+      at = first_g + i;
+      at_before = before;
+      before += group_a[i];
+      found = before > goal;
     }
-    __syncthreads();
-    lo = static_cast<long long>(s_group) * group;
-    count = static_cast<int>(min(static_cast<long long>(group), a.V - lo));
-    at.before = s_before;
+    at = __shfl_sync(0xffffffffu, at, who);
+    before = __shfl_sync(0xffffffffu, at_before, who);
+    const VerifyGroup* g = sums + at;
+    const long long part = lane < kFinishWarps ? corrected(__ldcg(&g->warp_a[lane]), __ldcg(&g->warp_b[lane])) : 0;
+    run = before + running_sum(part);
+    who = max(lane_of(part, run), 0);
+    before = __shfl_sync(0xffffffffu, run - part, who);
+    const int share = group / kFinishWarps;
+    lo = static_cast<long long>(at) * group + static_cast<long long>(who) * share;
+    count = static_cast<int>(max(min(static_cast<long long>(share), a.V - lo), 1ll));
   }
   // a token's share of the sum
   auto token_left = [&](long long i, float& x) {
     x = to_f<T>(row_p[i]);
-    const Pair p = mass(x, mp, table_h, table_l);
+    const Pair p = mass(x, mp, table);
     if (plain || kind != kResidual) return !plain && i == refused ? 0ll : fixed(p, unit);
-    const Pair q = mass(to_f<T>(row_q[i]), mq, table_h, table_l);
-    Pair d = sub(p, mul(q, ratio));
-    d.l -= k * q.h;
+    const Pair e = mass(to_f<T>(row_q[i]), mq, table);
+    Pair d = sub(p, mul(e, ratio));
+    d.l -= k * e.h;
     return max(fixed(d, unit), 0ll);
   };
   const int per = (count + kFinishThreads - 1) / kFinishThreads, t0 = min(tid * per, count), t1 = min(t0 + per, count);
-  mine = 0;
   float x = 0.f;
+  mine = 0;
   for (int i = t0; i < t1; ++i) mine += token_left(lo + i, x);
-  at = plain ? pick(mine, 0, -1) : pick(mine, at.before, at.goal);
-  if (tid == max(at.who, 0)) {
-    long long before = at.before;
+  run = running_sum(mine);
+  if (lane == 31) s_part[0][warp] = run;
+  __syncthreads();
+  long long base = before, total = 0;
+#pragma unroll
+  for (int w = 0; w < kFinishWarps; ++w) {
+    if (w < warp) base += s_part[0][w];
+    total += s_part[0][w];
+  }
+  if (plain) goal = goal_of(u, total);
+  const unsigned some_t = __ballot_sync(0xffffffffu, mine > 0), above_t = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
+  if (lane == 0) s_first[warp] = above_t != 0 ? tid + __ffs(above_t) - 1 : -1, s_some[warp] = some_t != 0 ? tid + 31 - __clz(some_t) : -1;
+  __syncthreads();
+  int last = 0;
+  who = -1;
+#pragma unroll
+  for (int w = kFinishWarps - 1; w >= 0; --w) {
+    if (s_first[w] >= 0) who = s_first[w];
+  }
+#pragma unroll
+  for (int w = 0; w < kFinishWarps; ++w) {
+    if (s_some[w] >= 0) last = s_some[w];
+  }
+  if (tid == (who >= 0 ? who : last)) {
+    before = base + run - mine;
     int token = -1;
     float chosen = 0.f;
     for (int i = t0; i < t1; ++i) {
@@ -675,7 +847,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
       token = static_cast<int>(lo + i);
       chosen = x;
       before += v;
-      if (before > at.goal) break;
+      if (before > goal) break;
     }
     // (a group whose sum is more than 0 only by rounding: its last token)
     if (token < 0) token = static_cast<int>(lo) + count - 1, chosen = to_f<T>(row_p[token]);
@@ -684,15 +856,37 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
   }
 }
 
+// CTAs of a sequence and tokens of a CTA: the shortest groups that come to no more than two
+// rounds of the CTAs that run at once.
+struct VerifySlices {
+  int ctas, group;
+};
+VerifySlices verify_slices(int S, int V, int sms) {
+  const long long at_most = 1ll * kFinishPerSm * sms, all = (V + kGroupStep - 1) / kGroupStep;
+  const long long steps = std::min(all, std::max((all + kGroupsMost - 1) / kGroupsMost, (S * all + at_most - 1) / at_most));
+  return VerifySlices{static_cast<int>((all + steps - 1) / steps), static_cast<int>(steps) * kGroupStep};
+}
+
+// Whether rows are scanned in turn.
+bool in_turn(const VerifyArgs& a, int sms) {
+  return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 8ll * 4 * sms;
+}
+
 template <typename T>
-cudaError_t run_verify(const VerifyArgs& a, const VerifySlices& c, cudaStream_t s) {
-  const int rows = a.n + 1 + (a.draft != nullptr ? a.n : 0);
-  const unsigned grid = static_cast<unsigned>(a.S) * rows * a.chunks;
-  ZSAA_LAUNCH(verify_scan_kernel<T>, dim3(grid), dim3(kScanThreads), 0, s, a, rows);
-  int bits = 0;  // units in which sums of up to V exponentials stay below 2^62
+cudaError_t run_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
+  const VerifySlices c = verify_slices(a.S, a.V, sms);
+  int bits = 10;  // units in which sums of up to V exponentials stay below 2^62
   while ((1 << bits) < a.V) ++bits;
-  ZSAA_LAUNCH(verify_finish_kernel<T>, dim3(static_cast<unsigned>(a.S) * c.ctas), dim3(kFinishThreads), 0, s, a, rows, c.ctas,
-              c.group, std::ldexp(1.f, 62 - std::max(bits, 10)));
+  const float unit = std::ldexp(1.f, 62 - bits);
+  const dim3 grid(static_cast<unsigned>(a.S) * a.rows * a.chunks), finish(static_cast<unsigned>(a.S) * c.ctas);
+  if (in_turn(a, sms)) {
+    ZSAA_LAUNCH(verify_start_kernel, dim3((a.S + 7) / 8), dim3(256), 0, s, a);
+    ZSAA_LAUNCH(verify_scan_in_turn_kernel<T>, dim3(static_cast<unsigned>(a.S) * (a.n + 1) * a.chunks), dim3(kScanThreads), 0, s, a);
+    ZSAA_LAUNCH((verify_finish_kernel<T, true>), finish, dim3(kFinishThreads), 0, s, a, c.ctas, c.group, unit);
+  } else {
+    ZSAA_LAUNCH(verify_scan_kernel<T>, grid, dim3(kScanThreads), 0, s, a);
+    ZSAA_LAUNCH((verify_finish_kernel<T, false>), finish, dim3(kFinishThreads), 0, s, a, c.ctas, c.group, unit);
+  }
   return cudaSuccess;
 }
 
@@ -700,19 +894,10 @@ cudaError_t run_verify(const VerifyArgs& a, const VerifySlices& c, cudaStream_t 
 
 // one more than the tokens fill: a row may start inside a 16-byte block
 int verify_chunks(int V) { return (V + 7 + kScanTokens - 1) / kScanTokens; }
-
-// CTAs of a sequence: as many as there are at once for it, each with 128 tokens a warp or more.
-static VerifySlices verify_slices(int V, long long at_once) {
-  const int tokens = kGroupStep * kFinishWarps, most = std::min((V + tokens - 1) / tokens, kGroupsMost / kFinishWarps);
-  const int ctas = static_cast<int>(std::max(1ll, std::min(static_cast<long long>(most), at_once)));
-  const int group = ((V + ctas * kFinishWarps - 1) / (ctas * kFinishWarps) + kGroupStep - 1) / kGroupStep * kGroupStep;
-  return VerifySlices{(V + group * kFinishWarps - 1) / (group * kFinishWarps), group};
-}
-int verify_groups_most(int V) { return verify_slices(V, kGroupsMost).ctas * kFinishWarps; }
+int verify_groups_most(int V) { return std::min((V + kGroupStep - 1) / kGroupStep, kGroupsMost); }
 
 cudaError_t launch_draft_verify(const VerifyArgs& a, int dtype, int sms, cudaStream_t s) {
-  const VerifySlices c = verify_slices(a.V, kFinishPerSm * sms / a.S);
-  return dtype == ZSAA_F32 ? run_verify<float>(a, c, s) : run_verify<bf16>(a, c, s);
+  return dtype == ZSAA_F32 ? run_verify<float>(a, sms, s) : run_verify<bf16>(a, sms, s);
 }
 
 }  // namespace zsaa

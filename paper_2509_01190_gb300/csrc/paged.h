@@ -118,25 +118,41 @@ struct alignas(16) VerifyChunk {
   float top;      // the maximum
   int first;      // its first place (where a temperature of 0 asks for it), or -1: a NaN or +inf among the logits
 };
-// A warp's tokens in the pass over the rows at which a sequence stops.
+// A CTA's tokens in the pass over the rows at which a sequence stops, and its warps'.
+constexpr int kVerifyWarps = 8;
 struct alignas(16) VerifyGroup {
   long long a, d;
-  float b;
+  float b, pad[3];
+  long long warp_a[kVerifyWarps];
+  float warp_b[kVerifyWarps];
 };
-struct VerifySlices {
-  int ctas, group;  // CTAs of a sequence, tokens of a warp
+struct VerifyRow {
+  float sum_h, sum_l;  // the sum of its exponentials, as a pair
+  float top;
+  int first;  // the first place of the maximum (temperature 0)
+  int ok;     // the row has a distribution
+};
+// A sequence's decisions, in the calls that make them while they scan.
+struct alignas(16) VerifyState {
+  int stop;           // no draft behind this one stands: at first the number of drafts; -1 without a temperature
+  int n, soft;        // drafts before the first that is no token; a temperature above 0
+  float temperature;
+  unsigned done;      // CTAs of the second kernel that have finished
+  int why[kVerifyMaxDrafts + 1];
+  unsigned scanned[kVerifyMaxDrafts + 1];  // stretches of a draft's rows that have been scanned
+  VerifyRow target[kVerifyMaxDrafts + 1], draft[kVerifyMaxDrafts + 1];
 };
 struct VerifyArgs {
   const void *target, *draft;  // draft or null
   long long ld, draft_ld;
-  int S, n, V, chunks;
+  int S, n, V, chunks, rows;                // rows of a sequence, stretches of a row
   const int32_t *drafts, *lens;             // lens or null
   const float *temperature, *uniform;       // temperature or null
   int32_t *accepted, *tokens, *lens_out;    // lens_out or null
   float* logp;                              // or null
   VerifyChunk* stat;                        // [S][n + 1 target rows, n draft rows][chunks]
-  VerifyGroup* groups;                      // [S][CTAs of a sequence][warps]
-  unsigned* done;                           // [S] CTAs that have finished
+  VerifyGroup* groups;                      // [S][CTAs of a sequence]
+  VerifyState* state;                       // [S]
 };
 int verify_chunks(int V);
 int verify_groups_most(int V);  // groups of a sequence, at most

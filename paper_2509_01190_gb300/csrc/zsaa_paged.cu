@@ -168,16 +168,16 @@ zsaa_status check_taking(int rows, int cols, int page) {
   return ZSAA_OK;
 }
 
-// offsets of a verification's parts in its workspace: chunks, groups, counters
-zsaa_status verify_sizes(int S, int n, int V, size_t* groups, size_t* done, size_t* bytes) {
+// offsets of a verification's parts in its workspace: stretches, groups, decisions
+zsaa_status verify_sizes(int S, int n, int V, size_t* groups, size_t* state, size_t* bytes) {
   if (S < 1 || V < 1) return bad("S and V must be >= 1");
   if (n < 0 || n > kVerifyMaxDrafts) return refuse(ZSAA_ERR_UNSUPPORTED, "n=%d drafts outside [0, %d]", n, kVerifyMaxDrafts);
   if (V > kVerifyMaxVocab) return bad("V must be at most 2^26");
   const long long items = static_cast<long long>(2 * n + 1) * verify_chunks(V);
   if (S > kMostInt / 16 / items) return bad("S*n*V too large");
   *groups = (static_cast<size_t>(S) * items * sizeof(VerifyChunk) + 31) & ~static_cast<size_t>(31);
-  *done = *groups + static_cast<size_t>(S) * verify_groups_most(V) * sizeof(VerifyGroup);
-  *bytes = *done + static_cast<size_t>(S) * sizeof(unsigned);
+  *state = *groups + static_cast<size_t>(S) * verify_groups_most(V) * sizeof(VerifyGroup);
+  *bytes = *state + static_cast<size_t>(S) * sizeof(VerifyState);
   return ZSAA_OK;
 }
 
@@ -400,16 +400,16 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
 zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes) {
   if (bytes == nullptr) return bad("null bytes");
   *bytes = 0;
-  size_t groups = 0, done = 0;
-  return verify_sizes(S, n, V, &groups, &done, bytes);
+  size_t groups = 0, state = 0;
+  return verify_sizes(S, n, V, &groups, &state, bytes);
 }
 
 zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* draft, int64_t draft_ld, int dtype, int S, int n,
                                  int V, const int32_t* drafts, const float* temperature, const float* uniform,
                                  int32_t* accepted, int32_t* tokens, float* logp, const int32_t* lens, int32_t* lens_out,
                                  void* ws, size_t ws_bytes, zsaa_stream stream) {
-  size_t groups = 0, done = 0, need = 0;
-  ZTRY(verify_sizes(S, n, V, &groups, &done, &need));
+  size_t groups = 0, state = 0, need = 0;
+  ZTRY(verify_sizes(S, n, V, &groups, &state, &need));
   if (dtype != ZSAA_F32 && dtype != ZSAA_BF16) return bad("bad dtype");
   if (n == 0) drafts = nullptr, draft = nullptr;
   if (target == nullptr || (n > 0 && drafts == nullptr) || uniform == nullptr || accepted == nullptr || tokens == nullptr ||
@@ -430,12 +430,12 @@ zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* dra
   ZTRY(device_sms(&sms));
   VerifyArgs a{};
   a.target = target, a.draft = draft, a.ld = ld, a.draft_ld = draft_ld;
-  a.S = S, a.n = n, a.V = V, a.chunks = verify_chunks(V);
+  a.S = S, a.n = n, a.V = V, a.chunks = verify_chunks(V), a.rows = n + 1 + (draft != nullptr ? n : 0);
   a.drafts = drafts, a.lens = lens, a.temperature = temperature, a.uniform = uniform;
   a.accepted = accepted, a.tokens = tokens, a.lens_out = lens_out, a.logp = logp;
   a.stat = static_cast<VerifyChunk*>(ws);
   a.groups = reinterpret_cast<VerifyGroup*>(static_cast<char*>(ws) + groups);
-  a.done = reinterpret_cast<unsigned*>(static_cast<char*>(ws) + done);
+  a.state = reinterpret_cast<VerifyState*>(static_cast<char*>(ws) + state);
   return launched("zsaa_op_draft_verify", launch_draft_verify(a, dtype, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 

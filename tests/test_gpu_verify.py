@@ -87,6 +87,23 @@ def test_verify(zlib, S, n, V, dtype, pad, offset):
     check(zlib, target, None, drafts, None, u, dtype=dtype, pad=pad, offset=offset)
 
 
+@pytest.mark.parametrize("lookup", [False, True])
+@pytest.mark.parametrize("S,n,V,dtype", [(700, 5, 60, "f32"), (5000, 1, 9, "bf16"), (400, 15, 1000, "f32"), (45, 4, 131072, "bf16"),
+                                         (40, 4, 140001, "f32")])
+def test_verify_large_calls(zlib, S, n, V, dtype, lookup):
+    """Calls that scan a draft's rows of all sequences before the next draft's, with every kind
+    of end: a draft refused, none left, a row without a distribution, a temperature of 0."""
+    temp = np.random.default_rng(1).choice([0.0, 0.7, 1.0, 1.4], S)
+    temp[S // 2] = -1.0
+    target, draft, drafts, u, r = draw(S, n, V, S + V, noise=0.5, temp=temp)
+    drafts = np.where(np.arange(n) < r.integers(0, n + 2, (S, 1)), drafts, -1)
+    for s in range(0, S, 7):
+        target[s, r.integers(0, n + 1), r.integers(0, V)] = (NAN, INF)[s % 2]
+    for s in range(3, S, 7):
+        draft[s, r.integers(0, n), r.integers(0, V)] = NAN
+    check(zlib, target, None if lookup else draft, drafts, temp, u, dtype=dtype, pad=1)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_verify_temperatures_bans_and_early_ends(zlib, dtype):
     temp = np.array([0, 0.05, 0.3, 0.7, 1.0, 1.5, 4.0, 60.0, 1e4, 0.0, 1.0, 2.0 ** -30, 2.0 ** -70, 2.0 ** 40], np.float32)
