@@ -34,11 +34,12 @@ cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, int 
 
 // ---------------------------------------------------------------- taking and giving up pages
 
-// One cluster does a call: its CTAs change the counts, meet, count the free pages of their
-// parts of the pool, exchange the counts, and hand out the pages.
+// One cluster, or one CTA where there is little, does a call: its CTAs change the counts, meet,
+// count the free pages of their parts of the pool, exchange the counts, and hand out the pages.
 constexpr int kTakeThreads = 1024, kTakeWarps = kTakeThreads / 32, kTakeCtas = 8;
 constexpr int kTakeBlock = 128;  // columns of a table row that a warp looks at together
 constexpr int kTakeMasks = 64;   // words of free pages that a warp keeps
+constexpr int kTakeFew = 16384;  // pages that one CTA looks through
 
 // pages of a warp's part of the pool
 __host__ __device__ inline int pages_part(int n_pages, int warps) { return ((n_pages + warps - 1) / warps + 31) & ~31; }
@@ -90,6 +91,10 @@ __device__ __forceinline__ TakeRow take_row(const PagesArgs& a, int i) {
 
 __device__ __forceinline__ void st_cluster_u32(uint32_t saddr, uint32_t rank, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(saddr, rank)), "r"(v) : "memory");
+}
+
+__device__ __forceinline__ void meet(int ctas) {
+  if (ctas > 1) cluster_sync_all(); else __syncthreads();
 }
 
 // The row of place k, at or behind row `lo`: the last with base[row] <= k (a whole warp).
@@ -208,9 +213,9 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   // pages given up or shared.  (A count that falls below 0 is found with the free pages.)
   if (!touched) {
     touch_pages<FORK>(a, gw, warps, [&](int i) { return make_int2(touch[i], end[i]); });
-    __threadfence();
+    if (ctas > 1) __threadfence();
   }
-  cluster_sync_all();
+  meet(ctas);
 
   // the free pages of this warp's part of the pool
   const int part = pages_part(a.n_pages, warps), words = part / 32;
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
     cta_total += warp_free[w];
   }
   if (tid < ctas) st_cluster_u32(smem_u32(&cta_free[rank]), tid, cta_total);
-  cluster_sync_all();
+  meet(ctas);
   int free_total = 0;
   for (int r = 0; r < ctas; ++r) {
     free_before += r < rank ? cta_free[r] : 0;
@@ -292,16 +297,17 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
 
 template <bool FORK>
 cudaError_t run_take(const PagesArgs& a, cudaStream_t s) {
-  const int words = pages_part(a.n_pages, kTakeCtas * kTakeWarps) / 32;
+  const long long units = static_cast<long long>(a.rows) * ((a.cols + kTakeBlock - 1) / kTakeBlock);
+  const int ctas = a.n_pages > kTakeFew || units > 2 * kTakeWarps ? kTakeCtas : 1;
+  const bool many = units > kTakeCtas * kTakeWarps;
+  const int words = pages_part(a.n_pages, ctas * kTakeWarps) / 32;
   const size_t smem = sizeof(int) * (3 * static_cast<size_t>(a.rows) + 1 + (words <= kTakeMasks ? words * kTakeWarps : 0));
   static OncePerDevice once;
   const cudaError_t e = set_smem_limit_once(once, pages_take_kernel<FORK>,
                                             static_cast<int>(sizeof(int)) * (3 * kPagesMaxRows + 1 + kTakeMasks * kTakeWarps));
   if (e != cudaSuccess) return e;
-  const long long units = static_cast<long long>(a.rows) * ((a.cols + kTakeBlock - 1) / kTakeBlock);
-  const bool many = units > kTakeCtas * kTakeWarps;
   if (many) ZSAA_LAUNCH(pages_touch_kernel<FORK>, dim3(static_cast<unsigned>(std::min((units + 7) / 8, 1024ll))), dim3(256), 0, s, a);
-  return launch_cluster(pages_take_kernel<FORK>, dim3(kTakeCtas), dim3(kTakeThreads), kTakeCtas, smem, s, a, many);
+  return launch_cluster(pages_take_kernel<FORK>, dim3(ctas), dim3(kTakeThreads), ctas, smem, s, a, many);
 }
 
 // ---------------------------------------------------------------- fork: the partly filled pages

@@ -810,16 +810,13 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     at = __shfl_sync(0xffffffffu, at, who);
     before = __shfl_sync(0xffffffffu, at_before, who);
     lo = static_cast<long long>(at) * group;
-    int length = group;
-    if (group > kGroupStep) {  // (a short group's tokens are looked at at once)
-      const VerifyGroup* g = sums + at;
-      const long long part = lane < kFinishWarps ? corrected(__ldcg(&g->warp_a[lane]), __ldcg(&g->warp_b[lane])) : 0;
-      run = before + running_sum(part);
-      who = max(lane_of(part, run), 0);
-      before = __shfl_sync(0xffffffffu, run - part, who);
-      length = group / kFinishWarps;
-      lo += static_cast<long long>(who) * length;
-    }
+    const VerifyGroup* g = sums + at;
+    const long long part = lane < kFinishWarps ? corrected(__ldcg(&g->warp_a[lane]), __ldcg(&g->warp_b[lane])) : 0;
+    run = before + running_sum(part);
+    who = max(lane_of(part, run), 0);
+    before = __shfl_sync(0xffffffffu, run - part, who);
+    const int length = group / kFinishWarps;
+    lo += static_cast<long long>(who) * length;
     count = static_cast<int>(max(min(static_cast<long long>(length), a.V - lo), 1ll));
   }
   // a token's share of the sum
