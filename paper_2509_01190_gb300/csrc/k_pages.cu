@@ -93,6 +93,21 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t saddr, uint32_t rank, ui
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(saddr, rank)), "r"(v) : "memory");
 }
 
+__device__ __forceinline__ int running_sum(int v) {  // over the warp's lanes, own one included
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+// the sum of the warps before this one, and of all (32 warps)
+__device__ __forceinline__ int before_warp(const int* of_warp, int& total) {
+  const int lane = threadIdx.x & 31, mine = of_warp[lane], run = running_sum(mine);
+  total = __shfl_sync(0xffffffffu, run, 31);
+  return __shfl_sync(0xffffffffu, run - mine, threadIdx.x >> 5);
+}
 __device__ __forceinline__ void meet(int ctas) {
   if (ctas > 1) cluster_sync_all(); else __syncthreads();
 }
@@ -115,10 +130,10 @@ __device__ __forceinline__ int row_of_place(const int* base, int lo, int rows, i
 template <bool FORK, typename Touch>
 __device__ __forceinline__ void touch_pages(const PagesArgs& a, int gw, int warps, Touch&& columns) {
   const int lane = threadIdx.x & 31, blocks = (a.cols + kTakeBlock - 1) / kTakeBlock;
-  const long long units = static_cast<long long>(a.rows) * blocks;
+  const unsigned units = static_cast<unsigned>(a.rows) * blocks;  // (a table has fewer than 2^31 entries)
 #pragma unroll 2
-  for (long long u = gw; u < units; u += warps) {
-    const int i = static_cast<int>(u / blocks), c0 = static_cast<int>(u - static_cast<long long>(i) * blocks) * kTakeBlock;
+  for (unsigned u = gw; u < units; u += warps) {
+    const int i = static_cast<int>(u / static_cast<unsigned>(blocks)), c0 = static_cast<int>(u - i * static_cast<unsigned>(blocks)) * kTakeBlock;
     const int2 t = columns(i);
     if (t.x >= c0 + kTakeBlock || t.y <= c0) continue;
     const int32_t* row = a.table + static_cast<size_t>(FORK ? a.parent[i] : i) * a.cols;
@@ -169,6 +184,7 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   int* touch = base + given.rows + 1;  // [rows]: first column given up or shared
   int* end = touch + given.rows;    // [rows]: the column behind the last; the first that gets a page
   unsigned* masks = reinterpret_cast<unsigned*>(end + given.rows);  // free pages of a warp's part, 32 to a word
+  __shared__ unsigned char lists[kTakeWarps * 256];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = static_cast<int>(cluster_rank()), ctas = static_cast<int>(cluster_size());
   const int gw = rank * kTakeWarps + warp, warps = ctas * kTakeWarps;
@@ -189,20 +205,11 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
     if (r.bad && rank == 0) atomicOr(a.status, kStatusBadIndex);
   }
   if (own < a.rows) own_row = take_row<FORK>(a, own);
-  int run = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += x;
-  }
+  const int run = running_sum(mine);
   if (lane == 31) warp_sum[warp] = run;
   __syncthreads();
-  int before = run - mine, total_need = 0;
-#pragma unroll
-  for (int w = 0; w < kTakeWarps; ++w) {
-    before += w < warp ? warp_sum[w] : 0;
-    total_need += warp_sum[w];
-  }
+  int total_need;
+  int before = run - mine + before_warp(warp_sum, total_need);
   for (int i = i0; i < i1; ++i) {
     const int need = base[i];
     base[i] = before;
@@ -223,36 +230,34 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   const long long p0 = static_cast<long long>(gw) * part;
   const int q0 = static_cast<int>(min(p0, static_cast<long long>(a.n_pages)));
   const int q1 = static_cast<int>(min(p0 + part, static_cast<long long>(a.n_pages)));
-  auto free_of = [&](int q, int c) {  // of the 32 pages from q on, with the count c at this lane's
-    if (c < 0) {  // more given up than there were
-      a.refs[q + lane] = 0;
-      atomicOr(a.status, kStatusBadIndex);
-    }
-    return __ballot_sync(0xffffffffu, c <= 0);
-  };
   auto count_at = [&](int q) { return q + lane < q1 ? __ldcg(a.refs + q + lane) : 1; };
   int n_free = 0;
   for (int w0 = 0; w0 < words && q0 + 32 * w0 < q1; w0 += 16) {
-    int c[16];
+    int c[16], least = 1;
+    unsigned mine_mask = 0;  // lane k: word w0 + k
 #pragma unroll
     for (int k = 0; k < 16; ++k)
       if (w0 + k < words) c[k] = count_at(q0 + 32 * (w0 + k));
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       if (w0 + k >= words) break;
-      const unsigned m = free_of(q0 + 32 * (w0 + k), c[k]);
-      if (kept && lane == 0) masks[warp * words + w0 + k] = m;
+      const unsigned m = __ballot_sync(0xffffffffu, c[k] <= 0);
+      least = min(least, c[k]);
+      if (lane == k) mine_mask = m;
       n_free += __popc(m);
+    }
+    if (kept && lane < 16 && w0 + lane < words) masks[warp * words + w0 + lane] = mine_mask;
+    if (least < 0) {  // more given up than there were
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        if (w0 + k < words && c[k] < 0) a.refs[q0 + 32 * (w0 + k) + lane] = 0;
+      atomicOr(a.status, kStatusBadIndex);
     }
   }
   if (lane == 0) warp_free[warp] = n_free;
   __syncthreads();
-  int free_before = 0, cta_total = 0;
-#pragma unroll
-  for (int w = 0; w < kTakeWarps; ++w) {
-    free_before += w < warp ? warp_free[w] : 0;
-    cta_total += warp_free[w];
-  }
+  int cta_total;
+  int free_before = before_warp(warp_free, cta_total);
   if (tid < ctas) st_cluster_u32(smem_u32(&cta_free[rank]), tid, cta_total);
   meet(ctas);
   int free_total = 0;
@@ -261,30 +266,40 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
     free_total += cta_free[r];
   }
 
-  // The free page of rank k goes to the k-th place that needs one.  A word's pages mostly go to
-  // one row, so the rows of its first and its last page are looked for by the whole warp.
-  int lo = 0;
-  bool found = false;
-  for (int w = 0; w < words; ++w) {
-    const int q = q0 + 32 * w;
-    if (q >= q1 || free_before >= total_need) break;
-    const unsigned mask = kept ? masks[warp * words + w] : free_of(q, count_at(q));
-    if (mask == 0) continue;
-    const int k = free_before + __popc(mask & ((1u << lane) - 1)), last = min(free_before + __popc(mask), total_need) - 1;
-    if (!found || base[lo + 1] <= free_before) lo = row_of_place(base, lo, a.rows, free_before);
-    found = true;
-    const int hi = base[lo + 1] > last ? lo : row_of_place(base, lo, a.rows, last);
-    free_before += __popc(mask);
-    if ((mask >> lane & 1) != 0 && k < total_need) {
-      int row = lo, n = hi - lo + 1;  // base[row] <= k < base[row + n]
-      while (n > 1) {
-        const int half = n >> 1;
-        if (base[row + half] <= k) row += half, n -= half; else n = half;
-      }
-      a.table_out[static_cast<size_t>(row) * a.cols + end[row] + (k - base[row])] = q + lane;
-      a.refs[q + lane] = 1;
+  // The free page of rank k goes to the k-th place that needs one.  A warp lists the free ones of
+  // 256 pages, so that its lanes then have neighbouring places, which mostly are in one row: the
+  // rows of the first and the last are looked for by the whole warp.
+  unsigned char* list = lists + warp * 256;
+  int lo = -1;
+  for (int w0 = 0; w0 < words && q0 + 32 * w0 < q1 && free_before < total_need; w0 += 8) {
+    int n = 0;
+    const int last_w = min(8, words - w0);
+    for (int w = 0; w < last_w; ++w) {
+      const int q = q0 + 32 * (w0 + w);
+      const unsigned mask = kept ? masks[warp * words + w0 + w] : __ballot_sync(0xffffffffu, count_at(q) <= 0);
+      if (mask >> lane & 1) list[n + __popc(mask & ((1u << lane) - 1))] = static_cast<unsigned char>(32 * w + lane);
+      n += __popc(mask);
     }
-    lo = hi;
+    __syncwarp();
+    const int wanted = min(n, total_need - free_before);
+    for (int i = 0; i < wanted; i += 32) {
+      const int first = free_before + i, k = first + lane, last = min(first + 32, free_before + wanted) - 1;
+      if (lo < 0 || base[lo + 1] <= first) lo = row_of_place(base, max(lo, 0), a.rows, first);
+      const int hi = base[lo + 1] > last ? lo : row_of_place(base, lo, a.rows, last);
+      if (k <= last) {
+        int row = lo, m = hi - lo + 1;  // base[row] <= k < base[row + m]
+        while (m > 1) {
+          const int half = m >> 1;
+          if (base[row + half] <= k) row += half, m -= half; else m = half;
+        }
+        const int page = q0 + 32 * w0 + list[i + lane];
+        a.table_out[static_cast<size_t>(row) * a.cols + end[row] + (k - base[row])] = page;
+        a.refs[page] = 1;
+      }
+      lo = hi;
+    }
+    free_before += n;
+    __syncwarp();  // (the list is written again)
   }
   for (int i = own; i < a.rows; i += ctas * kTakeThreads) {
     const TakeRow r = i == own ? own_row : take_row<FORK>(a, i);
