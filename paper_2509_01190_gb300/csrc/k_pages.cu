@@ -38,11 +38,17 @@ cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, int 
 // count the free pages of their parts of the pool, exchange the counts, and hand out the pages.
 constexpr int kTakeThreads = 1024, kTakeWarps = kTakeThreads / 32, kTakeCtas = 8;
 constexpr int kTakeBlock = 128;  // columns of a table row that a warp looks at together
-constexpr int kTakeMasks = 64;   // words of free pages that a warp keeps
+constexpr int kTakeMasks = 32;   // words of free pages that a warp keeps
 constexpr int kTakeFew = 16384;  // pages that one CTA looks through
 
-// pages of a warp's part of the pool
-__host__ __device__ inline int pages_part(int n_pages, int warps) { return ((n_pages + warps - 1) / warps + 31) & ~31; }
+constexpr int kTakeBlocks = 2048;
+
+// A pool in blocks of 256 pages, or larger ones where it would have more than kTakeBlocks.
+__host__ __device__ inline int block_shift(int n_pages) {
+  int shift = 8;
+  while (n_pages > (kTakeBlocks << shift)) ++shift;
+  return shift;
+}
 
 // What a call does with one row of its table.
 struct TakeRow {
@@ -178,7 +184,7 @@ __global__ void __launch_bounds__(256) pages_touch_kernel(const __grid_constant_
 template <bool FORK>
 __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __grid_constant__ PagesArgs given, bool touched) {
   extern __shared__ int dynamic[];
-  __shared__ int warp_sum[kTakeWarps], warp_free[kTakeWarps], cta_free[kTakeCtas];
+  __shared__ int warp_sum[kTakeWarps], in_block[kTakeBlocks];  // in_block: free pages of each block, then before it
   pdl_trigger();
   int* base = dynamic;             // [rows + 1]: pages that earlier rows need
   int* touch = base + given.rows + 1;  // [rows]: first column given up or shared
@@ -224,20 +230,25 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   }
   meet(ctas);
 
-  // the free pages of this warp's part of the pool
-  const int part = pages_part(a.n_pages, warps), words = part / 32;
+  // The free pages, block by block of the pool.  The lowest are taken first, so the warps' blocks
+  // alternate, and each CTA gets the counts of all.
+  const int shift = block_shift(a.n_pages), block_words = 1 << (shift - 5), blocks = (a.n_pages + (1 << shift) - 1) >> shift;
+  const int words = ((blocks + warps - 1) / warps) << (shift - 5);  // of a warp
   const bool kept = words <= kTakeMasks;
-  const long long p0 = static_cast<long long>(gw) * part;
-  const int q0 = static_cast<int>(min(p0, static_cast<long long>(a.n_pages)));
-  const int q1 = static_cast<int>(min(p0 + part, static_cast<long long>(a.n_pages)));
-  auto count_at = [&](int q) { return q + lane < q1 ? __ldcg(a.refs + q + lane) : 1; };
+  auto page_of = [&](int w) {  // first page of this warp's word w
+    return (static_cast<long long>((w >> (shift - 5)) * warps + gw) << shift) + 32 * (w & (block_words - 1));
+  };
+  auto count_at = [&](int w) {
+    const long long q = page_of(w) + lane;
+    return q < a.n_pages ? __ldcg(a.refs + q) : 1;
+  };
   int n_free = 0;
-  for (int w0 = 0; w0 < words && q0 + 32 * w0 < q1; w0 += 16) {
+  for (int w0 = 0; w0 < words && page_of(w0) < a.n_pages; w0 += 16) {
     int c[16], least = 1;
     unsigned mine_mask = 0;  // lane k: word w0 + k
 #pragma unroll
     for (int k = 0; k < 16; ++k)
-      if (w0 + k < words) c[k] = count_at(q0 + 32 * (w0 + k));
+      if (w0 + k < words) c[k] = count_at(w0 + k);
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       if (w0 + k >= words) break;
@@ -245,25 +256,45 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
       least = min(least, c[k]);
       if (lane == k) mine_mask = m;
       n_free += __popc(m);
+      if (((w0 + k + 1) & (block_words - 1)) == 0) {
+        const int block = ((w0 + k) >> (shift - 5)) * warps + gw;
+        if (lane < ctas && block < blocks) st_cluster_u32(smem_u32(&in_block[block]), lane, n_free);
+        n_free = 0;
+      }
     }
     if (kept && lane < 16 && w0 + lane < words) masks[warp * words + w0 + lane] = mine_mask;
     if (least < 0) {  // more given up than there were
 #pragma unroll
       for (int k = 0; k < 16; ++k)
-        if (w0 + k < words && c[k] < 0) a.refs[q0 + 32 * (w0 + k) + lane] = 0;
+        if (w0 + k < words && c[k] < 0) a.refs[page_of(w0 + k) + lane] = 0;
       atomicOr(a.status, kStatusBadIndex);
     }
   }
-  if (lane == 0) warp_free[warp] = n_free;
-  __syncthreads();
-  int cta_total;
-  int free_before = before_warp(warp_free, cta_total);
-  if (tid < ctas) st_cluster_u32(smem_u32(&cta_free[rank]), tid, cta_total);
   meet(ctas);
-  int free_total = 0;
-  for (int r = 0; r < ctas; ++r) {
-    free_before += r < rank ? cta_free[r] : 0;
-    free_total += cta_free[r];
+  int free_total, free_before = 0;  // (of the warp's first block)
+  if (blocks <= 32) {
+    const int here = lane < blocks ? in_block[lane] : 0, sum = running_sum(here);
+    free_total = __shfl_sync(0xffffffffu, sum, 31);
+    free_before = __shfl_sync(0xffffffffu, sum - here, gw & 31);
+  } else {
+    constexpr int PER = kTakeBlocks / kTakeThreads;
+    int of_block[PER], here = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      of_block[i] = tid * PER + i < blocks ? in_block[tid * PER + i] : 0;
+      here += of_block[i];
+    }
+    const int sum = running_sum(here);
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    int at = sum - here + before_warp(warp_sum, free_total);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (tid * PER + i < blocks) in_block[tid * PER + i] = at;
+      at += of_block[i];
+    }
+    __syncthreads();
+    if (gw < blocks) free_before = in_block[gw];
   }
 
   // The free page of rank k goes to the k-th place that needs one.  A warp lists the free ones of
@@ -271,12 +302,14 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   // rows of the first and the last are looked for by the whole warp.
   unsigned char* list = lists + warp * 256;
   int lo = -1;
-  for (int w0 = 0; w0 < words && q0 + 32 * w0 < q1 && free_before < total_need; w0 += 8) {
+  for (int w0 = 0; w0 < words && page_of(w0) < a.n_pages; w0 += 8) {
+    if (w0 > 0 && (w0 & (block_words - 1)) == 0) free_before = in_block[(w0 >> (shift - 5)) * warps + gw];
+    if (free_before >= total_need) break;
+    const int q0 = static_cast<int>(page_of(w0));
     int n = 0;
-    const int last_w = min(8, words - w0);
-    for (int w = 0; w < last_w; ++w) {
-      const int q = q0 + 32 * (w0 + w);
-      const unsigned mask = kept ? masks[warp * words + w0 + w] : __ballot_sync(0xffffffffu, count_at(q) <= 0);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const unsigned mask = kept ? masks[warp * words + w0 + w] : __ballot_sync(0xffffffffu, count_at(w0 + w) <= 0);
       if (mask >> lane & 1) list[n + __popc(mask & ((1u << lane) - 1))] = static_cast<unsigned char>(32 * w + lane);
       n += __popc(mask);
     }
@@ -292,7 +325,7 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
           const int half = m >> 1;
           if (base[row + half] <= k) row += half, m -= half; else m = half;
         }
-        const int page = q0 + 32 * w0 + list[i + lane];
+        const int page = q0 + list[i + lane];
         a.table_out[static_cast<size_t>(row) * a.cols + end[row] + (k - base[row])] = page;
         a.refs[page] = 1;
       }
@@ -315,7 +348,8 @@ cudaError_t run_take(const PagesArgs& a, cudaStream_t s) {
   const long long units = static_cast<long long>(a.rows) * ((a.cols + kTakeBlock - 1) / kTakeBlock);
   const int ctas = a.n_pages > kTakeFew || units > 2 * kTakeWarps ? kTakeCtas : 1;
   const bool many = units > kTakeCtas * kTakeWarps;
-  const int words = pages_part(a.n_pages, ctas * kTakeWarps) / 32;
+  const int shift = block_shift(a.n_pages), blocks = (a.n_pages + (1 << shift) - 1) >> shift;
+  const int words = ((blocks + ctas * kTakeWarps - 1) / (ctas * kTakeWarps)) << (shift - 5);
   const size_t smem = sizeof(int) * (3 * static_cast<size_t>(a.rows) + 1 + (words <= kTakeMasks ? words * kTakeWarps : 0));
   static OncePerDevice once;
   const cudaError_t e = set_smem_limit_once(once, pages_take_kernel<FORK>,
