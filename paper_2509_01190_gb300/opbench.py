@@ -11,6 +11,10 @@ stream, and prints the mean time with the algorithmic rate.
     python -m paper_2509_01190_gb300.opbench score_select --batch 32 --seq 4096 --dim 4096 --accel 4
     python -m paper_2509_01190_gb300.opbench paged_attention --model 8b --batch 64 --groups 1 --seq 8192 --own 600
     python -m paper_2509_01190_gb300.opbench beam_select --model 1b --batch 24 --beams 8
+    python -m paper_2509_01190_gb300.opbench draft_verify --model 8b --batch 64 --queries 5
+    python -m paper_2509_01190_gb300.opbench paged_compact --model 8b --batch 8 --own 2011 --accel 2 --layers 32
+    python -m paper_2509_01190_gb300.opbench paged_fork --model 8b --batch 128 --own 1190 --layers 32
+    python -m paper_2509_01190_gb300.opbench paged_resize --batch 512 --own 4000 --page 16
 
 GEMM names follow the layer: qkv (RoPE epilogue), o (residual), gate_up
 (SwiGLU), down (residual), lm_head (float32 logits).
@@ -58,7 +62,8 @@ def _time(fn, warmup: int, iters: int, graph: bool = False) -> float:
 
 def main(argv=None) -> None:
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["gemm", "attention", "colmass", "score_select", "paged_attention", "beam_select"])
+    ap.add_argument("op", choices=["gemm", "attention", "colmass", "score_select", "paged_attention", "beam_select",
+                                   "draft_verify", "paged_compact", "paged_fork", "paged_resize"])
     ap.add_argument("which", nargs="?", default="gate_up",
                     choices=["qkv", "o", "gate_up", "down", "lm_head"])
     ap.add_argument("--model", default="1b", choices=sorted(SHAPES))
@@ -68,9 +73,10 @@ def main(argv=None) -> None:
     ap.add_argument("--dim", type=int, default=4096)
     ap.add_argument("--accel", type=float, default=4.0)
     ap.add_argument("--groups", type=int, default=0, help="paged_attention: groups that share prefixes of --seq entries")
-    ap.add_argument("--own", type=int, default=128, help="paged_attention: a sequence's own entries")
-    ap.add_argument("--queries", type=int, default=1, help="paged_attention: new entries per sequence")
-    ap.add_argument("--page", type=int, default=64, help="paged_attention: entries of a page")
+    ap.add_argument("--own", type=int, default=128, help="paged_*: a sequence's own entries")
+    ap.add_argument("--queries", type=int, default=1, help="paged_attention: new entries per sequence; draft_verify: drafts")
+    ap.add_argument("--page", type=int, default=64, help="paged_*: entries of a page")
+    ap.add_argument("--layers", type=int, default=1, help="paged_compact, paged_fork: layers")
     ap.add_argument("--beams", type=int, default=8, help="beam_select: beams of a batch element, all kept")
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--iters", type=int, default=10)
@@ -157,6 +163,58 @@ def main(argv=None) -> None:
         us = _time(lambda: z.zsaa_op_beam_select(logits, V, B, W, V, scores, None, -1, W, best, parent, token, None, ws,
                                                  ws.numel()), a.warmup, a.iters, a.graph)
         print(f"beam_select B={B} W={W} V={V}: {us:.1f} us, {4.0 * B * W * V / us / 1e3:.0f} GB/s")
+    elif a.op == "draft_verify":
+        S, n, V = a.batch, a.queries, sh.vocab
+        target = 3 * torch.randn(S, n + 1, V, device=dev, generator=g)
+        draft = target[:, :n] + 0.8 * torch.randn(S, n, V, device=dev, generator=g)
+        noise = -torch.log(-torch.log(torch.rand(S, n, V, device=dev, generator=g).clamp_(1e-9, 1 - 1e-7)))
+        drafts = torch.argmax(draft + noise, 2).to(torch.int32) if n else None
+        u = torch.rand(S, n + 1, device=dev, generator=g)
+        accepted, tokens = (torch.empty(S, m, device=dev, dtype=torch.int32) for m in (1, n + 1))
+        ws = torch.empty(z.zsaa_op_draft_verify_workspace(S, n, V), device=dev, dtype=torch.uint8)
+        us = _time(lambda: z.zsaa_op_draft_verify(target, V, draft, V, z.ZSAA_F32, S, n, V, drafts, None, u, accepted, tokens,
+                                                  None, None, None, ws, ws.numel()), a.warmup, a.iters, a.graph)
+        print(f"draft_verify S={S} n={n} V={V}: {us:.1f} us, {4.0 * S * (2 * n + 1) * V / us / 1e3:.0f} GB/s of all rows, "
+              f"{accepted.float().mean().item():.2f} drafts stand")
+    elif a.op in ("paged_compact", "paged_fork", "paged_resize"):
+        S, page, n = a.batch, a.page, a.own
+        i32 = lambda x: torch.tensor(x, device=dev, dtype=torch.int32)
+        cols = -(-n // page) + 1
+        lens, none, got = i32([n] * S), i32([0] * S), i32([0] * S)
+        table = torch.full((S, cols), -1, device=dev, dtype=torch.int32)
+        if a.op == "paged_resize":
+            n_pages = 2 * S * cols
+            refs, turn = torch.zeros(n_pages, device=dev, dtype=torch.int32), [none, lens]
+
+            def step():
+                turn.reverse()
+                z.zsaa_op_paged_resize(refs, n_pages, page, S, table, cols, turn[1], turn[0], got)
+            us = _time(step, a.warmup + a.warmup % 2, a.iters, a.graph)
+            print(f"paged_resize S={S} to and from {n} entries, pages of {page}, pool of {n_pages}: {us:.1f} us")
+            return
+        parents = 1 if a.op == "paged_fork" else S
+        n_pages = parents * cols + S + 1
+        k, v = (torch.randn(a.layers, n_pages, Hkv, page, hd, device=dev, generator=g, dtype=bf) for _ in range(2))
+        layers = z.make_pages_list(list(k), list(v))
+        refs = torch.zeros(n_pages, device=dev, dtype=torch.int32)
+        z.zsaa_op_paged_resize(refs, n_pages, page, parents, table, cols, none, lens, got)
+        entry = 4.0 * Hkv * hd * a.layers
+        if a.op == "paged_fork":
+            kids, kid_lens = torch.full((S, cols), -1, device=dev, dtype=torch.int32), i32([0] * S)
+
+            def step():
+                z.zsaa_op_paged_resize(refs, n_pages, page, S, kids, cols, kid_lens, none, got)
+                z.zsaa_op_paged_fork(layers, refs, 1, table, cols, lens, S, none, None, kids, kid_lens)
+            us = _time(step, a.warmup, a.iters, a.graph)
+            print(f"paged_fork and release of {S} children of {n} entries, {a.layers} layers: {us:.1f} us, "
+                  f"{2 * S * (n % page) * entry / us / 1e3:.0f} GB/s")
+        else:
+            m = max(1, int(n / a.accel))
+            keep = torch.stack([torch.randperm(n, device=dev, generator=g)[:m].sort().values for _ in range(S)]).to(torch.int32)
+            n_keep = i32([m] * S)
+            us = _time(lambda: z.zsaa_op_paged_compact(layers, None, S, table, cols, lens, None, keep, m, n_keep, table, cols,
+                                                       got), a.warmup, a.iters, a.graph)
+            print(f"paged_compact S={S} {n} -> {m} entries in place, {a.layers} layers: {us:.1f} us, {2 * S * m * entry / us / 1e3:.0f} GB/s")
     else:
         B, L, dd = a.batch, a.seq, a.dim
         k = int(L // a.accel)

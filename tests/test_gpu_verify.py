@@ -206,6 +206,15 @@ def test_verify_logits_of_any_size(zlib, level):
     assert np.all(np.abs(logp - want_logp) <= 2.0 ** -17 + R.F32_HALF * np.abs(want_logp))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_verify_long_rows(zlib, dtype):
+    """More stretches and groups than a warp and a CTA hold at once."""
+    for S, n in ((1, 1), (2, 0)):
+        target, draft, drafts, u, _ = draw(S, n, 3000001, 13)
+        check(zlib, target, draft, drafts, None, u, dtype=dtype, offset=1)
+        check(zlib, target, None, drafts, np.zeros(S), u, dtype=dtype, offset=1)
+
+
 @pytest.mark.parametrize("spread", [0.0, 0.3, 3.0])
 @pytest.mark.parametrize("with_draft", [False, True])
 def test_verify_picks_tokens_as_64_bits_do(zlib, spread, with_draft):
