@@ -92,7 +92,7 @@ struct Pair {
   float h, l;
 };
 
-// 2^(i/32) as pairs of floats, all first parts, then all second parts
+// 2^(i/32) as pairs of floats: all first parts, then the second parts relative to the first
 struct Powers {
   float v[64];
 };
@@ -101,7 +101,7 @@ constexpr Powers powers() {
   double x = 1.0;
   for (int i = 0; i < 32; ++i) {
     p.v[i] = static_cast<float>(x);
-    p.v[32 + i] = static_cast<float>(x - static_cast<double>(p.v[i]));
+    p.v[32 + i] = static_cast<float>((x - static_cast<double>(p.v[i])) / static_cast<double>(p.v[i]));
     x *= 1.02189714865411667823;  // 2^(1/32)
   }
   return p;
@@ -112,40 +112,53 @@ __constant__ Powers kPowers = powers();
 // k / 32 and a rest f of at most 1/64; 2^(k/32) from a table of pairs, 2^f by its series, whose
 // first term is a pair too (|f ln 2| <= 0.0109: the terms from the second on are below 2^-14 and
 // their float32 errors below 2^-37, as is the first one left out).  0 below 2^-125.
+//
+// m is not the row's maximum but the next multiple above it of a power of two s <= T / log2(e)
+// (the maximum itself where that is one of s / 2): with d = x - m rounded, d + m and x - (d + m)
+// are then exact wherever 2^y counts.  For |d| <= 250 s, so m is a multiple of d's last place; d + m
+// is one too and no larger than x and half a place, of which d + m differs from x only where x
+// has finer places than d, so it fits a float; and x - (d + m) are low places of x.
 struct MassRow {
-  float m, ch, cl;  // the row's maximum; log2(e) / T
+  float m, ch, cl;  // m; log2(e) / T
 };
-__device__ __forceinline__ MassRow mass_row(float t) {  // without its maximum
+__device__ __forceinline__ MassRow mass_row(float t) {  // without its m
   constexpr float kLog2eH = 1.44269502162933349609375f;
   constexpr float kLog2eL = static_cast<float>(1.4426950408889634074 - static_cast<double>(kLog2eH));
   const float ch = kLog2eH / t;
   return MassRow{0.f, ch, (fmaf(-ch, t, kLog2eH) + kLog2eL) / t};
 }
+__device__ __forceinline__ MassRow row_at(MassRow r, float m) {
+  r.m = m;
+  return r;
+}
+__device__ __forceinline__ MassRow row_above(MassRow r, float top) {  // of a row with the maximum `top`
+  const int e = ilogbf(r.ch) + 1;  // ch < 2^e: s = 2^-e
+  r.m = fabsf(top) < ldexpf(1.f, 22 - e) ? ldexpf(ceilf(ldexpf(top, e)), -e) : top;
+  return r;
+}
 constexpr float kLn2H = 0.693147182464599609375f;  // ln 2 rounded to float, and what that leaves
 constexpr float kLn2L = static_cast<float>(0.69314718055994530942 - static_cast<double>(kLn2H));
 
 __device__ __forceinline__ Pair mass(float x, const MassRow& r, const float* table) {
-  const float d = x - r.m, b = d - x;
-  const float de = (x - (d - b)) + (-r.m - b);  // what rounding took off x - m
+  const float d = x - r.m, de = x - (d + r.m);  // what rounding took off x - m
   const float y = __fmul_rn(d, r.ch);  // (products whose rounding is kept are not fused into what follows)
-  const float ye = fmaf(d, r.ch, -y) + fmaf(d, r.cl, de * r.ch);
+  const float ye = fmaf(d, r.cl, fmaf(de, r.ch, fmaf(d, r.ch, -y)));
   const float magic = fmaf(y, 32.f, 0x1.8p23f);
   const int k = __float_as_int(magic) - __float_as_int(0x1.8p23f);
   const float f = fmaf(magic - 0x1.8p23f, -0.03125f, y);
   const float g = __fmul_rn(f, kLn2H);
-  const float ge = fmaf(f, kLn2H, -g) + fmaf(f, kLn2L, ye * kLn2H);
-  const float w = g + ge;
-  const float rest = ge + w * w * fmaf(w, fmaf(w, 1.f / 24.f, 1.f / 6.f), 0.5f);
-  const float th = table[k & 31], tl = table[32 + (k & 31)];
+  const float ge = fmaf(ye, kLn2H, fmaf(f, kLn2L, fmaf(f, kLn2H, -g)));
+  const float w = g + ge, tl = table[32 + (k & 31)];
+  const float rest = fmaf(tl, g, fmaf(w * w, fmaf(w, fmaf(w, 1.f / 24.f, 1.f / 6.f), 0.5f), ge)) + tl;
+  const float th = __int_as_float(__float_as_int(table[k & 31]) + ((k & ~31) << 18));  // times 2^(k/32 whole)
   const float ph = __fmul_rn(th, g);
-  const float pl = fmaf(th, g, -ph) + fmaf(th, rest, fmaf(tl, g, tl));
+  const float pl = fmaf(th, rest, fmaf(th, g, -ph));
   const float h = th + ph, l = (ph - (h - th)) + pl;
-  const float scale = __int_as_float((max(k >> 5, -126) + 127) << 23);
-  return y > -125.f ? Pair{h * scale, l * scale} : Pair{0.f, 0.f};
+  return y > -125.f ? Pair{h, l} : Pair{0.f, 0.f};
 }
 
 // The same of two tokens at once, in packed arithmetic (whose products are never fused into
-// what follows).  Negated products come from negated factors.
+// what follows).
 struct Pair2 {
   uint64_t h, l;
 };
@@ -153,47 +166,46 @@ struct Factor2 {
   uint64_t ch, nch, cl;
 };
 __device__ __forceinline__ uint64_t both(float x) { return f2pack(x, x); }
-__device__ __forceinline__ MassRow with_top(MassRow r, float top) {
-  r.m = top;
-  return r;
-}
+__device__ __forceinline__ uint64_t negated(uint64_t x) { return x ^ 0x8000000080000000ull; }
 __device__ __forceinline__ Factor2 factor2(const MassRow& r) { return Factor2{both(r.ch), both(-r.ch), both(r.cl)}; }
 __device__ __forceinline__ Pair2 mass2(float x0, float x1, uint64_t m, const Factor2& r, const float* table) {
   const uint64_t x = f2pack(x0, x1);
-  const uint64_t d = fsub2(x, m), b = fsub2(d, x);
-  const uint64_t de = fsub2(fsub2(x, fsub2(d, b)), fadd2(m, b));
+  const uint64_t d = fsub2(x, m), de = fsub2(x, fadd2(d, m));
   const uint64_t ny = fmul2(d, r.nch);
-  const uint64_t ye = fadd2(ffma2(d, r.ch, ny), ffma2(d, r.cl, fmul2(de, r.ch)));
+  const uint64_t ye = ffma2(d, r.cl, ffma2(de, r.ch, ffma2(d, r.ch, ny)));
   const uint64_t magic = ffma2(ny, both(-32.f), both(0x1.8p23f));
   const uint64_t nf = ffma2(fsub2(magic, both(0x1.8p23f)), both(0.03125f), ny);
-  const uint64_t g = fmul2(nf, both(-kLn2H)), ng = fmul2(nf, both(kLn2H));
-  const uint64_t ge = fadd2(ffma2(nf, both(-kLn2H), ng), ffma2(nf, both(-kLn2L), fmul2(ye, both(kLn2H))));
+  const uint64_t ng = fmul2(nf, both(kLn2H)), g = negated(ng);
+  const uint64_t ge = ffma2(ye, both(kLn2H), ffma2(nf, both(-kLn2L), ffma2(nf, both(-kLn2H), ng)));
   const uint64_t w = fadd2(g, ge);
-  const uint64_t rest = ffma2(fmul2(w, w), ffma2(w, ffma2(w, both(1.f / 24.f), both(1.f / 6.f)), both(0.5f)), ge);
   float magic0, magic1, ny0, ny1;
   f2unpack(magic, magic0, magic1);
   f2unpack(ny, ny0, ny1);
   const int k0 = __float_as_int(magic0) - __float_as_int(0x1.8p23f), k1 = __float_as_int(magic1) - __float_as_int(0x1.8p23f);
-  const uint64_t th = f2pack(table[k0 & 31], table[k1 & 31]), tl = f2pack(table[32 + (k0 & 31)], table[32 + (k1 & 31)]);
-  const uint64_t ph = fmul2(th, g), nph = fmul2(th, ng);
-  const uint64_t pl = fadd2(ffma2(th, g, nph), ffma2(th, rest, ffma2(tl, g, tl)));
+  const uint64_t tl = f2pack(table[32 + (k0 & 31)], table[32 + (k1 & 31)]);
+  const uint64_t th = f2pack(__int_as_float(__float_as_int(table[k0 & 31]) + ((k0 & ~31) << 18)),
+                             __int_as_float(__float_as_int(table[k1 & 31]) + ((k1 & ~31) << 18)));
+  const uint64_t series = ffma2(fmul2(w, w), ffma2(w, ffma2(w, both(1.f / 24.f), both(1.f / 6.f)), both(0.5f)), ge);
+  const uint64_t rest = fadd2(ffma2(tl, g, series), tl);
+  const uint64_t ph = fmul2(th, g);
+  const uint64_t pl = ffma2(th, rest, ffma2(th, g, negated(ph)));
   const uint64_t h = fadd2(th, ph), l = fadd2(fsub2(ph, fsub2(h, th)), pl);
-  // (2^(k/32 whole) where y > -125; elsewhere whatever it is, it is not taken)
-  const uint64_t scale = f2pack(__int_as_float(((k0 & ~31) << 18) + 0x3f800000), __int_as_float(((k1 & ~31) << 18) + 0x3f800000));
   float h0, h1, l0, l1;
-  f2unpack(fmul2(h, scale), h0, h1);
-  f2unpack(fmul2(l, scale), l0, l1);
+  f2unpack(h, h0, h1);
+  f2unpack(l, l0, l1);
+  // (where y is not above -125 they are whatever they are)
   return Pair2{f2pack(ny0 < 125.f ? h0 : 0.f, ny1 < 125.f ? h1 : 0.f), f2pack(ny0 < 125.f ? l0 : 0.f, ny1 < 125.f ? l1 : 0.f)};
 }
-__device__ __forceinline__ void add2(Pair2& s, uint64_t h, uint64_t l) {
-  const uint64_t t = fadd2(s.h, h), b = fsub2(t, s.h);
-  s.l = fadd2(s.l, fadd2(fadd2(fsub2(s.h, fsub2(t, b)), fsub2(h, b)), l));
+// to a sum whose first part is never smaller than h
+__device__ __forceinline__ void add_below2(Pair2& s, uint64_t h, uint64_t l) {
+  const uint64_t t = fadd2(s.h, h);
+  s.l = fadd2(s.l, fadd2(fsub2(h, fsub2(t, s.h)), l));
   s.h = t;
 }
 // a - c b with the pair c (nh, l: its negated first part and its second)
 __device__ __forceinline__ Pair2 less2(const Pair2& a, const Pair2& b, uint64_t ch, uint64_t nch, uint64_t cl) {
   const uint64_t nh = fmul2(b.h, nch), e = ffma2(b.h, ch, nh);  // -(b c) and what rounding took off
-  const uint64_t cb = fadd2(e, ffma2(b.h, cl, fmul2(b.l, ch)));
+  const uint64_t cb = ffma2(b.l, ch, ffma2(b.h, cl, e));
   const uint64_t h = fadd2(a.h, nh), c = fsub2(h, a.h);
   return Pair2{h, fadd2(fadd2(fsub2(a.h, fsub2(h, c)), fsub2(nh, c)), fsub2(a.l, cb))};
 }
@@ -243,11 +255,11 @@ __device__ __forceinline__ unsigned add_acq_rel(unsigned* p, unsigned v) {
 enum { kStands, kRefused, kNoDraft, kNoTarget };
 
 // u q(x) < p(x) from the logits alone, where the exponentials are too small for float pairs
-__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const VerifyRow& p, const VerifyRow& q) {
+__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const VerifyRow& p, const VerifyRow& q, bool lookup) {
   auto log_of = [t](float x, const VerifyRow& r) {
-    return (static_cast<double>(x) - static_cast<double>(r.top)) / t - log(static_cast<double>(r.sum_h) + static_cast<double>(r.sum_l));
+    return (static_cast<double>(x) - static_cast<double>(r.m)) / t - log(static_cast<double>(r.sum_h) + static_cast<double>(r.sum_l));
   };
-  const double lp = log_of(xp, p), lq = log_of(xq, q);
+  const double lp = log_of(xp, p), lq = lookup ? 0.0 : log_of(xq, q);
   return lp > -INFINITY && (lq == -INFINITY || u < exp(lp - lq));
 }
 
@@ -274,14 +286,14 @@ __device__ __forceinline__ int verdict(const Sequence& q, int j, int draft, floa
   if (!p.ok) return kNoTarget;
   if (j >= q.n) return kNoDraft;
   if (q.t.greedy) return p.first == draft ? kStands : kRefused;
+  if (!q.lookup && !draft_row.ok) return kNoDraft;
   // u q(x) < p(x); where q(x) = 0: 0 < p(x)
-  const VerifyRow r = q.lookup ? VerifyRow{1.f, 0.f, 0.f, 0, 1} : draft_row;
-  if (!r.ok) return kNoDraft;
-  if (q.lookup) xq = r.top;
-  const Pair ep = mass(xp, with_top(q.factor, p.top), table), eq = mass(xq, with_top(q.factor, r.top), table);
-  const Pair z = sub(mul(Pair{u, 0.f}, mul(eq, Pair{p.sum_h, p.sum_l})), mul(ep, Pair{r.sum_h, r.sum_l}));
+  const Pair one{1.f, 0.f}, ep = mass(xp, row_at(q.factor, p.m), table);
+  const Pair eq = q.lookup ? one : mass(xq, row_at(q.factor, draft_row.m), table);
+  const Pair zq = q.lookup ? one : Pair{draft_row.sum_h, draft_row.sum_l};
+  const Pair z = sub(mul(Pair{u, 0.f}, mul(eq, Pair{p.sum_h, p.sum_l})), mul(ep, zq));
   const bool near = ep.h > 0x1p-60f && eq.h > 0x1p-60f && u > 0x1p-30f;
-  return (near ? z.h + z.l < 0.f : stands_far(u, xp, xq, q.t.t, p, r)) ? kStands : kRefused;
+  return (near ? z.h + z.l < 0.f : stands_far(u, xp, xq, q.t.t, p, draft_row, q.lookup)) ? kStands : kRefused;
 }
 
 __device__ __forceinline__ VerifyChunk load_chunk(const VerifyChunk* p) {
@@ -313,12 +325,13 @@ __device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, Verify
   }
   Pair sum{0.f, 0.f};
   int first = V;
+  const MassRow m = row_above(q.factor, top);
   for (int i = l; i < n; i += lanes) {
     const VerifyChunk c = i == l ? mine : chunk_at(i);
     if (q.t.greedy) {
       if (c.top == top) first = min(first, c.first);
     } else {
-      const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, with_top(q.factor, top), table));
+      const Pair v = mul(pair_of(c.sum, 1.f / kSumScale), mass(c.top, m, table));
       if (c.top > -INFINITY) add(sum, v.h, v.l);
     }
   }
@@ -327,7 +340,7 @@ __device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, Verify
     add(sum, h, e);
     first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
   }
-  return VerifyRow{sum.h, sum.l, top, first, !q.t.bad && bad == 0 && top > -INFINITY};
+  return VerifyRow{sum.h, sum.l, m.m, first, !q.t.bad && bad == 0 && top > -INFINITY};
 }
 
 // ---------------------------------------------------------------- the rows' maxima and sums
@@ -507,7 +520,7 @@ __global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(co
     const VerifyRow mine = row_total(from_stat, load_chunk(from_stat + min(lane & 15, a.chunks - 1)), a.chunks, 16, q, a.V, table);
     auto from = [&](int at) {
       return VerifyRow{__shfl_sync(0xffffffffu, mine.sum_h, at), __shfl_sync(0xffffffffu, mine.sum_l, at),
-                       __shfl_sync(0xffffffffu, mine.top, at), __shfl_sync(0xffffffffu, mine.first, at), __shfl_sync(0xffffffffu, mine.ok, at)};
+                       __shfl_sync(0xffffffffu, mine.m, at), __shfl_sync(0xffffffffu, mine.first, at), __shfl_sync(0xffffffffu, mine.ok, at)};
     };
     p = from(0);
     d = from(16);
@@ -637,15 +650,15 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     stop = s_stop;
     why = s_why;
   }
-  // log p of a token with the logit x: (x - top) / t - log(sum), the rounding errors of each kept:
+  // log p of a token with the logit x: (x - m) / t - log(sum), the rounding errors of each kept:
   // log(sum) = g + log(sum exp(-g)) with g near it, and the latter is its argument less 1
   auto log_sum = [&](const VerifyRow& row) {
     const float g = logf(row.sum_h);
     const Pair e = mul(Pair{row.sum_h, row.sum_l}, mass(-g, mass_row(1.f), table));
     return Pair{g, (e.h - 1.f) + e.l};
   };
-  auto log_p = [&](float top, const Pair& sum, float x) {
-    const float d = x - top, b = d - x, de = (x - (d - b)) + (-top - b);
+  auto log_p = [&](float m, const Pair& sum, float x) {
+    const float d = x - m, b = d - x, de = (x - (d - b)) + (-m - b);
     const float h = d / q.t.t, l = (fmaf(-h, q.t.t, d) + de) / q.t.t;
     const Pair z = sub(Pair{h, l}, sum);
     return h > -INFINITY ? z.h + z.l : h;
@@ -655,7 +668,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
   if (cta == 0) {
     if (tid <= a.n && tid != stop) {
       tokens[tid] = tid < stop ? my_draft : -1;
-      if (logp != nullptr) logp[tid] = tid < stop && q.soft ? log_p(target[tid].top, log_sum(target[tid]), logit_at<T>(a, s, tid, my_draft)) : 0.f;
+      if (logp != nullptr) logp[tid] = tid < stop && q.soft ? log_p(target[tid].m, log_sum(target[tid]), logit_at<T>(a, s, tid, my_draft)) : 0.f;
     }
     if (tid == 0) {
       a.accepted[s] = stop;
@@ -673,7 +686,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
   const T* row_p = row_of<T>(a, s, stop);
   const T* row_q = kind == kResidual ? row_of<T>(a, s, a.n + 1 + stop) : row_p;
   const int refused = kind == kFromTarget ? -1 : after_wait(a.drafts)[static_cast<size_t>(s) * a.n + stop];
-  const MassRow mp = with_top(q.factor, row.top), mq = with_top(q.factor, other.top);
+  const MassRow mp = row_at(q.factor, row.m), mq = row_at(q.factor, other.m);
   const Pair ratio = kind == kResidual ? div(Pair{row.sum_h, row.sum_l}, Pair{other.sum_h, other.sum_l}) : Pair{0.f, 0.f};
 
   // this CTA's group of tokens
@@ -684,8 +697,11 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     const long long g0 = static_cast<long long>(cta) * group + static_cast<long long>(warp) * share + lane;
     const int left = static_cast<int>(min(static_cast<long long>(share), a.V - g0));  // (from this lane's first token on)
     const Factor2 f2 = factor2(q.factor);
-    const uint64_t m2 = both(row.top);
-    Pair2 plus{0, 0}, all{0, 0};
+    const uint64_t m2 = both(row.m);
+    // Sums of terms above 0, and of those below: each begins at twice the largest that a term can be
+    // (E <= 1), so that what a sum's rounding takes off needs no comparison.
+    const float most = kind == kResidual ? exp2f(static_cast<float>(max(ilogbf(ratio.h), 0) + 2)) : 2.f;
+    Pair2 plus{both(2.f), 0}, minus{both(-most), 0};
     float b = 0.f;
     auto load = [&](const T* from, int i0, float (&x)[4]) {
 #pragma unroll
@@ -695,7 +711,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
       }
     };
     if (kind == kResidual) {
-      const uint64_t mq2 = both(other.top), ch = both(ratio.h), nch = both(-ratio.h), cl = both(ratio.l);
+      const uint64_t mq2 = both(other.m), ch = both(ratio.h), nch = both(-ratio.h), cl = both(ratio.l);
       for (int i0 = 0; i0 < share; i0 += kWarpStep) {
         float x[4], y[4];
         load(row_p, i0, x);
@@ -704,13 +720,13 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
         for (int k = 0; k < 4; k += 2) {
           const Pair2 e = mass2(y[k], y[k + 1], mq2, f2, table);
           const Pair2 d = less2(mass2(x[k], x[k + 1], m2, f2, table), e, ch, nch, cl);
-          add2(all, d.h, d.l);
           float s0, s1, h0, h1, l0, l1, q0, q1;
           f2unpack(fadd2(d.h, d.l), s0, s1);
           f2unpack(d.h, h0, h1);
           f2unpack(d.l, l0, l1);
           f2unpack(e.h, q0, q1);
-          add2(plus, f2pack(s0 > 0.f ? h0 : 0.f, s1 > 0.f ? h1 : 0.f), f2pack(s0 > 0.f ? l0 : 0.f, s1 > 0.f ? l1 : 0.f));
+          add_below2(plus, f2pack(s0 > 0.f ? h0 : 0.f, s1 > 0.f ? h1 : 0.f), f2pack(s0 > 0.f ? l0 : 0.f, s1 > 0.f ? l1 : 0.f));
+          add_below2(minus, f2pack(s0 > 0.f ? 0.f : h0, s1 > 0.f ? 0.f : h1), f2pack(s0 > 0.f ? 0.f : l0, s1 > 0.f ? 0.f : l1));
           b += (s0 > 0.f ? q0 : 0.f) + (s1 > 0.f ? q1 : 0.f);
         }
       }
@@ -724,18 +740,18 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
           const int i = i0 + k * 32;
           const Pair2 e = mass2(i == skip && refused >= 0 ? -INFINITY : x[k],
                                 i + 32 == skip && refused >= 0 ? -INFINITY : x[k + 1], m2, f2, table);
-          add2(plus, e.h, e.l);
+          add_below2(plus, e.h, e.l);
         }
       }
     }
     // the two tokens' sums, in units
-    auto joined = [&](const Pair2& v) {
+    auto joined = [&](const Pair2& v, float begin) {
       float h0, h1, l0, l1;
-      f2unpack(v.h, h0, h1);
+      f2unpack(fsub2(v.h, both(begin)), h0, h1);
       f2unpack(v.l, l0, l1);
       return warp_sum_ll(fixed(Pair{h0, l0}, unit) + fixed(Pair{h1, l1}, unit));
     };
-    const long long sum_a = joined(plus), sum_d = kind == kResidual ? joined(all) : 0;
+    const long long sum_a = joined(plus, 2.f), sum_d = kind == kResidual ? sum_a + joined(minus, -most) : 0;
     b = warp_sum(b);
     if (lane == 0) s_part[0][warp] = sum_a, s_part[1][warp] = sum_d, s_b[warp] = b;
   }
@@ -886,7 +902,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     // (a group whose sum is more than 0 only by rounding: its last token)
     if (token < 0) token = static_cast<int>(lo) + count - 1, chosen = to_f<T>(row_p[token]);
     tokens[stop] = token;
-    if (logp != nullptr) logp[stop] = log_p(row.top, row_log, chosen);
+    if (logp != nullptr) logp[stop] = log_p(row.m, row_log, chosen);
   }
 }
 
@@ -901,9 +917,12 @@ VerifySlices verify_slices(int S, int V, int sms, int rounds) {
   return VerifySlices{static_cast<int>((all + steps - 1) / steps), static_cast<int>(steps) * kGroupStep};
 }
 
-// Whether rows are scanned in turn.
+// Whether rows are scanned in turn: from five rounds of the CTAs of the scan of all rows on (128256
+// float32 logits, drafts of which three of five stand, us for all rows and in turn: 8 sequences of 5
+// drafts 23 and 30, 16 34 and 36, 24 49 and 46, 48 82 and 76; 64 of one draft 61 and 56; 16 of 15
+// drafts 66 and 51).
 bool in_turn(const VerifyArgs& a, int sms) {
-  return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 8ll * 4 * sms;
+  return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 5ll * kScanPerSm * sms;
 }
 
 template <typename T>

@@ -127,8 +127,8 @@ struct alignas(16) VerifyGroup {
   float warp_b[kVerifyWarps];
 };
 struct VerifyRow {
-  float sum_h, sum_l;  // the sum of its exponentials, as a pair
-  float top;
+  float sum_h, sum_l;  // the sum of exp((x - m) / T), as a pair
+  float m;
   int first;  // the first place of the maximum (temperature 0)
   int ok;     // the row has a distribution
 };
