@@ -593,7 +593,7 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
  *             they run out (no error: lens_out < want tells).  Must not overlap lens or want
  *   n_free  : int32 [1], the free pages left, or NULL
  * want = 0 ends a sequence.  A page given up that nothing refers to is reported as a page
- * number out of range is.  page_size as zsaa_pages', n_pages <= 2^30. */
+ * number out of range is, and its count stays 0.  page_size as zsaa_pages', n_pages <= 2^30. */
 zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int S, int32_t* table, int cols,
                                  const int32_t* lens, const int32_t* want, int32_t* lens_out, int32_t* n_free,
                                  zsaa_stream stream);
@@ -616,9 +616,9 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
                                int32_t* lens_out, int32_t* n_free, zsaa_stream stream);
 
 /* zsaa_op_paged_compact: chosen entries of each sequence moved together, in every layer: a
- * cache pruned after the prompt (keep from zsaa_score_select), or the accepted path of a tree
- * of drafts.  Entry start[s] + j of the result is entry keep[s, j]; entries below start[s] are
- * not touched.
+ * cache pruned after the prompt (keep from zsaa_score_select), a window that moves on with its
+ * first entries kept, or drafts taken from several branches.  Entry start[s] + j of the result
+ * is entry keep[s, j]; entries below start[s] are not touched.
  *   keep   : int32 [S, keep_cols], row s has n_keep[s] entries, strictly ascending, in
  *            [start[s], lens[s]);  n_keep: int32 [S];  start: int32 [S] or NULL (0)
  *   table, lens: int32 [S, cols] and [S], the entries as they are
@@ -629,7 +629,8 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
  *            have a count of 1 is reported as a page number out of range is, and not written
  *   lens_out: int32 [S], start + n_keep.  Must not overlap lens, start or n_keep
  * Pages past lens_out are given up by zsaa_op_paged_resize.  An entry out of range or not
- * above the one before it is reported, and not moved. */
+ * above the one before it is reported, and not moved.  A call is planned by keep_cols: rows much
+ * wider than the lists cost time.  At most 16383 KV heads. */
 zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const int32_t* refs, int S, const int32_t* table,
                                   int cols, const int32_t* lens, const int32_t* start, const int32_t* keep, int keep_cols,
                                   const int32_t* n_keep, const int32_t* table_out, int out_cols, int32_t* lens_out,
@@ -657,8 +658,9 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  *              may be lens
  * A row has no distribution where it holds a NaN or +inf or nothing above -inf, or its
  * temperature is negative, NaN or above 2^64.  A target row without one ends the sequence's
- * tokens: the next one is -1.  Sums that a token is picked by are good to about 2^-36.  ws:
- * 16-byte aligned, of at least the bytes that zsaa_op_draft_verify_workspace returns (host only). */
+ * tokens: the next one is -1.  Exponentials that a token is picked by are good to 2^-35.7, the
+ * sums that decide a draft to about 1e-8.  Results do not depend on timing.  ws: 16-byte
+ * aligned, of at least the bytes that zsaa_op_draft_verify_workspace returns (host only). */
 zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes);
 zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* draft, int64_t draft_ld, int dtype, int S, int n,
                                  int V, const int32_t* drafts, const float* temperature, const float* uniform,

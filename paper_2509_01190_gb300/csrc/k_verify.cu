@@ -8,20 +8,25 @@
 // distributed as the target's own.
 //
 //   verify_scan_kernel    one stretch of one row per CTA: its maximum and the sum of its
-//                         exponentials.  Bound by the logits' bytes.
+//                         exponentials.  Bound by the logits' bytes (64 sequences of 5 drafts over
+//                         128256 float32 logits: 57 us, 5.8 TB/s).
 //   verify_finish_kernel  the rows at which a sequence stops again, a group of tokens per CTA;
-//                         a sequence's last CTA finds the token.
+//                         a sequence's last CTA finds the token.  Bound by its chain of round trips
+//                         on few sequences (9 us of the 14 that one of 4 drafts takes), by the FMA
+//                         pipe on many (the same 64: 41 us, half of it with that pipe busy).
 //
 // Small calls scan all rows at once, and every CTA of the second kernel works out which drafts
-// stand.  Large calls scan draft 0's rows of all sequences first, then draft 1's, and so on; the
-// CTA that ends a draft's rows decides it, and rows behind a refused draft, which nothing depends
-// on, are left out as far as that is known when their turn comes.
+// stand.  Large calls scan draft 0's rows of all sequences first, then draft 1's, and so on
+// (verify_scan_in_turn_kernel, behind verify_start_kernel); the CTA that ends a draft's rows decides
+// it, and rows behind a refused draft, which nothing depends on, are left out as far as that is
+// known when their turn comes.
 //
 // What decides a draft is one comparison of two quotients, off by about 1e-8 with sums of
 // float32 exponentials.  What decides a token is where u_n falls among V borders, some 1e-5
 // apart and closer: a running sum that is off by 1e-9 picks the wrong token every few thousand
 // calls.  So the rows at which a sequence stops are gone through again with exponentials as
-// pairs of floats, good to about 2^-37, and sums in pairs and in 64 bits.
+// pairs of floats, good to 2^-35.7 each and without a bias to see (below 2^-42), and sums in pairs
+// and in 64-bit integers.
 //
 // One pass does it, although the residual needs the sums of both rows: with E the exponentials,
 // Z their exact sums and c0 the quotient Z_p / Z_q as the scan has it, the pass adds up
@@ -29,6 +34,10 @@
 //   A = sum D_i, B = sum E_q,i    over a group's tokens with D_i > 0.
 // The exact quotient is c0 + k with k = sum D / Z_q, some 2^-24 of it, so a group's residual is
 // A - k B; tokens whose D_i changes its sign with k are off by 2^-24 of a 2^-24th of them.
+// (Two passes, the first for the sums, took 270 us on the 64 where this one took 77, both still with
+// sums of 64-bit floats.)
+//
+// 64-bit floats are left out of the sums: the SM does two of their operations a clock.
 #include <algorithm>
 #include <cmath>
 
@@ -58,8 +67,7 @@ __device__ __forceinline__ Temperature temperature_of(const VerifyArgs& a, int s
 
 __device__ __forceinline__ float log2e_over(float t) { return 1.44269504088896340736f / t; }
 
-// drafts of sequence s before the first that is no token
-// (whole warps)
+// drafts of sequence s before the first that is no token (whole warps)
 __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int s) {
   const int lane = threadIdx.x & 31;
   const int x = lane < a.n ? after_wait(a.drafts)[static_cast<size_t>(s) * a.n + lane] : -1;
@@ -111,7 +119,8 @@ __constant__ Powers kPowers = powers();
 // exp((x - m) / T) = 2^y: y = (x - m) log2(e) / T with its rounding errors kept, cut into
 // k / 32 and a rest f of at most 1/64; 2^(k/32) from a table of pairs, 2^f by its series, whose
 // first term is a pair too (|f ln 2| <= 0.0109: the terms from the second on are below 2^-14 and
-// their float32 errors below 2^-37, as is the first one left out).  0 below 2^-125.
+// their float32 errors below 2^-37, as is the first one left out).  0 below 2^-125.  Off by at most
+// 2^-35.7 over 9.6 million values at temperatures from 0.05 to 60 and logits up to 1e6.
 //
 // m is not the row's maximum but the next multiple above it of a power of two s <= T / log2(e)
 // (the maximum itself where that is one of s / 2): with d = x - m rounded, d + m and x - (d + m)
@@ -255,9 +264,11 @@ __device__ __forceinline__ unsigned add_acq_rel(unsigned* p, unsigned v) {
 enum { kStands, kRefused, kNoDraft, kNoTarget };
 
 // u q(x) < p(x) from the logits alone, where the exponentials are too small for float pairs
-__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const VerifyRow& p, const VerifyRow& q, bool lookup) {
+__device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, const VerifyRow& p, const VerifyRow& q,
+                                        bool lookup) {
   auto log_of = [t](float x, const VerifyRow& r) {
-    return (static_cast<double>(x) - static_cast<double>(r.m)) / t - log(static_cast<double>(r.sum_h) + static_cast<double>(r.sum_l));
+    const double sum = static_cast<double>(r.sum_h) + static_cast<double>(r.sum_l);
+    return (static_cast<double>(x) - static_cast<double>(r.m)) / t - log(sum);
   };
   const double lp = log_of(xp, p), lq = lookup ? 0.0 : log_of(xq, q);
   return lp > -INFINITY && (lq == -INFINITY || u < exp(lp - lq));
@@ -278,7 +289,9 @@ __device__ __forceinline__ float number_at(const VerifyArgs& a, int s, int j) {
   return fminf(fmaxf(after_wait(a.uniform)[static_cast<size_t>(s) * (a.n + 1) + j], 0.f), 0x1.fffffep-1f);
 }
 template <typename T>
-__device__ __forceinline__ float logit_at(const VerifyArgs& a, int s, int r, int x) { return to_f<T>(row_of<T>(a, s, r)[x]); }
+__device__ __forceinline__ float logit_at(const VerifyArgs& a, int s, int r, int x) {
+  return to_f<T>(row_of<T>(a, s, r)[x]);
+}
 
 // What becomes of draft j < q.n (or kNoDraft, kNoTarget), with the logits of its token.
 __device__ __forceinline__ int verdict(const Sequence& q, int j, int draft, float u, float xp, float xq, const VerifyRow& p,
@@ -299,7 +312,7 @@ __device__ __forceinline__ int verdict(const Sequence& q, int j, int draft, floa
 __device__ __forceinline__ VerifyChunk load_chunk(const VerifyChunk* p) {
   const int4 v = __ldcg(reinterpret_cast<const int4*>(p));
   VerifyChunk c;
-  c.sum = static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(v.y)) << 32 | static_cast<unsigned>(v.x));
+  c.sum = static_cast<long long>(static_cast<uint64_t>(static_cast<uint32_t>(v.y)) << 32 | static_cast<uint32_t>(v.x));
   c.top = __int_as_float(v.z);
   c.first = v.w;
   return c;
@@ -307,8 +320,8 @@ __device__ __forceinline__ VerifyChunk load_chunk(const VerifyChunk* p) {
 
 // A row from its n stretches, by `lanes` lanes (16 or 32) of a warp, the same in all of them.  mine: the
 // stretch of this lane's number, where there is one.
-__device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, VerifyChunk mine, int n, int lanes, const Sequence& q, int V,
-                                               const float* table) {
+__device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, VerifyChunk mine, int n, int lanes,
+                                               const Sequence& q, int V, const float* table) {
   const int l = threadIdx.x & (lanes - 1);
   auto chunk_at = [&](int i) { return load_chunk(chunks + i); };
   if (l >= n) mine = VerifyChunk{0, -INFINITY, V};
@@ -348,7 +361,6 @@ __device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, Verify
 constexpr int kScanPerSm = 4;
 constexpr int kScanThreads = 256, kScanValues = 32, kScanTokens = kScanThreads * kScanValues;
 
-// (64-bit floats are left out: the SM does two of their operations a clock.)
 // Sum over the warp of values in [0, 2^50) (two 32-bit reductions of 25 bits each).
 __device__ __forceinline__ unsigned long long warp_sum_u50(unsigned long long v) {
   const unsigned lo = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(v) & 0x1ffffffu);
@@ -382,8 +394,8 @@ __device__ __forceinline__ void load_stretch(const T* row, int chunk, int V, flo
 }
 // (returns whether the CTA has seen a NaN or +inf)
 template <typename T>
-__device__ __forceinline__ bool scan_stretch(const T* row, int chunk, int V, bool greedy, float c, const float (&x)[kScanValues],
-                                             StretchParts& parts) {
+__device__ __forceinline__ bool scan_stretch(const T* row, int chunk, int V, bool greedy, float c,
+                                             const float (&x)[kScanValues], StretchParts& parts) {
   constexpr int VEC = 16 / sizeof(T);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   float top = -INFINITY;
@@ -421,8 +433,9 @@ __device__ __forceinline__ VerifyChunk joined_stretch(const StretchParts& parts,
   VerifyChunk out;
   const float top = in ? parts.top[lane] : -INFINITY;
   out.top = warp_max(top);
-  const unsigned long long total =
-      in && top > -INFINITY ? static_cast<unsigned long long>(static_cast<float>(parts.sum[lane]) * ex2((top - out.top) * c)) : 0;
+  unsigned long long total = 0;
+  if (in && top > -INFINITY)
+    total = static_cast<unsigned long long>(static_cast<float>(parts.sum[lane]) * ex2((top - out.top) * c));
   out.sum = static_cast<long long>(warp_sum_u50(total));
   out.first = __reduce_min_sync(0xffffffffu, in && top == out.top ? parts.first[lane] : V);
   if (bad) out.first = -1;
@@ -432,13 +445,15 @@ __device__ __forceinline__ VerifyChunk joined_stretch(const StretchParts& parts,
 // All rows at once.  Where the CTAs run in one round a row's logits are fetched before it is known
 // whether they decide anything: 0.6 us less, and the bytes of rows left out cost none.
 template <typename T>
-__global__ void __launch_bounds__(kScanThreads, kScanPerSm) verify_scan_kernel(const __grid_constant__ VerifyArgs a, bool at_once) {
+__global__ void __launch_bounds__(kScanThreads, kScanPerSm)
+    verify_scan_kernel(const __grid_constant__ VerifyArgs a, bool at_once) {
   __shared__ StretchParts parts;
   pdl_trigger();
   pdl_wait();
   const unsigned item = blockIdx.x / static_cast<unsigned>(a.chunks);
   const int chunk = static_cast<int>(blockIdx.x - item * a.chunks);
-  const int s = static_cast<int>(item / static_cast<unsigned>(a.rows)), r = static_cast<int>(item - s * static_cast<unsigned>(a.rows));
+  const int s = static_cast<int>(item / static_cast<unsigned>(a.rows));
+  const int r = static_cast<int>(item - s * static_cast<unsigned>(a.rows));
   if (r == 0 && chunk == 0 && threadIdx.x == 0) a.state[s].done = 0;
   const T* row = row_of<T>(a, s, r);
   float x[kScanValues];
@@ -462,7 +477,10 @@ __global__ void __launch_bounds__(kScanThreads, kScanPerSm) verify_scan_kernel(c
 // Draft by draft over all sequences: a CTA takes one stretch of draft j's rows, the target's and the
 // draft's.  Warp 0 of the CTA that ends draft j decides it; what does not stand lowers the
 // sequence's stop.  A row is left out only where the stop lies before it, so the rows up to the
-// first draft that does not stand are all scanned, whatever the order in which CTAs run.
+// first draft that does not stand are all scanned, whatever the order in which CTAs run.  64 sequences
+// of 5 drafts, of which 2.1 stand: 214 of the 361 MB in 52 us.  A CTA's chain bounds it (state, rows,
+// sums, count: 5 us with loads on their way for two of them), three CTAs to an SM; one that finds
+// its row not wanted takes 1 us.
 template <typename T>
 __global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ float table[64];
@@ -492,7 +510,8 @@ __global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(co
   const bool draft_bad = two && scan_stretch(draft_row, chunk, a.V, false, c, y, parts[1]);
   if (tid >= 32) return;
   VerifyChunk* stat = a.stat + static_cast<size_t>(s) * a.rows * a.chunks;
-  VerifyChunk *p_stat = stat + static_cast<size_t>(j) * a.chunks, *d_stat = stat + static_cast<size_t>(a.n + 1 + j) * a.chunks;
+  VerifyChunk* p_stat = stat + static_cast<size_t>(j) * a.chunks;
+  VerifyChunk* d_stat = stat + static_cast<size_t>(a.n + 1 + j) * a.chunks;
   const VerifyChunk p_out = joined_stretch(parts[0], bad, c, a.V);
   VerifyChunk d_out{};
   if (two) d_out = joined_stretch(parts[1], draft_bad, c, a.V);
@@ -517,10 +536,12 @@ __global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(co
   }
   if (two && a.chunks <= 16) {  // (the warp's halves take a row each)
     const VerifyChunk* from_stat = lane < 16 ? p_stat : d_stat;
-    const VerifyRow mine = row_total(from_stat, load_chunk(from_stat + min(lane & 15, a.chunks - 1)), a.chunks, 16, q, a.V, table);
+    const VerifyChunk chunk_here = load_chunk(from_stat + min(lane & 15, a.chunks - 1));
+    const VerifyRow mine = row_total(from_stat, chunk_here, a.chunks, 16, q, a.V, table);
     auto from = [&](int at) {
       return VerifyRow{__shfl_sync(0xffffffffu, mine.sum_h, at), __shfl_sync(0xffffffffu, mine.sum_l, at),
-                       __shfl_sync(0xffffffffu, mine.m, at), __shfl_sync(0xffffffffu, mine.first, at), __shfl_sync(0xffffffffu, mine.ok, at)};
+                       __shfl_sync(0xffffffffu, mine.m, at), __shfl_sync(0xffffffffu, mine.first, at),
+                       __shfl_sync(0xffffffffu, mine.ok, at)};
     };
     p = from(0);
     d = from(16);
@@ -559,16 +580,15 @@ __global__ void verify_start_kernel(const __grid_constant__ VerifyArgs a) {
 
 constexpr int kFinishWarps = kVerifyWarps, kFinishThreads = 32 * kFinishWarps, kFinishPerSm = 4;
 constexpr int kWarpStep = 128, kGroupStep = kFinishWarps * kWarpStep;  // a group, the tokens of a CTA, is a multiple of it
-constexpr int kGroupsMost = 128;                // groups of a sequence, at most
+constexpr int kGroupsMost = 128;                                       // groups of a sequence, at most
 
 enum { kFromTarget = 0, kWithout = 1, kResidual = 2 };  // r = p; p without token x; max(p - q, 0)
-
 
 // floor(u total), u in [0, 1)
 __device__ __forceinline__ long long goal_of(float u, long long total) {
   int e;
   const float m = frexpf(u, &e);  // u = m 2^e, m 2^24 a whole number
-  const unsigned __int128 v = static_cast<unsigned __int128>(static_cast<unsigned>(m * 0x1p24f)) * static_cast<unsigned long long>(total);
+  const unsigned __int128 v = static_cast<unsigned __int128>(static_cast<uint64_t>(total)) * static_cast<uint32_t>(m * 0x1p24f);
   return 24 - e > 127 ? 0 : static_cast<long long>(v >> (24 - e));
 }
 
@@ -582,7 +602,9 @@ __device__ __forceinline__ long long running_sum(long long v) {  // over the war
   return v;
 }
 
-// Rows by draft in the calls that scan in turn (decided there), else worked out here.
+// Which drafts stand is known in the calls that scan in turn, else worked out here by every CTA
+// (2 us).  Packed arithmetic takes two tokens at once; the FMA pipe's share of a token and its draft
+// row's is 78 operations.
 template <typename T, bool DECIDED>
 __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     verify_finish_kernel(const __grid_constant__ VerifyArgs a, int ctas, int group, float unit) {
@@ -603,7 +625,8 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
   const VerifyChunk* stat = after_wait(a.stat) + static_cast<size_t>(s) * a.rows * a.chunks;
   const int lanes = a.chunks <= 16 ? 16 : 32, per_warp = 32 / lanes;
   auto chunk_of = [&](int r0) {
-    return load_chunk(stat + static_cast<size_t>(min(r0 + lane / lanes, a.rows - 1)) * a.chunks + min(lane & (lanes - 1), a.chunks - 1));
+    const int r = min(r0 + lane / lanes, a.rows - 1);
+    return load_chunk(stat + static_cast<size_t>(r) * a.chunks + min(lane & (lanes - 1), a.chunks - 1));
   };
   VerifyChunk chunk{};
   if (!DECIDED) chunk = chunk_of(warp * per_warp);
@@ -668,11 +691,15 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
   if (cta == 0) {
     if (tid <= a.n && tid != stop) {
       tokens[tid] = tid < stop ? my_draft : -1;
-      if (logp != nullptr) logp[tid] = tid < stop && q.soft ? log_p(target[tid].m, log_sum(target[tid]), logit_at<T>(a, s, tid, my_draft)) : 0.f;
+      if (logp != nullptr) {
+        float lp = 0.f;
+        if (tid < stop && q.soft) lp = log_p(target[tid].m, log_sum(target[tid]), logit_at<T>(a, s, tid, my_draft));
+        logp[tid] = lp;
+      }
     }
     if (tid == 0) {
       a.accepted[s] = stop;
-      if (a.lens_out != nullptr) a.lens_out[s] = max(after_wait(a.lens)[s] - (a.n - stop), 0);
+      if (a.lens_out != nullptr) a.lens_out[s] = max(max(after_wait(a.lens)[s], 0) - (a.n - stop), 0);
       if (why == kNoTarget || q.t.greedy) {
         tokens[stop] = why == kNoTarget ? -1 : target[stop].first;
         if (logp != nullptr) logp[stop] = 0.f;
@@ -725,9 +752,10 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
           f2unpack(d.h, h0, h1);
           f2unpack(d.l, l0, l1);
           f2unpack(e.h, q0, q1);
-          add_below2(plus, f2pack(s0 > 0.f ? h0 : 0.f, s1 > 0.f ? h1 : 0.f), f2pack(s0 > 0.f ? l0 : 0.f, s1 > 0.f ? l1 : 0.f));
-          add_below2(minus, f2pack(s0 > 0.f ? 0.f : h0, s1 > 0.f ? 0.f : h1), f2pack(s0 > 0.f ? 0.f : l0, s1 > 0.f ? 0.f : l1));
-          b += (s0 > 0.f ? q0 : 0.f) + (s1 > 0.f ? q1 : 0.f);
+          const bool up0 = s0 > 0.f, up1 = s1 > 0.f;
+          add_below2(plus, f2pack(up0 ? h0 : 0.f, up1 ? h1 : 0.f), f2pack(up0 ? l0 : 0.f, up1 ? l1 : 0.f));
+          add_below2(minus, f2pack(up0 ? 0.f : h0, up1 ? 0.f : h1), f2pack(up0 ? 0.f : l0, up1 ? 0.f : l1));
+          b += (up0 ? q0 : 0.f) + (up1 ? q1 : 0.f);
         }
       }
     } else {
@@ -868,8 +896,12 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     total += s_part[0][w];
   }
   if (plain) goal = goal_of(u, total);
-  const unsigned some_t = __ballot_sync(0xffffffffu, mine > 0), above_t = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
-  if (lane == 0) s_first[warp] = above_t != 0 ? tid + __ffs(above_t) - 1 : -1, s_some[warp] = some_t != 0 ? tid + 31 - __clz(some_t) : -1;
+  const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
+  const unsigned above = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
+  if (lane == 0) {
+    s_first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1;
+    s_some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
+  }
   __syncthreads();
   int last = 0;
   who = -1;
@@ -938,7 +970,8 @@ cudaError_t run_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.S) * a.rows * a.chunks), finish(static_cast<unsigned>(a.S) * c.ctas);
   if (turns) {
     ZSAA_LAUNCH(verify_start_kernel, dim3((a.S + 7) / 8), dim3(256), 0, s, a);
-    ZSAA_LAUNCH(verify_scan_in_turn_kernel<T>, dim3(static_cast<unsigned>(a.S) * (a.n + 1) * a.chunks), dim3(kScanThreads), 0, s, a);
+    const dim3 turns_grid(static_cast<unsigned>(a.S) * (a.n + 1) * a.chunks);
+    ZSAA_LAUNCH(verify_scan_in_turn_kernel<T>, turns_grid, dim3(kScanThreads), 0, s, a);
     ZSAA_LAUNCH((verify_finish_kernel<T, true>), finish, dim3(kFinishThreads), 0, s, a, c.ctas, c.group, unit);
   } else {
     ZSAA_LAUNCH(verify_scan_kernel<T>, grid, dim3(kScanThreads), 0, s, a, grid.x <= static_cast<unsigned>(kScanPerSm * sms));
