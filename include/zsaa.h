@@ -619,8 +619,8 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
  * cache pruned after the prompt (keep from zsaa_score_select), a window that moves on with its
  * first entries kept, or drafts taken from several branches.  Entry start[s] + j of the result
  * is entry keep[s, j]; entries below start[s] are not touched.
- *   keep   : int32 [S, keep_cols], row s has n_keep[s] entries, strictly ascending, in
- *            [start[s], lens[s]);  n_keep: int32 [S];  start: int32 [S] or NULL (0)
+ *   keep   : int32 [S, keep_cols], row s has n_keep[s] entries (negative: 0), strictly
+ *            ascending, in [start[s], lens[s]);  start: int32 [S] or NULL (0, as a negative one)
  *   table, lens: int32 [S, cols] and [S], the entries as they are
  *   table_out: int32 [S, out_cols], the pages that the result is written to (not changed):
  *            `table` itself for a move in place, or another.  A page that is written may be

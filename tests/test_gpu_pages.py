@@ -332,6 +332,84 @@ def test_compact_reports_what_is_out_of_range(zlib, bad):
     assert 0 <= got.item() <= 32
 
 
+def test_compact_into_rows_too_short(zlib):
+    """A result that its table row does not hold is cut, and reported."""
+    k, v = pools("bf16", 1, 6, 1, 16, 64, 0)
+    before, got = k.clone(), out_lens(1)
+    zlib.zsaa_op_paged_compact(zlib.make_pages_list(list(k), list(v)), None, 1, ints([[0, 1]]), 2, ints([32]), None,
+                               ints([list(range(2, 22))]), 20, ints([20]), ints([[5]]), 1, got)
+    reported(zlib)
+    assert got.tolist() == [16] and torch.equal(k[0, 5, 0, :14], before[0, 0, 0, 2:]) and torch.equal(k[0, :5], before[0, :5])
+
+
+def test_pages_far_into_a_large_pool(zlib):
+    """Element offsets past 2^31: the last pages of pools of 5 GB."""
+    z, n_pages, page = zlib, 40000, 64
+    k, v = (torch.empty(1, n_pages, 8, page, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    last = list(range(n_pages - 4, n_pages))
+    for x in (k, v):
+        x[:, last] = torch.randn(1, 4, 8, page, 128, device="cuda").to(torch.bfloat16)
+    kk, vv = np64(k[:, last]), np64(v[:, last])
+    layers = z.make_pages_list(list(k), list(v))
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    refs[n_pages - 2:] = 0
+    table, got, out = ints([[n_pages - 4, n_pages - 3]]), out_lens(1), ints([[-1, -1]])
+    z.zsaa_op_paged_fork(layers, refs, 1, table, 2, ints([100]), 1, ints([0]), None, out, got)
+    assert out.tolist() == [[n_pages - 4, n_pages - 2]] and got.tolist() == [100]
+    rel, r_refs, r_out = np.array([[0, 1]]), np.array([1, 1, 0, 0]), np.array([[-1, -1]])
+    P.fork(kk, vv, r_refs, page, rel, [100], [0], None, r_out)
+    keep = np.sort(np.random.default_rng(0).permutation(100)[:70])
+    z.zsaa_op_paged_compact(layers, None, 1, table, 2, ints([100]), None, ints([keep]), 70, ints([70]), table, 2, got)
+    P.compact(kk, vv, page, rel, None, keep[None], [70], rel)
+    np.testing.assert_array_equal(np64(k[:, last]), kk)
+    np.testing.assert_array_equal(np64(v[:, last]), vv)
+
+
+def test_fork_and_compact_into_a_graph_on_another_stream(zlib):
+    """Samples of a prompt that lose half of their entries, released and made again by a replayed
+    graph, as their parents' lengths and the entries chosen change."""
+    z, page, S, N, cols, n_pages = zlib, 16, 2, 4, 5, 40
+    k, v = pools("bf16", 2, n_pages, 2, page, 64, 9)
+    layers = z.make_pages_list(list(k), list(v))
+    refs, table, lens = ints(np.zeros(n_pages)), ints(np.full((S, cols), -1)), out_lens(S)
+    z.zsaa_op_paged_resize(refs, n_pages, page, S, table, cols, ints([0] * S), ints([cols * page] * S), lens)
+    kids, kid_lens, half, zero, parent = ints(np.full((N, cols), -1)), ints([0] * N), ints([0] * N), ints([0] * N), ints([0, 1, 1, 0])
+    at, keep, n_keep, own, left = ints([1] * N), ints(np.zeros((N, 40))), ints([0] * N), ints(np.full((N, cols), -1)), out_lens(N)
+
+    def call():
+        z.zsaa_op_paged_resize(refs, n_pages, page, N, own, cols, half, zero, left)
+        z.zsaa_op_paged_fork(layers, refs, S, table, cols, lens, N, parent, at, kids, kid_lens)
+        z.zsaa_op_paged_resize(refs, n_pages, page, N, own, cols, zero, n_keep, half)
+        z.zsaa_op_paged_compact(layers, refs, N, kids, cols, kid_lens, None, keep, 40, n_keep, own, cols, half)
+        z.zsaa_op_paged_resize(refs, n_pages, page, N, kids, cols, kid_lens, zero, left)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call()
+        for step in range(4):
+            r = np.random.default_rng(step)
+            sizes = r.integers(2, 70, N)
+            chosen = [np.sort(r.permutation(n)[:n // 2]) for n in sizes]
+            rows = np.zeros((N, 40), int)
+            for i, c in enumerate(chosen):
+                rows[i, :len(c)] = c
+            at.copy_(ints(sizes)), keep.copy_(ints(rows)), n_keep.copy_(ints([len(c) for c in chosen]))
+            kk, vv = np64(k), np64(v)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert refs.sum().item() == S * cols + sum(-(-len(c) // page) for c in chosen) and half.tolist() == [len(c) for c in chosen]
+            for i, c in enumerate(chosen):
+                for pool, was in ((np64(k), kk), (np64(v), vv)):
+                    for l in range(2):
+                        have = R.entries(pool[l], own[i].tolist(), len(c))
+                        np.testing.assert_array_equal(have, R.entries(was[l], table[parent[i]].tolist(), sizes[i])[:, c])
+
+
 def test_a_cache_is_pruned_and_attended(zlib):
     """Scores choose half of each sequence's entries, the cache is compacted and its pages are
     given up; attention then sees exactly the chosen entries.  Forks of a sequence prune on

@@ -244,6 +244,24 @@ def test_verify_the_same_bits_again_and_without_the_optional_outputs(zlib):
     np.testing.assert_array_equal(tok.cpu().numpy(), first[1])
 
 
+def test_verify_rows_far_apart_and_draft_rows_of_another_stride(zlib):
+    """Element offsets past 2^31, and draft rows closer together than the target's."""
+    z, S, n, V, ld, draft_ld = zlib, 3, 1, 1000, 1 << 29, 1003
+    target, draft, drafts, u, _ = draw(S, n, V, 3)
+    t = torch.empty((S * (n + 1) - 1) * ld + V, device="cuda")
+    for i, row in enumerate(target.reshape(-1, V)):
+        t[i * ld:i * ld + V] = torch.from_numpy(row).cuda()
+    d = torch.full((S * n, draft_ld), NAN, device="cuda")
+    d[:, :V] = torch.from_numpy(draft.reshape(-1, V)).cuda()
+    want = P.verify(target.astype(np.float64), draft.astype(np.float64), drafts, None, u)
+    assert want[3] > 2.0 ** -16 and want[4] > 2.0 ** -34
+    ws = torch.empty(z.zsaa_op_draft_verify_workspace(S, n, V), dtype=torch.uint8, device="cuda")
+    acc, tok = ints(np.zeros(S)), ints(np.zeros((S, n + 1)))
+    z.zsaa_op_draft_verify(t, ld, d, draft_ld, z.ZSAA_F32, S, n, V, ints(drafts), None, torch.from_numpy(u).cuda(), acc, tok, None,
+                           None, None, ws, ws.numel())
+    np.testing.assert_array_equal(tok.cpu().numpy(), want[1])
+
+
 def test_verify_lengths_in_place_and_graphs_on_two_streams(zlib):
     z, S, n, V = zlib, 3, 2, 9000
     runs = []
