@@ -610,7 +610,8 @@ zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int 
  *            up first (zsaa_op_paged_resize to 0).  Must not overlap the inputs; entries of
  *            table_out past a child's last page stay as they were
  *   n_free : as above
- * Where pages run out a child keeps its whole pages: lens_out = m / page_size * page_size. */
+ * Where pages run out a child keeps its whole pages: lens_out = m / page_size * page_size.
+ * At most 16383 KV heads. */
 zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* refs, int S, const int32_t* table, int cols,
                                const int32_t* lens, int N, const int32_t* parent, const int32_t* at, int32_t* table_out,
                                int32_t* lens_out, int32_t* n_free, zsaa_stream stream);

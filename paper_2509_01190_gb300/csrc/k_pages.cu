@@ -47,13 +47,12 @@ cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, int 
 // are taken lie in the lowest part; 28 with the counts changed by the cluster alone and a search for
 // each page's row.
 constexpr int kTakeThreads = 1024, kTakeWarps = kTakeThreads / 32, kTakeCtas = 8;
-constexpr int kTakeBlock = 128;  // columns of a table row that a warp looks at together
-constexpr int kTakeMasks = 32;   // words of free pages that a warp keeps
-constexpr int kTakeFew = 16384;  // pages that one CTA looks through
+constexpr int kTakeBlock = 128;    // columns of a table row that a warp looks at together
+constexpr int kTakeMasks = 32;     // words of free pages that a warp keeps
+constexpr int kTakeFew = 16384;    // pages that one CTA looks through
+constexpr int kTakeBlocks = 2048;  // blocks of a pool, at most
 
-constexpr int kTakeBlocks = 2048;
-
-// A pool in blocks of 256 pages, or larger ones where it would have more than kTakeBlocks.
+// A pool in blocks of 256 pages, or larger ones where there would be too many.
 __host__ __device__ inline int block_shift(int n_pages) {
   int shift = 8;
   while (n_pages > (kTakeBlocks << shift)) ++shift;
@@ -196,12 +195,12 @@ template <bool FORK>
 __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __grid_constant__ PagesArgs given, bool touched) {
   extern __shared__ int dynamic[];
   __shared__ int warp_sum[kTakeWarps], in_block[kTakeBlocks];  // in_block: free pages of each block, then before it
-  pdl_trigger();
-  int* base = dynamic;             // [rows + 1]: pages that earlier rows need
-  int* touch = base + given.rows + 1;  // [rows]: first column given up or shared
-  int* end = touch + given.rows;    // [rows]: the column behind the last; the first that gets a page
-  unsigned* masks = reinterpret_cast<unsigned*>(end + given.rows);  // free pages of a warp's part, 32 to a word
   __shared__ unsigned char lists[kTakeWarps * 256];
+  pdl_trigger();
+  int* base = dynamic;                 // [rows + 1]: pages that earlier rows need
+  int* touch = base + given.rows + 1;  // [rows]: first column given up or shared
+  int* end = touch + given.rows;       // [rows]: the column behind the last; the first that gets a page
+  unsigned* masks = reinterpret_cast<unsigned*>(end + given.rows);  // free pages of a warp's blocks, 32 to a word
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = static_cast<int>(cluster_rank()), ctas = static_cast<int>(cluster_size());
   const int gw = rank * kTakeWarps + warp, warps = ctas * kTakeWarps;

@@ -159,6 +159,9 @@ zsaa_status check_layers(const zsaa_pages* layers, int n_layers, PoolList* pools
   return ZSAA_OK;
 }
 
+// (a grid's third dimension, 4 CTAs to a head; a page's vectors in 31 bits)
+zsaa_status check_heads(int n) { return n <= 16383 ? ZSAA_OK : bad("more than 16383 KV heads"); }
+
 // rows of a table whose pages a call takes
 zsaa_status check_taking(int rows, int cols, int page) {
   if (rows < 1) return bad("a table needs 1 or more rows");
@@ -350,6 +353,7 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
   if (!words(refs, table, lens, parent, at, table_out, lens_out, n_free)) return bad("int32 arrays must be 4-byte aligned");
   const zsaa_pages& p = layers[0];
   if (S < 1) return bad("S must be >= 1");
+  ZTRY(check_heads(p.n_kv_heads));
   ZTRY(check_taking(N, cols, p.page_size));
   if (static_cast<long long>(S) * cols > kMostInt) return bad("a table must have fewer than 2^31 entries");
   const size_t in = 4 * static_cast<size_t>(S), out = 4 * static_cast<size_t>(N);
@@ -378,7 +382,7 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   if (!words(refs, table, lens, start, keep, n_keep, table_out, lens_out)) return bad("int32 arrays must be 4-byte aligned");
   const zsaa_pages& p = layers[0];
   if (S < 1 || keep_cols < 1) return bad("S and keep_cols must be >= 1");
-  if (p.n_kv_heads > 16383) return bad("more than 16383 KV heads");  // (a grid's third dimension, 4 CTAs to a head)
+  ZTRY(check_heads(p.n_kv_heads));
   ZTRY(check_cols(cols, p.page_size));
   ZTRY(check_cols(out_cols, p.page_size));
   const size_t row = 4 * static_cast<size_t>(S);

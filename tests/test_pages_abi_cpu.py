@@ -89,7 +89,8 @@ def test_unlike_layers_and_their_number(zlib):
         refused(zlib, lambda: compact(zlib, [pages(zlib), pages(zlib, **kw)]))
     refused(zlib, lambda: fork(zlib, [pages(zlib)] * 65))
     refused(zlib, lambda: compact(zlib, [pages(zlib)] * 65))
-    refused(zlib, lambda: compact(zlib, [pages(zlib, n_kv_heads=16384, n_pages=1)]))
+    for call in (fork, compact):
+        refused(zlib, lambda: call(zlib, [pages(zlib, n_kv_heads=16384, n_pages=1)]))
     L, one = zlib.lib(), pages(zlib)
     for layers, n in ((None, 1), (C.addressof(one), 0)):
         assert L.zsaa_op_paged_fork(layers, n, A, 1, B, 1, D, 1, E, None, FAR, FAR + 64, None, None) == zlib.ZSAA_ERR_INVALID_ARG
