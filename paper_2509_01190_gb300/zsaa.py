@@ -509,11 +509,13 @@ def zsaa_op_colmass_ex(qkv, lse, B: int, N: int, Hq: int, Hkv: int, hd: int, dty
 def _at(t, dtype, n, name, dev):
     """Pointer of a contiguous tensor of at least n elements on device `dev`, the
     current one (an int or None passes as it is)."""
+    if t is None:
+        return t
     try:
         if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= n:
             return t.data_ptr()
     except AttributeError:
-        if t is None or isinstance(t, int):
+        if isinstance(t, int):
             return t
     raise ZsaaError(ZSAA_ERR_INVALID_ARG,
                     f"{name}: needs a contiguous {dtype} tensor with {n} or more elements on the current device")
