@@ -74,16 +74,24 @@ __device__ __forceinline__ int drafts_of(const VerifyArgs& a, int s) {
   return __ffs(__ballot_sync(0xffffffffu, x < 0 || x >= a.V)) - 1;  // (lane 31 has no draft)
 }
 
+// 32 values of a thread as they are stored, 16 bytes to a vector.
+constexpr int kScanValues = 32;
 template <typename T>
-__device__ __forceinline__ void load16(const T* p, float* x) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  if constexpr (sizeof(T) == 2) {
-    x[0] = bf16lo(u.x), x[1] = bf16hi(u.x), x[2] = bf16lo(u.y), x[3] = bf16hi(u.y);
-    x[4] = bf16lo(u.z), x[5] = bf16hi(u.z), x[6] = bf16lo(u.w), x[7] = bf16hi(u.w);
-  } else {
-    x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
+struct Stored {
+  static constexpr int VEC = 16 / sizeof(T);
+  uint4 v[kScanValues / VEC];
+  __device__ __forceinline__ float at(int k) const {
+    const uint4& u = v[k / VEC];
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w = k % VEC < 2 ? u.x : k % VEC < 4 ? u.y : k % VEC < 6 ? u.z : u.w;
+      return k % 2 == 0 ? bf16lo(w) : bf16hi(w);
+    } else {
+      return __uint_as_float(k % VEC == 0 ? u.x : k % VEC == 1 ? u.y : k % VEC == 2 ? u.z : u.w);
+    }
   }
-}
+};
+__device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ uint32_t bits_of(bf16 x) { return __bfloat16_as_ushort(x); }
 
 // Row r of sequence s: target row r for r <= n, else draft row r - n - 1.
 template <typename T>
@@ -358,8 +366,15 @@ __device__ __forceinline__ VerifyRow row_total(const VerifyChunk* chunks, Verify
 
 // ---------------------------------------------------------------- the rows' maxima and sums
 
-constexpr int kScanPerSm = 4;
-constexpr int kScanThreads = 256, kScanValues = 32, kScanTokens = kScanThreads * kScanValues;
+// CTAs to an SM, for the scan of all rows and for the one in turn.  Threads keep their logits as they
+// are stored, so bf16 takes half the registers (us, 24 sequences of 3 drafts over 50257 bf16 logits:
+// unpacked, 4 to an SM 19.2, packed 4 18.8, 5 18.5, 6 18.9; in turn, 64 of 5 over 128256: 3 62.9,
+// 4 60.0, 5 62.0).
+template <typename T>
+constexpr int kScanPerSm = sizeof(T) == 2 ? 5 : 4;
+template <typename T>
+constexpr int kTurnPerSm = sizeof(T) == 2 ? 4 : 3;
+constexpr int kScanThreads = 256, kScanTokens = kScanThreads * kScanValues;
 
 // Sum over the warp of values in [0, 2^50) (two 32-bit reductions of 25 bits each).
 __device__ __forceinline__ unsigned long long warp_sum_u50(unsigned long long v) {
@@ -376,8 +391,8 @@ struct StretchParts {
   int first[kScanThreads / 32];
 };
 template <typename T>
-__device__ __forceinline__ void load_stretch(const T* row, int chunk, int V, float (&x)[kScanValues]) {
-  constexpr int VEC = 16 / sizeof(T);
+__device__ __forceinline__ void load_stretch(const T* row, int chunk, int V, Stored<T>& x) {
+  constexpr int VEC = Stored<T>::VEC, PER_WORD = 4 / sizeof(T);
   // the stretch starts on a 16-byte boundary, before the row's first token for the first one
   const int lead = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
   const int t0 = chunk * kScanTokens - lead;
@@ -385,25 +400,34 @@ __device__ __forceinline__ void load_stretch(const T* row, int chunk, int V, flo
   for (int k = 0; k < kScanValues / VEC; ++k) {
     const int at = t0 + (k * kScanThreads + static_cast<int>(threadIdx.x)) * VEC;
     if (at >= 0 && at <= V - VEC) {
-      load16(row + at, x + k * VEC);
+      x.v[k] = *reinterpret_cast<const uint4*>(row + at);
     } else {
+      uint32_t w[4];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[k * VEC + i] = at + i >= 0 && at + i < V ? to_f<T>(row[at + i]) : -INFINITY;
+      for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int j = 0; j < PER_WORD; ++j) {
+          const int t = at + i * PER_WORD + j;
+          w[i] |= bits_of(t >= 0 && t < V ? row[t] : from_f<T>(-INFINITY)) << (16 * j);
+        }
+      }
+      x.v[k] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
 }
 // (returns whether the CTA has seen a NaN or +inf)
 template <typename T>
 __device__ __forceinline__ bool scan_stretch(const T* row, int chunk, int V, bool greedy, float c,
-                                             const float (&x)[kScanValues], StretchParts& parts) {
-  constexpr int VEC = 16 / sizeof(T);
+                                             const Stored<T>& x, StretchParts& parts) {
+  constexpr int VEC = Stored<T>::VEC;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   float top = -INFINITY;
   bool bad = false;
 #pragma unroll
   for (int k = 0; k < kScanValues; ++k) {
-    top = fmaxf(top, x[k]);
-    bad |= !(x[k] < INFINITY);
+    top = fmaxf(top, x.at(k));
+    bad |= !(x.at(k) < INFINITY);
   }
   top = warp_max(top);
   unsigned long long total = 0;
@@ -413,14 +437,14 @@ __device__ __forceinline__ bool scan_stretch(const T* row, int chunk, int V, boo
 #pragma unroll
     for (int k = kScanValues - 1; k >= 0; --k) {
       const int at = t0 + ((k / VEC) * kScanThreads + tid) * VEC + k % VEC;
-      if (x[k] == top && at >= 0 && at < V) first = at;
+      if (x.at(k) == top && at >= 0 && at < V) first = at;
     }
     first = __reduce_min_sync(0xffffffffu, first);
   } else {
     const float ref = top == -INFINITY ? 0.f : top;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kScanValues; ++k) sum[k & 3] += ex2((x[k] - ref) * c);
+    for (int k = 0; k < kScanValues; ++k) sum[k & 3] += ex2((x.at(k) - ref) * c);
     // (bad rows have any sum)
     total = warp_sum_u50(static_cast<unsigned long long>(fminf((sum[0] + sum[1]) + (sum[2] + sum[3]), 64.f) * kSumScale));
   }
@@ -445,7 +469,7 @@ __device__ __forceinline__ VerifyChunk joined_stretch(const StretchParts& parts,
 // All rows at once.  Where the CTAs run in one round a row's logits are fetched before it is known
 // whether they decide anything: 0.6 us less, and the bytes of rows left out cost none.
 template <typename T>
-__global__ void __launch_bounds__(kScanThreads, kScanPerSm)
+__global__ void __launch_bounds__(kScanThreads, kScanPerSm<T>)
     verify_scan_kernel(const __grid_constant__ VerifyArgs a, bool at_once) {
   __shared__ StretchParts parts;
   pdl_trigger();
@@ -456,7 +480,7 @@ __global__ void __launch_bounds__(kScanThreads, kScanPerSm)
   const int r = static_cast<int>(item - s * static_cast<unsigned>(a.rows));
   if (r == 0 && chunk == 0 && threadIdx.x == 0) a.state[s].done = 0;
   const T* row = row_of<T>(a, s, r);
-  float x[kScanValues];
+  Stored<T> x;
   if (at_once) load_stretch(row, chunk, a.V, x);
   const Temperature t = temperature_of(a, s);
   const bool is_draft = r > a.n;
@@ -479,10 +503,11 @@ __global__ void __launch_bounds__(kScanThreads, kScanPerSm)
 // sequence's stop.  A row is left out only where the stop lies before it, so the rows up to the
 // first draft that does not stand are all scanned, whatever the order in which CTAs run.  64 sequences
 // of 5 drafts, of which 2.1 stand: 214 of the 361 MB in 52 us.  A CTA's chain bounds it (state, rows,
-// sums, count: 5 us with loads on their way for two of them), three CTAs to an SM; one that finds
-// its row not wanted takes 1 us.
+// sums, count: 5 us with loads on their way for two of them), three CTAs to an SM in float32; one that
+// finds its row not wanted takes 1 us.
 template <typename T>
-__global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kScanThreads, kTurnPerSm<T>)
+    verify_scan_in_turn_kernel(const __grid_constant__ VerifyArgs a) {
   __shared__ float table[64];
   __shared__ StretchParts parts[2];
   __shared__ int4 s_state;
@@ -502,7 +527,7 @@ __global__ void __launch_bounds__(kScanThreads, 3) verify_scan_in_turn_kernel(co
   const bool soft = v.z != 0, two = soft && a.draft != nullptr && j < n;
   const float temperature = __int_as_float(v.w), c = log2e_over(temperature);
   const T *row = row_of<T>(a, s, j), *draft_row = two ? row_of<T>(a, s, a.n + 1 + j) : row;
-  float x[kScanValues], y[kScanValues];
+  Stored<T> x, y;
   load_stretch(row, chunk, a.V, x);
   if (two) load_stretch(draft_row, chunk, a.V, y);
   if (tid < 64) table[tid] = kPowers.v[tid];
@@ -949,19 +974,18 @@ VerifySlices verify_slices(int S, int V, int sms, int rounds) {
   return VerifySlices{static_cast<int>((all + steps - 1) / steps), static_cast<int>(steps) * kGroupStep};
 }
 
-// Whether rows are scanned in turn: from five rounds of the CTAs of the scan of all rows on (128256
-// float32 logits, drafts of which three of five stand, us for all rows and in turn: 8 sequences of 5
-// drafts 23 and 30, 16 34 and 36, 24 49 and 46, 48 82 and 76; 64 of one draft 61 and 56; 16 of 15
-// drafts 66 and 51).
+// Whether rows are scanned in turn: from 20 stretches to an SM on (128256 float32 logits, drafts of
+// which three of five stand, us for all rows and in turn: 8 sequences of 5 drafts 23 and 30, 16 34 and
+// 36, 24 49 and 46, 48 82 and 76; 64 of one draft 61 and 56; 16 of 15 drafts 66 and 51).
 bool in_turn(const VerifyArgs& a, int sms) {
-  return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 5ll * kScanPerSm * sms;
+  return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 20ll * sms;
 }
 
 template <typename T>
 cudaError_t run_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
   // Two rounds where the decisions have been made: CTAs of sequences that end at once make room
   // (64 sequences, us: one round 90, two 81, three 82); one where every CTA makes them (24
-  // sequences of 50257 bf16 logits: one 19.9, two 23.5).
+  // sequences of 50257 bf16 logits: one 19.9, two 23.5, with logits unpacked).
   const bool turns = in_turn(a, sms);
   const VerifySlices c = verify_slices(a.S, a.V, sms, turns ? 2 : 1);
   int bits = 10;  // units in which sums of up to V exponentials stay below 2^62
@@ -974,7 +998,7 @@ cudaError_t run_verify(const VerifyArgs& a, int sms, cudaStream_t s) {
     ZSAA_LAUNCH(verify_scan_in_turn_kernel<T>, turns_grid, dim3(kScanThreads), 0, s, a);
     ZSAA_LAUNCH((verify_finish_kernel<T, true>), finish, dim3(kFinishThreads), 0, s, a, c.ctas, c.group, unit);
   } else {
-    ZSAA_LAUNCH(verify_scan_kernel<T>, grid, dim3(kScanThreads), 0, s, a, grid.x <= static_cast<unsigned>(kScanPerSm * sms));
+    ZSAA_LAUNCH(verify_scan_kernel<T>, grid, dim3(kScanThreads), 0, s, a, grid.x <= static_cast<unsigned>(kScanPerSm<T> * sms));
     ZSAA_LAUNCH((verify_finish_kernel<T, false>), finish, dim3(kFinishThreads), 0, s, a, c.ctas, c.group, unit);
   }
   return cudaSuccess;
