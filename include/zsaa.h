@@ -652,11 +652,11 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  *              the first of the largest logits, draft rows not read.  At most 2^64
  *   uniform  : float32 [S, n+1] in [0, 1), u_0 .. u_n (a NaN counts as 0, others as the nearest)
  *   accepted : int32 [S], how many drafts stand
- *   tokens   : int32 [S, n+1], those drafts, the next token, then -1 (must not overlap drafts)
+ *   tokens   : int32 [S, n+1], those drafts, the next token, then -1
  *   logp     : float32 [S, n+1] or NULL, log p_j of each token of `tokens`, 0 where there is none
  *   lens, lens_out: int32 [S], both or neither: lens - (n - accepted), not below 0: the entries
- *              that remain of a cache to which a token and n drafts were appended.  lens_out
- *              may be lens
+ *              that remain of a cache to which a token and n drafts were appended
+ * Outputs must not overlap inputs or one another, except that lens_out may be lens.
  * A row has no distribution where it holds a NaN or +inf or nothing above -inf, or its
  * temperature is negative, NaN or above 2^64.  A target row without one ends the sequence's
  * tokens: the next one is -1.  Exponentials that a token is picked by are good to 2^-35.7, the

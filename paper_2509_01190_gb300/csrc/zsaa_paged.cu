@@ -428,8 +428,20 @@ zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* dra
   if (!aligned(ws, 16)) return bad("ws must be 16-byte aligned");
   if (ws_bytes < need) return refuse(ZSAA_ERR_INVALID_ARG, "ws_bytes %zu, needs %zu", ws_bytes, need);
   const size_t row = 4 * static_cast<size_t>(S);
-  if (drafts != nullptr && overlap(drafts, row * n, tokens, row * (n + 1))) return bad("tokens overlap drafts");
-  if (lens != nullptr && lens != lens_out && overlap(lens, row, lens_out, row)) return bad("lens_out overlaps lens");
+  // CTAs of a sequence read what others of it write, so outputs lie over nothing else (but lens_out may be lens)
+  const struct {
+    const void* p;
+    size_t bytes;
+  } arrays[] = {{accepted, row},    {tokens, row * (n + 1)},  {logp, row * (n + 1)}, {lens_out, row},
+                {lens, row},        {drafts, row * n},        {temperature, row},    {uniform, row * (n + 1)}};
+  for (int o = 0; o < 4; ++o) {
+    for (int i = o + 1; i < 8; ++i) {
+      const bool in_place = o == 3 && i == 4 && lens == lens_out;
+      if (arrays[o].p != nullptr && arrays[i].p != nullptr && !in_place &&
+          overlap(arrays[o].p, arrays[o].bytes, arrays[i].p, arrays[i].bytes))
+        return bad("an output overlaps an input or another output");
+    }
+  }
   int sms = 0;
   ZTRY(device_sms(&sms));
   VerifyArgs a{};

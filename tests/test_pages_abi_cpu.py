@@ -108,6 +108,14 @@ def test_verify_refusals(zlib, kw):
     refused(zlib, lambda: verify(zlib, **kw))
 
 
+@pytest.mark.parametrize("kw", [
+    dict(logp=E), dict(logp=E + 60), dict(accepted=E + 12), dict(tokens=E - 4), dict(temperature=B, logp=B + 12), dict(accepted=D),
+    dict(accepted=FAR + 4096 - 12), dict(logp=FAR + 4096), dict(lens=B, lens_out=FAR + 12), dict(lens=B, lens_out=E),
+    dict(accepted=B, lens=B, lens_out=B + 4096), dict(lens=B, lens_out=B, temperature=B + 12)])
+def test_verify_refuses_outputs_over_anything_else(zlib, kw):
+    refused(zlib, lambda: verify(zlib, **kw))
+
+
 @pytest.mark.parametrize("n", [-1, 16])
 def test_verify_refuses_more_drafts_than_it_takes(zlib, n):
     refused(zlib, lambda: verify(zlib, n=n), zlib.ZSAA_ERR_UNSUPPORTED)
