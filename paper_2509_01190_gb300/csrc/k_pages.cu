@@ -245,15 +245,17 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   const int shift = block_shift(a.n_pages), block_words = 1 << (shift - 5), blocks = (a.n_pages + (1 << shift) - 1) >> shift;
   const int words = ((blocks + warps - 1) / warps) << (shift - 5);  // of a warp
   const bool kept = words <= kTakeMasks;
-  auto page_of = [&](int w) {  // first page of this warp's word w
-    return (static_cast<long long>((w >> (shift - 5)) * warps + gw) << shift) + 32 * (w & (block_words - 1));
+  auto block_of = [&](int w) { return (w >> (shift - 5)) * warps + gw; };  // of this warp's word w
+  auto page_of = [&](int w) {                                              // its first page
+    return (static_cast<long long>(block_of(w)) << shift) + 32 * (w & (block_words - 1));
   };
   auto count_at = [&](int w) {
     const long long q = page_of(w) + lane;
     return q < a.n_pages ? __ldcg(a.refs + q) : 1;
   };
   int n_free = 0;
-  for (int w0 = 0; w0 < words && page_of(w0) < a.n_pages; w0 += 16) {
+  // (a block that the pool's end cuts is gone through to its own end: its last word stores its count)
+  for (int w0 = 0; w0 < words && block_of(w0) < blocks; w0 += 16) {
     int c[16], least = 1;
     unsigned mine_mask = 0;  // lane k: word w0 + k
 #pragma unroll
@@ -267,7 +269,7 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
       if (lane == k) mine_mask = m;
       n_free += __popc(m);
       if (((w0 + k + 1) & (block_words - 1)) == 0) {
-        const int block = ((w0 + k) >> (shift - 5)) * warps + gw;
+        const int block = block_of(w0 + k);
         if (lane < ctas && block < blocks) st_cluster_u32(smem_u32(&in_block[block]), lane, n_free);
         n_free = 0;
       }
@@ -313,7 +315,7 @@ __global__ void __launch_bounds__(kTakeThreads, 1) pages_take_kernel(const __gri
   unsigned char* list = lists + warp * 256;
   int lo = -1;
   for (int w0 = 0; w0 < words && page_of(w0) < a.n_pages; w0 += 8) {
-    if (w0 > 0 && (w0 & (block_words - 1)) == 0) free_before = in_block[(w0 >> (shift - 5)) * warps + gw];
+    if (w0 > 0 && (w0 & (block_words - 1)) == 0) free_before = in_block[block_of(w0)];
     if (free_before >= total_need) break;
     const int q0 = static_cast<int>(page_of(w0));
     int n = 0;

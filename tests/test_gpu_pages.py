@@ -77,6 +77,34 @@ def test_resize(zlib, S, cols, page, n_pages):
     assert (led.refs[led.refs != 3] == 0).all()
 
 
+@pytest.mark.parametrize("n_pages", [600001, 1 << 20, (1 << 20) + 1, (1 << 20) + 300, (1 << 20) + 512, (1 << 20) + 513, 2000000,
+                                     (1 << 21) + 1, 5000000, (1 << 30) - 600])
+def test_resize_counts_pools_of_which_a_block_is_large(zlib, n_pages):
+    """Free pages here and there, the pool's last ones among them: what is left, and what a call gets
+    that asks for more than there are."""
+    r = np.random.default_rng(n_pages)
+    free = np.unique(np.concatenate([r.integers(0, n_pages, 4000), r.integers(n_pages - 200, n_pages, 50), [n_pages - 1]]))
+    refs = torch.full((n_pages,), 2, dtype=torch.int32, device="cuda")
+    refs[torch.from_numpy(free).cuda()] = 0
+    n, got, page, S, cols = len(free), out_lens(3), 16, 3, 3000
+    table, lens, left = ints(np.full((S, cols), -1)), ints([0, 0, 0]), out_lens(1)
+
+    def call(want):
+        zlib.zsaa_op_paged_resize(refs, n_pages, page, S, table, cols, lens, ints(want), got, left)
+        lens.copy_(got)
+
+    call([160, 0, 17])
+    assert left.item() == n - 12 and got.tolist() == [160, 0, 17] and (refs == 0).sum().item() == n - 12
+    call([2000 * page, 0, 3000 * page])  # (4988 more pages)
+    assert left.item() == 0 and got.tolist() == [2000 * page, 0, (n - 2000) * page] and (refs == 0).sum().item() == 0
+    taken = np.concatenate([free[:10], free[12:2002], free[10:12], free[2002:]])
+    np.testing.assert_array_equal(table.cpu().numpy()[[0] * 2000 + [2] * (n - 2000), [*range(2000), *range(n - 2000)]], taken)
+    call([2000 * page, 5 * page, 100 * page])  # what the last one gives up goes to the one before
+    assert left.item() == n - 2105 and got.tolist() == [2000 * page, 5 * page, 100 * page]
+    call([0, 0, 0])
+    assert left.item() == n and (refs == 0).sum().item() == n and refs.sum().item() == 2 * (n_pages - n)
+
+
 def test_resize_lengths_of_zero_one_and_around_pages(zlib):
     led = Ledger(zlib, 6, 4, 16, 40)
     for want in ([0, 1, 15, 16, 17, 64], [1, 0, 16, 17, 16, 63], [64, 48, 1, 33, 32, 0], [0] * 6):
@@ -204,6 +232,20 @@ def test_fork_no_child_and_every_place_of_a_page(zlib):
 def test_fork_runs_out_of_pages(zlib, spare):
     got = forked(zlib, "bf16", 2, 2, 128, 16, [37, 16, 50, 3], [0, 1, 2, 3, 0, 2], spare=spare)
     assert sorted(got % 16 > 0).count(True) == spare
+
+
+def test_fork_takes_the_last_pages_of_a_large_pool(zlib):
+    """2^20 + 300 pages, the last two free: the third of three children that need one gets none."""
+    n_pages, page = (1 << 20) + 300, 16
+    k, v = (torch.zeros(1, n_pages, 1, page, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    k[:, :2] = torch.randn(1, 2, 1, page, 64, device="cuda").to(torch.bfloat16)
+    refs, out, got, left = torch.ones(n_pages, dtype=torch.int32, device="cuda"), ints(np.full((3, 2), -1)), out_lens(3), out_lens(1)
+    refs[n_pages - 2:] = 0
+    zlib.zsaa_op_paged_fork(zlib.make_pages_list(list(k), list(v)), refs, 1, ints([[0, 1]]), 2, ints([25]), 3, ints([0, 0, 0]), None,
+                            out, got, left)
+    assert out.tolist() == [[0, n_pages - 2], [0, n_pages - 1], [0, -1]] and got.tolist() == [25, 25, 16] and left.item() == 0
+    assert torch.equal(k[0, -2, 0, :9], k[0, 1, 0, :9]) and torch.equal(k[0, -1, 0, :9], k[0, 1, 0, :9])
+    assert refs[0].item() == 4 and (k[0, -2:, 0, 9:] == 0).all()
 
 
 def test_fork_reports_bad_parents_pages_and_lengths(zlib):
