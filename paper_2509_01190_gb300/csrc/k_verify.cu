@@ -279,7 +279,8 @@ __device__ __noinline__ bool stands_far(float u, float xp, float xq, float t, co
     return (static_cast<double>(x) - static_cast<double>(r.m)) / t - log(sum);
   };
   const double lp = log_of(xp, p), lq = lookup ? 0.0 : log_of(xq, q);
-  return lp > -INFINITY && (lq == -INFINITY || u < exp(lp - lq));
+  // (u = 0: wherever p(x) > 0, however small; the quotient may be below the least number above 0)
+  return lp > -INFINITY && (lq == -INFINITY || u == 0.f || u < exp(lp - lq));
 }
 
 // What a sequence's rows have in common.

@@ -148,6 +148,29 @@ def test_verify_numbers_at_and_beyond_their_ends(zlib):
         check(zlib, target, draft, drafts, None, u)
 
 
+@pytest.mark.parametrize("S", [5, 1700])  # (the second scans draft by draft)
+@pytest.mark.parametrize("lookup", [False, True])
+@pytest.mark.parametrize("gap,t", [(800.0, 1.0), (40.0, 0.05), (1e30, 1.0), (90.0, 1.0)])
+def test_verify_the_number_0_takes_every_draft_that_is_possible(zlib, gap, t, lookup, S):
+    """u q(x) < p(x) is 0 < p(x) then, also where p(x) is e^-800 or smaller; a banned token has 0."""
+    V, x = 50, 5
+    target = np.zeros((S, 2, V), np.float32)
+    target[:, :, 7] = gap
+    draft = np.zeros((S, 1, V), np.float32)
+    draft[:, :, x] = gap
+    target[3, 0, x] = -INF
+    for v in (0.0, -1.0, NAN, 1e-45):
+        u = np.full((S, 2), 0.5, np.float32)
+        u[:, 0] = v
+        acc, tok, logp, _, _ = call(zlib, target, None if lookup else draft, np.full((S, 1), x), np.full(S, t), u)
+        # (1e-45 is e^-103.3: it refuses what is less likely than that)
+        stands = np.arange(S) != 3 if v != 1e-45 or gap == 90.0 else np.zeros(S, bool)
+        np.testing.assert_array_equal(acc, stands)
+        np.testing.assert_array_equal(tok, np.where(stands[:, None], [x, 7], [7, -1]))
+        want = -gap / float(np.float32(t))  # (as in check)
+        assert np.all(np.abs(logp[stands] - [want, 0.0]) <= 2.0 ** -17 + R.F32_HALF * abs(want))
+
+
 def test_verify_equal_rows_stand_and_opposite_ones_do_not(zlib):
     target, _, _, u, r = draw(6, 3, 4000, 6)
     drafts = np.argmax(target[:, :3] + r.gumbel(size=(6, 3, 4000)), 2)
