@@ -656,7 +656,8 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  *   logp     : float32 [S, n+1] or NULL, log p_j of each token of `tokens`, 0 where there is none
  *   lens, lens_out: int32 [S], both or neither: lens - (n - accepted), not below 0: the entries
  *              that remain of a cache to which a token and n drafts were appended
- * Outputs must not overlap inputs or one another, except that lens_out may be lens.
+ * Outputs and ws must not overlap inputs or one another, except that lens_out may be lens (what lies
+ * between rows of logits, past V, is free).
  * A row has no distribution where it holds a NaN or +inf or nothing above -inf, or its
  * temperature is negative, NaN or above 2^64.  A target row without one ends the sequence's
  * tokens: the next one is -1.  Exponentials that a token is picked by are good to 2^-35.7, the

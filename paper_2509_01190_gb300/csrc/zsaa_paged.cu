@@ -47,6 +47,14 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
+// with any of n rows of `width` bytes, `stride` bytes apart (what lies between them is no part of them)
+bool overlap_rows(const void* a, size_t an, const void* rows, size_t n, size_t stride, size_t width) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), r = reinterpret_cast<uintptr_t>(rows);
+  if (x <= r) return r - x < an;
+  const uintptr_t row = (x - r) / stride, at = (x - r) % stride;  // the last row that starts at or before x
+  return row < n && (at < width || (row + 1 < n && stride - at < an));
+}
+
 constexpr long long kMostInt = 0x7fffffff;
 constexpr int kMostPages = 1 << 30;
 
@@ -428,19 +436,24 @@ zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* dra
   if (!aligned(ws, 16)) return bad("ws must be 16-byte aligned");
   if (ws_bytes < need) return refuse(ZSAA_ERR_INVALID_ARG, "ws_bytes %zu, needs %zu", ws_bytes, need);
   const size_t row = 4 * static_cast<size_t>(S);
-  // CTAs of a sequence read what others of it write, so outputs lie over nothing else (but lens_out may be lens)
+  // CTAs of a sequence read what others of it write, so outputs and the workspace lie over nothing else (but
+  // lens_out may be lens)
+  const size_t e = element(dtype), drafted = draft != nullptr ? static_cast<size_t>(S) * n : 0;
   const struct {
     const void* p;
     size_t bytes;
-  } arrays[] = {{accepted, row},    {tokens, row * (n + 1)},  {logp, row * (n + 1)}, {lens_out, row},
+  } arrays[] = {{accepted, row},    {tokens, row * (n + 1)},  {logp, row * (n + 1)}, {lens_out, row}, {ws, need},
                 {lens, row},        {drafts, row * n},        {temperature, row},    {uniform, row * (n + 1)}};
-  for (int o = 0; o < 4; ++o) {
-    for (int i = o + 1; i < 8; ++i) {
-      const bool in_place = o == 3 && i == 4 && lens == lens_out;
-      if (arrays[o].p != nullptr && arrays[i].p != nullptr && !in_place &&
-          overlap(arrays[o].p, arrays[o].bytes, arrays[i].p, arrays[i].bytes))
-        return bad("an output overlaps an input or another output");
+  for (int o = 0; o < 5; ++o) {
+    if (arrays[o].p == nullptr) continue;
+    for (int i = o + 1; i < 9; ++i) {
+      const bool in_place = o == 3 && i == 5 && lens == lens_out;
+      if (arrays[i].p != nullptr && !in_place && overlap(arrays[o].p, arrays[o].bytes, arrays[i].p, arrays[i].bytes))
+        return bad("an output or the workspace overlaps another array");
     }
+    if (overlap_rows(arrays[o].p, arrays[o].bytes, target, static_cast<size_t>(S) * (n + 1), ld * e, V * e) ||
+        (drafted > 0 && overlap_rows(arrays[o].p, arrays[o].bytes, draft, drafted, draft_ld * e, V * e)))
+      return bad("an output or the workspace overlaps the logits");
   }
   int sms = 0;
   ZTRY(device_sms(&sms));

@@ -116,6 +116,35 @@ def test_verify_refuses_outputs_over_anything_else(zlib, kw):
     refused(zlib, lambda: verify(zlib, **kw))
 
 
+W = FAR + (5 << 36)  # a workspace apart from everything else
+TARGET, DRAFT = (15 * 1024 + 1000) * 4, (11 * 1100 + 1000) * 4  # bytes of rows 1024 and 1100 apart
+
+
+@pytest.mark.parametrize("kw,what", [
+    (dict(accepted=A), "logits"), (dict(accepted=A - 12), "logits"), (dict(accepted=A + TARGET - 4), "logits"),
+    (dict(accepted=A + 4 * 1021), "logits"), (dict(accepted=A + 4 * (7 * 1024 + 999)), "logits"), (dict(tokens=A + 4 * 1010), "logits"),
+    (dict(logp=B + 4), "logits"), (dict(logp=B + DRAFT - 4), "logits"), (dict(logp=B + 4 * 1090), "logits"),
+    (dict(lens=D + 4096, lens_out=B + 4 * 2200), "logits"), (dict(ws=A), "logits"), (dict(ws=B + 4 * 2196), "logits"),
+    (dict(ws=B - 64), "logits"), (dict(lens=A, lens_out=A), "logits"), (dict(ws=D), "array"), (dict(ws=E), "array"), (dict(ws=FAR), "array"),
+    (dict(ws=FAR + 4096 + 48), "array"), (dict(logp=W + 16), "array"), (dict(temperature=W + 64), "array"),
+    (dict(lens=W, lens_out=FAR + 8192), "array"), (dict(lens=D + 4096, lens_out=W), "array")])
+def test_verify_refuses_outputs_and_a_workspace_over_logits_or_one_another(zlib, kw, what):
+    with pytest.raises(zlib.ZsaaError, match="overlaps " + ("the logits" if what == "logits" else "another array")):
+        verify(zlib, **{**dict(ld=1024, draft_ld=1100, ws=W), **kw})
+
+
+@pytest.mark.parametrize("kw", [
+    dict(), dict(accepted=A + 4 * 1000), dict(accepted=A + 4 * 1020), dict(accepted=A + TARGET), dict(accepted=A - 16),
+    dict(logp=B + 4 * 1000), dict(logp=B + DRAFT), dict(logp=B + 4 * 1084), dict(lens=A, lens_out=FAR + 8192), dict(draft=A),
+    dict(ws=A + TARGET), dict(lens=FAR + 8192, lens_out=FAR + 8192), dict(n=0, drafts=A, draft=FAR)])
+def test_verify_takes_outputs_beside_and_between_rows_of_logits(zlib, kw):
+    """Nothing refuses them before a device is looked for."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("there is a device, and the addresses are none of its")
+    refused(zlib, lambda: verify(zlib, **{**dict(ld=1024, draft_ld=1100, ws=W), **kw}), zlib.ZSAA_ERR_CUDA)
+
+
 @pytest.mark.parametrize("n", [-1, 16])
 def test_verify_refuses_more_drafts_than_it_takes(zlib, n):
     refused(zlib, lambda: verify(zlib, n=n), zlib.ZSAA_ERR_UNSUPPORTED)
