@@ -590,8 +590,9 @@ zsaa_status zsaa_op_beam_reorder(const zsaa_pages* layers, int n_layers, int B, 
  * get pages, sequence by sequence, pages just given up among them.  Contents are not moved.
  *   table   : int32 [S, cols], changed in place: entries of pages given up stay, unused
  *   lens_out: int32 [S], the lengths reached: want, or what the pages suffice for where
- *             they run out (no error: lens_out < want tells).  Must not overlap lens or want
+ *             they run out (no error: lens_out < want tells)
  *   n_free  : int32 [1], the free pages left, or NULL
+ * refs, table, lens_out and n_free must not overlap one another, lens or want.
  * want = 0 ends a sequence.  A page given up that nothing refers to is reported as a page
  * number out of range is, and its count stays 0.  page_size as zsaa_pages', n_pages <= 2^30. */
 zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int S, int32_t* table, int cols,
@@ -607,9 +608,10 @@ zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int 
  *   table, lens: int32 [S, cols] and [S]
  *   parent : int32 [N] in [0, S), or -1 for no child (its lens_out is 0);  at: int32 [N] or NULL
  *   table_out, lens_out: int32 [N, cols] and [N], overwritten: rows that held pages give them
- *            up first (zsaa_op_paged_resize to 0).  Must not overlap the inputs; entries of
- *            table_out past a child's last page stay as they were
+ *            up first (zsaa_op_paged_resize to 0).  Entries of table_out past a child's last
+ *            page stay as they were
  *   n_free : as above
+ * refs, table_out, lens_out and n_free must not overlap one another or the other arrays.
  * Where pages run out a child keeps its whole pages: lens_out = m / page_size * page_size.
  * At most 16383 KV heads. */
 zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* refs, int S, const int32_t* table, int cols,
@@ -628,7 +630,7 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
  *            in use for nothing else but the same column of the same sequence's row of table
  *   refs   : the pool's counts or NULL; with them a page that is to be written and does not
  *            have a count of 1 is reported as a page number out of range is, and not written
- *   lens_out: int32 [S], start + n_keep.  Must not overlap lens, start or n_keep
+ *   lens_out: int32 [S], start + n_keep.  Must not overlap another array
  * Pages past lens_out are given up by zsaa_op_paged_resize.  An entry out of range or not
  * above the one before it is reported, and not moved.  A call is planned by keep_cols: rows much
  * wider than the lists cost time.  At most 16383 KV heads. */

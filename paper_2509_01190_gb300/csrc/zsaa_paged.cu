@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "common.cuh"
 #include "paged.h"
@@ -47,6 +48,21 @@ bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
+// Arrays that a call writes lie over none that it reads, and over no other that it writes.
+struct Array {
+  const void* p;  // or null
+  size_t bytes;
+};
+bool apart(std::initializer_list<Array> written, std::initializer_list<Array> read) {
+  for (const Array* w = written.begin(); w != written.end(); ++w) {
+    if (w->p == nullptr) continue;
+    for (const Array* o = w + 1; o != written.end(); ++o)
+      if (o->p != nullptr && overlap(w->p, w->bytes, o->p, o->bytes)) return false;
+    for (const Array& r : read)
+      if (r.p != nullptr && overlap(w->p, w->bytes, r.p, r.bytes)) return false;
+  }
+  return true;
+}
 // with any of n rows of `width` bytes, `stride` bytes apart (what lies between them is no part of them)
 bool overlap_rows(const void* a, size_t an, const void* rows, size_t n, size_t stride, size_t width) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), r = reinterpret_cast<uintptr_t>(rows);
@@ -341,8 +357,8 @@ zsaa_status zsaa_op_paged_resize(int32_t* refs, int n_pages, int page_size, int 
     return refuse(ZSAA_ERR_UNSUPPORTED, "page_size %d is not 16, 32, 64, 128 or 256", page_size);
   ZTRY(check_taking(S, cols, page_size));
   const size_t row = 4 * static_cast<size_t>(S);
-  if (overlap(lens, row, lens_out, row) || overlap(want, row, lens_out, row))
-    return bad("lens_out overlaps lens or want");
+  if (!apart({{refs, 4 * static_cast<size_t>(n_pages)}, {table, row * cols}, {lens_out, row}, {n_free, 4}}, {{lens, row}, {want, row}}))
+    return bad("refs, table, lens_out or n_free overlaps another array");
   PagesArgs a{};
   ZTRY(status_word(&a.status));
   a.refs = refs, a.table = a.table_out = table, a.lens = lens, a.want = want, a.lens_out = lens_out, a.n_free = n_free;
@@ -365,9 +381,9 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
   ZTRY(check_taking(N, cols, p.page_size));
   if (static_cast<long long>(S) * cols > kMostInt) return bad("a table must have fewer than 2^31 entries");
   const size_t in = 4 * static_cast<size_t>(S), out = 4 * static_cast<size_t>(N);
-  if (overlap(table, in * cols, table_out, out * cols)) return bad("table_out overlaps table");
-  if (overlap(lens, in, lens_out, out) || overlap(parent, out, lens_out, out) || (at != nullptr && overlap(at, out, lens_out, out)))
-    return bad("lens_out overlaps lens, parent or at");
+  if (!apart({{refs, 4 * static_cast<size_t>(p.n_pages)}, {table_out, out * cols}, {lens_out, out}, {n_free, 4}},
+             {{table, in * cols}, {lens, in}, {parent, out}, {at, out}}))
+    return bad("refs, table_out, lens_out or n_free overlaps another array");
   PagesArgs a{};
   ZTRY(status_word(&a.status));
   a.refs = refs, a.table = table, a.table_out = table_out, a.lens = lens, a.parent = parent, a.at = at;
@@ -394,9 +410,9 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   ZTRY(check_cols(cols, p.page_size));
   ZTRY(check_cols(out_cols, p.page_size));
   const size_t row = 4 * static_cast<size_t>(S);
-  if (overlap(lens, row, lens_out, row) || overlap(n_keep, row, lens_out, row) ||
-      (start != nullptr && overlap(start, row, lens_out, row)))
-    return bad("lens_out overlaps lens, start or n_keep");
+  if (!apart({{lens_out, row}}, {{table, row * cols}, {lens, row}, {start, row}, {keep, row * keep_cols}, {n_keep, row},
+                                 {table_out, row * out_cols}, {refs, 4 * static_cast<size_t>(p.n_pages)}}))
+    return bad("lens_out overlaps another array");
   int sms = 0;
   ZTRY(device_sms(&sms));
   CompactArgs a{};
@@ -438,21 +454,14 @@ zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* dra
   const size_t row = 4 * static_cast<size_t>(S);
   // CTAs of a sequence read what others of it write, so outputs and the workspace lie over nothing else (but
   // lens_out may be lens)
-  const size_t e = element(dtype), drafted = draft != nullptr ? static_cast<size_t>(S) * n : 0;
-  const struct {
-    const void* p;
-    size_t bytes;
-  } arrays[] = {{accepted, row},    {tokens, row * (n + 1)},  {logp, row * (n + 1)}, {lens_out, row}, {ws, need},
-                {lens, row},        {drafts, row * n},        {temperature, row},    {uniform, row * (n + 1)}};
-  for (int o = 0; o < 5; ++o) {
-    if (arrays[o].p == nullptr) continue;
-    for (int i = o + 1; i < 9; ++i) {
-      const bool in_place = o == 3 && i == 5 && lens == lens_out;
-      if (arrays[i].p != nullptr && !in_place && overlap(arrays[o].p, arrays[o].bytes, arrays[i].p, arrays[i].bytes))
-        return bad("an output or the workspace overlaps another array");
-    }
-    if (overlap_rows(arrays[o].p, arrays[o].bytes, target, static_cast<size_t>(S) * (n + 1), ld * e, V * e) ||
-        (drafted > 0 && overlap_rows(arrays[o].p, arrays[o].bytes, draft, drafted, draft_ld * e, V * e)))
+  const size_t e = element(dtype), drafted = draft != nullptr ? static_cast<size_t>(S) * n : 0, each = row * (n + 1);
+  if (!apart({{accepted, row}, {tokens, each}, {logp, each}, {lens_out, row}, {ws, need}},
+             {{lens != lens_out ? lens : nullptr, row}, {drafts, row * n}, {temperature, row}, {uniform, each}}))
+    return bad("an output or the workspace overlaps another array");
+  for (const Array& o : {Array{accepted, row}, {tokens, each}, {logp, each}, {lens_out, row}, {ws, need}}) {
+    if (o.p == nullptr) continue;
+    if (overlap_rows(o.p, o.bytes, target, static_cast<size_t>(S) * (n + 1), ld * e, V * e) ||
+        (drafted > 0 && overlap_rows(o.p, o.bytes, draft, drafted, draft_ld * e, V * e)))
       return bad("an output or the workspace overlaps the logits");
   }
   int sms = 0;

@@ -83,6 +83,44 @@ def test_compact_refusals(zlib, kw):
     refused(zlib, lambda: compact(zlib, **kw))
 
 
+OVER = "overlaps another array"
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n_free=D), dict(n_free=D + 12), dict(n_free=E + 4), dict(n_free=FAR), dict(n_free=A + 4 * 63), dict(n_free=B + 4 * 19),
+    dict(lens_out=A + 4 * 63), dict(lens_out=B - 12), dict(table=A + 4 * 63), dict(lens=A), dict(want=B + 76), dict(lens=D, want=A - 12)])
+def test_resize_refuses_arrays_over_what_it_writes(zlib, kw):
+    with pytest.raises(zlib.ZsaaError, match=OVER):
+        resize(zlib, **kw)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n_free=D + 12), dict(n_free=E + 20), dict(n_free=E + 4096), dict(n_free=B + 76), dict(n_free=FAR + 116), dict(n_free=FAR + 4096),
+    dict(n_free=A), dict(table_out=D - 116), dict(table_out=E), dict(table_out=E + 4100), dict(table_out=A + 252), dict(lens_out=B + 76),
+    dict(lens_out=A), dict(lens_out=FAR + 100), dict(lens=A), dict(parent=A + 240), dict(table=A)])
+def test_fork_refuses_arrays_over_what_it_writes(zlib, kw):
+    with pytest.raises(zlib.ZsaaError, match=OVER):
+        fork(zlib, **kw)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(lens_out=B + 76), dict(lens_out=E + 4 * 119), dict(lens_out=E - 12), dict(table_out=FAR - 76), dict(refs=FAR - 252)])
+def test_compact_refuses_lengths_over_another_array(zlib, kw):
+    with pytest.raises(zlib.ZsaaError, match=OVER):
+        compact(zlib, **kw)
+
+
+@pytest.mark.parametrize("call,kw", [
+    (resize, dict(n_free=D + 16)), (resize, dict(n_free=A + 256)), (resize, dict(want=D)), (resize, dict(lens_out=B + 80)),
+    (fork, dict(n_free=FAR + 120)), (fork, dict(table_out=B + 80, lens_out=D + 16)), (fork, dict(at=E)), (fork, dict(n_free=A - 4)),
+    (compact, dict(lens_out=B + 80)), (compact, dict(lens_out=D + 16)), (compact, dict(refs=FAR + 16))])
+def test_arrays_side_by_side_are_taken(zlib, call, kw):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("there is a device, and the addresses are none of its")
+    refused(zlib, lambda: call(zlib, **kw), zlib.ZSAA_ERR_CUDA)
+
+
 def test_unlike_layers_and_their_number(zlib):
     for kw in (dict(n_pages=65), dict(page_size=32), dict(n_kv_heads=1), dict(head_dim=128)):
         refused(zlib, lambda: fork(zlib, [pages(zlib), pages(zlib, **kw)]))
