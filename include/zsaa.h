@@ -626,8 +626,9 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
  *            ascending, in [start[s], lens[s]);  start: int32 [S] or NULL (0, as a negative one)
  *   table, lens: int32 [S, cols] and [S], the entries as they are
  *   table_out: int32 [S, out_cols], the pages that the result is written to (not changed):
- *            `table` itself for a move in place, or another.  A page that is written may be
- *            in use for nothing else but the same column of the same sequence's row of table
+ *            `table` itself for a move in place (out_cols = cols then, unless S = 1), or an
+ *            array apart from it.  A page that is written may be in use for nothing else but
+ *            the same column of the same sequence's row of table
  *   refs   : the pool's counts or NULL; with them a page that is to be written and does not
  *            have a count of 1 is reported as a page number out of range is, and not written
  *   lens_out: int32 [S], start + n_keep.  Must not overlap another array

@@ -413,6 +413,10 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   if (!apart({{lens_out, row}}, {{table, row * cols}, {lens, row}, {start, row}, {keep, row * keep_cols}, {n_keep, row},
                                  {table_out, row * out_cols}, {refs, 4 * static_cast<size_t>(p.n_pages)}}))
     return bad("lens_out overlaps another array");
+  // a sequence's row of one must not be another's, or another column of its own, of the other
+  const bool in_place = table_out == table && (out_cols == cols || S == 1);
+  if (!in_place && overlap(table, row * cols, table_out, row * out_cols))
+    return bad("table_out overlaps table and is not the same array of the same width");
   int sms = 0;
   ZTRY(device_sms(&sms));
   CompactArgs a{};

@@ -338,6 +338,58 @@ def test_compact_runs_shifts_and_ends(zlib, moved):
         compacted(zlib, "f32", 1, 1, 128, 64, [n], [list(keep)], moved=moved)
 
 
+@pytest.mark.parametrize("counted", [False, True])
+@pytest.mark.parametrize("same", ["all", "first", "last", "one"])
+@pytest.mark.parametrize("dtype,L,Hkv,hd,page,lens", [
+    ("bf16", 1, 1, 64, 16, [9001]), ("bf16", 2, 3, 128, 32, [333, 40, 0, 700]), ("f32", 1, 2, 32, 16, [5, 900]),
+    ("f32", 1, 4, 128, 64, [3000])])
+def test_compact_by_another_array_that_names_the_same_pages(zlib, dtype, L, Hkv, hd, page, lens, same, counted):
+    """table_out is no part of table, but some or all of its columns are the same: in place as far as
+    those go.  (The first shape is planned for several clusters to its list, and one does it.)"""
+    z, r = zlib, np.random.default_rng(len(same) + len(lens))
+    used = [P.pages_of(n, page) for n in lens]
+    cols = max(used)
+    out_cols = cols + 2
+    n_pages = 2 * sum(used) + 1
+    free = list(r.permutation(n_pages))
+    table, out = np.full((len(lens), cols), -1), np.full((len(lens), out_cols), -1)
+    for s, n in enumerate(used):
+        table[s, :n] = [free.pop() for _ in range(n)]
+        cut = r.integers(0, n + 1)
+        for c in range(n):
+            keeps = dict(all=True, first=c < cut, last=c >= cut, one=c == cut)[same]
+            out[s, c] = table[s, c] if keeps else free.pop()
+    keep = some_of(r, lens, 0.6)
+    width = max(len(x) for x in keep)
+    listed = np.zeros((len(lens), width), int)
+    for s, x in enumerate(keep):
+        listed[s, :len(x)] = x
+    refs = np.zeros(n_pages, int)
+    refs[out[out >= 0]] = 1
+    k, v = pools(dtype, L, n_pages, Hkv, page, hd, 4)
+    kk, vv, got = np64(k), np64(v), out_lens(len(lens))
+    want = P.compact(kk, vv, page, table, None, listed, [len(x) for x in keep], out)
+    z.zsaa_op_paged_compact(z.make_pages_list(list(k), list(v)), ints(refs) if counted else None, len(lens), ints(table), cols,
+                            ints(lens), None, ints(listed), width, ints([len(x) for x in keep]), ints(out), out_cols, got)
+    np.testing.assert_array_equal(got.cpu().numpy(), want)
+    np.testing.assert_array_equal(np64(k), kk)
+    np.testing.assert_array_equal(np64(v), vv)
+
+
+@pytest.mark.parametrize("out_cols", [2, 5])
+def test_compact_of_one_sequence_in_place_by_a_row_of_another_width(zlib, out_cols):
+    """One row that starts where the table does is the same row, as far as it goes."""
+    k, v = pools("bf16", 1, 6, 1, 16, 64, 0)
+    kk, vv, keep = np64(k), np64(v), np.array([[1, 5, *range(20, 48)]])
+    table, got = ints([[3, 1, 4, -1, -1]]), out_lens(1)
+    P.compact(kk, vv, 16, np.array([[3, 1, 4]]), None, keep, [30], np.array([[3, 1]]))
+    zlib.zsaa_op_paged_compact(zlib.make_pages_list(list(k), list(v)), None, 1, table, 3, ints([48]), None, ints(keep), 30, ints([30]),
+                               table, out_cols, got)
+    assert got.tolist() == [30]
+    np.testing.assert_array_equal(np64(k), kk)
+    np.testing.assert_array_equal(np64(v), vv)
+
+
 def test_compact_leaves_shared_pages_alone_where_it_moves_nothing(zlib):
     """Two sequences over one whole page, each with a page of its own: the kept entries of the
     shared page stay where they are, and with counts that is allowed."""

@@ -110,8 +110,17 @@ def test_compact_refuses_lengths_over_another_array(zlib, kw):
         compact(zlib, **kw)
 
 
+@pytest.mark.parametrize("kw", [
+    dict(out_cols=4), dict(out_cols=6), dict(out_cols=6, S=2), dict(table_out=B + 4), dict(table_out=B + 76), dict(table_out=B - 76),
+    dict(table_out=B + 20), dict(table_out=B + 4, S=1), dict(table_out=B + 4, S=1, out_cols=4)])
+def test_compact_refuses_tables_that_overlap_otherwise_than_in_place(zlib, kw):
+    with pytest.raises(zlib.ZsaaError, match="table_out overlaps table"):
+        compact(zlib, **kw)
+
+
 @pytest.mark.parametrize("call,kw", [
-    (resize, dict(n_free=D + 16)), (resize, dict(n_free=A + 256)), (resize, dict(want=D)), (resize, dict(lens_out=B + 80)),
+    (compact, dict()), (compact, dict(S=1, out_cols=3)), (compact, dict(S=1, out_cols=9)), (compact, dict(table_out=B + 80)),
+    (compact, dict(table_out=B - 80)), (resize, dict(n_free=D + 16)), (resize, dict(n_free=A + 256)), (resize, dict(want=D)), (resize, dict(lens_out=B + 80)),
     (fork, dict(n_free=FAR + 120)), (fork, dict(table_out=B + 80, lens_out=D + 16)), (fork, dict(at=E)), (fork, dict(n_free=A - 4)),
     (compact, dict(lens_out=B + 80)), (compact, dict(lens_out=D + 16)), (compact, dict(refs=FAR + 16))])
 def test_arrays_side_by_side_are_taken(zlib, call, kw):
