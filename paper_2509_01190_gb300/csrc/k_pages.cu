@@ -452,8 +452,8 @@ __global__ void __launch_bounds__(kCompactThreads, kCompactPerSm)
   const int listed = after_wait(a.n_keep)[s];
   const int n = min(min(max(listed, 0), a.keep_cols), min(len, out_cap) - min(start, out_cap));
   if (first_cta && rank == 0 && tid == 0) {
-    a.lens_out[s] = start + n;
-    if (given > cap || begin > len || listed > n) atomicOr(a.status, kStatusBadIndex);
+    a.lens_out[s] = min(start, out_cap) + n;
+    if (given > cap || begin > len || start > out_cap || listed > n) atomicOr(a.status, kStatusBadIndex);
   }
   const int32_t* keep = after_wait(a.keep) + static_cast<size_t>(s) * a.keep_cols;
   const int32_t* from_row = after_wait(a.table) + static_cast<size_t>(s) * a.cols;

@@ -436,6 +436,25 @@ def test_compact_into_rows_too_short(zlib):
     assert got.tolist() == [16] and torch.equal(k[0, 5, 0, :14], before[0, 0, 0, 2:]) and torch.equal(k[0, :5], before[0, :5])
 
 
+@pytest.mark.parametrize("n_keep", [0, 3])
+def test_compact_from_beyond_the_row_it_writes(zlib, n_keep):
+    """Entries below `start` that the other row has no place for: its length is what it holds, and
+    that is reported."""
+    k, v = pools("bf16", 1, 6, 1, 16, 64, 0)
+    before, got, layers = k.clone(), out_lens(2), zlib.make_pages_list(list(k), list(v))
+
+    def call(start):
+        zlib.zsaa_op_paged_compact(layers, None, 2, ints([[0, 1], [2, 3]]), 2, ints([32, 32]), ints([0, start]),
+                                   ints([[4, 5, 6], [28, 29, 31]]), 3, ints([0, n_keep]), ints([[4], [5]]), 1, got)
+
+    call(17)
+    reported(zlib)
+    assert got.tolist() == [0, 16] and torch.equal(k, before)
+    if n_keep == 0:
+        call(16)  # (and nothing to report: 16 entries below the start fill the row)
+        assert got.tolist() == [0, 16] and torch.equal(k, before)
+
+
 def test_pages_far_into_a_large_pool(zlib):
     """Element offsets past 2^31: the last pages of pools of 5 GB."""
     z, n_pages, page = zlib, 40000, 64
