@@ -632,6 +632,7 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
  *   refs   : the pool's counts or NULL; with them a page that is to be written and does not
  *            have a count of 1 is reported as a page number out of range is, and not written
  *   lens_out: int32 [S], start + n_keep.  Must not overlap another array
+ * A pool that several layers or both of a layer's sides name is moved once.
  * A result that its row of table_out does not hold is cut to it, and reported.  Pages past lens_out
  * are given up by zsaa_op_paged_resize.  An entry out of range or not above the one before it is
  * reported, and not moved.  A call is planned by keep_cols: rows much wider than the lists cost

@@ -183,6 +183,18 @@ zsaa_status check_layers(const zsaa_pages* layers, int n_layers, PoolList* pools
   return ZSAA_OK;
 }
 
+// The pools, each once: layers may share a cache, keys and values a pool, and entries that move in
+// place are moved by one CTA's reads and writes alone.
+PoolList each_once(const PoolList& given) {
+  PoolList out{};
+  for (int i = 0; i < given.n; ++i) {
+    bool again = false;
+    for (int j = 0; j < out.n; ++j) again |= out.p[j] == given.p[i];
+    if (!again) out.p[out.n++] = given.p[i];
+  }
+  return out;
+}
+
 // (a grid's third dimension, 4 CTAs to a head; a page's vectors in 31 bits)
 zsaa_status check_heads(int n) { return n <= 16383 ? ZSAA_OK : bad("more than 16383 KV heads"); }
 
@@ -426,7 +438,7 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
   a.S = S, a.cols = cols, a.out_cols = out_cols, a.keep_cols = keep_cols, a.n_pages = p.n_pages;
   a.page_shift = page_shift(p.page_size), a.Hkv = p.n_kv_heads;
   a.row_vecs = static_cast<int>(p.head_dim * element(p.dtype) / 16);
-  return launched("zsaa_op_paged_compact", launch_paged_compact(a, pools, sms, reinterpret_cast<cudaStream_t>(stream)));
+  return launched("zsaa_op_paged_compact", launch_paged_compact(a, each_once(pools), sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes) {

@@ -390,6 +390,23 @@ def test_compact_of_one_sequence_in_place_by_a_row_of_another_width(zlib, out_co
     np.testing.assert_array_equal(np64(v), vv)
 
 
+@pytest.mark.parametrize("n", [40, 5000])
+def test_compact_moves_a_pool_that_several_layers_name_once(zlib, n):
+    """Layers that share a cache, and one whose keys are its values."""
+    z, page = zlib, 16
+    used = P.pages_of(n, page)
+    k, v = pools("bf16", 3, used, 2, page, 64, n)
+    kk, vv, table = np64(k), np64(v), np.arange(used)[None]
+    keep = np.sort(np.random.default_rng(n).permutation(n)[:n * 2 // 3])
+    P.compact(kk, vv, page, table, None, keep[None], [len(keep)], table)
+    layers = z.make_pages_list([k[0], k[1], k[0], k[2], v[0], k[1]], [v[0], v[1], v[0], k[2], v[2], v[0]])
+    d_table, got = ints(table), out_lens(1)
+    z.zsaa_op_paged_compact(layers, None, 1, d_table, used, ints([n]), None, ints([keep]), len(keep), ints([len(keep)]), d_table, used,
+                            got)
+    np.testing.assert_array_equal(np64(k), kk)
+    np.testing.assert_array_equal(np64(v), vv)
+
+
 def test_compact_leaves_shared_pages_alone_where_it_moves_nothing(zlib):
     """Two sequences over one whole page, each with a page of its own: the kept entries of the
     shared page stay where they are, and with counts that is allowed."""
