@@ -288,10 +288,10 @@ struct Sequence {
   Temperature t;
   MassRow factor;
   bool soft, lookup;  // a temperature above 0; no draft rows
-  int s, n;           // n: drafts before the first that is no token
+  int n;              // drafts before the first that is no token
 };
-__device__ __forceinline__ Sequence sequence_with(const VerifyArgs& a, int s, const Temperature& t, int n) {
-  return Sequence{t, mass_row(t.t), !t.greedy && !t.bad, a.draft == nullptr, s, n};
+__device__ __forceinline__ Sequence sequence_with(const VerifyArgs& a, const Temperature& t, int n) {
+  return Sequence{t, mass_row(t.t), !t.greedy && !t.bad, a.draft == nullptr, n};
 }
 // numbers outside [0, 1) count as the nearest ones in it, a NaN as 0
 __device__ __forceinline__ float number_at(const VerifyArgs& a, int s, int j) {
@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(kScanThreads, kTurnPerSm<T>)
   __syncwarp();
   if (__shfl_sync(0xffffffffu, last, 0) == 0) return;
   // this stretch was draft j's last
-  const Sequence q = sequence_with(a, s, Temperature{temperature, !soft, false}, n);
+  const Sequence q = sequence_with(a, Temperature{temperature, !soft, false}, n);
   VerifyRow p, d{0.f, 0.f, 0.f, 0, 0};
   int draft = 0;
   float u = 0.f, xp = 0.f, xq = 0.f;
@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     t = temperature_of(a, s);
     n = drafts_of(a, s);
   }
-  const Sequence q = sequence_with(a, s, t, n);
+  const Sequence q = sequence_with(a, t, n);
   int my_draft = -1;
   if (tid < q.n) my_draft = after_wait(a.drafts)[static_cast<size_t>(s) * a.n + tid];
   if constexpr (DECIDED) {
