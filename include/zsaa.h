@@ -619,9 +619,9 @@ zsaa_status zsaa_op_paged_fork(const zsaa_pages* layers, int n_layers, int32_t* 
                                int32_t* lens_out, int32_t* n_free, zsaa_stream stream);
 
 /* zsaa_op_paged_compact: chosen entries of each sequence moved together, in every layer: a
- * cache pruned after the prompt (keep from zsaa_score_select), a window that moves on with its
- * first entries kept, or drafts taken from several branches.  Entry start[s] + j of the result
- * is entry keep[s, j]; entries below start[s] are not touched.
+ * cache pruned after the prompt (keep from zsaa_score_select), or a window that moves on with its
+ * first entries kept.  Entry start[s] + j of the result is entry keep[s, j]; entries below
+ * start[s] are not touched.
  *   keep   : int32 [S, keep_cols], row s has n_keep[s] entries (negative: 0), strictly
  *            ascending, in [start[s], lens[s]);  start: int32 [S] or NULL (0, as a negative one)
  *   table, lens: int32 [S, cols] and [S], the entries as they are
@@ -654,7 +654,7 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  *   drafts   : int32 [S, n]; a sequence's drafts end before the first that is no token (a -1)
  *              or whose draft row has no distribution
  *   temperature: float32 [S] or NULL (1).  0, and what is below 2^-64: all probability on
- *              the first of the largest logits, draft rows not read.  At most 2^64
+ *              the first of the largest logits, whatever draft rows hold.  At most 2^64
  *   uniform  : float32 [S, n+1] in [0, 1), u_0 .. u_n (a NaN counts as 0, others as the nearest)
  *   accepted : int32 [S], how many drafts stand
  *   tokens   : int32 [S, n+1], those drafts, the next token, then -1
@@ -666,8 +666,9 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  * A row has no distribution where it holds a NaN or +inf or nothing above -inf, or its
  * temperature is negative, NaN or above 2^64.  A target row without one ends the sequence's
  * tokens: the next one is -1.  Exponentials that a token is picked by are good to 2^-35.7, the
- * sums that decide a draft to about 1e-8.  Results do not depend on timing.  ws: 16-byte
- * aligned, of at least the bytes that zsaa_op_draft_verify_workspace returns (host only). */
+ * sums that decide a draft to about 2e-7, and to 2^-17 in any case.  Results do not depend on
+ * timing.  ws: 16-byte aligned, of at least the bytes that zsaa_op_draft_verify_workspace returns
+ * (host only); calls that may run at the same time need one each. */
 zsaa_status zsaa_op_draft_verify_workspace(int S, int n, int V, size_t* bytes);
 zsaa_status zsaa_op_draft_verify(const void* target, int64_t ld, const void* draft, int64_t draft_ld, int dtype, int S, int n,
                                  int V, const int32_t* drafts, const float* temperature, const float* uniform,

@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(256) fork_copy_kernel(const __grid_constant__ 
 // Moved into other pages no tile waits for another, and clusters as many as run at once share a list:
 // 16250 of 65000 entries of one layer 26 us (5.1 TB/s), where one cluster to a head takes 34 and a CTA
 // to a head 675.  (Two tiles on their way with the cluster's barrier split around the second's loads:
-// 43 against 39 for the cluster's form.)
+// 43 against 39 for the cluster's form.)  Three CTAs to an SM leave 80 registers a thread: 8 bytes spill.
 constexpr int kCompactPerSm = 3;
 constexpr int kCompactThreads = 256, kCompactUnroll = 8, kCompactVecs = kCompactThreads * kCompactUnroll;
 

@@ -21,19 +21,23 @@
 // it, and rows behind a refused draft, which nothing depends on, are left out as far as that is
 // known when their turn comes.
 //
-// What decides a draft is one comparison of two quotients, off by about 1e-8 with sums of
-// float32 exponentials.  What decides a token is where u_n falls among V borders, some 1e-5
-// apart and closer: a running sum that is off by 1e-9 picks the wrong token every few thousand
-// calls.  So the rows at which a sequence stops are gone through again with exponentials as
-// pairs of floats, good to 2^-35.7 each and without a bias to see (below 2^-42), and sums in pairs
-// and in 64-bit integers.
+// What decides a draft is one comparison of two quotients, off by some 1e-7 with sums of
+// float32 exponentials: a sum is off by 4e-8 as a rule and 1.6e-7 at most over rows of 128256
+// logits (normal ones of deviation 0.01, 3 and 30, and ones that fall as the logarithm of their
+// rank) at temperatures from 0.05 to 10, much of it log2(e) / T as one float; and by less than 2^-17
+// on any row (three roundings of an exponential's argument, its own 2^-22, the additions).
+// What decides a token is where u_n falls among V borders, some 1e-5 apart and closer: a running
+// sum that is off by 1e-9 picks the wrong token every few thousand calls.  So the rows at which
+// a sequence stops are gone through again with exponentials as pairs of floats, good to 2^-35.7
+// each and without a bias to see (below 2^-42), and sums in pairs and in 64-bit integers.
 //
 // One pass does it, although the residual needs the sums of both rows: with E the exponentials,
 // Z their exact sums and c0 the quotient Z_p / Z_q as the scan has it, the pass adds up
 //   D_i = E_p,i - c0 E_q,i        over all tokens, and
 //   A = sum D_i, B = sum E_q,i    over a group's tokens with D_i > 0.
-// The exact quotient is c0 + k with k = sum D / Z_q, some 2^-24 of it, so a group's residual is
-// A - k B; tokens whose D_i changes its sign with k are off by 2^-24 of a 2^-24th of them.
+// The exact quotient is c0 + k with k = sum D / Z_q, some 2^-21 of it (2^-16 at most), so a group's
+// residual is A - k B.  A token whose D_i changes its sign with k is off by k E_q,i at most, and such
+// tokens' quotients all lie within 2^-21 of Z_p / Z_q: as small a part of the mass, as a rule.
 // (Two passes, the first for the sums, took 270 us on the 64 where this one took 77, both still with
 // sums of 64-bit floats.)
 //
@@ -977,7 +981,11 @@ VerifySlices verify_slices(int S, int V, int sms, int rounds) {
 
 // Whether rows are scanned in turn: from 20 stretches to an SM on (128256 float32 logits, drafts of
 // which three of five stand, us for all rows and in turn: 8 sequences of 5 drafts 23 and 30, 16 34 and
-// 36, 24 49 and 46, 48 82 and 76; 64 of one draft 61 and 56; 16 of 15 drafts 66 and 51).
+// 36, 24 49 and 46, 48 82 and 76; 64 of one draft 61 and 56; 16 of 15 drafts 66 and 51).  By the same
+// rule: bf16, 24 of 5 drafts 41 and 40, 64 89 and 75; looked-up drafts, 48 of 5 49 and 35; 32003 logits, 64
+// of 5 (18 to an SM) 33 and 36, 100 48 and 47; 1000 logits, 700 of 5 55 and 53.  It does not pay for
+// one draft over rows shorter than a stretch: 1100 sequences of 1000 logits 38 and 45, 1700 of 50
+// with drafts looked up 44 and 52.
 bool in_turn(const VerifyArgs& a, int sms) {
   return a.n > 0 && static_cast<long long>(a.S) * a.rows * a.chunks > 20ll * sms;
 }
