@@ -647,7 +647,8 @@ zsaa_status zsaa_op_paged_compact(const zsaa_pages* layers, int n_layers, const 
  * j over the temperature, draft x_j stands where all before it do and u_j q_j(x_j) < p_j(x_j).
  * At a refused draft the next token is drawn from max(p_j - q_j, 0), behind the last draft from
  * p: the first token t whose running sum over tokens 0..t exceeds u_n times the whole sum.  So
- * tokens are distributed as the target's.  n = 0 draws one token from the target.
+ * tokens are distributed as the target's.  Where nothing is left of p_j - q_j (no more than 2^-33 in
+ * all) it is drawn from p_j.  n = 0 draws one token from the target.
  *   target   : [S, n+1, ld] logits of `dtype` (ZSAA_F32 or ZSAA_BF16; any alignment of the
  *              type), ld >= V (not read past V), V <= 2^26;  0 <= n <= 15
  *   draft    : [S, n, draft_ld], or NULL: drafts without probabilities (looked up; q_j is 1 at x_j)

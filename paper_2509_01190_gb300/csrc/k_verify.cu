@@ -37,7 +37,8 @@
 //   A = sum D_i, B = sum E_q,i    over a group's tokens with D_i > 0.
 // The exact quotient is c0 + k with k = sum D / Z_q, some 2^-21 of it (2^-16 at most), so a group's
 // residual is A - k B.  A token whose D_i changes its sign with k is off by k E_q,i at most, and such
-// tokens' quotients all lie within 2^-21 of Z_p / Z_q: as small a part of the mass, as a rule.
+// tokens' quotients all lie within 2^-21 of Z_p / Z_q: as small a part of the mass, as a rule.  (Where
+// they may not be, choose_alone goes through the tokens again.)
 // (Two passes, the first for the sums, took 270 us on the 64 where this one took 77, both still with
 // sums of 64-bit floats.)
 //
@@ -632,6 +633,121 @@ __device__ __forceinline__ long long running_sum(long long v) {  // over the war
   return v;
 }
 
+// A token's share of the sum that the next one is drawn by.
+template <typename T>
+struct Share {
+  const T *p, *q;
+  MassRow mp, mq;
+  Pair ratio;
+  float k, unit;
+  int kind, refused;
+  const float* table;
+  __device__ __forceinline__ long long operator()(long long i, float& x) const {
+    x = to_f<T>(p[i]);
+    const Pair e = mass(x, mp, table);
+    if (kind != kResidual) return i == refused ? 0ll : fixed(e, unit);
+    const Pair other = mass(to_f<T>(q[i]), mq, table);
+    Pair d = sub(e, mul(other, ratio));
+    d.l -= k * other.h;
+    return max(fixed(d, unit), 0ll);
+  }
+};
+struct ShareSums {
+  long long part[kFinishWarps];
+  int first[kFinishWarps], some[kFinishWarps];
+};
+struct Chosen {
+  int token;  // in the thread that has it, else -1
+  float x;    // its logit
+};
+
+// The CTA's first of `count` tokens from `lo` on whose running sum, that begins with `before`, exceeds
+// goal(their whole sum), or where none does the last one with any; a thread keeps KEPT of them.
+// `nothing` where the goal is below 0.
+template <int KEPT, typename T, typename Goal>
+__device__ __forceinline__ Chosen choose(const Share<T>& share, long long lo, int count, long long before, ShareSums& sums,
+                                         bool& nothing, Goal&& goal_from) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (count + kFinishThreads - 1) / kFinishThreads, t0 = min(tid * per, count), t1 = min(t0 + per, count);
+  long long kept[KEPT > 0 ? KEPT : 1], mine = 0;
+  float kept_x[KEPT > 0 ? KEPT : 1], x = 0.f;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) {
+    kept[i] = 0;
+    if (t0 + i < t1) kept[i] = share(lo + t0 + i, kept_x[i]);
+    mine += kept[i];
+  }
+  for (int i = t0 + KEPT; i < t1; ++i) mine += share(lo + i, x);
+  const long long run = running_sum(mine);
+  if (lane == 31) sums.part[warp] = run;
+  __syncthreads();
+  long long base = before, total = 0;
+#pragma unroll
+  for (int w = 0; w < kFinishWarps; ++w) {
+    if (w < warp) base += sums.part[w];
+    total += sums.part[w];
+  }
+  const long long goal = goal_from(total);
+  nothing = goal < 0;
+  if (nothing) return Chosen{-1, 0.f};
+  const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
+  const unsigned above = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
+  if (lane == 0) {
+    sums.first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1;
+    sums.some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
+  }
+  __syncthreads();
+  int last = 0, who = -1;
+#pragma unroll
+  for (int w = kFinishWarps - 1; w >= 0; --w) {
+    if (sums.first[w] >= 0) who = sums.first[w];
+  }
+#pragma unroll
+  for (int w = 0; w < kFinishWarps; ++w) {
+    if (sums.some[w] >= 0) last = sums.some[w];
+  }
+  Chosen out{-1, 0.f};
+  if (tid != (who >= 0 ? who : last)) return out;
+  before = base + run - mine;
+  bool found = false;
+  auto look = [&](int i, long long v, float x) {
+    if (found || v <= 0) return;
+    out = Chosen{static_cast<int>(lo + i), x};
+    before += v;
+    found = before > goal;
+  };
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) look(t0 + i, kept[i], kept_x[i]);
+  for (int i = t0 + KEPT; i < t1 && !found; ++i) {
+    const long long v = share(lo + i, x);
+    look(i, v, x);
+  }
+  // (tokens whose sum is more than 0 only by rounding: the last one that the target can give)
+  for (long long i = lo + count - 1; out.token < 0; --i) {
+    x = to_f<T>(share.p[i]);
+    if (i == lo || mass(x, share.mp, share.table).h > 0.f) out = Chosen{static_cast<int>(i), x};
+  }
+  return out;
+}
+
+// All tokens by one CTA, with the exact quotient; from p itself where no more than `least` is left of p - q.
+template <typename T>
+__device__ __forceinline__ Chosen choose_alone(Share<T> share, int V, float u, float least, ShareSums* sums) {
+  bool nothing = true;
+  Chosen out{-1, 0.f};
+  if (share.kind == kResidual) {
+    out = choose<0>(share, 0, V, 0, *sums, nothing,
+                    [&](long long total) { return __ll2float_rn(total) > share.unit * least ? goal_of(u, total) : -1ll; });
+    __syncthreads();
+  }
+  if (nothing) {
+    share.kind = kFromTarget;
+    share.refused = -1;
+    out = choose<0>(share, 0, V, 0, *sums, nothing, [&](long long total) { return goal_of(u, total); });
+  }
+  return out;
+}
+
 // Which drafts stand is known in the calls that scan in turn, else worked out here by every CTA
 // (2 us).  Packed arithmetic takes two tokens at once; the FMA pipe's share of a token and its draft
 // row's is 78 operations.
@@ -640,7 +756,8 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     verify_finish_kernel(const __grid_constant__ VerifyArgs a, int ctas, int group, float unit) {
   __shared__ float table[64];
   __shared__ VerifyRow target[kVerifyMaxDrafts + 1], draft_rows[kVerifyMaxDrafts + 1];
-  __shared__ int s_stop, s_why, s_last, s_first[kFinishWarps], s_some[kFinishWarps];
+  __shared__ int s_stop, s_why, s_last;
+  __shared__ ShareSums s_share;
   __shared__ long long s_part[2][kFinishWarps];
   __shared__ float s_b[kFinishWarps];
   pdl_trigger();
@@ -857,21 +974,30 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     group_a[i] = corrected(group_a[i], group_b[i]);
     mine += group_a[i];
   }
-  long long run = running_sum(mine), goal = goal_of(u, __shfl_sync(0xffffffffu, run, 31)), before = 0;
-  // the lane of the place looked for, among lanes with running sums `sum` that end with `part` of their own
-  auto lane_of = [&](long long part, long long sum) {
-    const unsigned some = __ballot_sync(0xffffffffu, part > 0), above = __ballot_sync(0xffffffffu, part > 0 && sum > goal);
-    return above != 0 ? __ffs(above) - 1 : 31 - __clz(some);
-  };
-  // (nothing is left of p - q, as far as can be told: the token is drawn from p, by this CTA alone)
-  int who = lane_of(mine, run);
-  const bool plain = who < 0;
-  long long lo = 0;
-  int count = a.V;
-  if (!plain) {
-    int at = 0;
-    before = run - mine;
-    long long at_before = before;
+  long long run = running_sum(mine);
+  const long long whole = __shfl_sync(0xffffffffu, run, 31);
+  Share<T> share{row_p, row_q, mp, mq, ratio, k, unit, kind, refused, table};
+  // What is left of p - q is told from nothing down to `least`: a token's D_i is off by 2^-35.7 of
+  // E_p,i + c0 E_q,i at most, all of them by 2^-34.7 of Z_p, and so is the k B that is taken off.
+  // At or below it the token is drawn from p.  And where all that is left is not far above k Z_q, tokens
+  // whose D_i has another sign than the exact one may be a part of it that counts (rows that
+  // are equal but for a few tokens).  Then this CTA goes through all tokens by itself with the exact
+  // quotient, 320 us over 128256 of them where rows apart take 18; a draft that was drawn from the
+  // draft row is refused over such rows, with 2^13 times k Z_q, once in thousands of calls.
+  const float least = row.sum_h * 0x1p-33f;
+  const bool alone = kind == kResidual ? __ll2float_rn(whole) <= unit * (least + 0x1p13f * fabsf(k) * other.sum_h) : whole == 0;
+  Chosen next;
+  if (alone) {
+    next = choose_alone(share, a.V, u, least, &s_share);
+  } else {
+    const long long goal = goal_of(u, whole);
+    // the lane of the place looked for, among lanes with running sums `sum` that end with `part` of their own
+    auto lane_of = [&](long long part, long long sum) {
+      const unsigned some = __ballot_sync(0xffffffffu, part > 0), above = __ballot_sync(0xffffffffu, part > 0 && sum > goal);
+      return above != 0 ? __ffs(above) - 1 : 31 - __clz(some);
+    };
+    int who = lane_of(mine, run), at = 0;
+    long long before = run - mine, at_before = before;
     bool found = false;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
@@ -883,7 +1009,7 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     }
     at = __shfl_sync(0xffffffffu, at, who);
     before = __shfl_sync(0xffffffffu, at_before, who);
-    lo = static_cast<long long>(at) * group;
+    long long lo = static_cast<long long>(at) * group;
     const VerifyGroup* g = sums + at;
     const long long part = lane < kFinishWarps ? corrected(__ldcg(&g->warp_a[lane]), __ldcg(&g->warp_b[lane])) : 0;
     run = before + running_sum(part);
@@ -891,80 +1017,13 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishPerSm)
     before = __shfl_sync(0xffffffffu, run - part, who);
     const int length = group / kFinishWarps;
     lo += static_cast<long long>(who) * length;
-    count = static_cast<int>(max(min(static_cast<long long>(length), a.V - lo), 1ll));
+    const int count = static_cast<int>(max(min(static_cast<long long>(length), a.V - lo), 1ll));
+    bool nothing;
+    next = choose<4>(share, lo, count, before, s_share, nothing, [&](long long) { return goal; });
   }
-  // a token's share of the sum
-  auto token_left = [&](long long i, float& x) {
-    x = to_f<T>(row_p[i]);
-    const Pair p = mass(x, mp, table);
-    if (plain || kind != kResidual) return !plain && i == refused ? 0ll : fixed(p, unit);
-    const Pair e = mass(to_f<T>(row_q[i]), mq, table);
-    Pair d = sub(p, mul(e, ratio));
-    d.l -= k * e.h;
-    return max(fixed(d, unit), 0ll);
-  };
-  const int per = (count + kFinishThreads - 1) / kFinishThreads, t0 = min(tid * per, count), t1 = min(t0 + per, count);
-  constexpr int KEPT = 4;  // tokens that a thread keeps
-  long long kept[KEPT];
-  float kept_x[KEPT];
-  mine = 0;
-#pragma unroll
-  for (int i = 0; i < KEPT; ++i) {
-    kept[i] = 0;
-    if (t0 + i < t1) kept[i] = token_left(lo + t0 + i, kept_x[i]);
-    mine += kept[i];
-  }
-  float x = 0.f;
-  for (int i = t0 + KEPT; i < t1; ++i) mine += token_left(lo + i, x);
-  run = running_sum(mine);
-  if (lane == 31) s_part[0][warp] = run;
-  __syncthreads();
-  long long base = before, total = 0;
-#pragma unroll
-  for (int w = 0; w < kFinishWarps; ++w) {
-    if (w < warp) base += s_part[0][w];
-    total += s_part[0][w];
-  }
-  if (plain) goal = goal_of(u, total);
-  const unsigned some = __ballot_sync(0xffffffffu, mine > 0);
-  const unsigned above = __ballot_sync(0xffffffffu, mine > 0 && base + run > goal);
-  if (lane == 0) {
-    s_first[warp] = above != 0 ? tid + __ffs(above) - 1 : -1;
-    s_some[warp] = some != 0 ? tid + 31 - __clz(some) : -1;
-  }
-  __syncthreads();
-  int last = 0;
-  who = -1;
-#pragma unroll
-  for (int w = kFinishWarps - 1; w >= 0; --w) {
-    if (s_first[w] >= 0) who = s_first[w];
-  }
-#pragma unroll
-  for (int w = 0; w < kFinishWarps; ++w) {
-    if (s_some[w] >= 0) last = s_some[w];
-  }
-  if (tid == (who >= 0 ? who : last)) {
-    before = base + run - mine;
-    int token = -1;
-    float chosen = 0.f;
-    bool found = false;
-    auto look = [&](int i, long long v, float x) {
-      if (found || v <= 0) return;
-      token = static_cast<int>(lo + i);
-      chosen = x;
-      before += v;
-      found = before > goal;
-    };
-#pragma unroll
-    for (int i = 0; i < KEPT; ++i) look(t0 + i, kept[i], kept_x[i]);
-    for (int i = t0 + KEPT; i < t1 && !found; ++i) {
-      const long long v = token_left(lo + i, x);
-      look(i, v, x);
-    }
-    // (a group whose sum is more than 0 only by rounding: its last token)
-    if (token < 0) token = static_cast<int>(lo) + count - 1, chosen = to_f<T>(row_p[token]);
-    tokens[stop] = token;
-    if (logp != nullptr) logp[stop] = log_p(row.m, row_log, chosen);
+  if (next.token >= 0) {
+    tokens[stop] = next.token;
+    if (logp != nullptr) logp[stop] = log_p(row.m, row_log, next.x);
   }
 }
 

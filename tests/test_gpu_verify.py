@@ -194,6 +194,31 @@ def test_verify_equal_rows_stand_and_opposite_ones_do_not(zlib):
     assert (acc == 3).all() and (tok == 7).all()
 
 
+@pytest.mark.parametrize("S,V", [(2000, 14), (400, 100), (500, 1000), (60, 20000), (12, 128256)])
+@pytest.mark.parametrize("differ", ["nowhere", "in one", "in the largest"])
+def test_verify_draft_rows_that_agree_with_the_targets(zlib, differ, S, V):
+    """A banned draft over rows that are equal leaves nothing of p - q: the token is drawn from p.  One
+    logit apart by little, it leaves a residual of 1e-9 and more, of which every token has a part."""
+    r = np.random.default_rng(V)
+    target = (2 * r.standard_normal((S, 2, V))).astype(np.float32)
+    drafts, seq = r.integers(0, V, (S, 1)), np.arange(S)
+    target[seq, :, drafts[:, 0]] = -INF
+    draft = target[:, :1].copy()
+    if differ != "nowhere":
+        i = (drafts[:, 0] + 1) % V if differ == "in one" else draft[:, 0].argmax(1)
+        draft[seq, 0, i] += (10 ** r.uniform(-7, -1, S)).astype(np.float32)
+    u = r.random((S, 2)).astype(np.float32)
+    acc, tok, logp, t64, d64 = call(zlib, target, draft, drafts, None, u, pad=1)  # (rows of both kinds start anywhere in 16 bytes)
+    assert (acc == 0).all() and (logp > -INF).all()
+    told = 0
+    for s in range(S):
+        _, want, _, _, border = P.verify(t64[s:s + 1], d64[s:s + 1], drafts[s:s + 1], None, u[s:s + 1])
+        if border > 2.0 ** -34:
+            told += 1
+            assert tok[s, 0] == want[0, 0], (s, border)
+    assert told > 0 or (differ != "nowhere" and V > 20000)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_verify_greedy_takes_the_first_of_equal_logits(zlib, dtype):
     target = np.zeros((4, 3, 20000), np.float32)
